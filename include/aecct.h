@@ -341,8 +341,8 @@ aecct_status aecct_check_device_arith(uint64_t *counts);
 /* ------------------------------------------------------------------------------------------
  * Quantisation-aware training step (Section 6, second phase; Section 4.1 Eq. 1-3): the forward
  * pass of a model whose in-block linear maps are AAP linear layers over latent fp32 weights, the
- * loss of the multiplicative noise, and the gradients of every parameter.  No optimiser: the
- * caller applies the gradients.
+ * loss of the multiplicative noise, and the gradients of every parameter; aecct_train_update
+ * applies them.
  *
  * Forward, per word: the inference model's steps, with each map's ternary weights and scale
  * recomputed from its current latent weights W and factor delta (Eq. 1: gamma = the 0.5 quantile
@@ -404,6 +404,137 @@ aecct_status aecct_train_grad(const aecct_trainer *tr, const aecct_train_params 
                               const float *xs, int64_t batch, const aecct_train_grads *grads, float *loss,
                               void *workspace, size_t workspace_bytes, void *stream);
 void aecct_train_destroy(aecct_trainer *tr);
+
+/* ------------------------------------------------------------------------------------------
+ * Operators around the ternary maps: the root-mean-square norm of rows with the residual's addition
+ * and Eq. 2 codes, its gradient, the norm of many gradient tensors with clipping, and the Adam update
+ * (Section 6).  They take no model: every pointer is device memory of the current HIP device.
+ * They enqueue on stream, and neither allocate nor synchronise, so a HIP graph may capture them; the
+ * same call gives the same bits.  Calls on different streams are safe if their outputs and workspaces
+ * differ; a workspace needs no clearing and holds nothing between calls.
+ * ---------------------------------------------------------------------------------------- */
+
+/* Types of values in device memory.  Sums, norms and moments are taken in fp32 or fp64; a 16-bit output is
+ * rounded once, to nearest even.  Every buffer is aligned to its own type at least; no other alignment is
+ * asked for. */
+typedef enum aecct_dtype { AECCT_F32 = 0, AECCT_BF16 = 1, AECCT_F16 = 2 } aecct_dtype;
+
+/* 8-bit codes of a row or of a group of its columns (Eq. 2): alpha = max |y| over them,
+ * code = y Q / alpha rounded to nearest even, value = code alpha / Q.  alpha = 0 gives codes 0. */
+typedef enum aecct_code {
+  AECCT_CODE_NONE = 0,
+  AECCT_CODE_I8 = 1,    /* Q = 127: the codes and scales that Eq. 3 and aecct_ternary_gemm take */
+  AECCT_CODE_E4M3 = 2   /* Q = 448, the largest number of the 8-bit float with 4 exponent and 3 mantissa bits */
+} aecct_code;
+
+/*
+ * Root-mean-square norm of `rows` rows of d values, ld* values apart:
+ *   h = x + res,   rho = 1 / sqrt(mean(h^2) + eps),   y = h rho gain,   codes and alpha of y.
+ * x, res, h and y are of one type; y and the codes are taken of the unrounded h, the codes of the unrounded y.
+ * A row with a NaN or an infinity gives what the formulas give (rho = NaN, or 0): its alphas are NaN where
+ * a value they span is NaN, and int8 codes of NaN are 0.  Squares that leave fp32's range are summed again in fp64.
+ */
+typedef struct aecct_rms_norm_args {
+  int64_t rows, d;             /* rows >= 0 (0: nothing is written), 1 <= d <= 65536 */
+  int32_t type;                /* aecct_dtype of x, res, h and y */
+  int32_t gain_type;           /* AECCT_F32, or the same as type */
+  float eps;                   /* finite, >= 0 */
+  int32_t code_type;           /* aecct_code */
+  int32_t group;               /* columns of one alpha: 0 (the whole row), 32, 64 or 128; the last group of a row may be
+                                  shorter.  ceil(d / group) alphas a row */
+  const void *x;   int64_t ldx;      /* [rows][d] */
+  const void *res; int64_t ldres;    /* [rows][d], or NULL: h = x */
+  const void *gain;                  /* [d], or NULL: 1 */
+  void *h;         int64_t ldh;      /* [rows][d] out, or NULL; may be x or res itself */
+  void *y;         int64_t ldy;      /* [rows][d] out, or NULL; may be x or res itself */
+  void *codes;     int64_t ldcodes;  /* int8 or e4m3 [rows][d] out; with code_type NONE: NULL */
+  float *alpha;                      /* fp32 [rows][alphas] out; with code_type NONE: NULL */
+} aecct_rms_norm_args;
+/* Inputs may be rows of any stride >= 0 (0: one row for all), outputs of strides >= d.  At least one of h, y
+ * and codes is asked for.  Outputs overlap neither each other nor an input, except that h or y may be x or
+ * res itself, and that columns of one wider buffer (equal strides) may be inputs and outputs side by side.
+ * Errors: INVALID_ARG (with a NULL input, a negative size or stride, an unknown type, an overlap), UNSUPPORTED
+ * (d > 65536), DEVICE. */
+aecct_status aecct_rms_norm(const aecct_rms_norm_args *a, void *stream);
+
+/*
+ * Its gradient.  h as the norm read it (x, or the h it wrote), dy the gradient of y (of the codes' values:
+ * rounding to codes passes it straight through, alpha's dependence ignored, as in the training step), dres the
+ * gradient that reaches h past the norm along the residual:
+ *   xh = h rho,  c = mean(dy gain xh),  dh = rho (dy gain - xh c) + dres,  dgain = sum over rows of dy xh.
+ * dh is the gradient of x and of res alike.
+ */
+typedef struct aecct_rms_norm_grad_args {
+  int64_t rows, d;
+  int32_t type;                /* aecct_dtype of h, dy, dres and dh */
+  int32_t gain_type;           /* AECCT_F32, or the same as type */
+  float eps;
+  const void *h;    int64_t ldh;
+  const void *dy;   int64_t lddy;
+  const void *dres; int64_t lddres;  /* or NULL: none */
+  const void *gain;                  /* [d], or NULL: 1 */
+  void *dh;         int64_t lddh;    /* [rows][d] out, or NULL; may be h, dy or dres itself */
+  float *dgain;                      /* fp32 [d] out (zeros for rows = 0), or NULL */
+} aecct_rms_norm_grad_args;
+/* Strides, overlaps and errors as above; WORKSPACE_TOO_SMALL.  The workspace is used for dgain only (may be NULL
+ * without it); aecct_rms_norm_grad_workspace_size tells its bytes (host call). */
+aecct_status aecct_rms_norm_grad_workspace_size(int64_t rows, int64_t d, size_t *bytes);
+aecct_status aecct_rms_norm_grad(const aecct_rms_norm_grad_args *a, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/* A tensor of a list: `count` >= 0 contiguous values.  Lists are host arrays, read before the call returns. */
+typedef struct aecct_tensor {
+  void *data;      /* device; may be NULL where count is 0 */
+  int64_t count;
+  int32_t type;    /* aecct_dtype */
+} aecct_tensor;
+
+/* Workspace bytes of the calls below on lists of n tensors (host call). */
+aecct_status aecct_update_workspace_size(int32_t n, size_t *bytes);
+
+/* norm (device fp32 [1]) = sqrt of the sum of the squares of every value of the list, summed in fp64 (0 for an
+ * empty list).  Tensors of any types; they may overlap.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE. */
+aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, void *workspace, size_t workspace_bytes,
+                             void *stream);
+
+/* Clipping by that norm: out[i] = grads[i] min(1, max_norm / norm).  out: a list of the same counts (any types), or
+ * NULL for in place.  norm as above, before clipping.  Where it is not finite the values are left unscaled.
+ * max_norm >= 0; +infinity clips nothing.  No output tensor overlaps another tensor of either list, except
+ * that out[i] may be grads[i] itself.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE. */
+aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out, int32_t n, double max_norm, float *norm,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct aecct_adam_options {
+  double lr;              /* finite; not read where lr_device is given */
+  double beta1, beta2;    /* in [0, 1) */
+  double eps;             /* finite, >= 0 */
+  double weight_decay;    /* finite, decoupled: the parameter itself shrinks by lr weight_decay */
+  double max_norm;        /* > 0: gradients clipped by their norm over the whole list; 0: not clipped */
+  const float *lr_device; /* device fp32 [1], or NULL: a learning rate that a captured graph reads at each replay */
+} aecct_adam_options;
+
+/*
+ * One Adam update of every tensor of a list (Section 6 trains with Adam), t = *step + 1:
+ *   g' = g min(1, max_norm / norm),  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),
+ * and *step = t.  Lists of n tensors with equal counts: params, m, v fp32, updated in place; grads of any types,
+ * read only; copies (or NULL): the updated parameter rounded to another type (a copy of count 0 is left out).
+ *   step   device int64 [1], the number of updates made;
+ *   norm   device fp32 [1], the norm of the gradients before clipping, or NULL.
+ * The norm is taken where max_norm > 0 or norm is given; where it then is not finite, nothing but norm is written.
+ * No written tensor overlaps another tensor of the call.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE.
+ */
+aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, const aecct_tensor *v,
+                             const aecct_tensor *grads, const aecct_tensor *copies, int32_t n,
+                             const aecct_adam_options *opt, int64_t *step, float *norm, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/* aecct_adam_step on a trainer's parameters: every tensor of aecct_train_grads' layouts (params, m, v and grads as that
+ * struct, device fp32; params, m and v are updated).  Workspace of aecct_update_workspace_size(22).  The
+ * current device must be the trainer's.  Errors as aecct_adam_step. */
+aecct_status aecct_train_update(const aecct_trainer *tr, const aecct_train_grads *params, const aecct_train_grads *m,
+                                const aecct_train_grads *v, const aecct_train_grads *grads, const aecct_adam_options *opt,
+                                int64_t *step, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Human-readable name of a status code (static string). */
 const char *aecct_status_string(aecct_status status);

@@ -19,6 +19,8 @@ PATH_AUTO, PATH_LAYERED, PATH_FUSED = 0, 1, 2
 ATTN_HPSA, ATTN_CASA = 0, 1
 LAYERED_ATTN_AUTO, LAYERED_ATTN_UNFUSED, LAYERED_ATTN_LDS_F32, LAYERED_ATTN_LDS_I16, LAYERED_ATTN_LDS_SPLIT = -1, 0, 1, 2, 3
 ACT_SCALE_TOKEN, ACT_SCALE_WORD = 0, 1
+F32, BF16, F16 = range(3)
+CODE_NONE, CODE_I8, CODE_E4M3 = range(3)
 LIN_Q, LIN_K, LIN_V, LIN_O, LIN_FF1, LIN_FF2 = range(6)
 
 _vp = C.c_void_p
@@ -65,6 +67,28 @@ class TrainParams(C.Structure):
 
 class TrainGrads(C.Structure):
     _fields_ = [(f, _vp) for f in _TRAIN_FIELDS if f != "pos"]
+
+
+class RmsNormArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("type", C.c_int32), ("gain_type", C.c_int32), ("eps", C.c_float),
+                ("code_type", C.c_int32), ("group", C.c_int32), ("x", _vp), ("ldx", C.c_int64), ("res", _vp),
+                ("ldres", C.c_int64), ("gain", _vp), ("h", _vp), ("ldh", C.c_int64), ("y", _vp), ("ldy", C.c_int64),
+                ("codes", _vp), ("ldcodes", C.c_int64), ("alpha", _vp)]
+
+
+class RmsNormGradArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("type", C.c_int32), ("gain_type", C.c_int32), ("eps", C.c_float),
+                ("h", _vp), ("ldh", C.c_int64), ("dy", _vp), ("lddy", C.c_int64), ("dres", _vp), ("lddres", C.c_int64),
+                ("gain", _vp), ("dh", _vp), ("lddh", C.c_int64), ("dgain", _vp)]
+
+
+class Tensor(C.Structure):
+    _fields_ = [("data", _vp), ("count", C.c_int64), ("type", C.c_int32)]
+
+
+class AdamOptions(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("max_norm", C.c_double), ("lr_device", _vp)]
 
 
 class AecctError(RuntimeError):
@@ -135,6 +159,25 @@ def lib():
         L.aecct_train_grad.restype = C.c_int
         L.aecct_train_grad.argtypes = [_vp, C.POINTER(TrainParams), _vp, _vp, C.c_int64, C.POINTER(TrainGrads), _vp,
                                        _vp, C.c_size_t, _vp]
+        L.aecct_rms_norm.restype = C.c_int
+        L.aecct_rms_norm.argtypes = [C.POINTER(RmsNormArgs), _vp]
+        L.aecct_rms_norm_grad_workspace_size.restype = C.c_int
+        L.aecct_rms_norm_grad_workspace_size.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
+        L.aecct_rms_norm_grad.restype = C.c_int
+        L.aecct_rms_norm_grad.argtypes = [C.POINTER(RmsNormGradArgs), _vp, C.c_size_t, _vp]
+        _tp = C.POINTER(Tensor)
+        L.aecct_update_workspace_size.restype = C.c_int
+        L.aecct_update_workspace_size.argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
+        L.aecct_grad_norm.restype = C.c_int
+        L.aecct_grad_norm.argtypes = [_tp, C.c_int32, _vp, _vp, C.c_size_t, _vp]
+        L.aecct_grad_clip.restype = C.c_int
+        L.aecct_grad_clip.argtypes = [_tp, _tp, C.c_int32, C.c_double, _vp, _vp, C.c_size_t, _vp]
+        L.aecct_adam_step.restype = C.c_int
+        L.aecct_adam_step.argtypes = [_tp, _tp, _tp, _tp, _tp, C.c_int32, C.POINTER(AdamOptions), _vp, _vp, _vp, C.c_size_t,
+                                      _vp]
+        _gp = C.POINTER(TrainGrads)
+        L.aecct_train_update.restype = C.c_int
+        L.aecct_train_update.argtypes = [_vp, _gp, _gp, _gp, _gp, C.POINTER(AdamOptions), _vp, _vp, _vp, C.c_size_t, _vp]
         L.aecct_check_device_arith.restype = C.c_int
         L.aecct_check_device_arith.argtypes = [C.POINTER(C.c_uint64)]
         _lib = L
@@ -236,6 +279,266 @@ def _stream_ptr(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _stream_scope(stream, device):
+    """Context in which new tensors belong to `stream` (None: the current one).  The tensors' device must be the
+    current one: the library launches there."""
+    import contextlib
+    import torch
+    if device.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
+def _dtype_code(t):
+    import torch
+    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"unsupported type {t.dtype}: float32, bfloat16 or float16")
+    return code
+
+
+def _rows_of(t, like, what):
+    """(address, row stride) of a tensor of rows [..., d] shaped like `like`, on its device."""
+    if t is None:
+        return None, 0
+    if t.shape != like.shape or t.device != like.device:
+        raise ValueError(f"{what} must have the shape {tuple(like.shape)} and the device {like.device}")
+    d = t.shape[-1]
+    if t.dim() == 2:
+        if t.stride(1) != 1 and d > 1:
+            raise ValueError(f"{what}: a row's values must be contiguous")
+        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: rows of more than two dimensions must be contiguous")
+    return t.data_ptr(), d
+
+
+def _gain_of(gain, like):
+    if gain is None:
+        return None, F32
+    if gain.shape != like.shape[-1:] or not gain.is_contiguous() or gain.device != like.device:
+        raise ValueError(f"gain must be {like.shape[-1]} contiguous values on {like.device}")
+    return gain.data_ptr(), _dtype_code(gain)
+
+
+def _same_type(like, **tensors):
+    for what, t in tensors.items():
+        if t is not None and t.dtype != like.dtype:
+            raise ValueError(f"{what} must be {like.dtype}")
+
+
+def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes=None, alpha=None, with_y: bool = True,
+             code_type=None, group: int = 0, stream=None):
+    """Root-mean-square norm of rows with the residual's addition: h = x + res, y = h / sqrt(mean(h^2) + eps) * gain, and
+    y's 8-bit codes (Eq. 2) with their alphas, one for a row or for `group` (32, 64 or 128) columns.
+
+    x, res: CUDA tensors [..., d] of one type (float32, bfloat16, float16); gain [d] float32 or that type.  code_type:
+    None, torch.int8 (value = code * alpha / 127) or torch.float8_e4m3fn (value = code * alpha / 448).  y, h, codes,
+    alpha: outputs to write to, else new tensors (h or y may be x or res itself).
+    Returns (y, h, codes, alpha), None where there is no such output: y without with_y, h without res."""
+    import torch
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be [..., d] with d >= 1")
+    d = x.shape[-1]
+    rows = x.numel() // d
+    kind = {None: CODE_NONE, torch.int8: CODE_I8, torch.float8_e4m3fn: CODE_E4M3}.get(code_type)
+    if kind is None:
+        raise ValueError("code_type must be None, torch.int8 or torch.float8_e4m3fn")
+    if kind == CODE_NONE and (codes is not None or alpha is not None or group):
+        raise ValueError("codes, alpha and group need a code_type")
+    if group not in (0, 32, 64, 128):
+        raise ValueError("group must be 0, 32, 64 or 128")
+    _same_type(x, res=res, y=y, h=h)
+    with _stream_scope(stream, x.device):
+        if y is None and with_y:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if h is None and res is not None:
+            h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if kind != CODE_NONE:
+            shape = x.shape[:-1] + ((d + group - 1) // group,) if group else x.shape[:-1]
+            if codes is None:
+                codes = torch.empty(x.shape, dtype=code_type, device=x.device)
+            elif codes.dtype != code_type:
+                raise ValueError(f"codes must be {code_type}")
+            if alpha is None:
+                alpha = torch.empty(shape, dtype=torch.float32, device=x.device)
+            elif alpha.shape != shape or alpha.dtype != torch.float32 or not alpha.is_contiguous() or alpha.device != x.device:
+                raise ValueError(f"alpha must be contiguous float32 {tuple(shape)} on {x.device}")
+        a = RmsNormArgs(rows, d, _dtype_code(x), 0, eps, kind, group)
+        a.x, a.ldx = _rows_of(x, x, "x")
+        a.res, a.ldres = _rows_of(res, x, "res")
+        a.gain, a.gain_type = _gain_of(gain, x)
+        a.h, a.ldh = _rows_of(h, x, "h")
+        a.y, a.ldy = _rows_of(y, x, "y")
+        a.codes, a.ldcodes = _rows_of(codes, x, "codes")
+        a.alpha = alpha.data_ptr() if alpha is not None else None
+        _check(lib().aecct_rms_norm(C.byref(a), _stream_ptr(stream)), "aecct_rms_norm")
+    return y, h, codes, alpha
+
+
+def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dgain=None, with_dgain: bool = True, stream=None):
+    """Gradient of rms_norm: h as the norm read it (x, or the h it returned), dy the gradient of y (or of the codes'
+    values), dres the gradient that reaches h along the residual.  Returns (dh, dgain): dh is the gradient of x and
+    of res, dgain float32 [d] (None without with_dgain)."""
+    import torch
+    if h.dim() < 1 or h.shape[-1] < 1:
+        raise ValueError("h must be [..., d] with d >= 1")
+    d = h.shape[-1]
+    rows = h.numel() // d
+    _same_type(h, dy=dy, dres=dres, dh=dh)
+    with _stream_scope(stream, h.device):
+        if dh is None:
+            dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        ws, need = None, 0
+        if dgain is not None and (dgain.shape != (d,) or dgain.dtype != torch.float32 or not dgain.is_contiguous()
+                                  or dgain.device != h.device):
+            raise ValueError(f"dgain must be {d} contiguous float32 values on {h.device}")
+        if with_dgain or dgain is not None:
+            size = C.c_size_t()
+            _check(lib().aecct_rms_norm_grad_workspace_size(rows, d, C.byref(size)), "aecct_rms_norm_grad_workspace_size")
+            need = size.value
+            ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+            if dgain is None:
+                dgain = torch.empty(d, dtype=torch.float32, device=h.device)
+        a = RmsNormGradArgs(rows, d, _dtype_code(h), 0, eps)
+        a.h, a.ldh = _rows_of(h, h, "h")
+        a.dy, a.lddy = _rows_of(dy, h, "dy")
+        a.dres, a.lddres = _rows_of(dres, h, "dres")
+        a.gain, a.gain_type = _gain_of(gain, h)
+        a.dh, a.lddh = _rows_of(dh, h, "dh")
+        a.dgain = dgain.data_ptr() if dgain is not None else None
+        _check(lib().aecct_rms_norm_grad(C.byref(a), ws.data_ptr() if ws is not None else None, need, _stream_ptr(stream)),
+               "aecct_rms_norm_grad")
+    return dh, dgain
+
+
+class TensorList:
+    """A list of contiguous CUDA tensors (float32, bfloat16, float16; one device) as the library takes it.  A program that
+    uses the same tensors again and again keeps the list; the calls below take any sequence of tensors too."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        self.array = (Tensor * n)()
+        self.device = self.tensors[0].device if n else None
+        for i, t in enumerate(self.tensors):
+            if not t.is_contiguous():
+                raise ValueError(f"tensor {i} must be contiguous")
+            if t.device != self.device or t.device.type != "cuda":
+                raise ValueError("the tensors must be on one GPU")
+            self.array[i] = Tensor(t.data_ptr(), t.numel(), _dtype_code(t))
+        size = C.c_size_t()
+        _check(lib().aecct_update_workspace_size(n, C.byref(size)), "aecct_update_workspace_size")
+        self.workspace_bytes = size.value
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _list(tensors):
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _update_device(*lists):
+    import torch
+    found = {t.device for t in lists if t is not None and t.device is not None}
+    if len(found) > 1:
+        raise ValueError("the lists must be on one GPU")
+    return found.pop() if found else torch.device("cuda", torch.cuda.current_device())
+
+
+def grad_norm(grads, stream=None):
+    """The norm over every value of a list of tensors (a TensorList or any sequence): one-element float32 tensor."""
+    import torch
+    g = _list(grads)
+    device = _update_device(g)
+    with _stream_scope(stream, device):
+        norm = torch.empty(1, dtype=torch.float32, device=device)
+        ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
+        _check(lib().aecct_grad_norm(g.array, len(g), norm.data_ptr(), ws.data_ptr(), g.workspace_bytes,
+                                     _stream_ptr(stream)), "aecct_grad_norm")
+    return norm
+
+
+def grad_clip(grads, max_norm: float, out=None, stream=None):
+    """Scales every gradient by min(1, max_norm / norm), in place or into the tensors of `out`; returns the norm before
+    clipping.  Where it is not finite the values stay unscaled."""
+    import torch
+    g = _list(grads)
+    o = None if out is None else _list(out)
+    if o is not None and len(o) != len(g):
+        raise ValueError(f"out must hold {len(g)} tensors")
+    device = _update_device(g, o)
+    with _stream_scope(stream, device):
+        norm = torch.empty(1, dtype=torch.float32, device=device)
+        ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
+        _check(lib().aecct_grad_clip(g.array, None if o is None else o.array, len(g), max_norm, norm.data_ptr(),
+                                     ws.data_ptr(), g.workspace_bytes, _stream_ptr(stream)), "aecct_grad_clip")
+    return norm
+
+
+def _adam_options(lr, betas, eps, weight_decay, max_norm):
+    lr_device = None
+    if hasattr(lr, "data_ptr"):
+        import torch
+        if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device.type != "cuda":
+            raise ValueError("lr must be a number or one float32 value on the GPU")
+        lr_device, lr = lr.data_ptr(), 0.0
+    return AdamOptions(lr, betas[0], betas[1], eps, weight_decay, 0.0 if max_norm is None else max_norm, lr_device)
+
+
+def _step_tensor(step, device):
+    import torch
+    if step is None:
+        return torch.zeros(1, dtype=torch.int64, device=device)
+    if step.dtype != torch.int64 or step.numel() != 1 or step.device != device:
+        raise ValueError(f"step must be one int64 value on {device}")
+    return step
+
+
+class Adam:
+    """Adam over a list of float32 tensors (Section 6), updated in place: moments m and v (zeros, or the given float32
+    tensors), the number of updates made in `step` (one int64 value on the GPU), decoupled weight decay, gradients
+    clipped to max_norm over the whole list (None: not), and optional 16-bit `copies` of the parameters.
+    lr: a number, or one float32 value on the GPU that captured graphs read at each replay."""
+
+    def __init__(self, params, lr=1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, max_norm=None,
+                 m=None, v=None, step=None, copies=None):
+        import torch
+        self.params = _list(params)
+        self.m = _list(m if m is not None else [torch.zeros_like(p) for p in self.params.tensors])
+        self.v = _list(v if v is not None else [torch.zeros_like(p) for p in self.params.tensors])
+        self.copies = None if copies is None else _list(copies)
+        for what, t in (("m", self.m), ("v", self.v), ("copies", self.copies)):
+            if t is not None and len(t) != len(self.params):
+                raise ValueError(f"{what} must hold {len(self.params)} tensors")
+        self.device = _update_device(self.params, self.m, self.v, self.copies)
+        self.lr, self.betas, self.eps, self.weight_decay, self.max_norm = lr, betas, eps, weight_decay, max_norm
+        self.step_count = _step_tensor(step, self.device)
+
+    def step(self, grads, lr=None, stream=None):
+        """One update from the gradients (a TensorList or any sequence, any of the types).  Returns the norm before
+        clipping (None without max_norm); where it is not finite nothing is updated."""
+        import torch
+        g = _list(grads)
+        if len(g) != len(self.params):
+            raise ValueError(f"grads must hold {len(self.params)} tensors")
+        _update_device(self.params, g)
+        opt = _adam_options(self.lr if lr is None else lr, self.betas, self.eps, self.weight_decay, self.max_norm)
+        with _stream_scope(stream, self.device):
+            norm = None if self.max_norm is None else torch.empty(1, dtype=torch.float32, device=self.device)
+            ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=self.device)
+            _check(lib().aecct_adam_step(self.params.array, self.m.array, self.v.array, g.array,
+                                         None if self.copies is None else self.copies.array, len(g), C.byref(opt),
+                                         self.step_count.data_ptr(), None if norm is None else norm.data_ptr(),
+                                         ws.data_ptr(), g.workspace_bytes, _stream_ptr(stream)), "aecct_adam_step")
+        return norm
 
 
 class Decoder:
@@ -491,3 +794,36 @@ class Trainer:
         _check(lib().aecct_train_grad(self._h, C.byref(tp), _ptr(y), _ptr(xs), B, C.byref(tg), _ptr(loss),
                                       _ptr(self._ws), self._ws.numel(), _stream_ptr(stream)), "aecct_train_grad")
         return loss, grads
+
+    def update_state(self, params: dict):
+        """A fresh Adam state for `update`: dict with the moments m and v (shaped like params, zeros) and the step."""
+        import torch
+        zeros = lambda: {k: (torch.zeros_like(t) if k not in ("w", "b") else {kk: torch.zeros_like(tt) for kk, tt in t.items()})  # noqa: E731
+                         for k, t in params.items() if k != "pos" and t is not None}
+        return {"m": zeros(), "v": zeros(), "step": _step_tensor(None, params["embed"].device)}
+
+    def update(self, params: dict, grads: dict, state: dict, lr, betas=(0.9, 0.999), eps: float = 1e-8,
+               weight_decay: float = 0.0, max_norm=None, stream=None):
+        """One Adam update of every parameter from `grad`'s gradients (aecct_train_update), in place.  Returns the norm
+        of the gradients before clipping (None without max_norm); where it is not finite nothing is updated."""
+        import torch
+        opt = _adam_options(lr, betas, eps, weight_decay, max_norm)
+        fields = [f for f, _ in TrainGrads._fields_]
+        lists = []
+        shapes = self._flat(params)
+        for d in (params, state["m"], state["v"], grads):
+            flat = self._flat(d)
+            for f in fields:
+                if flat[f].dtype != torch.float32 or flat[f].numel() != shapes[f].numel():
+                    raise ValueError(f"{f} must be float32, {shapes[f].numel()} values")
+            lists.append(TrainGrads(**{f: _ptr(flat[f]) for f in fields}))
+        device = params["embed"].device
+        with _stream_scope(stream, device):
+            norm = None if max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
+            size = C.c_size_t()
+            _check(lib().aecct_update_workspace_size(len(fields), C.byref(size)), "aecct_update_workspace_size")
+            ws = torch.empty(size.value, dtype=torch.uint8, device=device)
+            _check(lib().aecct_train_update(self._h, *[C.byref(t) for t in lists], C.byref(opt), state["step"].data_ptr(),
+                                            None if norm is None else norm.data_ptr(), ws.data_ptr(), size.value,
+                                            _stream_ptr(stream)), "aecct_train_update")
+        return norm

@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaecct.so")
 SOURCES = ["host.cpp", "host_fused.cpp", "aap.cpp", "kernels_layered.hip", "kernel_fused.hip", "arith_check.hip", "spe.hip",
-           "train.hip", "train_host.cpp"]
+           "train.hip", "train_host.cpp", "norm.hip", "norm_host.cpp", "update.hip", "update_host.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wno-unused-function",

@@ -391,4 +391,28 @@ aecct_status aecct_train_grad(const aecct_trainer *tr, const aecct_train_params 
   return AECCT_OK;
 }
 
+aecct_status aecct_train_update(const aecct_trainer *tr, const aecct_train_grads *params, const aecct_train_grads *m,
+                                const aecct_train_grads *v, const aecct_train_grads *grads, const aecct_adam_options *opt,
+                                int64_t *step, float *norm, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!tr || !params || !m || !v || !grads) return AECCT_ERR_INVALID_ARG;
+  int cur = -1;
+  if (hipGetDevice(&cur) != hipSuccess) return AECCT_ERR_DEVICE;
+  if (cur != tr->device) return AECCT_ERR_INVALID_ARG;
+  const int64_t L = tr->L, d = tr->d, N = tr->N, dff = tr->dff, n = tr->n;
+  // the tensors in the order of the struct
+  const int64_t counts[] = {L * d, N * d * d, N * d * d, N * d * d, N * d * d, N * d * dff, N * dff * d, N * 6,
+                            N * d, N * d, N * d, N * d, N * dff, N * d, N * d, N * d, N * d, N * d,
+                            d, 1, L * n, n};
+  constexpr int kTensors = sizeof(counts) / sizeof(counts[0]);
+  static_assert(sizeof(aecct_train_grads) == kTensors * sizeof(float *), "one pointer a tensor");
+  aecct_tensor t[4][kTensors];
+  const aecct_train_grads *const lists[4] = {params, m, v, grads};
+  for (int l = 0; l < 4; ++l) {
+    float *ptr[kTensors];
+    std::memcpy(ptr, lists[l], sizeof(ptr));
+    for (int i = 0; i < kTensors; ++i) t[l][i] = aecct_tensor{ptr[i], counts[i], AECCT_F32};
+  }
+  return aecct_adam_step(t[0], t[1], t[2], t[3], nullptr, kTensors, opt, step, norm, workspace, workspace_bytes, stream);
+}
+
 }  // extern "C"
