@@ -19,10 +19,11 @@ __device__ __forceinline__ double block_sum(double v, double *lds) {
   return v;
 }
 
-// The tensor that unit u belongs to.
+// The tensor of unit u, from that of an earlier unit.
 template <int N>
-__device__ __forceinline__ int tensor_of(const Units<N> &t, int u) {
-  int lo = 0, hi = t.n - 1;
+__device__ __forceinline__ int tensor_of(const Units<N> &t, int u, int k) {
+  if (u < t.unit0[k + 1]) return k;
+  int lo = k + 1, hi = t.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
     if (t.unit0[mid] <= u) lo = mid;
@@ -31,25 +32,53 @@ __device__ __forceinline__ int tensor_of(const Units<N> &t, int u) {
   return lo;
 }
 
-__device__ __forceinline__ float load_typed(const void *p, int type, int64_t i) {
-  return type == 0 ? ((const float *)p)[i] : type == 1 ? (float)((const bf16_t *)p)[i] : (float)((const f16_t *)p)[i];
+// Four values of any type; n of them are there.
+__device__ __forceinline__ void load4(const void *p, int type, int64_t i, int64_t n, float (&f)[4]) {
+  const int k = n >= 4 ? 4 : (int)n;
+  if (type == 0) load_part<float, 4>((const float *)p + i, k, f);
+  else if (type == 1) load_part<bf16_t, 4>((const bf16_t *)p + i, k, f);
+  else load_part<f16_t, 4>((const f16_t *)p + i, k, f);
 }
-__device__ __forceinline__ void store_typed(void *p, int type, int64_t i, float v) {
-  if (type == 0) ((float *)p)[i] = v;
-  else if (type == 1) ((bf16_t *)p)[i] = (bf16_t)v;
-  else ((f16_t *)p)[i] = (f16_t)v;
+__device__ __forceinline__ void store4(void *p, int type, int64_t i, int64_t n, const float (&f)[4]) {
+  const int k = n >= 4 ? 4 : (int)n;
+  if (type == 0) store_part<float, 4>((float *)p + i, k, f);
+  else if (type == 1) store_part<bf16_t, 4>((bf16_t *)p + i, k, f);
+  else store_part<f16_t, 4>((f16_t *)p + i, k, f);
+}
+
+constexpr int kSteps = kUnit / (4 * kThreads);   // of four values a thread in a unit
+
+// Sum of squares of a unit's values from i0 on, n in all: 16 bytes a load.
+template <class T>
+__device__ __forceinline__ double unit_squares(const T *g, int64_t n) {
+  constexpr int V = 16 / sizeof(T), J = kUnit / (V * kThreads);
+  float f[J][V];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int i = (j * kThreads + (int)threadIdx.x) * V;
+    load_part<T, V>(g + i, n - i >= V ? V : (int)(n - i), f[j]);
+  }
+  double s = 0, q = 0;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      s += (double)f[j][i] * (double)f[j][i];
+      q += (double)f[j][i + 1] * (double)f[j][i + 1];
+    }
+  return s + q;
 }
 
 __global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable t, double *part) {
   __shared__ double lds[kThreads / 64];
   double s = 0;
+  int k = 0;
   for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
-    const int k = tensor_of(t, u);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit, n = t.count[k];
-    for (int64_t i = i0 + threadIdx.x; i < i0 + kUnit && i < n; i += kThreads) {
-      const double g = load_typed(t.g[k], t.type[k], i);
-      s += g * g;
-    }
+    k = tensor_of(t, u, k);
+    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit, n = t.count[k] - i0;
+    if (t.type[k] == 0) s += unit_squares((const float *)t.g[k] + i0, n);
+    else if (t.type[k] == 1) s += unit_squares((const bf16_t *)t.g[k] + i0, n);
+    else s += unit_squares((const f16_t *)t.g[k] + i0, n);
   }
   s = block_sum(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -78,11 +107,19 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable t, const double *pa
   const double n = norm_of(part, parts, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
   const float f = clip_factor(n, max_norm);
+  int k = 0;
   for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
-    const int k = tensor_of(t, u);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit, c = t.count[k];
-    for (int64_t i = i0 + threadIdx.x; i < i0 + kUnit && i < c; i += kThreads)
-      store_typed(t.out[k], t.out_type[k], i, load_typed(t.g[k], t.type[k], i) * f);
+    k = tensor_of(t, u, k);
+    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit + 4 * threadIdx.x, c = t.count[k];
+    float g[kSteps][4];
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) load4(t.g[k], t.type[k], i0 + 4 * kThreads * j, c - i0 - 4 * kThreads * j, g[j]);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[j][i] *= f;
+      store4(t.out[k], t.out_type[k], i0 + 4 * kThreads * j, c - i0 - 4 * kThreads * j, g[j]);
+    }
   }
 }
 
@@ -104,18 +141,30 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable t, const double *pa
   const float size = (float)(lr / (1 - pow(o.beta1, (double)now))), root = (float)(1 / sqrt(1 - pow(o.beta2, (double)now)));
   const float b1 = (float)o.beta1, c1 = (float)(1 - o.beta1), b2 = (float)o.beta2, c2 = (float)(1 - o.beta2);
   const float decay = (float)(lr * o.weight_decay), eps = (float)o.eps;
+  int k = 0;
   for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
-    const int k = tensor_of(t, u);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit, c = t.count[k];
-    for (int64_t i = i0 + threadIdx.x; i < i0 + kUnit && i < c; i += kThreads) {
-      const float g = load_typed(t.g[k], t.type[k], i) * f;
-      const float m = fmaf(b1, t.m[k][i], c1 * g), v = fmaf(b2, t.v[k][i], c2 * (g * g));
-      const float p0 = t.p[k][i];
-      const float p = p0 - fmaf(decay, p0, size * m / fmaf(sqrtf(v), root, eps));
-      t.m[k][i] = m;
-      t.v[k][i] = v;
-      t.p[k][i] = p;
-      if (t.copy[k]) store_typed(t.copy[k], t.copy_type[k], i, p);
+    k = tensor_of(t, u, k);
+    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit + 4 * threadIdx.x, c = t.count[k];
+#pragma unroll 2
+    for (int j = 0; j < kSteps; ++j) {
+      const int64_t at = i0 + 4 * kThreads * j, left = c - at;
+      const int n = left >= 4 ? 4 : (int)left;
+      float g[4], p[4], m[4], v[4];
+      load4(t.g[k], t.type[k], at, left, g);
+      load_part<float, 4>(t.p[k] + at, n, p);
+      load_part<float, 4>(t.m[k] + at, n, m);
+      load_part<float, 4>(t.v[k] + at, n, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = g[i] * f;
+        m[i] = fmaf(b1, m[i], c1 * x);
+        v[i] = fmaf(b2, v[i], c2 * (x * x));
+        p[i] -= fmaf(decay, p[i], size * m[i] / fmaf(sqrtf(v[i]), root, eps));
+      }
+      store_part<float, 4>(t.m[k] + at, n, m);
+      store_part<float, 4>(t.v[k] + at, n, v);
+      store_part<float, 4>(t.p[k] + at, n, p);
+      if (t.copy[k]) store4(t.copy[k], t.copy_type[k], at, left, p);
     }
   }
 }
