@@ -281,56 +281,58 @@ def _stream_ptr(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _stream_scope(stream, device):
-    """Context in which new tensors belong to `stream` (None: the current one).  The tensors' device must be the
-    current one: the library launches there."""
-    import contextlib
+def _on_stream(stream):
+    """Context in which torch's allocations and the library's launches belong to `stream`."""
     import torch
-    if device.type != "cuda":
-        raise ValueError("tensors must be on the GPU")
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    if stream is None:
-        return contextlib.nullcontext()
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
-def _dtype_code(t):
+def _on_current_gpu(index: int):
+    """Refuses tensors of another GPU than the current one, where the library launches (index: get_device())."""
     import torch
-    code = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(t.dtype)
+    if index < 0:
+        raise ValueError("tensors must be on the GPU")
+    if index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+_DTYPES: dict = {}
+
+
+def _dtype_code(t):
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"unsupported type {t.dtype}: float32, bfloat16 or float16")
     return code
 
 
-def _rows_of(t, like, what):
+def _rows_of(t, like, dtype, what):
     """(address, row stride) of a tensor of rows [..., d] shaped like `like`, on its device."""
     if t is None:
         return None, 0
-    if t.shape != like.shape or t.device != like.device:
-        raise ValueError(f"{what} must have the shape {tuple(like.shape)} and the device {like.device}")
-    d = t.shape[-1]
-    if t.dim() == 2:
-        if t.stride(1) != 1 and d > 1:
+    shape = t.shape
+    if shape != like.shape or t.get_device() != like.get_device() or t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(like.shape)} on {like.device}")
+    d = shape[-1]
+    if len(shape) == 2:
+        ld, one = t.stride()
+        if one != 1 and d > 1:
             raise ValueError(f"{what}: a row's values must be contiguous")
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
+        return t.data_ptr(), ld if shape[0] > 1 else d
     if not t.is_contiguous():
-        raise ValueError(f"{what}: rows of more than two dimensions must be contiguous")
+        raise ValueError(f"{what}: rows of other than two dimensions must be contiguous")
     return t.data_ptr(), d
 
 
 def _gain_of(gain, like):
     if gain is None:
         return None, F32
-    if gain.shape != like.shape[-1:] or not gain.is_contiguous() or gain.device != like.device:
+    if gain.shape != like.shape[-1:] or not gain.is_contiguous() or gain.get_device() != like.get_device():
         raise ValueError(f"gain must be {like.shape[-1]} contiguous values on {like.device}")
     return gain.data_ptr(), _dtype_code(gain)
-
-
-def _same_type(like, **tensors):
-    for what, t in tensors.items():
-        if t is not None and t.dtype != like.dtype:
-            raise ValueError(f"{what} must be {like.dtype}")
 
 
 def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes=None, alpha=None, with_y: bool = True,
@@ -343,42 +345,53 @@ def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes
     alpha: outputs to write to, else new tensors (h or y may be x or res itself).
     Returns (y, h, codes, alpha), None where there is no such output: y without with_y, h without res."""
     import torch
-    if x.dim() < 1 or x.shape[-1] < 1:
+    if stream is not None:
+        with _on_stream(stream):
+            return rms_norm(x, gain, res, eps, y=y, h=h, codes=codes, alpha=alpha, with_y=with_y, code_type=code_type,
+                            group=group)
+    shape = x.shape
+    if not shape or shape[-1] < 1:
         raise ValueError("x must be [..., d] with d >= 1")
-    d = x.shape[-1]
-    rows = x.numel() // d
-    kind = {None: CODE_NONE, torch.int8: CODE_I8, torch.float8_e4m3fn: CODE_E4M3}.get(code_type)
-    if kind is None:
+    d, dtype = shape[-1], x.dtype
+    kind = CODE_NONE if code_type is None else CODE_I8 if code_type == torch.int8 else \
+        CODE_E4M3 if code_type == torch.float8_e4m3fn else -1
+    if kind < 0:
         raise ValueError("code_type must be None, torch.int8 or torch.float8_e4m3fn")
     if kind == CODE_NONE and (codes is not None or alpha is not None or group):
         raise ValueError("codes, alpha and group need a code_type")
     if group not in (0, 32, 64, 128):
         raise ValueError("group must be 0, 32, 64 or 128")
-    _same_type(x, res=res, y=y, h=h)
-    with _stream_scope(stream, x.device):
-        if y is None and with_y:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if h is None and res is not None:
-            h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if kind != CODE_NONE:
-            shape = x.shape[:-1] + ((d + group - 1) // group,) if group else x.shape[:-1]
-            if codes is None:
-                codes = torch.empty(x.shape, dtype=code_type, device=x.device)
-            elif codes.dtype != code_type:
-                raise ValueError(f"codes must be {code_type}")
-            if alpha is None:
-                alpha = torch.empty(shape, dtype=torch.float32, device=x.device)
-            elif alpha.shape != shape or alpha.dtype != torch.float32 or not alpha.is_contiguous() or alpha.device != x.device:
-                raise ValueError(f"alpha must be contiguous float32 {tuple(shape)} on {x.device}")
-        a = RmsNormArgs(rows, d, _dtype_code(x), 0, eps, kind, group)
-        a.x, a.ldx = _rows_of(x, x, "x")
-        a.res, a.ldres = _rows_of(res, x, "res")
-        a.gain, a.gain_type = _gain_of(gain, x)
-        a.h, a.ldh = _rows_of(h, x, "h")
-        a.y, a.ldy = _rows_of(y, x, "y")
-        a.codes, a.ldcodes = _rows_of(codes, x, "codes")
-        a.alpha = alpha.data_ptr() if alpha is not None else None
-        _check(lib().aecct_rms_norm(C.byref(a), _stream_ptr(stream)), "aecct_rms_norm")
+    _on_current_gpu(x.get_device())
+    px, ldx = _rows_of(x, x, dtype, "x")
+    pres, ldres = _rows_of(res, x, dtype, "res")
+    pgain, gain_type = _gain_of(gain, x)
+    if y is None and with_y:
+        y = x.new_empty(shape)
+        py, ldy = y.data_ptr(), d
+    else:
+        py, ldy = _rows_of(y, x, dtype, "y")
+    if h is None and res is not None:
+        h = x.new_empty(shape)
+        ph, ldh = h.data_ptr(), d
+    else:
+        ph, ldh = _rows_of(h, x, dtype, "h")
+    pcodes, ldcodes, palpha = None, 0, None
+    if kind != CODE_NONE:
+        if codes is None:
+            codes = x.new_empty(shape, dtype=code_type)
+            pcodes, ldcodes = codes.data_ptr(), d
+        else:
+            pcodes, ldcodes = _rows_of(codes, x, code_type, "codes")
+        scales = shape[:-1] + ((d + group - 1) // group,) if group else shape[:-1]
+        if alpha is None:
+            alpha = x.new_empty(scales, dtype=torch.float32)
+        elif alpha.shape != scales or alpha.dtype != torch.float32 or not alpha.is_contiguous() \
+                or alpha.get_device() != x.get_device():
+            raise ValueError(f"alpha must be contiguous float32 {tuple(scales)} on {x.device}")
+        palpha = alpha.data_ptr()
+    a = RmsNormArgs(x.numel() // d, d, _dtype_code(x), gain_type, eps, kind, group, px, ldx, pres, ldres, pgain, ph, ldh, py,
+                    ldy, pcodes, ldcodes, palpha)
+    _check(lib().aecct_rms_norm(C.byref(a), _stream_ptr(None)), "aecct_rms_norm")
     return y, h, codes, alpha
 
 
@@ -387,34 +400,40 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
     values), dres the gradient that reaches h along the residual.  Returns (dh, dgain): dh is the gradient of x and
     of res, dgain float32 [d] (None without with_dgain)."""
     import torch
-    if h.dim() < 1 or h.shape[-1] < 1:
+    if stream is not None:
+        with _on_stream(stream):
+            return rms_norm_grad(h, dy, gain, dres, eps, dh=dh, dgain=dgain, with_dgain=with_dgain)
+    shape = h.shape
+    if not shape or shape[-1] < 1:
         raise ValueError("h must be [..., d] with d >= 1")
-    d = h.shape[-1]
+    d, dtype = shape[-1], h.dtype
     rows = h.numel() // d
-    _same_type(h, dy=dy, dres=dres, dh=dh)
-    with _stream_scope(stream, h.device):
-        if dh is None:
-            dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        ws, need = None, 0
-        if dgain is not None and (dgain.shape != (d,) or dgain.dtype != torch.float32 or not dgain.is_contiguous()
-                                  or dgain.device != h.device):
+    _on_current_gpu(h.get_device())
+    ph, ldh = _rows_of(h, h, dtype, "h")
+    pdy, lddy = _rows_of(dy, h, dtype, "dy")
+    pres, lddres = _rows_of(dres, h, dtype, "dres")
+    pgain, gain_type = _gain_of(gain, h)
+    if dh is None:
+        dh = h.new_empty(shape)
+        pdh, lddh = dh.data_ptr(), d
+    else:
+        pdh, lddh = _rows_of(dh, h, dtype, "dh")
+    pdgain = pws = None
+    need = 0
+    if dgain is not None or with_dgain:
+        if dgain is None:
+            dgain = h.new_empty((d,), dtype=torch.float32)
+        elif dgain.shape != (d,) or dgain.dtype != torch.float32 or not dgain.is_contiguous() \
+                or dgain.get_device() != h.get_device():
             raise ValueError(f"dgain must be {d} contiguous float32 values on {h.device}")
-        if with_dgain or dgain is not None:
-            size = C.c_size_t()
-            _check(lib().aecct_rms_norm_grad_workspace_size(rows, d, C.byref(size)), "aecct_rms_norm_grad_workspace_size")
-            need = size.value
-            ws = torch.empty(need, dtype=torch.uint8, device=h.device)
-            if dgain is None:
-                dgain = torch.empty(d, dtype=torch.float32, device=h.device)
-        a = RmsNormGradArgs(rows, d, _dtype_code(h), 0, eps)
-        a.h, a.ldh = _rows_of(h, h, "h")
-        a.dy, a.lddy = _rows_of(dy, h, "dy")
-        a.dres, a.lddres = _rows_of(dres, h, "dres")
-        a.gain, a.gain_type = _gain_of(gain, h)
-        a.dh, a.lddh = _rows_of(dh, h, "dh")
-        a.dgain = dgain.data_ptr() if dgain is not None else None
-        _check(lib().aecct_rms_norm_grad(C.byref(a), ws.data_ptr() if ws is not None else None, need, _stream_ptr(stream)),
-               "aecct_rms_norm_grad")
+        pdgain = dgain.data_ptr()
+        size = C.c_size_t()
+        _check(lib().aecct_rms_norm_grad_workspace_size(rows, d, C.byref(size)), "aecct_rms_norm_grad_workspace_size")
+        need = size.value
+        ws = h.new_empty((need,), dtype=torch.uint8)
+        pws = ws.data_ptr()
+    a = RmsNormGradArgs(rows, d, _dtype_code(h), gain_type, eps, ph, ldh, pdy, lddy, pres, lddres, pgain, pdh, lddh, pdgain)
+    _check(lib().aecct_rms_norm_grad(C.byref(a), pws, need, _stream_ptr(None)), "aecct_rms_norm_grad")
     return dh, dgain
 
 
@@ -426,11 +445,11 @@ class TensorList:
         self.tensors = list(tensors)
         n = len(self.tensors)
         self.array = (Tensor * n)()
-        self.device = self.tensors[0].device if n else None
+        self.device = self.tensors[0].get_device() if n else None
         for i, t in enumerate(self.tensors):
             if not t.is_contiguous():
                 raise ValueError(f"tensor {i} must be contiguous")
-            if t.device != self.device or t.device.type != "cuda":
+            if t.get_device() != self.device or self.device < 0:
                 raise ValueError("the tensors must be on one GPU")
             self.array[i] = Tensor(t.data_ptr(), t.numel(), _dtype_code(t))
         size = C.c_size_t()
@@ -445,24 +464,33 @@ def _list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
-def _update_device(*lists):
+def _one_gpu(*lists):
+    """The GPU of the lists, which must be the current one."""
     import torch
-    found = {t.device for t in lists if t is not None and t.device is not None}
-    if len(found) > 1:
-        raise ValueError("the lists must be on one GPU")
-    return found.pop() if found else torch.device("cuda", torch.cuda.current_device())
+    index = None
+    for t in lists:
+        if t is not None and t.device is not None:
+            if index is not None and t.device != index:
+                raise ValueError("the lists must be on one GPU")
+            index = t.device
+    if index is None:
+        return torch.cuda.current_device()
+    _on_current_gpu(index)
+    return index
 
 
 def grad_norm(grads, stream=None):
     """The norm over every value of a list of tensors (a TensorList or any sequence): one-element float32 tensor."""
     import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return grad_norm(grads)
     g = _list(grads)
-    device = _update_device(g)
-    with _stream_scope(stream, device):
-        norm = torch.empty(1, dtype=torch.float32, device=device)
-        ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
-        _check(lib().aecct_grad_norm(g.array, len(g), norm.data_ptr(), ws.data_ptr(), g.workspace_bytes,
-                                     _stream_ptr(stream)), "aecct_grad_norm")
+    device = _one_gpu(g)
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
+    _check(lib().aecct_grad_norm(g.array, len(g), norm.data_ptr(), ws.data_ptr(), g.workspace_bytes, _stream_ptr(None)),
+           "aecct_grad_norm")
     return norm
 
 
@@ -470,16 +498,18 @@ def grad_clip(grads, max_norm: float, out=None, stream=None):
     """Scales every gradient by min(1, max_norm / norm), in place or into the tensors of `out`; returns the norm before
     clipping.  Where it is not finite the values stay unscaled."""
     import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return grad_clip(grads, max_norm, out)
     g = _list(grads)
     o = None if out is None else _list(out)
     if o is not None and len(o) != len(g):
         raise ValueError(f"out must hold {len(g)} tensors")
-    device = _update_device(g, o)
-    with _stream_scope(stream, device):
-        norm = torch.empty(1, dtype=torch.float32, device=device)
-        ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
-        _check(lib().aecct_grad_clip(g.array, None if o is None else o.array, len(g), max_norm, norm.data_ptr(),
-                                     ws.data_ptr(), g.workspace_bytes, _stream_ptr(stream)), "aecct_grad_clip")
+    device = _one_gpu(g, o)
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
+    _check(lib().aecct_grad_clip(g.array, None if o is None else o.array, len(g), max_norm, norm.data_ptr(), ws.data_ptr(),
+                                 g.workspace_bytes, _stream_ptr(None)), "aecct_grad_clip")
     return norm
 
 
@@ -487,18 +517,18 @@ def _adam_options(lr, betas, eps, weight_decay, max_norm):
     lr_device = None
     if hasattr(lr, "data_ptr"):
         import torch
-        if lr.dtype != torch.float32 or lr.numel() != 1 or lr.device.type != "cuda":
-            raise ValueError("lr must be a number or one float32 value on the GPU")
+        if lr.dtype != torch.float32 or lr.numel() != 1 or lr.get_device() != torch.cuda.current_device():
+            raise ValueError("lr must be a number or one float32 value on the current GPU")
         lr_device, lr = lr.data_ptr(), 0.0
     return AdamOptions(lr, betas[0], betas[1], eps, weight_decay, 0.0 if max_norm is None else max_norm, lr_device)
 
 
-def _step_tensor(step, device):
+def _step_tensor(step, device: int):
     import torch
     if step is None:
         return torch.zeros(1, dtype=torch.int64, device=device)
-    if step.dtype != torch.int64 or step.numel() != 1 or step.device != device:
-        raise ValueError(f"step must be one int64 value on {device}")
+    if step.dtype != torch.int64 or step.numel() != 1 or step.get_device() != device:
+        raise ValueError(f"step must be one int64 value on cuda:{device}")
     return step
 
 
@@ -518,7 +548,7 @@ class Adam:
         for what, t in (("m", self.m), ("v", self.v), ("copies", self.copies)):
             if t is not None and len(t) != len(self.params):
                 raise ValueError(f"{what} must hold {len(self.params)} tensors")
-        self.device = _update_device(self.params, self.m, self.v, self.copies)
+        self.device = _one_gpu(self.params, self.m, self.v, self.copies)
         self.lr, self.betas, self.eps, self.weight_decay, self.max_norm = lr, betas, eps, weight_decay, max_norm
         self.step_count = _step_tensor(step, self.device)
 
@@ -526,18 +556,20 @@ class Adam:
         """One update from the gradients (a TensorList or any sequence, any of the types).  Returns the norm before
         clipping (None without max_norm); where it is not finite nothing is updated."""
         import torch
+        if stream is not None:
+            with _on_stream(stream):
+                return self.step(grads, lr)
         g = _list(grads)
         if len(g) != len(self.params):
             raise ValueError(f"grads must hold {len(self.params)} tensors")
-        _update_device(self.params, g)
+        device = _one_gpu(self.params, g) if len(g) else self.device
         opt = _adam_options(self.lr if lr is None else lr, self.betas, self.eps, self.weight_decay, self.max_norm)
-        with _stream_scope(stream, self.device):
-            norm = None if self.max_norm is None else torch.empty(1, dtype=torch.float32, device=self.device)
-            ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=self.device)
-            _check(lib().aecct_adam_step(self.params.array, self.m.array, self.v.array, g.array,
-                                         None if self.copies is None else self.copies.array, len(g), C.byref(opt),
-                                         self.step_count.data_ptr(), None if norm is None else norm.data_ptr(),
-                                         ws.data_ptr(), g.workspace_bytes, _stream_ptr(stream)), "aecct_adam_step")
+        norm = None if self.max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
+        ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
+        _check(lib().aecct_adam_step(self.params.array, self.m.array, self.v.array, g.array,
+                                     None if self.copies is None else self.copies.array, len(g), C.byref(opt),
+                                     self.step_count.data_ptr(), None if norm is None else norm.data_ptr(), ws.data_ptr(),
+                                     g.workspace_bytes, _stream_ptr(None)), "aecct_adam_step")
         return norm
 
 
@@ -800,30 +832,33 @@ class Trainer:
         import torch
         zeros = lambda: {k: (torch.zeros_like(t) if k not in ("w", "b") else {kk: torch.zeros_like(tt) for kk, tt in t.items()})  # noqa: E731
                          for k, t in params.items() if k != "pos" and t is not None}
-        return {"m": zeros(), "v": zeros(), "step": _step_tensor(None, params["embed"].device)}
+        return {"m": zeros(), "v": zeros(), "step": _step_tensor(None, params["embed"].get_device())}
 
     def update(self, params: dict, grads: dict, state: dict, lr, betas=(0.9, 0.999), eps: float = 1e-8,
                weight_decay: float = 0.0, max_norm=None, stream=None):
         """One Adam update of every parameter from `grad`'s gradients (aecct_train_update), in place.  Returns the norm
         of the gradients before clipping (None without max_norm); where it is not finite nothing is updated."""
         import torch
+        if stream is not None:
+            with _on_stream(stream):
+                return self.update(params, grads, state, lr, betas, eps, weight_decay, max_norm)
         opt = _adam_options(lr, betas, eps, weight_decay, max_norm)
         fields = [f for f, _ in TrainGrads._fields_]
         lists = []
-        shapes = self._flat(params)
-        for d in (params, state["m"], state["v"], grads):
-            flat = self._flat(d)
+        flat = [self._flat(d) for d in (params, state["m"], state["v"], grads)]
+        device = params["embed"].get_device()
+        _on_current_gpu(device)
+        for d in flat:
             for f in fields:
-                if flat[f].dtype != torch.float32 or flat[f].numel() != shapes[f].numel():
-                    raise ValueError(f"{f} must be float32, {shapes[f].numel()} values")
-            lists.append(TrainGrads(**{f: _ptr(flat[f]) for f in fields}))
-        device = params["embed"].device
-        with _stream_scope(stream, device):
-            norm = None if max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
-            size = C.c_size_t()
-            _check(lib().aecct_update_workspace_size(len(fields), C.byref(size)), "aecct_update_workspace_size")
-            ws = torch.empty(size.value, dtype=torch.uint8, device=device)
-            _check(lib().aecct_train_update(self._h, *[C.byref(t) for t in lists], C.byref(opt), state["step"].data_ptr(),
-                                            None if norm is None else norm.data_ptr(), ws.data_ptr(), size.value,
-                                            _stream_ptr(stream)), "aecct_train_update")
+                if d[f].dtype != torch.float32 or d[f].numel() != flat[0][f].numel() or d[f].get_device() != device:
+                    raise ValueError(f"{f} must be float32, {flat[0][f].numel()} values on cuda:{device}")
+            lists.append(TrainGrads(*[_ptr(d[f]) for f in fields]))
+        step = _step_tensor(state["step"], device)
+        norm = None if max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
+        size = C.c_size_t()
+        _check(lib().aecct_update_workspace_size(len(fields), C.byref(size)), "aecct_update_workspace_size")
+        ws = torch.empty(size.value, dtype=torch.uint8, device=device)
+        _check(lib().aecct_train_update(self._h, *[C.byref(t) for t in lists], C.byref(opt), step.data_ptr(),
+                                        None if norm is None else norm.data_ptr(), ws.data_ptr(), size.value,
+                                        _stream_ptr(None)), "aecct_train_update")
         return norm

@@ -70,14 +70,21 @@ __device__ __forceinline__ bool in_range(float s) { return s >= 1e-24f && s <= 1
 // two first, `unit`, and by a second that takes rho into [1, 2), so that products with h stay in range; h rho is
 // unchanged and the rho of the row as it was is rho unit.
 __device__ __forceinline__ float far_up(float ss) { return in_range(ss) ? 1.0f : ss < 1.0f ? 0x1p100f : 0x1p-100f; }
-__device__ __forceinline__ float far_rho_of(float ss, float up, int d, float eps, float &more) {
-  const float rho = (float)(1.0 / sqrt((double)ss / d + (double)eps * up * up));
-  const int e = rho > 0 && rho < __builtin_inff() ? __builtin_amdgcn_frexp_expf(rho) - 1 : 0;
-  more = ldexpf(1.0f, e);
-  return ldexpf(rho, -e);
+__device__ __forceinline__ float far_rho_of(float ss, float up, float inv_d, float eps, float &more) {
+  float rho;
+  int e = 0;
+  if (up > 1.0f && eps >= 1e-30f) {   // eps up^2 would overflow: the mean as it was, to which tiny squares add little
+    rho = __builtin_amdgcn_rsqf(fmaf(ss * 0x1p-100f * 0x1p-100f, inv_d, eps));
+    e = -100;
+  } else {
+    rho = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps * up * up));
+  }
+  const int k = rho > 0 && rho < __builtin_inff() ? __builtin_amdgcn_frexp_expf(rho) - 1 : 0;
+  more = ldexpf(1.0f, e + k);
+  return ldexpf(rho, -k);
 }
 template <int TPR, int N>
-__device__ __forceinline__ float far_rho(float ss, float (&h)[N], int d, float eps, float &unit, float2 *lds) {
+__device__ __forceinline__ float far_rho(float ss, float (&h)[N], float inv_d, float eps, float &unit, float2 *lds) {
   const float up = far_up(ss);
   float none = 0;
   ss = 0;
@@ -88,7 +95,7 @@ __device__ __forceinline__ float far_rho(float ss, float (&h)[N], int d, float e
   }
   row_join<Sum, TPR>(ss, none, lds);
   float more;
-  const float rho = far_rho_of(ss, up, d, eps, more);
+  const float rho = far_rho_of(ss, up, inv_d, eps, more);
 #pragma unroll
   for (int i = 0; i < N; ++i) h[i] *= more;
   unit = up * more;
@@ -107,6 +114,68 @@ __device__ __forceinline__ void load_gain(const void *gain, bool f32, int c, int
   }
 }
 
+// Where a thread's columns lie: vector j starts at column col(j).  A row of d = V k + tail values ends in a vector of
+// `tail` values, the jt-th of one lane; only that lane runs the code for single values, once for all j.
+template <int V, int TPR, int NV>
+struct Columns {
+  int d, lane, tail, jt;
+  bool last;   // this lane holds the short vector
+  __device__ __forceinline__ Columns(int d, int lane)
+      : d(d), lane(lane), tail(d % V), jt(d / V / TPR), last(tail && d / V % TPR == lane) {}
+  __device__ __forceinline__ int col(int j) const { return (j * TPR + lane) * V; }
+  __device__ __forceinline__ bool full(int j) const { return col(j) + V <= d; }
+  template <class T>
+  __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      v[j] = Raw<T, V>{};
+      if (live && full(j)) load_raw<T, V>(p + col(j), v[j]);
+    }
+    if (live && last) {
+      Raw<T, V> t;
+      load_raw_part<T, V>(p + col(jt), tail, t);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (j == jt) v[j] = t;
+    }
+  }
+  template <class T, class F>   // f(j, v): the V values of vector j
+  __device__ __forceinline__ void store(T *p, bool live, F f) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[V];
+      f(j, v);
+      if (live && full(j)) store_vec<T, V>(p + col(j), v);
+      if (live && last && j == jt) store_part<T, V>(p + col(j), tail, v);
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ void gain(const void *p, bool f32, float (&g)[NV * V]) const {
+    if (!p) {
+#pragma unroll
+      for (int i = 0; i < NV * V; ++i) g[i] = 1.0f;
+    } else if (f32) {
+      Raw<float, V> v[NV];
+      load<float>((const float *)p, true, v);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) unpack<float, V>(v[j], (float (&)[V])g[j * V]);
+    } else {
+      Raw<T, V> v[NV];
+      load<T>((const T *)p, true, v);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) unpack<T, V>(v[j], (float (&)[V])g[j * V]);
+    }
+  }
+};
+
+// Which of a block's rows this thread works on; one row a wavefront or a block is told to the compiler as such.
+template <int TPR, int BLOCK>
+__device__ __forceinline__ int row_of_block() {
+  if constexpr (TPR == BLOCK) return 0;
+  else if constexpr (TPR == 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  else return threadIdx.x / TPR;
+}
+
 // ---- codes -----------------------------------------------------------------------------------------------------
 // code = round(p Q / A) with p = h gain and A = max |p|: rho is a factor of both y and alpha and drops out.  The quotient
 // is taken as (p + e)(q + q1), e the rounding error of p, q a near quotient Q / A and q1 its remainder's: a code then
@@ -123,9 +192,8 @@ __device__ __forceinline__ CodeScale code_scale(float A, float most) {
   return s;
 }
 template <int V>
-__device__ __forceinline__ void store_codes(uint8_t *to, int n, int code, float A, const float *h, const float *g) {
+__device__ __forceinline__ void codes_of(int code, float A, const float *h, const float *g, uint32_t (&w)[V / 4]) {
   const CodeScale s = code_scale(A, code == 1 ? 127.0f : 448.0f);
-  uint32_t w[V / 4];
   float v[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -146,6 +214,9 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, int code, float 
       w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], lo, true);
     }
   }
+}
+template <int V>
+__device__ __forceinline__ void store_codes(uint8_t *to, int n, const uint32_t (&w)[V / 4]) {
   if (n >= V) {
     __builtin_memcpy(to, w, V);
   } else {
@@ -156,76 +227,83 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, int code, float 
 }
 
 // ---- the norm ---------------------------------------------------------------------------------------------------
-template <class T, int TPR, int NV, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void k_rms_norm(NormRows a) {
+// A block takes every gridDim.x-th of its sets of rows; the next one's inputs are read before the present one is joined
+// and written (loads issued ahead of the stores, so that waiting for them does not wait for the stores).
+template <class T, int TPR, int NV, int BLOCK, int WAVES>
+__global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR;
   __shared__ float2 lds[BLOCK / 64];
-  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR, sub = row_of_block<TPR, BLOCK>();
   const float inv_d = 1.0f / (float)a.d;
+  const Columns<V, TPR, NV> cols(a.d, lane);
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  Raw<T, V> nx[NV], nres[NV];
+  const auto fetch = [&](int64_t r) {
+    cols.load((const T *)a.x + r * a.ldx, r < a.rows, nx);
+    if (a.res) cols.load((const T *)a.res + r * a.ldres, r < a.rows, nres);
+  };
+  fetch((int64_t)blockIdx.x * RPB + sub);
   float g[NV * V];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (j * TPR + lane) * V;
-    load_gain<T, V>(a.gain, a.gain_f32, c, a.d - c, (float (&)[V])g[j * V]);
-  }
-  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
+  cols.template gain<T>(a.gain, a.gain_f32, g);
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + sub;
     const bool live = r < a.rows;
     float h[NV * V];
     float ss = 0, A = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, n = live ? a.d - c : 0;
       float (&v)[V] = (float (&)[V])h[j * V];
-      load_part<T, V>((const T *)a.x + r * a.ldx + c, n, v);
+      unpack<T, V>(nx[j], v);
       if (a.res) {
         float w[V];
-        load_part<T, V>((const T *)a.res + r * a.ldres + c, n, w);
+        unpack<T, V>(nres[j], w);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] += w[i];
       }
     }
+    if (r0 + step < a.rows) fetch(r + step);
+    if (a.h)
+      cols.store((T *)a.h + r * a.ldh, live, [&](int j, float (&v)[V]) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, n = live ? a.d - c : 0;
-      float (&v)[V] = (float (&)[V])h[j * V];
-      if (a.h) store_part<T, V>((T *)a.h + r * a.ldh + c, n, v);
+        for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
+      });
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        ss = fmaf(v[i], v[i], ss);
-        A = Max::join(A, fabsf(v[i] * g[j * V + i]));
-      }
+    for (int i = 0; i < NV * V; ++i) {
+      ss = fmaf(h[i], h[i], ss);
+      A = Max::join(A, fabsf(h[i] * g[i]));
     }
     row_join<Max, TPR>(ss, A, lds);
     float rho = near_rho(ss, inv_d, a.eps);
     if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
       float unit, none = 0;
-      rho = far_rho<TPR>(ss, h, a.d, a.eps, unit, lds);
+      rho = far_rho<TPR>(ss, h, inv_d, a.eps, unit, lds);
       A = 0;
 #pragma unroll
       for (int i = 0; i < NV * V; ++i) A = Max::join(A, fabsf(h[i] * g[i]));
       row_join<Max, TPR>(none, A, lds);
     }
+    if (a.y)
+      cols.store((T *)a.y + r * a.ldy, live, [&](int j, float (&v)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = h[j * V + i] * g[j * V + i] * rho;
+      });
+    if (!a.code) continue;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, n = live ? a.d - c : 0;
-      if (a.y) {
-        float y[V];
+      const int c = cols.col(j);
+      float B = A;
+      if (a.alphas > 1) {
+        B = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = h[j * V + i] * g[j * V + i] * rho;
-        store_part<T, V>((T *)a.y + r * a.ldy + c, n, y);
+        for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
+        B = lanes_join<Max>(B, a.group / V);
       }
-      if (a.code) {
-        float B = A;
-        if (a.alphas > 1) {
-          B = 0;
-#pragma unroll
-          for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
-          B = lanes_join<Max>(B, a.group / V);
-        }
-        store_codes<V>(a.codes + r * a.ldcodes + c, n, a.code, B, h + j * V, g + j * V);
-        if (n > 0 && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
-      }
+      uint32_t w[V / 4];
+      codes_of<V>(a.code, B, h + j * V, g + j * V, w);
+      uint8_t *to = a.codes + r * a.ldcodes + c;
+      if (live && cols.full(j)) __builtin_memcpy(to, w, V);
+      if (live && cols.last && j == cols.jt) store_codes<V>(to, cols.tail, w);
+      if (live && c < a.d && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
     }
   }
 }
@@ -272,7 +350,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
     if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
       up = far_up(ss);
       sums(up, 1.0f);
-      rho = far_rho_of(ss, up, a.d, a.eps, more);
+      rho = far_rho_of(ss, up, inv_d, a.eps, more);
       sums(up, more);
     }
     // every thread of a wavefront takes part in a group's maximum: columns past the row are zeros
@@ -298,7 +376,9 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
           for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[i] * g[i]));
           B = lanes_join<Max>(B, a.group / V);
         }
-        store_codes<V>(a.codes + r * a.ldcodes + c, n, a.code, B, h, g);
+        uint32_t w[V / 4];
+        codes_of<V>(a.code, B, h, g, w);
+        store_codes<V>(a.codes + r * a.ldcodes + c, n, w);
         if (n > 0 && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
       }
     }
@@ -307,31 +387,37 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
 
 // ---- its gradient ------------------------------------------------------------------------------------------------
 // Block b sums dy xh over its rows per column and leaves the sums in part[b].
-template <class T, int TPR, int NV, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void k_rms_norm_grad(NormGradRows a) {
+template <class T, int TPR, int NV, int BLOCK, int WAVES>
+__global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR, N = NV * V;
   __shared__ float2 lds[BLOCK / 64];
-  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR, sub = row_of_block<TPR, BLOCK>();
   const float inv_d = 1.0f / (float)a.d;
+  const Columns<V, TPR, NV> cols(a.d, lane);
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  Raw<T, V> nh[NV], ndy[NV];
+  const auto fetch = [&](int64_t r) {
+    cols.load((const T *)a.h + r * a.ldh, r < a.rows, nh);
+    cols.load((const T *)a.dy + r * a.lddy, r < a.rows, ndy);
+  };
+  fetch((int64_t)blockIdx.x * RPB + sub);
   float g[N], dg[N];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (j * TPR + lane) * V;
-    load_gain<T, V>(a.gain, a.gain_f32, c, a.d - c, (float (&)[V])g[j * V]);
-  }
+  cols.template gain<T>(a.gain, a.gain_f32, g);
 #pragma unroll
   for (int i = 0; i < N; ++i) dg[i] = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + sub;
     const bool live = r < a.rows;
     float h[N], dy[N];
+    Raw<T, V> res[NV];
     float ss = 0, dot = 0;
+    if (a.dres) cols.load((const T *)a.dres + r * a.lddres, live, res);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, n = live ? a.d - c : 0;
-      load_part<T, V>((const T *)a.h + r * a.ldh + c, n, (float (&)[V])h[j * V]);
-      load_part<T, V>((const T *)a.dy + r * a.lddy + c, n, (float (&)[V])dy[j * V]);
+      unpack<T, V>(nh[j], (float (&)[V])h[j * V]);
+      unpack<T, V>(ndy[j], (float (&)[V])dy[j * V]);
     }
+    if (r0 + step < a.rows) fetch(r + step);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       ss = fmaf(h[i], h[i], ss);
@@ -341,7 +427,7 @@ __global__ __launch_bounds__(BLOCK) void k_rms_norm_grad(NormGradRows a) {
     float rho = near_rho(ss, inv_d, a.eps), unit = 1.0f;
     if (!in_range(ss) || !(fabsf(dot) <= 1e37f)) {
       float none = 0;
-      rho = far_rho<TPR>(ss, h, a.d, a.eps, unit, lds);
+      rho = far_rho<TPR>(ss, h, inv_d, a.eps, unit, lds);
       dot = 0;
 #pragma unroll
       for (int i = 0; i < N; ++i) dot = fmaf(dy[i] * g[i], h[i], dot);
@@ -349,26 +435,20 @@ __global__ __launch_bounds__(BLOCK) void k_rms_norm_grad(NormGradRows a) {
     }
     const float m = dot * rho * inv_d, rho1 = rho * unit;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V, n = live ? a.d - c : 0;
-      float o[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int k = j * V + i;
-        const float xh = h[k] * rho;
-        if (live) dg[k] = fmaf(dy[k], xh, dg[k]);
-        o[i] = rho1 * fmaf(-m, xh, dy[k] * g[k]);
-      }
-      if (a.dh) {
-        if (a.dres) {
-          float w[V];
-          load_part<T, V>((const T *)a.dres + r * a.lddres + c, n, w);
-#pragma unroll
-          for (int i = 0; i < V; ++i) o[i] += w[i];
-        }
-        store_part<T, V>((T *)a.dh + r * a.lddh + c, n, o);
-      }
+    for (int i = 0; i < N; ++i) {
+      h[i] *= rho;
+      if (live) dg[i] = fmaf(dy[i], h[i], dg[i]);
     }
+    if (a.dh)
+      cols.store((T *)a.dh + r * a.lddh, live, [&](int j, float (&o)[V]) {
+        float w[V];
+        if (a.dres) unpack<T, V>(res[j], w);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          o[i] = rho1 * fmaf(-m, h[j * V + i], dy[j * V + i] * g[j * V + i]);
+          if (a.dres) o[i] += w[i];
+        }
+      });
   }
   if (!a.part) return;
   if constexpr (RPB > 1) {   // the block's rows in a fixed order
@@ -384,11 +464,10 @@ __global__ __launch_bounds__(BLOCK) void k_rms_norm_grad(NormGradRows a) {
       a.part[(int64_t)blockIdx.x * a.d + c] = s;
     }
   } else {
+    cols.store(a.part + (int64_t)blockIdx.x * a.d, true, [&](int j, float (&v)[V]) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = (j * TPR + lane) * V;
-      store_part<float, V>(a.part + (int64_t)blockIdx.x * a.d + c, a.d - c, (float (&)[V])dg[j * V]);
-    }
+      for (int i = 0; i < V; ++i) v[i] = dg[j * V + i];
+    });
   }
 }
 
@@ -425,7 +504,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
     if (!in_range(ss) || !(fabsf(dot) <= 1e37f)) {
       up = far_up(ss);
       sums(up, 1.0f);
-      rho = far_rho_of(ss, up, a.d, a.eps, more);
+      rho = far_rho_of(ss, up, inv_d, a.eps, more);
       sums(up, more);
     }
     const float m = dot * rho * inv_d, rho1 = rho * (up * more);
@@ -462,19 +541,21 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
   }
 }
 
-// dgain[c] = the sum of `rows` partial rows: 16 columns a block, 16 threads a column, thread k the rows k, k + 16, ...
-__global__ __launch_bounds__(256) void k_rms_norm_dgain(const float *part, int rows, int d, float *dgain) {
-  __shared__ float lds[256];
+// dgain[c] = the sum of `rows` partial rows: 16 columns a block, 64 threads a column, thread k the rows k, k + 64, ...
+__global__ __launch_bounds__(1024) void k_rms_norm_dgain(const float *part, int rows, int d, float *dgain) {
+  __shared__ float lds[1024];
   const int c = blockIdx.x * 16 + threadIdx.x % 16;
   float s = 0;
-  if (c < d)
-    for (int r = threadIdx.x / 16; r < rows; r += 16) s += part[(int64_t)r * d + c];
-  lds[threadIdx.x] = s;
-  __syncthreads();
-  if (threadIdx.x < 16 && c < d) {
-    for (int k = 1; k < 16; ++k) s += lds[16 * k + threadIdx.x];
-    dgain[c] = s;
+  if (c < d) {
+#pragma unroll 4
+    for (int r = threadIdx.x / 16; r < rows; r += 64) s += part[(int64_t)r * d + c];
   }
+  lds[threadIdx.x] = s;
+  for (int half = 512; half >= 16; half /= 2) {
+    __syncthreads();
+    if (threadIdx.x < half) lds[threadIdx.x] += lds[threadIdx.x + half];
+  }
+  if (threadIdx.x < 16 && c < d) dgain[c] = lds[threadIdx.x];
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
@@ -489,9 +570,9 @@ hipError_t by_width(int d, const F &f) {
   if (n <= 128) return f.template run<64, 2, 256>();
   if (n <= 256) return f.template run<256, 1, 256>();
   if (n <= 512) return f.template run<256, 2, 256>();
-  if (n <= 1024) return f.template run<256, 4, 256>();
+  if (n <= 1024) return f.template run<512, 2, 512>();
   if (n <= 2048) return f.template run<1024, 2, 1024>();
-  if constexpr (V == 4) {
+  if constexpr (V == 4 && F::kDeep) {
     if (n <= 4096) return f.template run<1024, 4, 1024>();
   }
   return f.wide();
@@ -499,13 +580,15 @@ hipError_t by_width(int d, const F &f) {
 
 template <class T>
 struct NormLaunch {
+  static constexpr bool kDeep = true;
   const NormRows &a;
   int cu_count;
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR), most = (int64_t)cu_count * (2048 / BLOCK);
-    k_rms_norm<T, TPR, NV, BLOCK><<<(unsigned)(blocks < most ? blocks : most), BLOCK, 0, s>>>(a);
+    constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 ? 6 : 4;   // wavefronts a SIMD
+    const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR), most = (int64_t)cu_count * (W * 256 / BLOCK);
+    k_rms_norm<T, TPR, NV, BLOCK, W><<<(unsigned)(blocks < most ? blocks : most), BLOCK, 0, s>>>(a);
     return hipGetLastError();
   }
   hipError_t wide() const {
@@ -518,16 +601,18 @@ struct NormLaunch {
 constexpr int kPartRows = 1024;
 template <class T>
 struct NormGradLaunch {
+  static constexpr bool kDeep = false;   // four vectors of each input and the sums do not fit 128 registers
   const NormGradRows &a;
   int cu_count;
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
+    constexpr int V = 16 / sizeof(T), W = NV * V <= 8 ? 5 : 4;
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
-    int64_t most = (int64_t)cu_count * (1024 / BLOCK);
+    int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);
     if (most > kPartRows) most = kPartRows;
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-    if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK><<<grid, BLOCK, 0, s>>>(a);
+    if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK, W><<<grid, BLOCK, 0, s>>>(a);
     return dgain(grid);
   }
   hipError_t wide() const {
@@ -537,7 +622,7 @@ struct NormGradLaunch {
     return dgain(grid);
   }
   hipError_t dgain(unsigned rows) const {
-    if (a.part) k_rms_norm_dgain<<<(a.d + 15) / 16, 256, 0, s>>>(a.part, (int)rows, a.d, a.dgain);
+    if (a.part) k_rms_norm_dgain<<<(a.d + 15) / 16, 1024, 0, s>>>(a.part, (int)rows, a.d, a.dgain);
     return hipGetLastError();
   }
 };

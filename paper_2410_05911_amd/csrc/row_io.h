@@ -19,19 +19,54 @@ struct alignas(sizeof(T)) Vec {
 };
 
 template <class T, int V>
-__device__ __forceinline__ void load_vec(const T *p, float (&f)[V]) {
-  Vec<T, V> t;
-  __builtin_memcpy(&t, p, sizeof(t));
-#pragma unroll
-  for (int i = 0; i < V; ++i) f[i] = (float)t.v[i];
-}
-
-template <class T, int V>
 __device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
   Vec<T, V> t;
 #pragma unroll
   for (int i = 0; i < V; ++i) t.v[i] = (T)f[i];
   __builtin_memcpy(p, &t, sizeof(t));
+}
+
+// The same in two steps, for values that are read ahead: as stored, two 16-bit values a register, then as fp32.
+template <class T, int V>
+struct Raw {
+  uint32_t w[V * sizeof(T) / 4];
+};
+template <class T, int V>
+__device__ __forceinline__ void load_raw(const T *p, Raw<T, V> &r) {
+  __builtin_memcpy(r.w, p, sizeof(r.w));
+}
+template <class T, int V>   // the first n < V values, the others 0
+__device__ __forceinline__ void load_raw_part(const T *p, int n, Raw<T, V> &r) {
+#pragma unroll
+  for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) {
+    if constexpr (sizeof(T) == 4) {
+      r.w[i] = i < n ? ((const uint32_t *)p)[i] : 0u;
+    } else {
+      const uint16_t *q = (const uint16_t *)p;
+      const uint32_t lo = 2 * i < n ? q[2 * i] : 0u, hi = 2 * i + 1 < n ? q[2 * i + 1] : 0u;
+      r.w[i] = lo | hi << 16;
+    }
+  }
+}
+template <class T, int V>
+__device__ __forceinline__ void unpack(const Raw<T, V> &r, float (&f)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      f[i] = __builtin_bit_cast(float, r.w[i]);
+    } else if constexpr (__is_same(T, bf16_t)) {
+      f[i] = __builtin_bit_cast(float, i % 2 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+    } else {
+      f[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)(r.w[i / 2] >> (16 * (i % 2))));
+    }
+  }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void load_vec(const T *p, float (&f)[V]) {
+  Raw<T, V> r;
+  load_raw<T, V>(p, r);
+  unpack<T, V>(r, f);
 }
 
 // The first `n` (clamped to 0..V) of V values; the others are 0 (load) or left alone (store).

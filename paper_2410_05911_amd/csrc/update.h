@@ -8,48 +8,54 @@
 
 namespace aecct {
 
-// A list is cut into units of kUnit values, none of which spans two tensors; a launch takes the tensors of one
-// table, passed by value.  Tensor i has units unit0[i] .. unit0[i + 1).
+// A list is cut into units of kUnit values, none of which spans two ranges; a launch takes the ranges of one table,
+// passed by value.  A range is a tensor, or tensors that lie back to back.  Range i has units unit0[i] .. unit0[i + 1).
+// The most ranges of a table keep it below 4 KB; tables of up to kFew are passed in a shorter form.
 constexpr int kUnit = 4096;
-constexpr int kSumTensors = 160, kClipTensors = 96, kAdamTensors = 56;
+constexpr int kFew = 24, kSumRanges = 160, kClipRanges = 96, kAdamRanges = 56;
 constexpr int kMaxSumBlocks = 2048;
 
 template <int N>
 struct Units {
-  int n;                  // tensors
+  static constexpr int kMost = N;
+  int n;                  // ranges
   int unit0[N + 1];
   int64_t count[N];
-  uint8_t type[N];        // of the tensor read (aecct_dtype)
+  uint8_t type[N];        // of the values read (aecct_dtype)
 };
-struct SumTable : Units<kSumTensors> {
-  const void *g[kSumTensors];
+template <int N>
+struct SumTable : Units<N> {
+  const void *g[N];
 };
-struct ClipTable : Units<kClipTensors> {
-  const void *g[kClipTensors];
-  void *out[kClipTensors];
-  uint8_t out_type[kClipTensors];
+template <int N>
+struct ClipTable : Units<N> {
+  const void *g[N];
+  void *out[N];
+  uint8_t out_type[N];
 };
-struct AdamTable : Units<kAdamTensors> {
-  const void *g[kAdamTensors];
-  float *p[kAdamTensors], *m[kAdamTensors], *v[kAdamTensors];
-  void *copy[kAdamTensors];
-  uint8_t copy_type[kAdamTensors];
+template <int N>
+struct AdamTable : Units<N> {
+  const void *g[N];
+  float *p[N], *m[N], *v[N];
+  void *copy[N];
+  uint8_t copy_type[N];
 };
 struct AdamScalars {
   double lr, beta1, beta2, eps, weight_decay, max_norm;
   const float *lr_device;
 };
 
-// Sums of squares of the table's tensors, one double a block, to part[0 .. blocks).
-hipError_t launch_sum_squares(const SumTable &t, double *part, int blocks, hipStream_t s);
+// Sums of squares of the table's values, one double a block, to part[0 .. blocks); with step, *next = *step + 1.
+hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, const int64_t *step, int64_t *next,
+                              hipStream_t s);
 // *norm from `parts` sums.
 hipError_t launch_norm(const double *part, int parts, float *norm, hipStream_t s);
-hipError_t launch_clip(const ClipTable &t, const double *part, int parts, double max_norm, float *norm, int cu_count,
-                       hipStream_t s);
+hipError_t launch_clip(const ClipTable<kClipRanges> &t, const double *part, int parts, double max_norm, float *norm,
+                       int cu_count, hipStream_t s);
 // *next = *step + 1
 hipError_t launch_next_step(const int64_t *step, int64_t *next, hipStream_t s);
 // parts = 0: no norm.  step (of one launch of a call, else null) and norm (may be null) are written.
-hipError_t launch_adam(const AdamTable &t, const double *part, int parts, const AdamScalars &o, const int64_t *next,
-                       int64_t *step, float *norm, int cu_count, hipStream_t s);
+hipError_t launch_adam(const AdamTable<kAdamRanges> &t, const double *part, int parts, const AdamScalars &o,
+                       const int64_t *next, int64_t *step, float *norm, int cu_count, hipStream_t s);
 
 }  // namespace aecct

@@ -69,8 +69,10 @@ __device__ __forceinline__ double unit_squares(const T *g, int64_t n) {
   return s + q;
 }
 
-__global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable t, double *part) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable<N> t, double *part, const int64_t *step, int64_t *next) {
   __shared__ double lds[kThreads / 64];
+  if (step && blockIdx.x == 0 && threadIdx.x == 0) *next = *step + 1;
   double s = 0;
   int k = 0;
   for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
@@ -87,7 +89,13 @@ __global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable t, double *pa
 // The norm from the blocks' sums; every block that asks gets the same bits.
 __device__ __forceinline__ double norm_of(const double *part, int parts, double *lds) {
   double s = 0;
-  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  for (int i = threadIdx.x; i < parts; i += 8 * kThreads) {   // eight loads in flight: this is all latency
+    double v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = i + j * kThreads < parts ? part[i + j * kThreads] : 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[j];
+  }
   return sqrt(block_sum(s, lds));
 }
 
@@ -102,7 +110,8 @@ __device__ __forceinline__ float clip_factor(double norm, double max_norm) {
   return norm > max_norm && norm <= 1.7976931348623157e308 ? (float)(max_norm / norm) : 1.0f;
 }
 
-__global__ __launch_bounds__(kThreads) void k_clip(ClipTable t, const double *part, int parts, double max_norm, float *norm) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double *part, int parts, double max_norm, float *norm) {
   __shared__ double lds[kThreads / 64];
   const double n = norm_of(part, parts, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
@@ -125,7 +134,8 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable t, const double *pa
 
 __global__ void k_next_step(const int64_t *step, int64_t *next) { *next = *step + 1; }
 
-__global__ __launch_bounds__(kThreads) void k_adam(AdamTable t, const double *part, int parts, AdamScalars o,
+template <int N>
+__global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double *part, int parts, AdamScalars o,
                                                    const int64_t *next, int64_t *step, float *norm) {
   __shared__ double lds[kThreads / 64];
   float f = 1.0f;
@@ -171,28 +181,74 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable t, const double *pa
 
 int grid_of(int units, int most) { return units < 1 ? 1 : units < most ? units : most; }
 
+// The shorter form of a table of at most kFew ranges.
+template <int N>
+void few(const Units<N> &t, Units<kFew> &f) {
+  f.n = t.n;
+  for (int i = 0; i <= t.n; ++i) f.unit0[i] = t.unit0[i];
+  for (int i = 0; i < t.n; ++i) {
+    f.count[i] = t.count[i];
+    f.type[i] = t.type[i];
+  }
+}
+
 }  // namespace
 
-hipError_t launch_sum_squares(const SumTable &t, double *part, int blocks, hipStream_t s) {
-  k_sum_squares<<<blocks, kThreads, 0, s>>>(t, part);
+hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, const int64_t *step, int64_t *next,
+                              hipStream_t s) {
+  if (t.n <= kFew) {
+    SumTable<kFew> f;
+    few(t, f);
+    for (int i = 0; i < t.n; ++i) f.g[i] = t.g[i];
+    k_sum_squares<<<blocks, kThreads, 0, s>>>(f, part, step, next);
+  } else {
+    k_sum_squares<<<blocks, kThreads, 0, s>>>(t, part, step, next);
+  }
   return hipGetLastError();
 }
 hipError_t launch_norm(const double *part, int parts, float *norm, hipStream_t s) {
   k_norm<<<1, kThreads, 0, s>>>(part, parts, norm);
   return hipGetLastError();
 }
-hipError_t launch_clip(const ClipTable &t, const double *part, int parts, double max_norm, float *norm, int cu_count,
-                       hipStream_t s) {
-  k_clip<<<grid_of(t.unit0[t.n], 8 * cu_count), kThreads, 0, s>>>(t, part, parts, max_norm, norm);
+hipError_t launch_clip(const ClipTable<kClipRanges> &t, const double *part, int parts, double max_norm, float *norm,
+                       int cu_count, hipStream_t s) {
+  const int grid = grid_of(t.unit0[t.n], 8 * cu_count);
+  if (t.n <= kFew) {
+    ClipTable<kFew> f;
+    few(t, f);
+    for (int i = 0; i < t.n; ++i) {
+      f.g[i] = t.g[i];
+      f.out[i] = t.out[i];
+      f.out_type[i] = t.out_type[i];
+    }
+    k_clip<<<grid, kThreads, 0, s>>>(f, part, parts, max_norm, norm);
+  } else {
+    k_clip<<<grid, kThreads, 0, s>>>(t, part, parts, max_norm, norm);
+  }
   return hipGetLastError();
 }
 hipError_t launch_next_step(const int64_t *step, int64_t *next, hipStream_t s) {
   k_next_step<<<1, 1, 0, s>>>(step, next);
   return hipGetLastError();
 }
-hipError_t launch_adam(const AdamTable &t, const double *part, int parts, const AdamScalars &o, const int64_t *next,
-                       int64_t *step, float *norm, int cu_count, hipStream_t s) {
-  k_adam<<<grid_of(t.unit0[t.n], 8 * cu_count), kThreads, 0, s>>>(t, part, parts, o, next, step, norm);
+hipError_t launch_adam(const AdamTable<kAdamRanges> &t, const double *part, int parts, const AdamScalars &o,
+                       const int64_t *next, int64_t *step, float *norm, int cu_count, hipStream_t s) {
+  const int grid = grid_of(t.unit0[t.n], 8 * cu_count);
+  if (t.n <= kFew) {
+    AdamTable<kFew> f;
+    few(t, f);
+    for (int i = 0; i < t.n; ++i) {
+      f.g[i] = t.g[i];
+      f.p[i] = t.p[i];
+      f.m[i] = t.m[i];
+      f.v[i] = t.v[i];
+      f.copy[i] = t.copy[i];
+      f.copy_type[i] = t.copy_type[i];
+    }
+    k_adam<<<grid, kThreads, 0, s>>>(f, part, parts, o, next, step, norm);
+  } else {
+    k_adam<<<grid, kThreads, 0, s>>>(t, part, parts, o, next, step, norm);
+  }
   return hipGetLastError();
 }
 

@@ -48,43 +48,76 @@ bool span_of(const aecct_tensor &t, bool written, Span &s) {
   s = Span{(uintptr_t)t.data, (uintptr_t)t.data + (uintptr_t)(t.count * type_size(t.type)), written};
   return t.count > 0;
 }
-bool conflict(std::vector<Span> &v) {
-  // lists usually come in ascending order of addresses already, one after the other
-  if (!std::is_sorted(v.begin(), v.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; }))
-    std::sort(v.begin(), v.end(), [](const Span &a, const Span &b) { return a.begin < b.begin; });
-  uintptr_t any = 0, written = 0;   // the furthest ends so far
-  for (const Span &s : v) {
-    if (s.begin < written || (s.written && s.begin < any)) return true;
-    any = std::max(any, s.end);
-    if (s.written) written = std::max(written, s.end);
+struct Spans {
+  std::vector<Span> v;
+  explicit Spans(size_t most) { v.reserve(most); }
+  static bool before(const Span &a, const Span &b) { return a.begin < b.begin; }
+  // Adds a list (without tensors that are `but`'s own), which usually lies in ascending order already.
+  void add(const aecct_tensor *t, int32_t n, bool written, const aecct_tensor *but = nullptr) {
+    const size_t old = v.size();
+    Span x;
+    for (int i = 0; i < n; ++i)
+      if (!(but && t[i].data == but[i].data && t[i].type == but[i].type) && span_of(t[i], written, x)) v.push_back(x);
+    join(old);
   }
-  return false;
-}
+  void add(const void *p, size_t bytes) {
+    v.push_back(Span{(uintptr_t)p, (uintptr_t)p + bytes, true});
+    join(v.size() - 1);
+  }
+  void join(size_t old) {
+    if (!std::is_sorted(v.begin() + old, v.end(), before)) std::sort(v.begin() + old, v.end(), before);
+    if (old && old < v.size() && before(v[old], v[old - 1])) std::inplace_merge(v.begin(), v.begin() + old, v.end(), before);
+  }
+  bool conflict() const {
+    uintptr_t any = 0, written = 0;   // the furthest ends so far
+    for (const Span &s : v) {
+      if (s.begin < written || (s.written && s.begin < any)) return true;
+      any = std::max(any, s.end);
+      if (s.written) written = std::max(written, s.end);
+    }
+    return false;
+  }
+};
 
 int64_t units_of(int64_t count) { return (count + kUnit - 1) / kUnit; }
 
-// Calls f(first, end) for every run of tensors that one launch takes.
-template <class F>
-hipError_t for_launches(const aecct_tensor *t, int32_t n, int most, F f) {
-  for (int i = 0; i < n;) {
-    int k = i;
-    int64_t units = 0;
-    while (k < n && k - i < most && units + units_of(t[k].count) <= kMaxUnits) units += units_of(t[k++].count);
-    const hipError_t e = f(i, k);
-    if (e != hipSuccess) return e;
-    i = k;
-  }
-  return hipSuccess;
-}
-template <class Table>
-void add_units(Table &t, const aecct_tensor &x) {
-  t.count[t.n] = x.count;
-  t.type[t.n] = (uint8_t)x.type;
-  t.unit0[t.n + 1] = t.unit0[t.n] + (int)units_of(x.count);
-  ++t.n;
+// Whether tensor b follows a run of `count` values at a.
+bool follows(const void *a, int64_t count, int32_t type, const aecct_tensor &b) {
+  return b.type == type && (uintptr_t)a + (uintptr_t)(count * type_size(type)) == (uintptr_t)b.data;
 }
 
-size_t sum_launches(int32_t n) { return ((size_t)n + kSumTensors - 1) / kSumTensors; }
+// Fills tables with a list's tensors, one table a launch: extends(t, i) whether tensor i goes on where the table's last
+// range ends, put(t, i) sets a new range's addresses, launch(t).
+template <class Table, class Extends, class Put, class Launch>
+hipError_t for_tables(const aecct_tensor *list, int32_t n, Extends extends, Put put, Launch launch) {
+  Table t;
+  t.n = 0;
+  t.unit0[0] = 0;
+  for (int i = 0; i < n; ++i) {
+    if (list[i].count == 0) continue;
+    if (t.n && extends(t, i)) {
+      const int64_t count = t.count[t.n - 1] + list[i].count, units = t.unit0[t.n - 1] + units_of(count);
+      if (count <= kMaxCount && units <= kMaxUnits) {
+        t.count[t.n - 1] = count;
+        t.unit0[t.n] = (int)units;
+        continue;
+      }
+    }
+    if (t.n == Table::kMost || t.unit0[t.n] + units_of(list[i].count) > kMaxUnits) {
+      const hipError_t e = launch(t);
+      if (e != hipSuccess) return e;
+      t.n = 0;
+    }
+    put(t, i);
+    t.count[t.n] = list[i].count;
+    t.type[t.n] = (uint8_t)list[i].type;
+    t.unit0[t.n + 1] = t.unit0[t.n] + (int)units_of(list[i].count);
+    ++t.n;
+  }
+  return t.n ? launch(t) : hipSuccess;
+}
+
+size_t sum_launches(int32_t n) { return ((size_t)n + kSumRanges - 1) / kSumRanges; }
 size_t need_bytes(int32_t n) { return 2 * kAlign + std::max<size_t>(1, sum_launches(n)) * kMaxSumBlocks * sizeof(double); }
 
 struct Work {
@@ -96,23 +129,20 @@ Work work_of(void *workspace) {
   return Work{(int64_t *)w, (double *)(w + kAlign)};
 }
 
-hipError_t sums(const aecct_tensor *g, int32_t n, double *part, int &parts, hipStream_t s) {
+// The norm's partial sums, and *next = *step + 1 if step is given.
+hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, const int64_t *step, hipStream_t s) {
   parts = 0;
-  return for_launches(g, n, kSumTensors, [&](int i, int k) {
-    SumTable t;
-    t.n = 0;
-    t.unit0[0] = 0;
-    for (; i < k; ++i)
-      if (g[i].count) {
-        t.g[t.n] = g[i].data;
-        add_units(t, g[i]);
-      }
-    if (!t.n) return hipSuccess;
-    const int blocks = std::min(t.unit0[t.n], kMaxSumBlocks);
-    const hipError_t e = launch_sum_squares(t, part + parts, blocks, s);
-    parts += blocks;
-    return e;
-  });
+  using Table = SumTable<kSumRanges>;
+  const hipError_t e = for_tables<Table>(
+      g, n, [&](const Table &t, int i) { return follows(t.g[t.n - 1], t.count[t.n - 1], t.type[t.n - 1], g[i]); },
+      [&](Table &t, int i) { t.g[t.n] = g[i].data; },
+      [&](const Table &t) {
+        const int blocks = std::min(t.unit0[t.n], kMaxSumBlocks);
+        const hipError_t r = launch_sum_squares(t, w.part + parts, blocks, parts ? nullptr : step, w.next, s);
+        parts += blocks;
+        return r;
+      });
+  return e == hipSuccess && !parts && step ? launch_next_step(step, w.next, s) : e;
 }
 
 aecct_status st(hipError_t e) { return e == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE; }
@@ -147,7 +177,7 @@ aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, 
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  const hipError_t e = sums(grads, n, w.part, parts, s);
+  const hipError_t e = sums(grads, n, w, parts, nullptr, s);
   return st(e != hipSuccess ? e : launch_norm(w.part, parts, norm, s));
 }
 
@@ -159,15 +189,11 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    std::vector<Span> v;
-    v.reserve(2 * (size_t)n + 1);
-    Span x;
-    for (int i = 0; i < n; ++i)
-      if (span_of(out[i], true, x)) v.push_back(x);
-    for (int i = 0; i < n; ++i)
-      if (!(grads[i].data == out[i].data && grads[i].type == out[i].type) && span_of(grads[i], false, x)) v.push_back(x);
-    v.push_back(Span{(uintptr_t)norm, (uintptr_t)(norm + 1), true});
-    if (conflict(v)) return AECCT_ERR_INVALID_ARG;
+    Spans v(2 * (size_t)n + 1);
+    v.add(out, n, true);
+    v.add(grads, n, false, out);
+    v.add(norm, sizeof(float));
+    if (v.conflict()) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
   }
@@ -176,22 +202,22 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  hipError_t e = sums(grads, n, w.part, parts, s);
+  const hipError_t e = sums(grads, n, w, parts, nullptr, s);
   if (e != hipSuccess) return st(e);
   if (!parts) return st(launch_norm(w.part, 0, norm, s));
-  return st(for_launches(grads, n, kClipTensors, [&](int i, int k) {
-    ClipTable t;
-    t.n = 0;
-    t.unit0[0] = 0;
-    for (; i < k; ++i)
-      if (grads[i].count) {
+  using Table = ClipTable<kClipRanges>;
+  return st(for_tables<Table>(
+      grads, n,
+      [&](const Table &t, int i) {
+        const int k = t.n - 1;
+        return follows(t.g[k], t.count[k], t.type[k], grads[i]) && follows(t.out[k], t.count[k], t.out_type[k], out[i]);
+      },
+      [&](Table &t, int i) {
         t.g[t.n] = grads[i].data;
         t.out[t.n] = out[i].data;
         t.out_type[t.n] = (uint8_t)out[i].type;
-        add_units(t, grads[i]);
-      }
-    return t.n ? launch_clip(t, w.part, parts, max_norm, norm, cus, s) : hipSuccess;
-  }));
+      },
+      [&](const Table &t) { return launch_clip(t, w.part, parts, max_norm, norm, cus, s); }));
 }
 
 aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, const aecct_tensor *v,
@@ -213,16 +239,15 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    std::vector<Span> all;
-    all.reserve(5 * (size_t)n + 2);
-    Span x;
-    const aecct_tensor *lists[5] = {params, m, v, copies, grads};
-    for (int l = 0; l < 5; ++l)
-      for (int i = 0; lists[l] && i < n; ++i)
-        if (span_of(lists[l][i], l < 4, x)) all.push_back(x);
-    all.push_back(Span{(uintptr_t)step, (uintptr_t)(step + 1), true});
-    if (norm) all.push_back(Span{(uintptr_t)norm, (uintptr_t)(norm + 1), true});
-    if (conflict(all)) return AECCT_ERR_INVALID_ARG;
+    Spans spans(5 * (size_t)n + 2);
+    spans.add(params, n, true);
+    spans.add(m, n, true);
+    spans.add(v, n, true);
+    if (copies) spans.add(copies, n, true);
+    spans.add(grads, n, false);
+    spans.add(step, sizeof(int64_t));
+    if (norm) spans.add(norm, sizeof(float));
+    if (spans.conflict()) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
   }
@@ -231,34 +256,37 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  hipError_t e = launch_next_step(step, w.next, s);
-  if (e == hipSuccess && (opt->max_norm > 0 || norm)) e = sums(grads, n, w.part, parts, s);
+  hipError_t e = opt->max_norm > 0 || norm ? sums(grads, n, w, parts, step, s) : launch_next_step(step, w.next, s);
   if (e != hipSuccess) return st(e);
   const AdamScalars o{opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay, opt->max_norm, opt->lr_device};
+  using Table = AdamTable<kAdamRanges>;
   bool first = true;
-  auto launch = [&](const AdamTable &t) {
+  const auto launch = [&](const Table &t) {
     const hipError_t r = launch_adam(t, w.part, parts, o, w.next, first ? step : nullptr, first ? norm : nullptr, cus, s);
     first = false;
     return r;
   };
-  e = for_launches(params, n, kAdamTensors, [&](int i, int k) {
-    AdamTable t;
-    t.n = 0;
-    t.unit0[0] = 0;
-    for (; i < k; ++i)
-      if (params[i].count) {
+  const auto copy_of = [&](int i) { return copies && copies[i].count ? copies[i].data : nullptr; };
+  e = for_tables<Table>(
+      grads, n,
+      [&](const Table &t, int i) {
+        const int k = t.n - 1;
+        const int64_t c = t.count[k];
+        return follows(t.g[k], c, t.type[k], grads[i]) && follows(t.p[k], c, AECCT_F32, params[i]) &&
+               follows(t.m[k], c, AECCT_F32, m[i]) && follows(t.v[k], c, AECCT_F32, v[i]) &&
+               (t.copy[k] ? copy_of(i) && follows(t.copy[k], c, t.copy_type[k], copies[i]) : !copy_of(i));
+      },
+      [&](Table &t, int i) {
         t.g[t.n] = grads[i].data;
         t.p[t.n] = (float *)params[i].data;
         t.m[t.n] = (float *)m[i].data;
         t.v[t.n] = (float *)v[i].data;
-        t.copy[t.n] = copies && copies[i].count ? copies[i].data : nullptr;
+        t.copy[t.n] = copy_of(i);
         t.copy_type[t.n] = copies ? (uint8_t)copies[i].type : 0;
-        add_units(t, grads[i]);
-      }
-    return t.n ? launch(t) : hipSuccess;
-  });
+      },
+      launch);
   if (e == hipSuccess && first) {   // no value at all: the step counts, the norm is 0
-    AdamTable t;
+    Table t;
     t.n = 0;
     t.unit0[0] = 0;
     e = launch(t);
