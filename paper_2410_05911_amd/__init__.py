@@ -277,6 +277,9 @@ def _ptr(t):
 def _stream_ptr(stream):
     import torch
     if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the handle without a Stream object around it
+        if raw is not None:
+            return raw(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -363,15 +366,16 @@ def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes
         raise ValueError("group must be 0, 32, 64 or 128")
     _on_current_gpu(x.get_device())
     px, ldx = _rows_of(x, x, dtype, "x")
+    dense = x.is_contiguous()
     pres, ldres = _rows_of(res, x, dtype, "res")
     pgain, gain_type = _gain_of(gain, x)
     if y is None and with_y:
-        y = x.new_empty(shape)
+        y = torch.empty_like(x) if dense else x.new_empty(shape)
         py, ldy = y.data_ptr(), d
     else:
         py, ldy = _rows_of(y, x, dtype, "y")
     if h is None and res is not None:
-        h = x.new_empty(shape)
+        h = torch.empty_like(x) if dense else x.new_empty(shape)
         ph, ldh = h.data_ptr(), d
     else:
         ph, ldh = _rows_of(h, x, dtype, "h")
@@ -414,7 +418,7 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
     pres, lddres = _rows_of(dres, h, dtype, "dres")
     pgain, gain_type = _gain_of(gain, h)
     if dh is None:
-        dh = h.new_empty(shape)
+        dh = torch.empty_like(h) if h.is_contiguous() else h.new_empty(shape)
         pdh, lddh = dh.data_ptr(), d
     else:
         pdh, lddh = _rows_of(dh, h, dtype, "dh")

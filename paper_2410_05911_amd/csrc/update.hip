@@ -46,43 +46,76 @@ __device__ __forceinline__ void store4(void *p, int type, int64_t i, int64_t n, 
   else store_part<f16_t, 4>((f16_t *)p + i, k, f);
 }
 
-constexpr int kSteps = kUnit / (4 * kThreads);   // of four values a thread in a unit
-
-// Sum of squares of a unit's values from i0 on, n in all: 16 bytes a load.
-template <class T>
-__device__ __forceinline__ double unit_squares(const T *g, int64_t n) {
-  constexpr int V = 16 / sizeof(T), J = kUnit / (V * kThreads);
-  float f[J][V];
+// The unit of a thread of the sums: four vectors of 16 bytes, read a unit ahead of their use.
+struct SumUnit {
+  Raw<float, 4> w[4];
+  template <class T>
+  __device__ __forceinline__ void load(const T *g, int64_t n) {
+    constexpr int V = 16 / sizeof(T);
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int i = (j * kThreads + (int)threadIdx.x) * V;
-    load_part<T, V>(g + i, n - i >= V ? V : (int)(n - i), f[j]);
-  }
-  double s = 0, q = 0;
-#pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (int i = 0; i < V; i += 2) {
-      s += (double)f[j][i] * (double)f[j][i];
-      q += (double)f[j][i + 1] * (double)f[j][i + 1];
+    for (int j = 0; j < 4; ++j) {
+      const int i = (j * kThreads + (int)threadIdx.x) * V;
+      Raw<T, V> r;
+      if (i + V <= n) load_raw<T, V>(g + i, r);
+      else load_raw_part<T, V>(g + i, (int)(n - i), r);
+      __builtin_memcpy(w[j].w, r.w, 16);
     }
-  return s + q;
+  }
+  template <class T>
+  __device__ __forceinline__ void add_squares(double &s, double &q) const {
+    constexpr int V = 16 / sizeof(T);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      Raw<T, V> r;
+      __builtin_memcpy(r.w, w[j].w, 16);
+      float f[V];
+      unpack<T, V>(r, f);
+#pragma unroll
+      for (int i = 0; i < V; i += 2) {
+        s = fma((double)f[i], (double)f[i], s);
+        q = fma((double)f[i + 1], (double)f[i + 1], q);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void set_now(AdamNow *now, const int64_t *step, const AdamScalars &o) {
+  const int64_t t = *step + 1;
+  now->step = t;
+  now->grow1 = (float)(1 / (1 - pow(o.beta1, (double)t)));
+  now->root2 = (float)(1 / sqrt(1 - pow(o.beta2, (double)t)));
 }
+__global__ void k_now(const int64_t *step, AdamNow *now, AdamScalars o) { set_now(now, step, o); }
 
 template <int N>
-__global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable<N> t, double *part, const int64_t *step, int64_t *next) {
+__global__ __launch_bounds__(kThreads) void k_sum_squares(SumTable<N> t, double *part, const int64_t *step, AdamNow *now,
+                                                          AdamScalars o) {
   __shared__ double lds[kThreads / 64];
-  if (step && blockIdx.x == 0 && threadIdx.x == 0) *next = *step + 1;
-  double s = 0;
+  if (now && blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) set_now(now, step, o);
+  double s = 0, q = 0;
+  SumUnit x;
   int k = 0;
-  for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
+  const auto fetch = [&](int u) {
     k = tensor_of(t, u, k);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit, n = t.count[k] - i0;
-    if (t.type[k] == 0) s += unit_squares((const float *)t.g[k] + i0, n);
-    else if (t.type[k] == 1) s += unit_squares((const bf16_t *)t.g[k] + i0, n);
-    else s += unit_squares((const f16_t *)t.g[k] + i0, n);
+    const int type = t.type[k];
+    const int64_t i0 = (int64_t)(u - t.unit0[k]) * t.unit_of(type), n = t.count[k] - i0;
+    if (type == 0) x.load((const float *)t.g[k] + i0, n);
+    else x.load((const bf16_t *)t.g[k] + i0, n);
+    return type;
+  };
+  const int units = t.unit0[t.n];
+  int u = blockIdx.x, type = 0;
+  if (u < units) type = fetch(u);
+  while (u < units) {
+    const SumUnit y = x;
+    const int ty = type;
+    u += gridDim.x;
+    if (u < units) type = fetch(u);
+    if (ty == 0) y.add_squares<float>(s, q);
+    else if (ty == 1) y.add_squares<bf16_t>(s, q);
+    else y.add_squares<f16_t>(s, q);
   }
-  s = block_sum(s, lds);
+  s = block_sum(s + q, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
@@ -119,7 +152,8 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double 
   int k = 0;
   for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
     k = tensor_of(t, u, k);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit + 4 * threadIdx.x, c = t.count[k];
+    const int64_t i0 = (int64_t)(u - t.unit0[k]) * t.kUnit + 4 * threadIdx.x, c = t.count[k];
+    constexpr int kSteps = ClipTable<N>::kUnit / (4 * kThreads);
     float g[kSteps][4];
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) load4(t.g[k], t.type[k], i0 + 4 * kThreads * j, c - i0 - 4 * kThreads * j, g[j]);
@@ -132,12 +166,42 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double 
   }
 }
 
-__global__ void k_next_step(const int64_t *step, int64_t *next) { *next = *step + 1; }
-
+// Four values of each tensor a thread in a unit; the next unit's are read before the present ones are worked on, the
+// first unit's before the norm is known.
 template <int N>
 __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double *part, int parts, AdamScalars o,
-                                                   const int64_t *next, int64_t *step, float *norm) {
+                                                   const AdamNow *now, int64_t *step, float *norm) {
   __shared__ double lds[kThreads / 64];
+  Raw<float, 4> np, nm, nv, ng;   // ng: two words for a 16-bit type
+  int k = 0;
+  const auto at_of = [&](int u) { return (int64_t)(u - t.unit0[k]) * t.kUnit + 4 * threadIdx.x; };
+  const auto fetch = [&](int u) {
+    k = tensor_of(t, u, k);
+    const int64_t at = at_of(u), left = t.count[k] - at;
+    if (left >= 4) {
+      load_raw<float, 4>(t.p[k] + at, np);
+      load_raw<float, 4>(t.m[k] + at, nm);
+      load_raw<float, 4>(t.v[k] + at, nv);
+      if (t.type[k] == 0) load_raw<float, 4>((const float *)t.g[k] + at, ng);
+      else __builtin_memcpy(ng.w, (const bf16_t *)t.g[k] + at, 8);
+    } else {
+      const int n = (int)left;
+      load_raw_part<float, 4>(t.p[k] + at, n, np);
+      load_raw_part<float, 4>(t.m[k] + at, n, nm);
+      load_raw_part<float, 4>(t.v[k] + at, n, nv);
+      if (t.type[k] == 0) {
+        load_raw_part<float, 4>((const float *)t.g[k] + at, n, ng);
+      } else {
+        Raw<bf16_t, 4> h;
+        load_raw_part<bf16_t, 4>((const bf16_t *)t.g[k] + at, n, h);
+        ng.w[0] = h.w[0];
+        ng.w[1] = h.w[1];
+      }
+    }
+  };
+  int u = blockIdx.x;
+  const int units = t.unit0[t.n];
+  if (u < units) fetch(u);
   float f = 1.0f;
   if (parts) {
     const double n = norm_of(part, parts, lds);
@@ -145,37 +209,40 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double 
     if (!(n <= 1.7976931348623157e308)) return;
     if (o.max_norm > 0) f = clip_factor(n, o.max_norm);
   }
-  const int64_t now = *next;
-  if (step && blockIdx.x == 0 && threadIdx.x == 0) *step = now;
-  const double lr = o.lr_device ? (double)*o.lr_device : o.lr;
-  const float size = (float)(lr / (1 - pow(o.beta1, (double)now))), root = (float)(1 / sqrt(1 - pow(o.beta2, (double)now)));
+  if (step && blockIdx.x == 0 && threadIdx.x == 0) *step = now->step;
+  const float lr = o.lr_device ? *o.lr_device : (float)o.lr, size = lr * now->grow1, root = now->root2;
   const float b1 = (float)o.beta1, c1 = (float)(1 - o.beta1), b2 = (float)o.beta2, c2 = (float)(1 - o.beta2);
-  const float decay = (float)(lr * o.weight_decay), eps = (float)o.eps;
-  int k = 0;
-  for (int u = blockIdx.x; u < t.unit0[t.n]; u += gridDim.x) {
-    k = tensor_of(t, u, k);
-    const int64_t i0 = (int64_t)(u - t.unit0[k]) * kUnit + 4 * threadIdx.x, c = t.count[k];
-#pragma unroll 2
-    for (int j = 0; j < kSteps; ++j) {
-      const int64_t at = i0 + 4 * kThreads * j, left = c - at;
-      const int n = left >= 4 ? 4 : (int)left;
-      float g[4], p[4], m[4], v[4];
-      load4(t.g[k], t.type[k], at, left, g);
-      load_part<float, 4>(t.p[k] + at, n, p);
-      load_part<float, 4>(t.m[k] + at, n, m);
-      load_part<float, 4>(t.v[k] + at, n, v);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = g[i] * f;
-        m[i] = fmaf(b1, m[i], c1 * x);
-        v[i] = fmaf(b2, v[i], c2 * (x * x));
-        p[i] -= fmaf(decay, p[i], size * m[i] / fmaf(sqrtf(v[i]), root, eps));
-      }
-      store_part<float, 4>(t.m[k] + at, n, m);
-      store_part<float, 4>(t.v[k] + at, n, v);
-      store_part<float, 4>(t.p[k] + at, n, p);
-      if (t.copy[k]) store4(t.copy[k], t.copy_type[k], at, left, p);
+  const float decay = lr * (float)o.weight_decay, eps = (float)o.eps;
+  while (u < units) {
+    float g[4], p[4], m[4], v[4];
+    const int kc = k;
+    const int64_t at = at_of(u), left = t.count[k] - at;
+    unpack<float, 4>(np, p);
+    unpack<float, 4>(nm, m);
+    unpack<float, 4>(nv, v);
+    if (t.type[k] == 0) {
+      unpack<float, 4>(ng, g);
+    } else if (t.type[k] == 1) {
+      const Raw<bf16_t, 4> h{{ng.w[0], ng.w[1]}};
+      unpack<bf16_t, 4>(h, g);
+    } else {
+      const Raw<f16_t, 4> h{{ng.w[0], ng.w[1]}};
+      unpack<f16_t, 4>(h, g);
     }
+    u += gridDim.x;
+    if (u < units) fetch(u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = g[i] * f;
+      m[i] = fmaf(b1, m[i], c1 * x);
+      v[i] = fmaf(b2, v[i], c2 * (x * x));
+      p[i] -= fmaf(decay, p[i], size * m[i] / fmaf(sqrtf(v[i]), root, eps));
+    }
+    const int n = left >= 4 ? 4 : (int)left;
+    store_part<float, 4>(t.m[kc] + at, n, m);
+    store_part<float, 4>(t.v[kc] + at, n, v);
+    store_part<float, 4>(t.p[kc] + at, n, p);
+    if (t.copy[kc]) store4(t.copy[kc], t.copy_type[kc], at, left, p);
   }
 }
 
@@ -194,15 +261,15 @@ void few(const Units<N> &t, Units<kFew> &f) {
 
 }  // namespace
 
-hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, const int64_t *step, int64_t *next,
-                              hipStream_t s) {
+hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, const int64_t *step, AdamNow *now,
+                              const AdamScalars &o, hipStream_t s) {
   if (t.n <= kFew) {
     SumTable<kFew> f;
     few(t, f);
     for (int i = 0; i < t.n; ++i) f.g[i] = t.g[i];
-    k_sum_squares<<<blocks, kThreads, 0, s>>>(f, part, step, next);
+    k_sum_squares<<<blocks, kThreads, 0, s>>>(f, part, step, now, o);
   } else {
-    k_sum_squares<<<blocks, kThreads, 0, s>>>(t, part, step, next);
+    k_sum_squares<<<blocks, kThreads, 0, s>>>(t, part, step, now, o);
   }
   return hipGetLastError();
 }
@@ -227,12 +294,12 @@ hipError_t launch_clip(const ClipTable<kClipRanges> &t, const double *part, int 
   }
   return hipGetLastError();
 }
-hipError_t launch_next_step(const int64_t *step, int64_t *next, hipStream_t s) {
-  k_next_step<<<1, 1, 0, s>>>(step, next);
+hipError_t launch_now(const int64_t *step, AdamNow *now, const AdamScalars &o, hipStream_t s) {
+  k_now<<<1, 1, 0, s>>>(step, now, o);
   return hipGetLastError();
 }
 hipError_t launch_adam(const AdamTable<kAdamRanges> &t, const double *part, int parts, const AdamScalars &o,
-                       const int64_t *next, int64_t *step, float *norm, int cu_count, hipStream_t s) {
+                       const AdamNow *now, int64_t *step, float *norm, int cu_count, hipStream_t s) {
   const int grid = grid_of(t.unit0[t.n], 8 * cu_count);
   if (t.n <= kFew) {
     AdamTable<kFew> f;
@@ -245,9 +312,9 @@ hipError_t launch_adam(const AdamTable<kAdamRanges> &t, const double *part, int 
       f.copy[i] = t.copy[i];
       f.copy_type[i] = t.copy_type[i];
     }
-    k_adam<<<grid, kThreads, 0, s>>>(f, part, parts, o, next, step, norm);
+    k_adam<<<grid, kThreads, 0, s>>>(f, part, parts, o, now, step, norm);
   } else {
-    k_adam<<<grid, kThreads, 0, s>>>(t, part, parts, o, next, step, norm);
+    k_adam<<<grid, kThreads, 0, s>>>(t, part, parts, o, now, step, norm);
   }
   return hipGetLastError();
 }

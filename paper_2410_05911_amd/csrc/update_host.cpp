@@ -19,7 +19,7 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 constexpr int64_t kMaxCount = (int64_t)1 << 40;   // values of a tensor
-constexpr int kMaxUnits = 1 << 30;                // of a launch
+constexpr int64_t kMaxUnits = (int64_t)1 << 30;   // of a launch: a tensor of 2^40 values is as many units of 1024
 
 int64_t type_size(int32_t t) { return t == AECCT_F32 ? 4 : 2; }
 bool tensor_ok(const aecct_tensor &t) {
@@ -79,8 +79,6 @@ struct Spans {
   }
 };
 
-int64_t units_of(int64_t count) { return (count + kUnit - 1) / kUnit; }
-
 // Whether tensor b follows a run of `count` values at a.
 bool follows(const void *a, int64_t count, int32_t type, const aecct_tensor &b) {
   return b.type == type && (uintptr_t)a + (uintptr_t)(count * type_size(type)) == (uintptr_t)b.data;
@@ -90,20 +88,21 @@ bool follows(const void *a, int64_t count, int32_t type, const aecct_tensor &b) 
 // range ends, put(t, i) sets a new range's addresses, launch(t).
 template <class Table, class Extends, class Put, class Launch>
 hipError_t for_tables(const aecct_tensor *list, int32_t n, Extends extends, Put put, Launch launch) {
+  const auto units_of = [](int64_t count, int type) { return (count + Table::unit_of(type) - 1) / Table::unit_of(type); };
   Table t;
   t.n = 0;
   t.unit0[0] = 0;
   for (int i = 0; i < n; ++i) {
     if (list[i].count == 0) continue;
     if (t.n && extends(t, i)) {
-      const int64_t count = t.count[t.n - 1] + list[i].count, units = t.unit0[t.n - 1] + units_of(count);
+      const int64_t count = t.count[t.n - 1] + list[i].count, units = t.unit0[t.n - 1] + units_of(count, t.type[t.n - 1]);
       if (count <= kMaxCount && units <= kMaxUnits) {
         t.count[t.n - 1] = count;
         t.unit0[t.n] = (int)units;
         continue;
       }
     }
-    if (t.n == Table::kMost || t.unit0[t.n] + units_of(list[i].count) > kMaxUnits) {
+    if (t.n == Table::kMost || t.unit0[t.n] + units_of(list[i].count, list[i].type) > kMaxUnits) {
       const hipError_t e = launch(t);
       if (e != hipSuccess) return e;
       t.n = 0;
@@ -111,7 +110,7 @@ hipError_t for_tables(const aecct_tensor *list, int32_t n, Extends extends, Put 
     put(t, i);
     t.count[t.n] = list[i].count;
     t.type[t.n] = (uint8_t)list[i].type;
-    t.unit0[t.n + 1] = t.unit0[t.n] + (int)units_of(list[i].count);
+    t.unit0[t.n + 1] = t.unit0[t.n] + (int)units_of(list[i].count, list[i].type);
     ++t.n;
   }
   return t.n ? launch(t) : hipSuccess;
@@ -121,16 +120,17 @@ size_t sum_launches(int32_t n) { return ((size_t)n + kSumRanges - 1) / kSumRange
 size_t need_bytes(int32_t n) { return 2 * kAlign + std::max<size_t>(1, sum_launches(n)) * kMaxSumBlocks * sizeof(double); }
 
 struct Work {
-  int64_t *next;
+  AdamNow *now;
   double *part;
 };
 Work work_of(void *workspace) {
   unsigned char *w = (unsigned char *)align_up((size_t)(uintptr_t)workspace);
-  return Work{(int64_t *)w, (double *)(w + kAlign)};
+  return Work{(AdamNow *)w, (double *)(w + kAlign)};
 }
 
-// The norm's partial sums, and *next = *step + 1 if step is given.
-hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, const int64_t *step, hipStream_t s) {
+// The norm's partial sums, and *w.now from *step if that is given.
+hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, const int64_t *step, const AdamScalars &o,
+                hipStream_t s) {
   parts = 0;
   using Table = SumTable<kSumRanges>;
   const hipError_t e = for_tables<Table>(
@@ -138,11 +138,11 @@ hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, con
       [&](Table &t, int i) { t.g[t.n] = g[i].data; },
       [&](const Table &t) {
         const int blocks = std::min(t.unit0[t.n], kMaxSumBlocks);
-        const hipError_t r = launch_sum_squares(t, w.part + parts, blocks, parts ? nullptr : step, w.next, s);
+        const hipError_t r = launch_sum_squares(t, w.part + parts, blocks, step, step && !parts ? w.now : nullptr, o, s);
         parts += blocks;
         return r;
       });
-  return e == hipSuccess && !parts && step ? launch_next_step(step, w.next, s) : e;
+  return e == hipSuccess && !parts && step ? launch_now(step, w.now, o, s) : e;
 }
 
 aecct_status st(hipError_t e) { return e == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE; }
@@ -177,7 +177,7 @@ aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, 
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  const hipError_t e = sums(grads, n, w, parts, nullptr, s);
+  const hipError_t e = sums(grads, n, w, parts, nullptr, AdamScalars{}, s);
   return st(e != hipSuccess ? e : launch_norm(w.part, parts, norm, s));
 }
 
@@ -202,7 +202,7 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  const hipError_t e = sums(grads, n, w, parts, nullptr, s);
+  const hipError_t e = sums(grads, n, w, parts, nullptr, AdamScalars{}, s);
   if (e != hipSuccess) return st(e);
   if (!parts) return st(launch_norm(w.part, 0, norm, s));
   using Table = ClipTable<kClipRanges>;
@@ -256,13 +256,13 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  hipError_t e = opt->max_norm > 0 || norm ? sums(grads, n, w, parts, step, s) : launch_next_step(step, w.next, s);
-  if (e != hipSuccess) return st(e);
   const AdamScalars o{opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay, opt->max_norm, opt->lr_device};
+  hipError_t e = opt->max_norm > 0 || norm ? sums(grads, n, w, parts, step, o, s) : launch_now(step, w.now, o, s);
+  if (e != hipSuccess) return st(e);
   using Table = AdamTable<kAdamRanges>;
   bool first = true;
   const auto launch = [&](const Table &t) {
-    const hipError_t r = launch_adam(t, w.part, parts, o, w.next, first ? step : nullptr, first ? norm : nullptr, cus, s);
+    const hipError_t r = launch_adam(t, w.part, parts, o, w.now, first ? step : nullptr, first ? norm : nullptr, cus, s);
     first = false;
     return r;
   };
