@@ -21,6 +21,7 @@ struct NormRows {
   uint8_t *codes;
   float *alpha;
   int64_t ldx, ldres, ldh, ldy, ldcodes;
+  bool past_in, past_out;      // inputs are read, outputs written past the caches
 };
 hipError_t launch_rms_norm(int type, const NormRows &a, int cu_count, hipStream_t s);
 
@@ -34,6 +35,7 @@ struct NormGradRows {
   int64_t ldh, lddy, lddres, lddh;
   float *part;                 // partial sums of dgain, or null: no dgain
   float *dgain;
+  bool past_in, past_out;
 };
 // Blocks at most, so rows of the partial sums: norm_grad_part_rows(rows, d) of d floats each.
 int64_t norm_grad_part_rows(int64_t rows, int d);

@@ -102,18 +102,6 @@ __device__ __forceinline__ float far_rho(float ss, float (&h)[N], float inv_d, f
   return rho;
 }
 
-template <class T, int V>
-__device__ __forceinline__ void load_gain(const void *gain, bool f32, int c, int n, float (&g)[V]) {
-  if (!gain) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) g[i] = 1.0f;
-  } else if (f32) {
-    load_part<float, V>((const float *)gain + c, n, g);
-  } else {
-    load_part<T, V>((const T *)gain + c, n, g);
-  }
-}
-
 // Where a thread's columns lie: vector j starts at column col(j).  A row of d = V k + tail values ends in a vector of
 // `tail` values, the jt-th of one lane; only that lane runs the code for single values, once for all j.
 template <int V, int TPR, int NV>
@@ -121,16 +109,22 @@ struct Columns {
   int d, lane, tail, jt;
   bool last;   // this lane holds the short vector
   __device__ __forceinline__ Columns(int d, int lane)
-      : d(d), lane(lane), tail(d % V), jt(d / V / TPR), last(tail && d / V % TPR == lane) {}
+      : d(d), lane(lane), tail(d % V), jt(d / V / TPR), last(tail && jt < NV && d / V % TPR == lane) {}
   __device__ __forceinline__ int col(int j) const { return (j * TPR + lane) * V; }
   __device__ __forceinline__ bool full(int j) const { return col(j) + V <= d; }
-  template <class T>
-  __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
+  template <bool NT, class T>
+  __device__ __forceinline__ void load_full(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      v[j] = Raw<T, V>{};
-      if (live && full(j)) load_raw<T, V>(p + col(j), v[j]);
-    }
+    for (int j = 0; j < NV; ++j)
+      if (live && full(j)) load_raw<T, V, NT>(p + col(j), v[j]);
+  }
+  // past: read past the caches
+  template <class T>
+  __device__ __forceinline__ void load(const T *p, bool live, bool past, Raw<T, V> (&v)[NV]) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = Raw<T, V>{};
+    if (past) load_full<true>(p, live, v);
+    else load_full<false>(p, live, v);
     if (live && last) {
       Raw<T, V> t;
       load_raw_part<T, V>(p + col(jt), tail, t);
@@ -140,12 +134,15 @@ struct Columns {
     }
   }
   template <class T, class F>   // f(j, v): the V values of vector j
-  __device__ __forceinline__ void store(T *p, bool live, F f) const {
+  __device__ __forceinline__ void store(T *p, bool live, bool past, F f) const {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float v[V];
       f(j, v);
-      if (live && full(j)) store_vec<T, V>(p + col(j), v);
+      if (live && full(j)) {
+        if (past) store_vec<T, V, true>(p + col(j), v);
+        else store_vec<T, V>(p + col(j), v);
+      }
       if (live && last && j == jt) store_part<T, V>(p + col(j), tail, v);
     }
   }
@@ -156,12 +153,12 @@ struct Columns {
       for (int i = 0; i < NV * V; ++i) g[i] = 1.0f;
     } else if (f32) {
       Raw<float, V> v[NV];
-      load<float>((const float *)p, true, v);
+      load<float>((const float *)p, true, false, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<float, V>(v[j], (float (&)[V])g[j * V]);
     } else {
       Raw<T, V> v[NV];
-      load<T>((const T *)p, true, v);
+      load<T>((const T *)p, true, false, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<T, V>(v[j], (float (&)[V])g[j * V]);
     }
@@ -227,6 +224,35 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, const uint32_t (
 }
 
 // ---- the norm ---------------------------------------------------------------------------------------------------
+// y and the codes of a row's columns from `off` on, those that cols holds.
+template <class T, int V, int TPR, int NV>
+__device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, TPR, NV> &cols, int off, int64_t r, bool live,
+                                           const float (&h)[NV * V], const float (&g)[NV * V], float A, float rho) {
+  if (a.y)
+    cols.store((T *)a.y + r * a.ldy + off, live, a.past_out, [&](int j, float (&v)[V]) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = h[j * V + i] * g[j * V + i] * rho;
+    });
+  if (!a.code) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = off + cols.col(j);
+    float B = A;
+    if (a.alphas > 1) {
+      B = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
+      B = lanes_join<Max>(B, a.group / V);
+    }
+    uint32_t w[V / 4];
+    codes_of<V>(a.code, B, h + j * V, g + j * V, w);
+    uint8_t *to = a.codes + r * a.ldcodes + c;
+    if (live && cols.full(j)) __builtin_memcpy(to, w, V);
+    if (live && cols.last && j == cols.jt) store_codes<V>(to, cols.tail, w);
+    if (live && c < a.d && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
+  }
+}
+
 // A block takes every gridDim.x-th of its sets of rows; the next one's inputs are read before the present one is joined
 // and written (loads issued ahead of the stores, so that waiting for them does not wait for the stores).
 template <class T, int TPR, int NV, int BLOCK, int WAVES>
@@ -239,15 +265,15 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> nx[NV], nres[NV];
   const auto fetch = [&](int64_t r) {
-    cols.load((const T *)a.x + r * a.ldx, r < a.rows, nx);
-    if (a.res) cols.load((const T *)a.res + r * a.ldres, r < a.rows, nres);
+    cols.load((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, a.past_in, nx);
+    if (a.res) cols.load((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, a.past_in, nres);
   };
   fetch((int64_t)blockIdx.x * RPB + sub);
   float g[NV * V];
   cols.template gain<T>(a.gain, a.gain_f32, g);
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + sub;
-    const bool live = r < a.rows;
+    const bool live = RPB == 1 || r < a.rows;
     float h[NV * V];
     float ss = 0, A = 0;
 #pragma unroll
@@ -263,7 +289,7 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
     }
     if (r0 + step < a.rows) fetch(r + step);
     if (a.h)
-      cols.store((T *)a.h + r * a.ldh, live, [&](int j, float (&v)[V]) {
+      cols.store((T *)a.h + r * a.ldh, live, a.past_out, [&](int j, float (&v)[V]) {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
       });
@@ -282,62 +308,51 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
       for (int i = 0; i < NV * V; ++i) A = Max::join(A, fabsf(h[i] * g[i]));
       row_join<Max, TPR>(none, A, lds);
     }
-    if (a.y)
-      cols.store((T *)a.y + r * a.ldy, live, [&](int j, float (&v)[V]) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = h[j * V + i] * g[j * V + i] * rho;
-      });
-    if (!a.code) continue;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = cols.col(j);
-      float B = A;
-      if (a.alphas > 1) {
-        B = 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
-        B = lanes_join<Max>(B, a.group / V);
-      }
-      uint32_t w[V / 4];
-      codes_of<V>(a.code, B, h + j * V, g + j * V, w);
-      uint8_t *to = a.codes + r * a.ldcodes + c;
-      if (live && cols.full(j)) __builtin_memcpy(to, w, V);
-      if (live && cols.last && j == cols.jt) store_codes<V>(to, cols.tail, w);
-      if (live && c < a.d && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
-    }
+    write_norm<T, V, TPR, NV>(a, cols, 0, r, live, h, g, A, rho);
   }
 }
 
-// Rows too long for registers, a block of 1024 threads each: the first pass reads the row and writes nothing, the
-// second reads it again (from the caches) and writes; a thread reads and writes the same columns, so h and y may lie on
-// the inputs here too.
-constexpr int kWideThreads = 1024;
+// Rows too long for registers, a block of 1024 threads each, 16 values a thread at a time: the first pass reads the row
+// and writes nothing, the second reads it again (from the caches) and writes; a thread reads and writes the same columns,
+// so h and y may lie on the inputs here too.
+constexpr int kWideThreads = 1024, kWideValues = 16, kWideStep = kWideThreads * kWideValues;
+template <class T>
+__device__ __forceinline__ const void *gain_at(const void *gain, bool f32, int off) {
+  return !gain ? nullptr : f32 ? (const void *)((const float *)gain + off) : (const void *)((const T *)gain + off);
+}
+
 template <class T>
 __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
-  constexpr int V = 16 / sizeof(T), STEP = kWideThreads * V;
+  constexpr int V = 16 / sizeof(T), NV = kWideValues / V, N = kWideValues;
+  using Cols = Columns<V, kWideThreads, NV>;
   __shared__ float2 lds[kWideThreads / 64];
-  const int c0 = threadIdx.x * V;
   const float inv_d = 1.0f / (float)a.d;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T *x = (const T *)a.x + r * a.ldx, *res = (const T *)a.res + r * a.ldres;
-    const auto load_h = [&](int c, float (&h)[V]) {
-      load_part<T, V>(x + c, a.d - c, h);
-      if (a.res) {
-        float w[V];
-        load_part<T, V>(res + c, a.d - c, w);
+    const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&g)[N]) {
+      Raw<T, V> x[NV], res[NV];
+      cols.load((const T *)a.x + r * a.ldx + off, true, false, x);
+      if (a.res) cols.load((const T *)a.res + r * a.ldres + off, true, false, res);
+      cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) h[i] += w[i];
+      for (int j = 0; j < NV; ++j) {
+        float (&v)[V] = (float (&)[V])h[j * V];
+        unpack<T, V>(x[j], v);
+        if (a.res) {
+          float w[V];
+          unpack<T, V>(res[j], w);
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] += w[i];
+        }
       }
     };
     float ss, A;
     const auto sums = [&](float up, float more) {
       ss = A = 0;
-      for (int c = c0; c < a.d; c += STEP) {
-        float h[V], g[V];
-        load_h(c, h);
-        load_gain<T, V>(a.gain, a.gain_f32, c, a.d - c, g);
+      for (int off = 0; off < a.d; off += kWideStep) {
+        float h[N], g[N];
+        read(Cols(a.d - off, threadIdx.x), off, h, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < N; ++i) {
           h[i] = h[i] * up * more;
           ss = fmaf(h[i], h[i], ss);
           A = Max::join(A, fabsf(h[i] * g[i]));
@@ -353,41 +368,26 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
       rho = far_rho_of(ss, up, inv_d, a.eps, more);
       sums(up, more);
     }
-    // every thread of a wavefront takes part in a group's maximum: columns past the row are zeros
-    for (int c = c0; c - c0 < a.d; c += STEP) {
-      const int n = a.d - c;
-      float h[V], g[V];
-      load_gain<T, V>(a.gain, a.gain_f32, c, n, g);
-      load_h(c, h);
-      if (a.h) store_part<T, V>((T *)a.h + r * a.ldh + c, n, h);
+    for (int off = 0; off < a.d; off += kWideStep) {
+      const Cols cols(a.d - off, threadIdx.x);
+      float h[N], g[N];
+      read(cols, off, h, g);
+      if (a.h)
+        cols.store((T *)a.h + r * a.ldh + off, true, a.past_out, [&](int j, float (&v)[V]) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) h[i] = h[i] * up * more;
-      if (a.y) {
-        float y[V];
+          for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
+        });
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = h[i] * g[i] * rho;
-        store_part<T, V>((T *)a.y + r * a.ldy + c, n, y);
-      }
-      if (a.code) {
-        float B = A;
-        if (a.alphas > 1) {
-          B = 0;
-#pragma unroll
-          for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[i] * g[i]));
-          B = lanes_join<Max>(B, a.group / V);
-        }
-        uint32_t w[V / 4];
-        codes_of<V>(a.code, B, h, g, w);
-        store_codes<V>(a.codes + r * a.ldcodes + c, n, w);
-        if (n > 0 && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
-      }
+      for (int i = 0; i < N; ++i) h[i] = h[i] * up * more;
+      write_norm<T, V, kWideThreads, NV>(a, cols, off, r, true, h, g, A, rho);
     }
   }
 }
 
 // ---- its gradient ------------------------------------------------------------------------------------------------
 // Block b sums dy xh over its rows per column and leaves the sums in part[b].
-template <class T, int TPR, int NV, int BLOCK, int WAVES>
+// AHEAD: the next rows are read ahead, as above.
+template <class T, int TPR, int NV, int BLOCK, int WAVES, bool AHEAD>
 __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR, N = NV * V;
   __shared__ float2 lds[BLOCK / 64];
@@ -397,27 +397,28 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> nh[NV], ndy[NV];
   const auto fetch = [&](int64_t r) {
-    cols.load((const T *)a.h + r * a.ldh, r < a.rows, nh);
-    cols.load((const T *)a.dy + r * a.lddy, r < a.rows, ndy);
+    cols.load((const T *)a.h + r * a.ldh, RPB == 1 || r < a.rows, a.past_in, nh);
+    cols.load((const T *)a.dy + r * a.lddy, RPB == 1 || r < a.rows, a.past_in, ndy);
   };
-  fetch((int64_t)blockIdx.x * RPB + sub);
+  if constexpr (AHEAD) fetch((int64_t)blockIdx.x * RPB + sub);
   float g[N], dg[N];
   cols.template gain<T>(a.gain, a.gain_f32, g);
 #pragma unroll
   for (int i = 0; i < N; ++i) dg[i] = 0;
   for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + sub;
-    const bool live = r < a.rows;
+    const bool live = RPB == 1 || r < a.rows;
     float h[N], dy[N];
     Raw<T, V> res[NV];
     float ss = 0, dot = 0;
-    if (a.dres) cols.load((const T *)a.dres + r * a.lddres, live, res);
+    if constexpr (!AHEAD) fetch(r);
+    if (a.dres) cols.load((const T *)a.dres + r * a.lddres, live, a.past_in, res);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       unpack<T, V>(nh[j], (float (&)[V])h[j * V]);
       unpack<T, V>(ndy[j], (float (&)[V])dy[j * V]);
     }
-    if (r0 + step < a.rows) fetch(r + step);
+    if (AHEAD && r0 + step < a.rows) fetch(r + step);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       ss = fmaf(h[i], h[i], ss);
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
       if (live) dg[i] = fmaf(dy[i], h[i], dg[i]);
     }
     if (a.dh)
-      cols.store((T *)a.dh + r * a.lddh, live, [&](int j, float (&o)[V]) {
+      cols.store((T *)a.dh + r * a.lddh, live, a.past_out, [&](int j, float (&o)[V]) {
         float w[V];
         if (a.dres) unpack<T, V>(res[j], w);
 #pragma unroll
@@ -464,34 +465,42 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
       a.part[(int64_t)blockIdx.x * a.d + c] = s;
     }
   } else {
-    cols.store(a.part + (int64_t)blockIdx.x * a.d, true, [&](int j, float (&v)[V]) {
+    cols.store(a.part + (int64_t)blockIdx.x * a.d, true, false, [&](int j, float (&v)[V]) {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = dg[j * V + i];
     });
   }
 }
 
-// Rows too long for registers: two passes as above; the block's partial row is added to in memory, each column by one
-// thread.
+// Rows too long for registers: two passes as above.  The block's sums of dgain do not stay in registers either: its
+// partial row in memory is added to, each column by one thread.
 template <class T>
 __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRows a) {
-  constexpr int V = 16 / sizeof(T), STEP = kWideThreads * V;
+  constexpr int V = 16 / sizeof(T), N = kWideValues, NV = N / V, STEP = kWideThreads * N;
+  using Cols = Columns<V, kWideThreads, NV>;
   __shared__ float2 lds[kWideThreads / 64];
-  const int c0 = threadIdx.x * V;
   const float inv_d = 1.0f / (float)a.d;
-  float *part = a.part + (int64_t)blockIdx.x * a.d;
+  float *const part = a.part + (int64_t)blockIdx.x * a.d;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T *ph = (const T *)a.h + r * a.ldh, *pdy = (const T *)a.dy + r * a.lddy;
+    const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&dy)[N], float (&g)[N]) {
+      Raw<T, V> x[NV], y[NV];
+      cols.load((const T *)a.h + r * a.ldh + off, true, false, x);
+      cols.load((const T *)a.dy + r * a.lddy + off, true, false, y);
+      cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        unpack<T, V>(x[j], (float (&)[V])h[j * V]);
+        unpack<T, V>(y[j], (float (&)[V])dy[j * V]);
+      }
+    };
     float ss, dot;
     const auto sums = [&](float up, float more) {
       ss = dot = 0;
-      for (int c = c0; c < a.d; c += STEP) {
-        float h[V], dy[V], g[V];
-        load_part<T, V>(ph + c, a.d - c, h);
-        load_part<T, V>(pdy + c, a.d - c, dy);
-        load_gain<T, V>(a.gain, a.gain_f32, c, a.d - c, g);
+      for (int off = 0; off < a.d; off += STEP) {
+        float h[N], dy[N], g[N];
+        read(Cols(a.d - off, threadIdx.x), off, h, dy, g);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < N; ++i) {
           h[i] = h[i] * up * more;
           ss = fmaf(h[i], h[i], ss);
           dot = fmaf(dy[i] * g[i], h[i], dot);
@@ -508,34 +517,37 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
       sums(up, more);
     }
     const float m = dot * rho * inv_d, rho1 = rho * (up * more);
-    for (int c = c0; c < a.d; c += STEP) {
-      const int n = a.d - c;
-      float h[V], dy[V], g[V], o[V];
-      load_part<T, V>(ph + c, n, h);
-      load_part<T, V>(pdy + c, n, dy);
-      load_gain<T, V>(a.gain, a.gain_f32, c, n, g);
+    for (int off = 0; off < a.d; off += STEP) {
+      const Cols cols(a.d - off, threadIdx.x);
+      float h[N], dy[N], g[N];
+      Raw<T, V> res[NV];
+      if (a.dres) cols.load((const T *)a.dres + r * a.lddres + off, true, false, res);
+      read(cols, off, h, dy, g);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        h[i] = h[i] * up * more * rho;
-        o[i] = rho1 * fmaf(-m, h[i], dy[i] * g[i]);
-      }
-      if (a.dh) {
-        if (a.dres) {
+      for (int i = 0; i < N; ++i) h[i] = h[i] * up * more * rho;
+      if (a.dh)
+        cols.store((T *)a.dh + r * a.lddh + off, true, a.past_out, [&](int j, float (&o)[V]) {
           float w[V];
-          load_part<T, V>((const T *)a.dres + r * a.lddres + c, n, w);
+          if (a.dres) unpack<T, V>(res[j], w);
 #pragma unroll
-          for (int i = 0; i < V; ++i) o[i] += w[i];
-        }
-        store_part<T, V>((T *)a.dh + r * a.lddh + c, n, o);
-      }
+          for (int i = 0; i < V; ++i) {
+            o[i] = rho1 * fmaf(-m, h[j * V + i], dy[j * V + i] * g[j * V + i]);
+            if (a.dres) o[i] += w[i];
+          }
+        });
       if (a.part) {
-        float s[V];
+        Raw<float, V> sum[NV];
+        if (r != blockIdx.x) {
+          cols.template load<float>(part + off, true, false, sum);
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = 0;
-        if (r != blockIdx.x) load_part<float, V>(part + c, n, s);
+          for (int j = 0; j < NV; ++j) sum[j] = Raw<float, V>{};
+        }
+        cols.store(part + off, true, false, [&](int j, float (&o)[V]) {
+          unpack<float, V>(sum[j], o);
 #pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = fmaf(dy[i], h[i], s[i]);
-        store_part<float, V>(part + c, n, s);
+          for (int i = 0; i < V; ++i) o[i] = fmaf(dy[j * V + i], h[j * V + i], o[i]);
+        });
       }
     }
   }
@@ -572,7 +584,7 @@ hipError_t by_width(int d, const F &f) {
   if (n <= 512) return f.template run<256, 2, 256>();
   if (n <= 1024) return f.template run<512, 2, 512>();
   if (n <= 2048) return f.template run<1024, 2, 1024>();
-  if constexpr (V == 4 && F::kDeep) {
+  if constexpr (V == 4) {
     if (n <= 4096) return f.template run<1024, 4, 1024>();
   }
   return f.wide();
@@ -580,7 +592,6 @@ hipError_t by_width(int d, const F &f) {
 
 template <class T>
 struct NormLaunch {
-  static constexpr bool kDeep = true;
   const NormRows &a;
   int cu_count;
   hipStream_t s;
@@ -601,18 +612,18 @@ struct NormLaunch {
 constexpr int kPartRows = 1024;
 template <class T>
 struct NormGradLaunch {
-  static constexpr bool kDeep = false;   // four vectors of each input and the sums do not fit 128 registers
   const NormGradRows &a;
   int cu_count;
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
     constexpr int V = 16 / sizeof(T), W = NV * V <= 8 ? 5 : 4;
+    constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
     int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);
     if (most > kPartRows) most = kPartRows;
     const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-    if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK, W><<<grid, BLOCK, 0, s>>>(a);
+    if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD><<<grid, BLOCK, 0, s>>>(a);
     return dgain(grid);
   }
   hipError_t wide() const {

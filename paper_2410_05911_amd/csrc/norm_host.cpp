@@ -40,6 +40,12 @@ bool stride_ok(const void *p, int64_t rows, int64_t ld, int64_t least) {
   return !p || (ld >= least && ld <= kMaxSpan / (rows > 0 ? rows : 1));
 }
 
+// Which sizes go past the 256 MB of cache between the chip and its memory.  Inputs of more than half of it will not be
+// found there again, and leave it to the outputs if they go past (16384 x 4096 bf16 with residual: 102 -> 81 us); smaller
+// ones often lie there still, from the kernel that made them (49152 x 128 fp32: 14.7 us, past it 16.3).  Outputs go past
+// it where they are well over its size (16384 x 8192 to 8-bit codes 183 -> 170 us; 16384 x 4096, 268 MB, 81 -> 94).
+constexpr int64_t kPastInputs = (int64_t)128 << 20, kPastOutputs = (int64_t)384 << 20;
+
 }  // namespace
 
 extern "C" {
@@ -78,9 +84,11 @@ aecct_status aecct_rms_norm(const aecct_rms_norm_args *a, void *stream) {
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     return AECCT_ERR_DEVICE;
+  const int64_t values = a->rows * a->d, in_bytes = values * size * (a->res ? 2 : 1),
+                out_bytes = values * (size * ((a->h ? 1 : 0) + (a->y ? 1 : 0)) + (coded ? 1 : 0));
   const aecct::NormRows n{a->rows, (int)a->d, a->eps, a->gain_type == AECCT_F32, a->code_type, (int)group, (int)alphas,
                           a->x, a->res, a->gain, a->h, a->y, (uint8_t *)a->codes, a->alpha, a->ldx, a->ldres, a->ldh,
-                          a->ldy, a->ldcodes};
+                          a->ldy, a->ldcodes, in_bytes > kPastInputs, out_bytes > kPastOutputs};
   return aecct::launch_rms_norm(a->type, n, cus, (hipStream_t)stream) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
 }
 
@@ -122,8 +130,10 @@ aecct_status aecct_rms_norm_grad(const aecct_rms_norm_grad_args *a, void *worksp
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     return AECCT_ERR_DEVICE;
+  const int64_t values = a->rows * a->d;
   const aecct::NormGradRows n{a->rows, (int)a->d, a->eps, a->gain_type == AECCT_F32, a->h, a->dy, a->dres, a->gain, a->dh,
-                              a->ldh, a->lddy, a->lddres, a->lddh, part, a->dgain};
+                              a->ldh, a->lddy, a->lddres, a->lddh, part, a->dgain,
+                              values * size * (a->dres ? 3 : 2) > kPastInputs, a->dh && values * size > kPastOutputs};
   return aecct::launch_rms_norm_grad(a->type, n, cus, (hipStream_t)stream) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
 }
 

@@ -18,12 +18,37 @@ struct alignas(sizeof(T)) Vec {
   T v[V];
 };
 
-template <class T, int V>
+// B bytes (8 or 16) at any 2-byte address; NT: marked as not to be used again soon.
+template <int B>
+struct Wide {
+  typedef uint32_t type __attribute__((ext_vector_type(B / 4), aligned(2)));
+};
+template <int B, bool NT>
+__device__ __forceinline__ void copy_in(const void *p, uint32_t *w) {
+  if constexpr (NT && (B == 8 || B == 16)) {
+    const typename Wide<B>::type t = __builtin_nontemporal_load((const typename Wide<B>::type *)p);
+    __builtin_memcpy(w, &t, B);
+  } else {
+    __builtin_memcpy(w, p, B);
+  }
+}
+template <int B, bool NT>
+__device__ __forceinline__ void copy_out(void *p, const void *w) {
+  if constexpr (NT && (B == 8 || B == 16)) {
+    typename Wide<B>::type t;
+    __builtin_memcpy(&t, w, B);
+    __builtin_nontemporal_store(t, (typename Wide<B>::type *)p);
+  } else {
+    __builtin_memcpy(p, w, B);
+  }
+}
+
+template <class T, int V, bool NT = false>
 __device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
   Vec<T, V> t;
 #pragma unroll
   for (int i = 0; i < V; ++i) t.v[i] = (T)f[i];
-  __builtin_memcpy(p, &t, sizeof(t));
+  copy_out<(int)sizeof(t), NT>(p, &t);
 }
 
 // The same in two steps, for values that are read ahead: as stored, two 16-bit values a register, then as fp32.
@@ -31,9 +56,9 @@ template <class T, int V>
 struct Raw {
   uint32_t w[V * sizeof(T) / 4];
 };
-template <class T, int V>
+template <class T, int V, bool NT = false>
 __device__ __forceinline__ void load_raw(const T *p, Raw<T, V> &r) {
-  __builtin_memcpy(r.w, p, sizeof(r.w));
+  copy_in<(int)sizeof(r.w), NT>(p, r.w);
 }
 template <class T, int V>   // the first n < V values, the others 0
 __device__ __forceinline__ void load_raw_part(const T *p, int n, Raw<T, V> &r) {
@@ -62,27 +87,27 @@ __device__ __forceinline__ void unpack(const Raw<T, V> &r, float (&f)[V]) {
   }
 }
 
-template <class T, int V>
+template <class T, int V, bool NT = false>
 __device__ __forceinline__ void load_vec(const T *p, float (&f)[V]) {
   Raw<T, V> r;
-  load_raw<T, V>(p, r);
+  load_raw<T, V, NT>(p, r);
   unpack<T, V>(r, f);
 }
 
 // The first `n` (clamped to 0..V) of V values; the others are 0 (load) or left alone (store).
-template <class T, int V>
+template <class T, int V, bool NT = false>
 __device__ __forceinline__ void load_part(const T *p, int n, float (&f)[V]) {
   if (n >= V) {
-    load_vec<T, V>(p, f);
+    load_vec<T, V, NT>(p, f);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = i < n ? (float)p[i] : 0.0f;
   }
 }
-template <class T, int V>
+template <class T, int V, bool NT = false>
 __device__ __forceinline__ void store_part(T *p, int n, const float (&f)[V]) {
   if (n >= V) {
-    store_vec<T, V>(p, f);
+    store_vec<T, V, NT>(p, f);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i)

@@ -57,8 +57,9 @@ struct AdamScalars {
 };
 
 // Sums of squares of the table's values, one double a block, to part[0 .. blocks); with now, *now from *step too.
-hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, const int64_t *step, AdamNow *now,
-                              const AdamScalars &o, hipStream_t s);
+// alone: no pass over the values follows.
+hipError_t launch_sum_squares(const SumTable<kSumRanges> &t, double *part, int blocks, bool alone, const int64_t *step,
+                              AdamNow *now, const AdamScalars &o, hipStream_t s);
 // *norm from `parts` sums.
 hipError_t launch_norm(const double *part, int parts, float *norm, hipStream_t s);
 hipError_t launch_clip(const ClipTable<kClipRanges> &t, const double *part, int parts, double max_norm, float *norm,

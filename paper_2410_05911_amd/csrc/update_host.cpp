@@ -129,8 +129,8 @@ Work work_of(void *workspace) {
 }
 
 // The norm's partial sums, and *w.now from *step if that is given.
-hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, const int64_t *step, const AdamScalars &o,
-                hipStream_t s) {
+hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, bool alone, const int64_t *step,
+                const AdamScalars &o, hipStream_t s) {
   parts = 0;
   using Table = SumTable<kSumRanges>;
   const hipError_t e = for_tables<Table>(
@@ -138,7 +138,7 @@ hipError_t sums(const aecct_tensor *g, int32_t n, const Work &w, int &parts, con
       [&](Table &t, int i) { t.g[t.n] = g[i].data; },
       [&](const Table &t) {
         const int blocks = std::min(t.unit0[t.n], kMaxSumBlocks);
-        const hipError_t r = launch_sum_squares(t, w.part + parts, blocks, step, step && !parts ? w.now : nullptr, o, s);
+        const hipError_t r = launch_sum_squares(t, w.part + parts, blocks, alone, step, step && !parts ? w.now : nullptr, o, s);
         parts += blocks;
         return r;
       });
@@ -177,7 +177,7 @@ aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, 
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  const hipError_t e = sums(grads, n, w, parts, nullptr, AdamScalars{}, s);
+  const hipError_t e = sums(grads, n, w, parts, true, nullptr, AdamScalars{}, s);
   return st(e != hipSuccess ? e : launch_norm(w.part, parts, norm, s));
 }
 
@@ -202,7 +202,7 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
-  const hipError_t e = sums(grads, n, w, parts, nullptr, AdamScalars{}, s);
+  const hipError_t e = sums(grads, n, w, parts, false, nullptr, AdamScalars{}, s);
   if (e != hipSuccess) return st(e);
   if (!parts) return st(launch_norm(w.part, 0, norm, s));
   using Table = ClipTable<kClipRanges>;
@@ -257,7 +257,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
   const AdamScalars o{opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay, opt->max_norm, opt->lr_device};
-  hipError_t e = opt->max_norm > 0 || norm ? sums(grads, n, w, parts, step, o, s) : launch_now(step, w.now, o, s);
+  hipError_t e = opt->max_norm > 0 || norm ? sums(grads, n, w, parts, false, step, o, s) : launch_now(step, w.now, o, s);
   if (e != hipSuccess) return st(e);
   using Table = AdamTable<kAdamRanges>;
   bool first = true;
