@@ -35,7 +35,7 @@ struct NormGradRows {
   int64_t ldh, lddy, lddres, lddh;
   float *part;                 // partial sums of dgain, or null: no dgain
   float *dgain;
-  bool past_in, past_out;
+  bool past_in;
 };
 // Blocks at most, so rows of the partial sums: norm_grad_part_rows(rows, d) of d floats each.
 int64_t norm_grad_part_rows(int64_t rows, int d);

@@ -133,7 +133,7 @@ aecct_status aecct_rms_norm_grad(const aecct_rms_norm_grad_args *a, void *worksp
   const int64_t values = a->rows * a->d;
   const aecct::NormGradRows n{a->rows, (int)a->d, a->eps, a->gain_type == AECCT_F32, a->h, a->dy, a->dres, a->gain, a->dh,
                               a->ldh, a->lddy, a->lddres, a->lddh, part, a->dgain,
-                              values * size * (a->dres ? 3 : 2) > kPastInputs, a->dh && values * size > kPastOutputs};
+                              values * size * (a->dres ? 3 : 2) > kPastInputs};
   return aecct::launch_rms_norm_grad(a->type, n, cus, (hipStream_t)stream) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
 }
 
