@@ -596,9 +596,12 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dgain(const float *part, int 
   __shared__ float lds[1024];
   const int c = blockIdx.x * 16 + threadIdx.x % 16;
   float s = 0;
-  if (c < d) {
-#pragma unroll 4
-    for (int r = threadIdx.x / 16; r < rows; r += 64) s += part[(int64_t)r * d + c];
+  for (int r = threadIdx.x / 16; r < rows; r += 64 * 8) {   // eight loads in flight
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c < d && r + 64 * j < rows ? part[(int64_t)(r + 64 * j) * d + c] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[j];
   }
   lds[threadIdx.x] = s;
   for (int half = 512; half >= 16; half /= 2) {
@@ -668,7 +671,9 @@ struct NormGradLaunch {
     constexpr int V = 16 / sizeof(T), W = NV * V <= 8 ? 5 : 4;
     constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
-    int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);
+    // A long row leaves a long partial sum, so half the blocks (4096 x 4096 bf16 26.7 -> 24.0 us); for shorter rows they
+    // hide more (3001 x 1111 fp16 18.0 us, with half 20.0).
+    int64_t most = (int64_t)cu_count * (W * 256 / BLOCK) / (TPR == 256 && NV * V == 16 ? 2 : 1);
     if (most > kPartRows) most = kPartRows;
     const unsigned grid = even_grid(blocks, most);
     if (grid && a.past_in) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, true><<<grid, BLOCK, 0, s>>>(a);
