@@ -493,12 +493,13 @@ typedef struct aecct_tensor {
 aecct_status aecct_update_workspace_size(int32_t n, size_t *bytes);
 
 /* norm (device fp32 [1]) = sqrt of the sum of the squares of every value of the list, summed in fp64 (0 for an
- * empty list).  Tensors of any types; they may overlap.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE. */
+ * empty list; infinity where finite values have a norm past fp32).  Tensors of any types; they may overlap.  Errors:
+ * INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE. */
 aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, void *workspace, size_t workspace_bytes,
                              void *stream);
 
 /* Clipping by that norm: out[i] = grads[i] min(1, max_norm / norm).  out: a list of the same counts (any types), or
- * NULL for in place.  norm as above, before clipping.  Where it is not finite the values are left unscaled.
+ * NULL for in place.  norm as above, before clipping.  Where any value is not finite, none is scaled.
  * max_norm >= 0; +infinity clips nothing.  No output tensor overlaps another tensor of either list, except
  * that out[i] may be grads[i] itself.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE. */
 aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out, int32_t n, double max_norm, float *norm,
@@ -521,7 +522,8 @@ typedef struct aecct_adam_options {
  * read only; copies (or NULL): the updated parameter rounded to another type (a copy of count 0 is left out).
  *   step   device int64 [1], the number of updates made;
  *   norm   device fp32 [1], the norm of the gradients before clipping, or NULL.
- * The norm is taken where max_norm > 0 or norm is given; where it then is not finite, nothing but norm is written.
+ * The norm is taken where max_norm > 0 or norm is given; where any gradient then is not finite, nothing but norm is
+ * written.
  * No written tensor overlaps another tensor of the call.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE.
  */
 aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, const aecct_tensor *v,

@@ -443,7 +443,8 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
 
 class TensorList:
     """A list of contiguous CUDA tensors (float32, bfloat16, float16; one device) as the library takes it.  A program that
-    uses the same tensors again and again keeps the list; the calls below take any sequence of tensors too."""
+    uses the same tensors again and again keeps the list; the calls below take any sequence of tensors too.  The list
+    keeps the tensors, whose memory must stay where it is (no resize_ or set_ on them)."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -500,7 +501,7 @@ def grad_norm(grads, stream=None):
 
 def grad_clip(grads, max_norm: float, out=None, stream=None):
     """Scales every gradient by min(1, max_norm / norm), in place or into the tensors of `out`; returns the norm before
-    clipping.  Where it is not finite the values stay unscaled."""
+    clipping.  Where any value is not finite, none is scaled."""
     import torch
     if stream is not None:
         with _on_stream(stream):
@@ -558,7 +559,7 @@ class Adam:
 
     def step(self, grads, lr=None, stream=None):
         """One update from the gradients (a TensorList or any sequence, any of the types).  Returns the norm before
-        clipping (None without max_norm); where it is not finite nothing is updated."""
+        clipping (None without max_norm); where any gradient then is not finite nothing is updated."""
         import torch
         if stream is not None:
             with _on_stream(stream):
@@ -841,7 +842,8 @@ class Trainer:
     def update(self, params: dict, grads: dict, state: dict, lr, betas=(0.9, 0.999), eps: float = 1e-8,
                weight_decay: float = 0.0, max_norm=None, stream=None):
         """One Adam update of every parameter from `grad`'s gradients (aecct_train_update), in place.  Returns the norm
-        of the gradients before clipping (None without max_norm); where it is not finite nothing is updated."""
+        of the gradients before clipping (None without max_norm); where any gradient then is not finite nothing is
+        updated."""
         import torch
         if stream is not None:
             with _on_stream(stream):

@@ -154,9 +154,20 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double *part, int parts
   if (threadIdx.x == 0) *norm = (float)n;
 }
 
-// min(1, max_norm / norm), and 1 for a norm that is not finite
-__device__ __forceinline__ float clip_factor(double norm, double max_norm) {
-  return norm > max_norm && norm <= 1.7976931348623157e308 ? (float)(max_norm / norm) : 1.0f;
+// min(1, max_norm / norm), and 1 for a norm that is not finite.  A factor below fp32's normal range (a norm past it) is
+// taken in two, the first a power of two.
+struct Factor {
+  float up = 1.0f, f = 1.0f;
+  __device__ __forceinline__ float of(float g) const { return g * up * f; }
+};
+__device__ __forceinline__ Factor clip_factor(double norm, double max_norm) {
+  Factor r;
+  if (norm > max_norm && norm <= 1.7976931348623157e308) {
+    const double f = max_norm / norm;
+    r.up = f < 0x1p-100 ? 0x1p-64f : 1.0f;
+    r.f = (float)(f < 0x1p-100 ? f * 0x1p64 : f);
+  }
+  return r;
 }
 
 template <int N>
@@ -164,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double 
   __shared__ double lds[kThreads / 64];
   const double n = norm_of(part, parts, lds);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-  const float f = clip_factor(n, max_norm);
+  const Factor f = clip_factor(n, max_norm);
   int k = t.n - 1;
   for (int u = t.unit0[t.n] - 1 - (int)blockIdx.x; u >= 0; u -= gridDim.x) {
     k = range_of(t, u, k);
@@ -176,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double 
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[j][i] *= f;
+      for (int i = 0; i < 4; ++i) g[j][i] = f.of(g[j][i]);
       store4(t.out[k], t.out_type[k], i0 + 4 * kThreads * j, c - i0 - 4 * kThreads * j, g[j]);
     }
   }
@@ -217,7 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double 
   };
   int u = t.unit0[t.n] - 1 - (int)blockIdx.x;
   if (u >= 0) fetch(u);
-  float f = 1.0f;
+  Factor f;
   if (parts) {
     const double n = norm_of(part, parts, lds);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
@@ -248,7 +259,7 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double 
     if (u >= 0) fetch(u);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float x = g[i] * f;
+      const float x = f.of(g[i]);
       m[i] = fmaf(b1, m[i], c1 * x);
       v[i] = fmaf(b2, v[i], c2 * (x * x));
       p[i] -= fmaf(decay, p[i], size * m[i] / fmaf(sqrtf(v[i]), root, eps));

@@ -383,3 +383,58 @@ def test_norm_binding_refuses(P):
     with pytest.raises(P.AecctError) as e:
         P.rms_norm(torch.zeros(1, 65537, device="cuda"))
     assert e.value.status == P.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,d,type", [(50003, 4096, "bf16"), (33001, 2051, "fp32"), (9001, 16384, "fp32"), (1200003, 128, "fp16")])
+def test_norm_of_large_batches(P, rows, d, type):
+    """Inputs and outputs larger than the caches (read and written past them), many rows a block; compared on a spread of
+    rows, and dgain in whole."""
+    print(f"[norm] {rows} x {d} {type}", flush=True)
+    t = TYPES[type]
+    x, res = _rand(rows, d, t, 1), _rand(rows, d, t, 2)
+    gain = 1 + 0.3 * torch.randn(d, device="cuda")
+    y, h, codes, alpha = P.rms_norm(x, gain, res, code_type=torch.int8, group=64)
+    at = torch.cat([torch.arange(0, rows, 97, device="cuda"), torch.arange(rows - 40, rows, device="cuda")])
+    _check_norm((y[at], h[at], codes[at], alpha[at]), x[at], gain, res[at], 1e-5, "int8", 64)
+    dh, dgain = P.rms_norm_grad(h, x, gain, res)
+    want, bound, _, _ = _grad_formula(h[at], x[at], gain, res[at], float(np.float32(1e-5)))
+    _near(dh[at], want, bound, "dh")
+    total, size = torch.zeros(d, dtype=torch.float64, device="cuda"), torch.zeros(d, dtype=torch.float64, device="cuda")
+    for hp, xp in zip(h.split(4096), x.split(4096)):
+        hd = hp.double()
+        terms = xp.double() * hd / torch.sqrt((hd * hd).mean(1, keepdim=True) + float(np.float32(1e-5)))
+        total += terms.sum(0)
+        size += terms.abs().sum(0)
+    _near(dgain, total, U * (60 + 600 + rows / 256) * size, "dgain")
+
+
+def test_norm_of_more_rows_than_32_bits_count(P):
+    """2^31 + 70 rows of one value, all of them one row of memory."""
+    rows = 2 ** 31 + 70
+    x = torch.tensor([[-3.0]], device="cuda", dtype=torch.bfloat16)
+    y = torch.zeros(rows, 1, device="cuda", dtype=torch.bfloat16)
+    P.rms_norm(x.expand(rows, 1), None, None, 0.0, y=y)
+    assert (y[:100] == -1).all() and (y[-100:] == -1).all() and y.min().item() == -1 and y.max().item() == -1
+
+
+@pytest.mark.parametrize("d", [7, 200, 3001, 20000])
+def test_norm_with_single_outputs(P, d):
+    """h alone, codes alone, dgain alone (through the C ABI, which takes any of them)."""
+    import ctypes as C
+    x, res = _rand(37, d, torch.bfloat16, 1), _rand(37, d, torch.bfloat16, 2)
+    y, h, codes, alpha = P.rms_norm(x, None, res, code_type=torch.float8_e4m3fn)
+    h2 = torch.empty_like(x)
+    P.rms_norm(x, None, res, h=h2, with_y=False)
+    assert torch.equal(h2, h)
+    none, _, c2, a2 = P.rms_norm(h, None, None, with_y=False, code_type=torch.int8)
+    c3 = P.rms_norm(h, None, None, code_type=torch.int8)
+    assert none is None and torch.equal(c2, c3[2]) and torch.equal(a2, c3[3])
+    dh, dgain = P.rms_norm_grad(h, x)
+    only = torch.empty(d, device="cuda")
+    size = C.c_size_t()
+    assert P.lib().aecct_rms_norm_grad_workspace_size(37, d, C.byref(size)) == P.OK
+    for shift in (0, 4):     # a workspace at any place
+        ws = torch.full((size.value + shift,), 255, dtype=torch.uint8, device="cuda")
+        a = P.RmsNormGradArgs(37, d, P.BF16, P.F32, 1e-5, h.data_ptr(), d, x.data_ptr(), d, None, 0, None, None, 0, only.data_ptr())
+        assert P.lib().aecct_rms_norm_grad(C.byref(a), ws.data_ptr() + shift, size.value, None) == P.OK
+        assert torch.equal(only, dgain)

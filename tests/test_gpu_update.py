@@ -345,3 +345,48 @@ def test_update_binding_refuses(P):
     with pytest.raises(P.AecctError):
         P.Adam([torch.zeros(8, device="cuda", dtype=torch.float16)], m=[torch.zeros(8, device="cuda")],
                v=[torch.zeros(8, device="cuda")]).step([a])
+
+
+def test_lists_of_more_values_than_32_bits_count(P):
+    n = 2 ** 31 + 4100
+    g = torch.full((n,), 0.5, device="cuda", dtype=torch.bfloat16)
+    g[-1] = 3.0
+    want = math.sqrt(0.25 * (n - 1) + 9.0)
+    assert abs(P.grad_norm([g]).item() - want) <= 1.01 * U * want
+    P.grad_clip([g], want / 2)
+    assert (g[:5000] == 0.25).all() and (g[-5000:-1] == 0.25).all() and g[-1] == 1.5 and (g[2 ** 30:2 ** 30 + 9] == 0.25).all()
+    p, m, v = (torch.zeros(n, device="cuda") for _ in range(3))
+    P.Adam([p], lr=1.0, m=[m], v=[v]).step([g])
+    for part in (p[:5000], p[2 ** 31 - 5000:2 ** 31 + 4099]):
+        assert ((part + 1).abs() < 1e-4).all()
+    assert abs(m[-1].item() - 0.15) < 1e-6 and abs(v[-1].item() - 2.25e-3) < 1e-8
+
+
+def test_norm_past_fp32_still_clips(P):
+    """Finite values whose norm is past fp32: it is written as infinity, and they are scaled all the same."""
+    g = [torch.full((10000,), 3e38, device="cuda"), torch.full((3,), -3e38, device="cuda")]
+    assert math.isinf(P.grad_clip(g, 1.0).item())
+    want = 1 / math.sqrt(10003)
+    assert (g[0] - want).abs().max().item() <= 4 * U * want and (g[1] + want).abs().max().item() <= 4 * U * want
+    p = [torch.zeros(5, device="cuda")]
+    opt = P.Adam(p, lr=0.5, max_norm=1e-3)
+    assert math.isinf(opt.step([torch.full((5,), 3e38, device="cuda")]).item()) and opt.step_count.item() == 1
+    assert (p[0] + 0.5).abs().max().item() < 1e-4
+
+
+def test_tensors_back_to_back_and_apart_agree(P):
+    """Lists that lie back to back are taken as one range, in any cut; the values do not depend on it."""
+    n = 50021
+    flat = torch.randn(n, device="cuda") * 0.01
+    cuts = [1, 4095, 1, 0, 9000, 4097, n - 17194]
+    whole, parts, apart = [flat.clone()], list(flat.clone().split(cuts)), [t.clone() for t in flat.split(cuts)]
+    norms = [P.grad_clip(ts, 0.05).item() for ts in (whole, parts, apart)]
+    assert max(norms) - min(norms) <= 2 * U * norms[0]
+    assert torch.equal(torch.cat(parts), whole[0])            # one range either way: the same sum
+    assert (torch.cat(apart) - whole[0]).abs().max().item() <= 4 * U * whole[0].abs().max().item()
+    back = list(reversed(parts))                              # the list in another order than memory
+    before = [t.clone() for t in back]
+    P.grad_clip(back, 0.01)
+    f = 0.01 / _norm64(before)
+    for t, b in zip(back, before):
+        _near(t, b.double() * f, 2.1 * U * (b.double() * f).abs(), "reversed")
