@@ -19,6 +19,9 @@ struct Max {   // of non-negative floats, whose bits order like them; NaN is abo
     return __builtin_bit_cast(float, max(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)));
   }
 };
+struct Largest {   // of any floats
+  static __device__ __forceinline__ float join(float a, float b) { return fmaxf(a, b); }
+};
 template <class Op, int CTRL>
 __device__ __forceinline__ float dpp_join(float v) {
   return Op::join(v, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true)));
@@ -185,28 +188,47 @@ __device__ __forceinline__ int row_of_block() {
 }
 
 // ---- codes -----------------------------------------------------------------------------------------------------
-// code = round(p Q / A) with p = h gain and A = max |p|: rho is a factor of both y and alpha and drops out.  The quotient
-// is taken as (p + e)(q + q1), e the rounding error of p, q a near quotient Q / A and q1 its remainder's: a code then
-// differs from the exact one only where the quotient is within about 2^-24 of a tie.  `up` keeps A and q normal numbers.
+// code = round(p Q / A) with p = h gain and A = max |p|: rho is a factor of both y and alpha and drops out.  Everything is
+// taken with its rounding error beside it, p + e and A + E, and the quotient as (p + e)(q + q1), q a near Q / A and q1
+// what it lacks: a code then differs from the exact one only where the quotient is within 2^-24 of a tie.
+constexpr float kNoTail = -3e38f;
+// The largest rounding error among the values whose |p| is A.
+template <int N>
+__device__ __forceinline__ float tail_of(float A, const float *h, const float *g) {
+  float E = kNoTail;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float p = fabsf(h[i]) * fabsf(g[i]), e = fmaf(fabsf(h[i]), fabsf(g[i]), -p);
+    E = p == A ? fmaxf(E, e) : E;
+  }
+  return E;
+}
 struct CodeScale {
-  float up, q, q1;
+  float up, q, q1;   // up: a power of two that keeps A and q normal numbers
 };
-__device__ __forceinline__ CodeScale code_scale(float A, float most) {
+__device__ __forceinline__ CodeScale code_scale(float A, float E, float most) {
   CodeScale s;
   s.up = A < 0x1p-60f ? 0x1p60f : A > 0x1p60f ? 0x1p-60f : 1.0f;
-  const float b = A * s.up, r = __builtin_amdgcn_rcpf(b);
+  const float b = A * s.up, r = __builtin_amdgcn_rcpf(b), t = E > kNoTail ? E * s.up : 0.0f;
   s.q = A == 0.0f ? 0.0f : most * r;
-  s.q1 = A == 0.0f || !(b <= 3e38f) ? 0.0f : fmaf(-s.q, b, most) * r;
+  s.q1 = A == 0.0f || !(b <= 3e38f) ? 0.0f : fmaf(-s.q, t, fmaf(-s.q, b, most)) * r;
   return s;
 }
 template <int V>
-__device__ __forceinline__ void codes_of(int code, float A, const float *h, const float *g, uint32_t (&w)[V / 4]) {
-  const CodeScale s = code_scale(A, code == 1 ? 127.0f : 448.0f);
+__device__ __forceinline__ void codes_of(int code, float A, float E, const float *h, const float *g, uint32_t (&w)[V / 4]) {
+  const CodeScale s = code_scale(A, E, code == 1 ? 127.0f : 448.0f);
   float v[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float x = h[i] * s.up, p = x * g[i], e = fmaf(x, g[i], -p);
+    const float p = h[i] * g[i], e = fmaf(h[i], g[i], -p);
     v[i] = fmaf(p, s.q, fmaf(p, s.q1, e * s.q));
+  }
+  if (s.up != 1.0f) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float x = h[i] * s.up, p = x * g[i], e = fmaf(x, g[i], -p);
+      v[i] = fmaf(p, s.q, fmaf(p, s.q1, e * s.q));
+    }
   }
   if (code == 1) {
     const uint32_t keep = A == A ? 0xffffffffu : 0u;
@@ -238,7 +260,7 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, const uint32_t (
 // y and the codes of a row's columns from `off` on, those that cols holds.
 template <class T, int V, int TPR, int NV>
 __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, TPR, NV> &cols, int off, int64_t r, bool live,
-                                           const float (&h)[NV * V], const float (&g)[NV * V], float A, float rho) {
+                                           const float (&h)[NV * V], const float (&g)[NV * V], float A, float E, float rho) {
   if (a.y)
     cols.store((T *)a.y + r * a.ldy + off, live, a.past_out, [&](int j, float (&v)[V]) {
 #pragma unroll
@@ -248,15 +270,16 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = off + cols.col(j);
-    float B = A;
+    float B = A, F = E;
     if (a.alphas > 1) {
       B = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
       B = lanes_join<Max>(B, a.group / V);
+      F = lanes_join<Largest>(tail_of<V>(B, h + j * V, g + j * V), a.group / V);
     }
     uint32_t w[V / 4];
-    codes_of<V>(a.code, B, h + j * V, g + j * V, w);
+    codes_of<V>(a.code, B, F, h + j * V, g + j * V, w);
     uint8_t *to = a.codes + r * a.ldcodes + c;
     if (live && cols.full(j)) __builtin_memcpy(to, w, V);
     if (live && cols.last && j == cols.jt) store_codes<V>(to, cols.tail, w);
@@ -319,7 +342,13 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
       for (int i = 0; i < NV * V; ++i) A = Max::join(A, fabsf(h[i] * g[i]));
       row_join<Max, TPR>(none, A, lds);
     }
-    write_norm<T, V, TPR, NV>(a, cols, 0, r, live, h, g, A, rho);
+    float E = kNoTail;
+    if (a.code && a.alphas == 1) {
+      float none = 0;
+      E = tail_of<NV * V>(A, h, g);
+      row_join<Largest, TPR>(none, E, lds);
+    }
+    write_norm<T, V, TPR, NV>(a, cols, 0, r, live, h, g, A, E, rho);
   }
 }
 
@@ -356,9 +385,10 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
         }
       }
     };
-    float ss, A;
+    float ss, A, E;
     const auto sums = [&](float up, float more) {
       ss = A = 0;
+      E = kNoTail;
       for (int off = 0; off < a.d; off += kWideStep) {
         float h[N], g[N];
         read(Cols(a.d - off, threadIdx.x), off, h, g);
@@ -366,10 +396,18 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
         for (int i = 0; i < N; ++i) {
           h[i] = h[i] * up * more;
           ss = fmaf(h[i], h[i], ss);
-          A = Max::join(A, fabsf(h[i] * g[i]));
+          const float p = fabsf(h[i]) * fabsf(g[i]), e = fmaf(fabsf(h[i]), fabsf(g[i]), -p), B = Max::join(A, p);
+          E = B != A ? e : p == A ? fmaxf(E, e) : E;
+          A = B;
         }
       }
+      const float own = A;
       row_join<Max, kWideThreads>(ss, A, lds);
+      if (a.code) {
+        float none = 0;
+        E = own == A ? E : kNoTail;
+        row_join<Largest, kWideThreads>(none, E, lds);
+      }
     };
     sums(1.0f, 1.0f);
     float rho = near_rho(ss, inv_d, a.eps), up = 1.0f, more = 1.0f;
@@ -390,7 +428,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
         });
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = h[i] * up * more;
-      write_norm<T, V, kWideThreads, NV>(a, cols, off, r, true, h, g, A, rho);
+      write_norm<T, V, kWideThreads, NV>(a, cols, off, r, true, h, g, A, E, rho);
     }
   }
 }

@@ -438,3 +438,20 @@ def test_norm_with_single_outputs(P, d):
         a = P.RmsNormGradArgs(37, d, P.BF16, P.F32, 1e-5, h.data_ptr(), d, x.data_ptr(), d, None, 0, None, None, 0, only.data_ptr())
         assert P.lib().aecct_rms_norm_grad(C.byref(a), ws.data_ptr() + shift, size.value, None) == P.OK
         assert torch.equal(only, dgain)
+
+
+@pytest.mark.parametrize("d,group", [(32, 0), (128, 0), (1000, 0), (1000, 32), (4096, 128), (9001, 0), (9001, 64), (30000, 0), (30000, 128)])
+def test_norm_codes_are_the_exact_ones_but_at_ties(P, d, group):
+    """Without a residual h is exact, and a code's quotient h gain Q / max|h gain| (rho drops out) is off by its own last
+    rounding only, u of it: the code is the nearest to the exact quotient, or the quotient is within u of a tie."""
+    rows = 400 if d < 5000 else 60
+    for type in TYPES:
+        x = _rand(rows, d, TYPES[type], d)
+        gain = 1 + 0.3 * torch.randn(d, device="cuda")
+        p = x.double() * gain.double()
+        a = torch.stack([q.abs().amax(1) for q in p.split(group or d, 1)], 1)[:, torch.arange(d, device="cuda") // (group or d)]
+        for code, (kind, most) in CODES.items():
+            q = p * most / a
+            got = P.rms_norm(x, gain, None, 1e-5, with_y=False, code_type=kind, group=group)[2].to(torch.float32).double()
+            step = torch.ones_like(q) if code == "int8" else torch.exp2(torch.floor(torch.log2(q.abs().clamp_min(2.0 ** -6))) - 3)
+            _near(got, q, 0.5 * step + 1.01 * U * q.abs(), (type, code))
