@@ -118,22 +118,20 @@ struct Columns {
   template <bool NT, class T>
   __device__ __forceinline__ void load_full(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) {
       if (live && full(j)) load_raw<T, V, NT>(p + col(j), v[j]);
+      else v[j] = Raw<T, V>{};
+    }
   }
   // past: read past the caches
   template <class T>
   __device__ __forceinline__ void load(const T *p, bool live, bool past, Raw<T, V> (&v)[NV]) const {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = Raw<T, V>{};
     if (past) load_full<true>(p, live, v);
     else load_full<false>(p, live, v);
     load_last(p, live, v);
   }
   template <bool PAST, class T>
   __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = Raw<T, V>{};
     load_full<PAST>(p, live, v);
     load_last(p, live, v);
   }
@@ -192,6 +190,19 @@ __device__ __forceinline__ int row_of_block() {
 // taken with its rounding error beside it, p + e and A + E, and the quotient as (p + e)(q + q1), q a near Q / A and q1
 // what it lacks: a code then differs from the exact one only where the quotient is within 2^-24 of a tie.
 constexpr float kNoTail = -3e38f;
+// max |p| of each vector of a thread's values
+template <int V, int NV>
+__device__ __forceinline__ float vector_max(const float *h, const float *g, float (&m)[NV]) {
+  float A = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    m[j] = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m[j] = Max::join(m[j], fabsf(h[j * V + i] * g[j * V + i]));
+    A = Max::join(A, m[j]);
+  }
+  return A;
+}
 // The largest rounding error among the values whose |p| is A.
 template <int N>
 __device__ __forceinline__ float tail_of(float A, const float *h, const float *g) {
@@ -260,7 +271,8 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, const uint32_t (
 // y and the codes of a row's columns from `off` on, those that cols holds.
 template <class T, int V, int TPR, int NV>
 __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, TPR, NV> &cols, int off, int64_t r, bool live,
-                                           const float (&h)[NV * V], const float (&g)[NV * V], float A, float E, float rho) {
+                                           const float (&h)[NV * V], const float (&g)[NV * V], const float (&m)[NV], float A,
+                                           float E, float rho) {
   if (a.y)
     cols.store((T *)a.y + r * a.ldy + off, live, a.past_out, [&](int j, float (&v)[V]) {
 #pragma unroll
@@ -272,10 +284,7 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
     const int c = off + cols.col(j);
     float B = A, F = E;
     if (a.alphas > 1) {
-      B = 0;
-#pragma unroll
-      for (int i = 0; i < V; ++i) B = Max::join(B, fabsf(h[j * V + i] * g[j * V + i]));
-      B = lanes_join<Max>(B, a.group / V);
+      B = lanes_join<Max>(m[j], a.group / V);
       F = lanes_join<Largest>(tail_of<V>(B, h + j * V, g + j * V), a.group / V);
     }
     uint32_t w[V / 4];
@@ -328,18 +337,15 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
         for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
       });
 #pragma unroll
-    for (int i = 0; i < NV * V; ++i) {
-      ss = fmaf(h[i], h[i], ss);
-      A = Max::join(A, fabsf(h[i] * g[i]));
-    }
+    for (int i = 0; i < NV * V; ++i) ss = fmaf(h[i], h[i], ss);
+    float m[NV];
+    A = vector_max<V, NV>(h, g, m);
     row_join<Max, TPR>(ss, A, lds);
     float rho = near_rho(ss, inv_d, a.eps);
     if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
       float unit, none = 0;
       rho = far_rho<TPR>(ss, h, inv_d, a.eps, unit, lds);
-      A = 0;
-#pragma unroll
-      for (int i = 0; i < NV * V; ++i) A = Max::join(A, fabsf(h[i] * g[i]));
+      A = vector_max<V, NV>(h, g, m);
       row_join<Max, TPR>(none, A, lds);
     }
     float E = kNoTail;
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
       E = tail_of<NV * V>(A, h, g);
       row_join<Largest, TPR>(none, E, lds);
     }
-    write_norm<T, V, TPR, NV>(a, cols, 0, r, live, h, g, A, E, rho);
+    write_norm<T, V, TPR, NV>(a, cols, 0, r, live, h, g, m, A, E, rho);
   }
 }
 
@@ -428,7 +434,9 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
         });
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = h[i] * up * more;
-      write_norm<T, V, kWideThreads, NV>(a, cols, off, r, true, h, g, A, E, rho);
+      float m[NV];
+      (void)vector_max<V, NV>(h, g, m);
+      write_norm<T, V, kWideThreads, NV>(a, cols, off, r, true, h, g, m, A, E, rho);
     }
   }
 }
