@@ -159,7 +159,7 @@ def test_norm_shapes_and_broadcast_rows(P):
     assert y.shape == (0, 64) and alpha.shape == (0, 2)
 
 
-@pytest.mark.parametrize("d", [5, 32, 300, 2000, 20000])
+@pytest.mark.parametrize("d", [5, 32, 50, 100, 250, 300, 2000, 3000, 9000, 20000])
 def test_norm_of_extreme_rows(P, d):
     """Zeros, one outlier, squares past fp32's range at both ends, NaN and infinities, beside ordinary rows."""
     x = torch.randn(10, d, device="cuda")
@@ -188,6 +188,23 @@ def test_norm_of_extreme_rows(P, d):
     if group is not None:                            # only the group that holds the infinity has no scale
         k = (d // 3) // 32
         assert group[0, k].isnan() and (torch.cat([group[0, :k], group[0, k + 1:]]) == 0).all()
+
+
+@pytest.mark.parametrize("d", [20, 60, 100, 200, 250, 900, 1500, 3000, 6000, 10000])
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+def test_norm_grad_of_extreme_rows(P, d, type):
+    """Rows whose squares leave fp32's range beside ordinary ones, which keep their values bit for bit."""
+    h, dy = _rand(37, d, TYPES[type], 1), _rand(37, d, TYPES[type], 2)
+    plain, _ = P.rms_norm_grad(h, dy)
+    odd = torch.arange(0, 37, 5, device="cuda")
+    far = h.clone()
+    for i, r in enumerate(odd.tolist()):
+        far[r] *= (1e25, 1e-25, 0.0, 1e30)[i % 4]
+    dh, dgain = P.rms_norm_grad(far, dy)
+    keep = torch.ones(37, dtype=torch.bool, device="cuda")
+    keep[odd] = False
+    assert torch.equal(dh[keep], plain[keep])
+    _check_grad((dh, dgain), far, dy, None, None)
 
 
 def test_norm_codes_of_tiny_values(P):
