@@ -7,6 +7,7 @@ library and raises if it is missing; there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -277,9 +278,6 @@ def _ptr(t):
 def _stream_ptr(stream):
     import torch
     if stream is None:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the handle without a Stream object around it
-        if raw is not None:
-            return raw(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -293,10 +291,17 @@ def _on_stream(stream):
 def _on_current_gpu(index: int):
     """Refuses tensors of another GPU than the current one, where the library launches (index: get_device())."""
     import torch
-    if index < 0:
-        raise ValueError("tensors must be on the GPU")
-    if index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+    current = torch.cuda.current_device() if index >= 0 else -1
+    if index != current or index < 0:
+        raise ValueError("tensors must be on the GPU" if index < 0 else
+                         f"tensors are on cuda:{index}, the current device is cuda:{current}")
+
+
+def _current_stream(index: int) -> int:
+    """Handle of the current stream of a GPU, without a Stream object around it where torch hands it out."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 _DTYPES: dict = {}
@@ -312,29 +317,28 @@ def _dtype_code(t):
     return code
 
 
-def _rows_of(t, like, dtype, what):
-    """(address, row stride) of a tensor of rows [..., d] shaped like `like`, on its device."""
+def _rows_of(t, shape, dtype, index: int, what):
+    """(address, row stride) of a tensor of rows [..., d] of that shape, type and GPU."""
     if t is None:
         return None, 0
-    shape = t.shape
-    if shape != like.shape or t.get_device() != like.get_device() or t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype} of shape {tuple(like.shape)} on {like.device}")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)} on cuda:{index}")
     d = shape[-1]
-    if len(shape) == 2:
-        ld, one = t.stride()
-        if one != 1 and d > 1:
-            raise ValueError(f"{what}: a row's values must be contiguous")
-        return t.data_ptr(), ld if shape[0] > 1 else d
-    if not t.is_contiguous():
+    if t.is_contiguous():
+        return t.data_ptr(), d
+    if len(shape) != 2:
         raise ValueError(f"{what}: rows of other than two dimensions must be contiguous")
-    return t.data_ptr(), d
+    ld, one = t.stride()
+    if one != 1 and d > 1:
+        raise ValueError(f"{what}: a row's values must be contiguous")
+    return t.data_ptr(), ld if shape[0] > 1 else d
 
 
-def _gain_of(gain, like):
+def _gain_of(gain, d: int, index: int):
     if gain is None:
         return None, F32
-    if gain.shape != like.shape[-1:] or not gain.is_contiguous() or gain.get_device() != like.get_device():
-        raise ValueError(f"gain must be {like.shape[-1]} contiguous values on {like.device}")
+    if gain.dim() != 1 or gain.numel() != d or not gain.is_contiguous() or gain.get_device() != index:
+        raise ValueError(f"gain must be {d} contiguous values on cuda:{index}")
     return gain.data_ptr(), _dtype_code(gain)
 
 
@@ -364,39 +368,42 @@ def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes
         raise ValueError("codes, alpha and group need a code_type")
     if group not in (0, 32, 64, 128):
         raise ValueError("group must be 0, 32, 64 or 128")
-    _on_current_gpu(x.get_device())
-    px, ldx = _rows_of(x, x, dtype, "x")
-    dense = x.is_contiguous()
-    pres, ldres = _rows_of(res, x, dtype, "res")
-    pgain, gain_type = _gain_of(gain, x)
-    if y is None and with_y:
-        y = torch.empty_like(x) if dense else x.new_empty(shape)
-        py, ldy = y.data_ptr(), d
-    else:
-        py, ldy = _rows_of(y, x, dtype, "y")
-    if h is None and res is not None:
-        h = torch.empty_like(x) if dense else x.new_empty(shape)
-        ph, ldh = h.data_ptr(), d
-    else:
-        ph, ldh = _rows_of(h, x, dtype, "h")
+    index = x.get_device()
+    _on_current_gpu(index)
+    px, ldx = _rows_of(x, shape, dtype, index, "x")
+    pres, ldres = _rows_of(res, shape, dtype, index, "res")
+    pgain, gain_type = _gain_of(gain, d, index)
+    like = x if x.is_contiguous() else x.new_empty(shape)   # what new outputs are made like
+    fresh_y = y is None and with_y
+    if fresh_y:
+        y = torch.empty_like(like)
+    py, ldy = (y.data_ptr(), d) if fresh_y else _rows_of(y, shape, dtype, index, "y")
+    fresh_h = h is None and res is not None
+    if fresh_h:
+        h = like if like is not x else torch.empty_like(x)
+    ph, ldh = (h.data_ptr(), d) if fresh_h else _rows_of(h, shape, dtype, index, "h")
     pcodes, ldcodes, palpha = None, 0, None
     if kind != CODE_NONE:
         if codes is None:
-            codes = x.new_empty(shape, dtype=code_type)
-            pcodes, ldcodes = codes.data_ptr(), d
-        else:
-            pcodes, ldcodes = _rows_of(codes, x, code_type, "codes")
+            codes = torch.empty_like(like, dtype=code_type)
+        pcodes, ldcodes = _rows_of(codes, shape, code_type, index, "codes")
         scales = shape[:-1] + ((d + group - 1) // group,) if group else shape[:-1]
         if alpha is None:
-            alpha = x.new_empty(scales, dtype=torch.float32)
-        elif alpha.shape != scales or alpha.dtype != torch.float32 or not alpha.is_contiguous() \
-                or alpha.get_device() != x.get_device():
-            raise ValueError(f"alpha must be contiguous float32 {tuple(scales)} on {x.device}")
+            alpha = torch.empty(scales, dtype=torch.float32, device=x.device)
+        elif alpha.shape != scales or alpha.dtype != torch.float32 or not alpha.is_contiguous() or alpha.get_device() != index:
+            raise ValueError(f"alpha must be contiguous float32 {tuple(scales)} on cuda:{index}")
         palpha = alpha.data_ptr()
     a = RmsNormArgs(x.numel() // d, d, _dtype_code(x), gain_type, eps, kind, group, px, ldx, pres, ldres, pgain, ph, ldh, py,
                     ldy, pcodes, ldcodes, palpha)
-    _check(lib().aecct_rms_norm(C.byref(a), _stream_ptr(None)), "aecct_rms_norm")
+    _check(lib().aecct_rms_norm(C.byref(a), _current_stream(index)), "aecct_rms_norm")
     return y, h, codes, alpha
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_grad_workspace(rows: int, d: int) -> int:
+    size = C.c_size_t()
+    _check(lib().aecct_rms_norm_grad_workspace_size(rows, d, C.byref(size)), "aecct_rms_norm_grad_workspace_size")
+    return size.value
 
 
 def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dgain=None, with_dgain: bool = True, stream=None):
@@ -412,32 +419,28 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
         raise ValueError("h must be [..., d] with d >= 1")
     d, dtype = shape[-1], h.dtype
     rows = h.numel() // d
-    _on_current_gpu(h.get_device())
-    ph, ldh = _rows_of(h, h, dtype, "h")
-    pdy, lddy = _rows_of(dy, h, dtype, "dy")
-    pres, lddres = _rows_of(dres, h, dtype, "dres")
-    pgain, gain_type = _gain_of(gain, h)
+    index = h.get_device()
+    _on_current_gpu(index)
+    ph, ldh = _rows_of(h, shape, dtype, index, "h")
+    pdy, lddy = _rows_of(dy, shape, dtype, index, "dy")
+    pres, lddres = _rows_of(dres, shape, dtype, index, "dres")
+    pgain, gain_type = _gain_of(gain, d, index)
     if dh is None:
         dh = torch.empty_like(h) if h.is_contiguous() else h.new_empty(shape)
-        pdh, lddh = dh.data_ptr(), d
-    else:
-        pdh, lddh = _rows_of(dh, h, dtype, "dh")
+    pdh, lddh = _rows_of(dh, shape, dtype, index, "dh")
     pdgain = pws = None
     need = 0
     if dgain is not None or with_dgain:
         if dgain is None:
-            dgain = h.new_empty((d,), dtype=torch.float32)
-        elif dgain.shape != (d,) or dgain.dtype != torch.float32 or not dgain.is_contiguous() \
-                or dgain.get_device() != h.get_device():
-            raise ValueError(f"dgain must be {d} contiguous float32 values on {h.device}")
+            dgain = torch.empty(d, dtype=torch.float32, device=h.device)
+        elif dgain.shape != (d,) or dgain.dtype != torch.float32 or not dgain.is_contiguous() or dgain.get_device() != index:
+            raise ValueError(f"dgain must be {d} contiguous float32 values on cuda:{index}")
         pdgain = dgain.data_ptr()
-        size = C.c_size_t()
-        _check(lib().aecct_rms_norm_grad_workspace_size(rows, d, C.byref(size)), "aecct_rms_norm_grad_workspace_size")
-        need = size.value
-        ws = h.new_empty((need,), dtype=torch.uint8)
+        need = _norm_grad_workspace(rows, d)
+        ws = torch.empty(need, dtype=torch.uint8, device=h.device)
         pws = ws.data_ptr()
     a = RmsNormGradArgs(rows, d, _dtype_code(h), gain_type, eps, ph, ldh, pdy, lddy, pres, lddres, pgain, pdh, lddh, pdgain)
-    _check(lib().aecct_rms_norm_grad(C.byref(a), pws, need, _stream_ptr(None)), "aecct_rms_norm_grad")
+    _check(lib().aecct_rms_norm_grad(C.byref(a), pws, need, _current_stream(index)), "aecct_rms_norm_grad")
     return dh, dgain
 
 
@@ -494,7 +497,7 @@ def grad_norm(grads, stream=None):
     device = _one_gpu(g)
     norm = torch.empty(1, dtype=torch.float32, device=device)
     ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
-    _check(lib().aecct_grad_norm(g.array, len(g), norm.data_ptr(), ws.data_ptr(), g.workspace_bytes, _stream_ptr(None)),
+    _check(lib().aecct_grad_norm(g.array, len(g), norm.data_ptr(), ws.data_ptr(), g.workspace_bytes, _current_stream(device)),
            "aecct_grad_norm")
     return norm
 
@@ -514,7 +517,7 @@ def grad_clip(grads, max_norm: float, out=None, stream=None):
     norm = torch.empty(1, dtype=torch.float32, device=device)
     ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
     _check(lib().aecct_grad_clip(g.array, None if o is None else o.array, len(g), max_norm, norm.data_ptr(), ws.data_ptr(),
-                                 g.workspace_bytes, _stream_ptr(None)), "aecct_grad_clip")
+                                 g.workspace_bytes, _current_stream(device)), "aecct_grad_clip")
     return norm
 
 
@@ -574,7 +577,7 @@ class Adam:
         _check(lib().aecct_adam_step(self.params.array, self.m.array, self.v.array, g.array,
                                      None if self.copies is None else self.copies.array, len(g), C.byref(opt),
                                      self.step_count.data_ptr(), None if norm is None else norm.data_ptr(), ws.data_ptr(),
-                                     g.workspace_bytes, _stream_ptr(None)), "aecct_adam_step")
+                                     g.workspace_bytes, _current_stream(device)), "aecct_adam_step")
         return norm
 
 
@@ -866,5 +869,5 @@ class Trainer:
         ws = torch.empty(size.value, dtype=torch.uint8, device=device)
         _check(lib().aecct_train_update(self._h, *[C.byref(t) for t in lists], C.byref(opt), step.data_ptr(),
                                         None if norm is None else norm.data_ptr(), ws.data_ptr(), size.value,
-                                        _stream_ptr(None)), "aecct_train_update")
+                                        _current_stream(device)), "aecct_train_update")
         return norm
