@@ -1,4 +1,12 @@
 // Norm of many tensors, clipping by it, and the Adam update.
+//
+// All are bound by device memory; a list is worked on as one range of units, whatever its tensors' sizes.  The norm
+// needs every value before any is scaled, so clipping and the update are two launches: sums of squares, one double a
+// block, then a pass in which every block adds those sums up in the same order (2048 doubles, eight loads in flight)
+// while its first unit's values are on their way.  Squares and sums are fp64, so that no finite gradient is out of
+// range.  Measured on an MI355X (a copy of 1 GB 5.1 TB/s, reads alone 6.4): the norm of 250e6 fp32 values 155 us
+// (6.4 TB/s), the update of 120e6 parameters from bf16 gradients with clipping and bf16 copies 45 + 605 us (5.5 TB/s in
+// the second), of the 2.1e6 parameters of LDPC(256,128) 5 + 12 us.
 #include "row_io.h"
 #include "update.h"
 
@@ -62,7 +70,8 @@ __device__ __forceinline__ void store4(void *p, int type, int64_t i, int64_t n, 
   else store_part<f16_t, 4, kLast>((f16_t *)p + i, k, f);
 }
 
-// The unit of a thread of the sums: four vectors of 16 bytes, read a unit ahead of their use.
+// The unit of a thread of the sums: four vectors of 16 bytes, read a unit ahead of their use (eight, not read ahead: 191 us
+// for 250e6 fp32 values where these take 155 to 167).
 struct SumUnit {
   Raw<float, 4> w[4];
   template <class T, bool NT>
@@ -194,7 +203,8 @@ __global__ __launch_bounds__(kThreads) void k_clip(ClipTable<N> t, const double 
 }
 
 // Four values of each tensor a thread in a unit; the next unit's are read before the present ones are worked on, the
-// first unit's before the norm is known.
+// first unit's before the norm is known.  Units of 1024 values, so that 2.1e6 parameters fill the card (of 4096: 15.1 us, of
+// 1024 13.7); the powers of beta are taken once, by the sums' last block (by every block here: 19.9 us).
 template <int N>
 __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double *part, int parts, AdamScalars o,
                                                    const AdamNow *now, int64_t *step, float *norm) {
