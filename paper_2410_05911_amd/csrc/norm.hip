@@ -130,13 +130,6 @@ struct Columns {
       else v[j] = Raw<T, V>{};
     }
   }
-  // past: read past the caches
-  template <class T>
-  __device__ __forceinline__ void load(const T *p, bool live, bool past, Raw<T, V> (&v)[NV]) const {
-    if (past) load_full<true>(p, live, v);
-    else load_full<false>(p, live, v);
-    load_last(p, live, v);
-  }
   template <bool PAST, class T>
   __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
     load_full<PAST>(p, live, v);
@@ -172,12 +165,12 @@ struct Columns {
       for (int i = 0; i < NV * V; ++i) g[i] = 1.0f;
     } else if (f32) {
       Raw<float, V> v[NV];
-      load<float>((const float *)p, true, false, v);
+      load<false>((const float *)p, true, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<float, V>(v[j], (float (&)[V])g[j * V]);
     } else {
       Raw<T, V> v[NV];
-      load<T>((const T *)p, true, false, v);
+      load<false>((const T *)p, true, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<T, V>(v[j], (float (&)[V])g[j * V]);
     }
@@ -307,7 +300,7 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
 // and written (loads issued ahead of the stores, so that waiting for them does not wait for the stores): 16384 x 8192
 // bf16 182 -> 175 us, its gradient 125 -> 108 at 4096 columns.  What waits stays as it was stored, 16-bit values two to a
 // register.
-template <class T, int TPR, int NV, int BLOCK, int WAVES>
+template <class T, int TPR, int NV, int BLOCK, int WAVES, bool PAST>
 __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR;
   __shared__ float2 lds[BLOCK / 64];
@@ -317,8 +310,11 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> nx[NV], nres[NV];
   const auto fetch = [&](int64_t r) {
-    cols.load((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, a.past_in, nx);
-    if (a.res) cols.load((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, a.past_in, nres);
+    cols.template load<PAST>((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, nx);
+    if (a.res) {
+      if (PAST) wait_loads();   // one stream of reads from the memory at a time: 20000 x 5000 bf16 157 -> 150 us
+      cols.template load<PAST>((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, nres);
+    }
   };
   fetch((int64_t)blockIdx.x * RPB + sub);
   float g[NV * V];
@@ -385,8 +381,8 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&g)[N]) {
       Raw<T, V> x[NV], res[NV];
-      cols.load((const T *)a.x + r * a.ldx + off, true, false, x);
-      if (a.res) cols.load((const T *)a.res + r * a.ldres + off, true, false, res);
+      cols.template load<false>((const T *)a.x + r * a.ldx + off, true, x);
+      if (a.res) cols.template load<false>((const T *)a.res + r * a.ldres + off, true, res);
       cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -577,8 +573,8 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&dy)[N], float (&g)[N]) {
       Raw<T, V> x[NV], y[NV];
-      cols.load((const T *)a.h + r * a.ldh + off, true, false, x);
-      cols.load((const T *)a.dy + r * a.lddy + off, true, false, y);
+      cols.template load<false>((const T *)a.h + r * a.ldh + off, true, x);
+      cols.template load<false>((const T *)a.dy + r * a.lddy + off, true, y);
       cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -614,7 +610,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
       const Cols cols(a.d - off, threadIdx.x);
       float h[N], dy[N], g[N];
       Raw<T, V> res[NV];
-      if (a.dres) cols.load((const T *)a.dres + r * a.lddres + off, true, false, res);
+      if (a.dres) cols.template load<false>((const T *)a.dres + r * a.lddres + off, true, res);
       read(cols, off, h, dy, g);
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = h[i] * up * more * rho;
@@ -631,7 +627,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
       if (a.part) {
         Raw<float, V> sum[NV];
         if (r != blockIdx.x) {
-          cols.template load<float>(part + off, true, false, sum);
+          cols.template load<false>(part + off, true, sum);
         } else {
 #pragma unroll
           for (int j = 0; j < NV; ++j) sum[j] = Raw<float, V>{};
@@ -710,7 +706,8 @@ struct NormLaunch {
   hipError_t run() const {
     constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 ? 6 : 4;   // wavefronts a SIMD
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR), most = (int64_t)cu_count * (W * 256 / BLOCK);
-    k_rms_norm<T, TPR, NV, BLOCK, W><<<even_grid(blocks, most), BLOCK, 0, s>>>(a);
+    if (a.past_in) k_rms_norm<T, TPR, NV, BLOCK, W, true><<<even_grid(blocks, most), BLOCK, 0, s>>>(a);
+    else k_rms_norm<T, TPR, NV, BLOCK, W, false><<<even_grid(blocks, most), BLOCK, 0, s>>>(a);
     return hipGetLastError();
   }
   hipError_t wide() const {
