@@ -113,7 +113,7 @@ __device__ __forceinline__ float far_rho(float ss, float (&h)[N], float inv_d, f
 }
 
 // Where a thread's columns lie: vector j starts at column col(j).  A row of d = V k + tail values ends in a vector of
-// `tail` values, the jt-th of one lane; only that lane runs the code for single values, once for all j.
+// `tail` values, the jt-th of one lane; only that lane runs the code for it, once for all j.
 template <int V, int TPR, int NV>
 struct Columns {
   int d, lane, tail, jt;
@@ -122,27 +122,33 @@ struct Columns {
       : d(d), lane(lane), tail(d % V), jt(d / V / TPR), last(tail && jt < NV && d / V % TPR == lane) {}
   __device__ __forceinline__ int col(int j) const { return (j * TPR + lane) * V; }
   __device__ __forceinline__ bool full(int j) const { return col(j) + V <= d; }
-  template <bool NT, class T>
-  __device__ __forceinline__ void load_full(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
+  // PAST: past the caches.  ENDS, for rows of d >= V values that no thread writes before all have settled theirs: the
+  // short vector is read as the V values that end the row, by one load as the others', and nothing waits until settle()
+  // moves them to their place (20000 rows of 5007 bf16 values 102 -> 80 us, their gradient 146 -> 119).
+  template <bool PAST, bool ENDS, class T>
+  __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      if (live && full(j)) load_raw<T, V, NT>(p + col(j), v[j]);
+      const int c = col(j);
+      if (live && (ENDS ? c < d : full(j))) load_raw<T, V, PAST>(p + (ENDS && c > d - V ? d - V : c), v[j]);
       else v[j] = Raw<T, V>{};
     }
-  }
-  template <bool PAST, class T>
-  __device__ __forceinline__ void load(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
-    load_full<PAST>(p, live, v);
-    load_last(p, live, v);
+    if constexpr (!ENDS) {
+      if (live && last) {
+        Raw<T, V> t;
+        load_raw_part<T, V>(p + col(jt), tail, t);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (j == jt) v[j] = t;
+      }
+    }
   }
   template <class T>
-  __device__ __forceinline__ void load_last(const T *p, bool live, Raw<T, V> (&v)[NV]) const {
-    if (live && last) {
-      Raw<T, V> t;
-      load_raw_part<T, V>(p + col(jt), tail, t);
+  __device__ __forceinline__ void settle(Raw<T, V> (&v)[NV]) const {
+    if (last) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (j == jt) v[j] = t;
+        if (j == jt) move_down(v[j], V - tail);
     }
   }
   template <class T, class F>   // f(j, v): the V values of vector j
@@ -165,12 +171,12 @@ struct Columns {
       for (int i = 0; i < NV * V; ++i) g[i] = 1.0f;
     } else if (f32) {
       Raw<float, V> v[NV];
-      load<false>((const float *)p, true, v);
+      load<false, false>((const float *)p, true, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<float, V>(v[j], (float (&)[V])g[j * V]);
     } else {
       Raw<T, V> v[NV];
-      load<false>((const T *)p, true, v);
+      load<false, false>((const T *)p, true, v);
 #pragma unroll
       for (int j = 0; j < NV; ++j) unpack<T, V>(v[j], (float (&)[V])g[j * V]);
     }
@@ -300,7 +306,7 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
 // and written (loads issued ahead of the stores, so that waiting for them does not wait for the stores): 16384 x 8192
 // bf16 182 -> 175 us, its gradient 125 -> 108 at 4096 columns.  What waits stays as it was stored, 16-bit values two to a
 // register.
-template <class T, int TPR, int NV, int BLOCK, int WAVES, bool PAST>
+template <class T, int TPR, int NV, int BLOCK, int WAVES, bool PAST, bool ENDS>
 __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR;
   __shared__ float2 lds[BLOCK / 64];
@@ -310,10 +316,10 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> nx[NV], nres[NV];
   const auto fetch = [&](int64_t r) {
-    cols.template load<PAST>((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, nx);
+    cols.template load<PAST, ENDS>((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, nx);
     if (a.res) {
       if (PAST) wait_loads();   // one stream of reads from the memory at a time: 20000 x 5000 bf16 157 -> 150 us
-      cols.template load<PAST>((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, nres);
+      cols.template load<PAST, ENDS>((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, nres);
     }
   };
   fetch((int64_t)blockIdx.x * RPB + sub);
@@ -324,6 +330,8 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
     const bool live = RPB == 1 || r < a.rows;
     float h[NV * V];
     float ss = 0, A = 0;
+    if (ENDS) cols.settle(nx);
+    if (ENDS && a.res) cols.settle(nres);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float (&v)[V] = (float (&)[V])h[j * V];
@@ -336,16 +344,20 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
       }
     }
     if (r0 + step < a.rows) fetch(r + step);
-    if (a.h)
-      cols.store((T *)a.h + r * a.ldh, live, a.past_out, [&](int j, float (&v)[V]) {
+    const auto store_h = [&] {
+      if (a.h)
+        cols.store((T *)a.h + r * a.ldh, live, a.past_out, [&](int j, float (&v)[V]) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
-      });
+          for (int i = 0; i < V; ++i) v[i] = h[j * V + i];
+        });
+    };
+    if (!ENDS) store_h();
 #pragma unroll
     for (int i = 0; i < NV * V; ++i) ss = fmaf(h[i], h[i], ss);
     float m[NV];
     A = vector_max<V, NV>(h, g, m);
     row_join<Max, TPR>(ss, A, lds);
+    if (ENDS) store_h();   // behind the join: h may lie on an input, whose row's last lane reads columns of its neighbour's
     float rho = near_rho(ss, inv_d, a.eps);
     if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
       float unit, none = 0;
@@ -381,8 +393,8 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&g)[N]) {
       Raw<T, V> x[NV], res[NV];
-      cols.template load<false>((const T *)a.x + r * a.ldx + off, true, x);
-      if (a.res) cols.template load<false>((const T *)a.res + r * a.ldres + off, true, res);
+      cols.template load<false, false>((const T *)a.x + r * a.ldx + off, true, x);
+      if (a.res) cols.template load<false, false>((const T *)a.res + r * a.ldres + off, true, res);
       cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -451,7 +463,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
 // AHEAD: the next rows are read ahead, as above.  Where 128 registers do not hold everything (16 values a thread, two to a
 // register while they wait), each thread keeps its gains in LDS: a few registers spilled to memory instead cost 20 to 30 %
 // (20000 x 5000 fp16 157 us, bf16 with fewer of them 119).
-template <class T, int TPR, int NV, int BLOCK, int WAVES, bool AHEAD, bool PAST>
+template <class T, int TPR, int NV, int BLOCK, int WAVES, bool AHEAD, bool PAST, bool ENDS>
 __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR, N = NV * V;
   __shared__ float2 lds[BLOCK / 64];
@@ -461,8 +473,8 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
   const int64_t step = (int64_t)gridDim.x * RPB;
   Raw<T, V> nh[NV], ndy[NV];
   const auto fetch = [&](int64_t r) {
-    cols.template load<PAST>((const T *)a.h + r * a.ldh, RPB == 1 || r < a.rows, nh);
-    cols.template load<PAST>((const T *)a.dy + r * a.lddy, RPB == 1 || r < a.rows, ndy);
+    cols.template load<PAST, ENDS>((const T *)a.h + r * a.ldh, RPB == 1 || r < a.rows, nh);
+    cols.template load<PAST, ENDS>((const T *)a.dy + r * a.lddy, RPB == 1 || r < a.rows, ndy);
   };
   if constexpr (AHEAD) fetch((int64_t)blockIdx.x * RPB + sub);
   constexpr bool GAIN_LDS = sizeof(T) == 2 && NV == 2;
@@ -494,7 +506,9 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
     Raw<T, V> res[NV];
     float ss = 0, dot = 0;
     if constexpr (!AHEAD) fetch(r);
-    if (a.dres) cols.template load<PAST>((const T *)a.dres + r * a.lddres, live, res);
+    if (a.dres) cols.template load<PAST, ENDS>((const T *)a.dres + r * a.lddres, live, res);
+    if (ENDS) cols.settle(nh);
+    if (ENDS) cols.settle(ndy);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       unpack<T, V>(nh[j], (float (&)[V])h[j * V]);
@@ -514,6 +528,7 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
 #pragma unroll
     for (int i = 0; i < N; ++i) ss = fmaf(h[i], h[i], ss);
     add_dot();
+    if (ENDS && a.dres) cols.settle(res);   // before the join: behind it the others write dh, perhaps where dres lies
     row_join<Sum, TPR>(ss, dot, lds);
     float rho = near_rho(ss, inv_d, a.eps), unit = 1.0f;
     if (!in_range(ss) || !(fabsf(dot) <= 1e37f)) {
@@ -573,8 +588,8 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const auto read = [&](const Cols &cols, int off, float (&h)[N], float (&dy)[N], float (&g)[N]) {
       Raw<T, V> x[NV], y[NV];
-      cols.template load<false>((const T *)a.h + r * a.ldh + off, true, x);
-      cols.template load<false>((const T *)a.dy + r * a.lddy + off, true, y);
+      cols.template load<false, false>((const T *)a.h + r * a.ldh + off, true, x);
+      cols.template load<false, false>((const T *)a.dy + r * a.lddy + off, true, y);
       cols.template gain<T>(gain_at<T>(a.gain, a.gain_f32, off), a.gain_f32, g);
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -610,7 +625,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
       const Cols cols(a.d - off, threadIdx.x);
       float h[N], dy[N], g[N];
       Raw<T, V> res[NV];
-      if (a.dres) cols.template load<false>((const T *)a.dres + r * a.lddres + off, true, res);
+      if (a.dres) cols.template load<false, false>((const T *)a.dres + r * a.lddres + off, true, res);
       read(cols, off, h, dy, g);
 #pragma unroll
       for (int i = 0; i < N; ++i) h[i] = h[i] * up * more * rho;
@@ -627,7 +642,7 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_grad_wide(NormGradRow
       if (a.part) {
         Raw<float, V> sum[NV];
         if (r != blockIdx.x) {
-          cols.template load<false>(part + off, true, sum);
+          cols.template load<false, false>(part + off, true, sum);
         } else {
 #pragma unroll
           for (int j = 0; j < NV; ++j) sum[j] = Raw<float, V>{};
@@ -704,10 +719,18 @@ struct NormLaunch {
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 ? 6 : 4;   // wavefronts a SIMD
+    constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 && BLOCK < 1024 ? 6 : 4;   // wavefronts a SIMD
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR), most = (int64_t)cu_count * (W * 256 / BLOCK);
-    if (a.past_in) k_rms_norm<T, TPR, NV, BLOCK, W, true><<<even_grid(blocks, most), BLOCK, 0, s>>>(a);
-    else k_rms_norm<T, TPR, NV, BLOCK, W, false><<<even_grid(blocks, most), BLOCK, 0, s>>>(a);
+    constexpr bool ENDS = !(V == 4 && NV == 4);   // no registers left for it there
+    const unsigned grid = even_grid(blocks, most);
+    if constexpr (TPR == 8 && NV == 1) {
+      if (a.d < V) {
+        k_rms_norm<T, TPR, NV, BLOCK, W, false, false><<<grid, BLOCK, 0, s>>>(a);
+        return hipGetLastError();
+      }
+    }
+    if (a.past_in) k_rms_norm<T, TPR, NV, BLOCK, W, true, ENDS><<<grid, BLOCK, 0, s>>>(a);
+    else k_rms_norm<T, TPR, NV, BLOCK, W, false, ENDS><<<grid, BLOCK, 0, s>>>(a);
     return hipGetLastError();
   }
   hipError_t wide() const {
@@ -724,7 +747,7 @@ struct NormGradLaunch {
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    constexpr int V = 16 / sizeof(T), W = NV * V <= 8 ? 5 : 4;
+    constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;
     constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
     // A long row leaves a long partial sum, so half the blocks (4096 x 4096 bf16 26.7 -> 24.0 us); for shorter rows they
@@ -732,8 +755,14 @@ struct NormGradLaunch {
     int64_t most = (int64_t)cu_count * (W * 256 / BLOCK) / (TPR == 256 && NV * V == 16 ? 2 : 1);
     if (most > kPartRows) most = kPartRows;
     const unsigned grid = even_grid(blocks, most);
-    if (grid && a.past_in) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, true><<<grid, BLOCK, 0, s>>>(a);
-    else if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, false><<<grid, BLOCK, 0, s>>>(a);
+    if constexpr (TPR == 8 && NV == 1) {
+      if (grid && a.d < V) {
+        k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, false, false><<<grid, BLOCK, 0, s>>>(a);
+        return dgain(grid);
+      }
+    }
+    if (grid && a.past_in) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, true, AHEAD><<<grid, BLOCK, 0, s>>>(a);
+    else if (grid) k_rms_norm_grad<T, TPR, NV, BLOCK, W, AHEAD, false, AHEAD><<<grid, BLOCK, 0, s>>>(a);
     return dgain(grid);
   }
   hipError_t wide() const {

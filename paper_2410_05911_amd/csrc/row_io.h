@@ -102,6 +102,23 @@ __device__ __forceinline__ void load_raw_part(const T *p, int n, Raw<T, V> &r) {
   bytes_in(p, n > 0 ? n * (int)sizeof(T) : 0, r.w);
   wait_loads();
 }
+// Value i + n of r to value i, 0 where there is none; 0 < n < V.
+template <class T, int V>
+__device__ __forceinline__ void move_down(Raw<T, V> &r, int n) {
+  constexpr int W = V * (int)sizeof(T) / 4;
+  const int words = sizeof(T) == 4 ? n : n / 2;
+  if (sizeof(T) == 2 && n % 2) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) r.w[i] = (r.w[i] >> 16) | (i + 1 < W ? r.w[i + 1] << 16 : 0u);
+  }
+#pragma unroll
+  for (int k = 1; k < W; k *= 2) {
+    if (words & k) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) r.w[i] = i + k < W ? r.w[i + k] : 0u;
+    }
+  }
+}
 template <class T, int V>
 __device__ __forceinline__ void unpack(const Raw<T, V> &r, float (&f)[V]) {
 #pragma unroll

@@ -141,6 +141,28 @@ def test_norm_in_place_and_beside(P, type):
         assert (guard == 9).all()
 
 
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("d", [1, 3, 5, 7, 259, 770, 1541, 2051, 2561, 4097, 5635, 8197, 12289, 16385])
+def test_in_place_with_short_ends(P, type, d):
+    """Rows whose last few values are another lane's or wavefront's neighbours, written over every input in turn."""
+    t, rows = TYPES[type], 700
+    x, res, dy = (_rand(rows, d, t, k) for k in (5, 6, 7))
+    gain = torch.randn(d, device="cuda")
+    want = P.rms_norm(x, gain, res, code_type=torch.int8)
+    for k in range(2):
+        a = [x.clone(), res.clone()]
+        got = P.rms_norm(a[0], gain, a[1], h=a[k], y=a[1 - k], code_type=torch.int8)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    alone = P.rms_norm(x, gain)[0]
+    a = x.clone()
+    assert torch.equal(P.rms_norm(a, gain, y=a)[0], alone)
+    dh, dg = P.rms_norm_grad(x, dy, gain, res)
+    for k in range(3):
+        a = [x.clone(), dy.clone(), res.clone()]
+        got, g2 = P.rms_norm_grad(a[0], a[1], gain, a[2], dh=a[k])
+        assert torch.equal(got, dh) and torch.equal(g2, dg)
+
+
 def test_norm_shapes_and_broadcast_rows(P):
     x = _rand(24, 40, torch.bfloat16, 1).view(2, 3, 4, 40)
     y, h, codes, alpha = P.rms_norm(x, code_type=torch.int8, group=32)
