@@ -432,7 +432,8 @@ typedef enum aecct_code {
  *   h = x + res,   rho = 1 / sqrt(mean(h^2) + eps),   y = h rho gain,   codes and alpha of y.
  * x, res, h and y are of one type; y and the codes are taken of the unrounded h, the codes of the unrounded y.
  * A row with a NaN or an infinity gives what the formulas give (rho = NaN, or 0): its alphas are NaN where
- * a value they span is NaN, and int8 codes of NaN are 0.  Squares that leave fp32's range are summed again in fp64.
+ * a value they span is NaN, and int8 codes of NaN are 0.  Where squares leave fp32's range the row is
+ * summed again, scaled by a power of two.
  */
 typedef struct aecct_rms_norm_args {
   int64_t rows, d;             /* rows >= 0 (0: nothing is written), 1 <= d <= 65536 */
@@ -482,7 +483,8 @@ aecct_status aecct_rms_norm_grad_workspace_size(int64_t rows, int64_t d, size_t 
 aecct_status aecct_rms_norm_grad(const aecct_rms_norm_grad_args *a, void *workspace, size_t workspace_bytes,
                                  void *stream);
 
-/* A tensor of a list: `count` >= 0 contiguous values.  Lists are host arrays, read before the call returns. */
+/* A tensor of a list: `count` >= 0 contiguous values, at most 2^40 in a list.  Lists are host arrays, read before the
+ * call returns. */
 typedef struct aecct_tensor {
   void *data;      /* device; may be NULL where count is 0 */
   int64_t count;
@@ -524,7 +526,8 @@ typedef struct aecct_adam_options {
  *   norm   device fp32 [1], the norm of the gradients before clipping, or NULL.
  * The norm is taken where max_norm > 0 or norm is given; where any gradient then is not finite, nothing but norm is
  * written.
- * No written tensor overlaps another tensor of the call.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, DEVICE.
+ * No written tensor overlaps another tensor of the call, nor lr_device.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL,
+ * DEVICE.
  */
 aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, const aecct_tensor *v,
                              const aecct_tensor *grads, const aecct_tensor *copies, int32_t n,

@@ -543,7 +543,7 @@ def _step_tensor(step, device: int):
 class Adam:
     """Adam over a list of float32 tensors (Section 6), updated in place: moments m and v (zeros, or the given float32
     tensors), the number of updates made in `step` (one int64 value on the GPU), decoupled weight decay, gradients
-    clipped to max_norm over the whole list (None: not), and optional 16-bit `copies` of the parameters.
+    clipped to max_norm over the whole list (None: not; 0: not, but measured), and optional 16-bit `copies` of the parameters.
     lr: a number, or one float32 value on the GPU that captured graphs read at each replay."""
 
     def __init__(self, params, lr=1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, max_norm=None,

@@ -18,7 +18,7 @@ using namespace aecct;
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
-constexpr int64_t kMaxCount = (int64_t)1 << 40;   // values of a tensor
+constexpr int64_t kMaxCount = (int64_t)1 << 40;   // values of a list: its sums then need no more launches than its ranges ask for
 constexpr int64_t kMaxUnits = (int64_t)1 << 30;   // of a launch: a tensor of 2^40 values is as many units of 1024
 
 int64_t type_size(int32_t t) { return t == AECCT_F32 ? 4 : 2; }
@@ -28,8 +28,9 @@ bool tensor_ok(const aecct_tensor &t) {
 }
 bool list_ok(const aecct_tensor *t, int32_t n) {
   if (n < 0 || (n > 0 && !t)) return false;
+  int64_t count = 0;
   for (int i = 0; i < n; ++i)
-    if (!tensor_ok(t[i])) return false;
+    if (!tensor_ok(t[i]) || (count += t[i].count) > kMaxCount) return false;
   return true;
 }
 bool same_counts(const aecct_tensor *a, const aecct_tensor *b, int32_t n) {
@@ -60,8 +61,8 @@ struct Spans {
       if (!(but && t[i].data == but[i].data && t[i].type == but[i].type) && span_of(t[i], written, x)) v.push_back(x);
     join(old);
   }
-  void add(const void *p, size_t bytes) {
-    v.push_back(Span{(uintptr_t)p, (uintptr_t)p + bytes, true});
+  void add(const void *p, size_t bytes, bool written = true) {
+    v.push_back(Span{(uintptr_t)p, (uintptr_t)p + bytes, written});
     join(v.size() - 1);
   }
   void join(size_t old) {
@@ -96,7 +97,7 @@ hipError_t for_tables(const aecct_tensor *list, int32_t n, Extends extends, Put 
     if (list[i].count == 0) continue;
     if (t.n && extends(t, i)) {
       const int64_t count = t.count[t.n - 1] + list[i].count, units = t.unit0[t.n - 1] + units_of(count, t.type[t.n - 1]);
-      if (count <= kMaxCount && units <= kMaxUnits) {
+      if (units <= kMaxUnits) {
         t.count[t.n - 1] = count;
         t.unit0[t.n] = (int)units;
         continue;
@@ -239,7 +240,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    Spans spans(5 * (size_t)n + 2);
+    Spans spans(5 * (size_t)n + 3);
     spans.add(params, n, true);
     spans.add(m, n, true);
     spans.add(v, n, true);
@@ -247,6 +248,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
     spans.add(grads, n, false);
     spans.add(step, sizeof(int64_t));
     if (norm) spans.add(norm, sizeof(float));
+    if (opt->lr_device) spans.add(opt->lr_device, sizeof(float), false);
     if (spans.conflict()) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;

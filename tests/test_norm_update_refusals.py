@@ -105,6 +105,15 @@ def test_lists_with_bad_tensors_are_refused(P, item):
     assert P.lib().aecct_grad_clip(t, None, 2, 1.0, NORM, WS, big, None) == P.ERR_INVALID_ARG
 
 
+def test_lists_hold_at_most_two_to_the_forty_values(P):
+    """Tensors that are in range one by one, and lie apart, but together need more launches than the workspace holds."""
+    half = 1 << 39
+    lists = _list(P, *[(BASE, half, 1)] * 3), _list(P, *[(BASE + i * (1 << 41), half, 1) for i in range(3)])
+    for three in lists:
+        assert P.lib().aecct_grad_norm(three, 3, 16, WS, 1 << 30, None) == P.ERR_INVALID_ARG
+        assert P.lib().aecct_grad_clip(three, None, 3, 1.0, 16, WS, 1 << 30, None) == P.ERR_INVALID_ARG
+
+
 def test_grad_norm_refuses(P):
     t = _list(P, (BASE, 8, 0), (BASE + 64, 8, 1))
     need = _bytes(P, 2)
@@ -178,6 +187,11 @@ def test_adam_refuses_lists(P):
     assert _adam(P, copies=_list(P, (far, 8, 5), (far + 64, 8, 1))) == P.ERR_INVALID_ARG
     assert _adam(P, copies=_list(P, (BASE + 32, 8, 1), (far + 64, 8, 1))) == P.ERR_INVALID_ARG
     assert _adam(P, step=BASE + 24) == P.ERR_INVALID_ARG and _adam(P, norm=STEP + 4) == P.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("at", [BASE, BASE + 60, BASE + (2 << 30), STEP + 4, NORM])
+def test_adam_refuses_a_rate_that_it_writes(P, at):
+    assert _adam(P, {"lr_device": at}) == P.ERR_INVALID_ARG
 
 
 def test_train_update_refuses_null(P):
