@@ -318,7 +318,8 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
   const auto fetch = [&](int64_t r) {
     cols.template load<PAST, ENDS>((const T *)a.x + r * a.ldx, RPB == 1 || r < a.rows, nx);
     if (a.res) {
-      if (PAST) wait_loads();   // one stream of reads from the memory at a time: 20000 x 5000 bf16 157 -> 150 us
+      // one stream of reads from the memory at a time: 20000 x 5000 bf16 157 -> 150 us (x + one row for all 126, waiting 188)
+      if (PAST && a.ldx && a.ldres) wait_loads();
       cols.template load<PAST, ENDS>((const T *)a.res + r * a.ldres, RPB == 1 || r < a.rows, nres);
     }
   };

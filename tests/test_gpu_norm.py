@@ -456,6 +456,21 @@ def test_norm_of_more_rows_than_32_bits_count(P):
     assert (y[:100] == -1).all() and (y[-100:] == -1).all() and y.min().item() == -1 and y.max().item() == -1
 
 
+@pytest.mark.parametrize("rows,d,type", [(60011, 1203, "bf16"), (40009, 512, "fp32")])
+def test_large_inputs_beside_one_broadcast_row(P, rows, d, type):
+    """x, res, dy and dres in turn one row for all, beside more than the caches hold: as with the row written out."""
+    x, row = _rand(rows, d, TYPES[type], 1), _rand(1, d, TYPES[type], 2).expand(rows, d)
+    full = row.contiguous()
+    for a, b in (((x, row), (x, full)), ((row, x), (full, x))):
+        got, want = P.rms_norm(a[0], None, a[1], code_type=torch.int8), P.rms_norm(b[0], None, b[1], code_type=torch.int8)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    for k in range(3):
+        a, b = [x, x, x], [x, x, x]
+        a[k], b[k] = row, full
+        got, want = (P.rms_norm_grad(s[0], s[1], None, s[2]) for s in (a, b))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("d", [7, 200, 3001, 20000])
 def test_norm_with_single_outputs(P, d):
     """h alone, codes alone, dgain alone (through the C ABI, which takes any of them)."""
