@@ -10,6 +10,8 @@
 // rows of 8192 bf16 to e4m3 codes 170 us (5.5 TB/s; about 30 vector instructions a value, 0.6 of
 // the time), of 49152 rows of 128 fp32 to int8 codes 14.5 us (5.6 TB/s), of 16384 rows of 4096 bf16 81 us (6.6 TB/s);
 // the gradient of the last 71 us (5.7 TB/s); of one row 3 to 4 us, all latency.
+#include <algorithm>
+
 #include "device_common.h"
 #include "norm.h"
 #include "row_io.h"
@@ -681,9 +683,10 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dgain(const float *part, int 
 // ---- launches ----------------------------------------------------------------------------------------------------
 // f.run<TPR, NV, BLOCK>() for the narrowest shape that holds d values of V a vector, f.wide() past the widest.  Eight
 // values a thread where a row fits a wavefront or less, so two vectors in fp32 (one: 49152 x 128 14.8 -> 14.3 us with two)
-// and one in 16 bits (with two the gradient of 100000 x 200 34 -> 47 us, of 100000 x 512 66 -> 79).  Long rows have 16 a
-// thread: 1024 threads with 8 a row of 8192 bf16 take 232 us for 16384 rows where 512 with 16 take 174 (and 18.4 where
-// these take 19.8 for the gradient of 777 x 5003).
+// and one in 16 bits (with two the gradient of 100000 x 200 26 -> 37 us, of 100000 x 512 55 -> 77).  Long rows have two
+// vectors a thread in the norm (with one 16384 x 8192 bf16 to codes 173 -> 221 us, 2000 x 8192 23 -> 25) and one in the
+// gradient (F::kThin), which holds more of each: 777 x 5003 fp16 18.5 -> 15.8 us, 2000 x 8192 bf16 25.7 -> 23.3,
+// 4096 x 2048 fp32 21.9 -> 20.5, 16384 x 4096 bf16 the same.
 template <int V, class F>
 hipError_t by_width(int d, const F &f) {
   const int n = (d + V - 1) / V;   // vectors a row
@@ -699,8 +702,13 @@ hipError_t by_width(int d, const F &f) {
   }
   if (n <= 128) return f.template run<64, 2, 256>();
   if (n <= 256) return f.template run<256, 1, 256>();
-  if (n <= 512) return f.template run<256, 2, 256>();
-  if (n <= 1024) return f.template run<512, 2, 512>();
+  if constexpr (F::kThin) {
+    if (n <= 512) return f.template run<512, 1, 512>();
+    if (n <= 1024) return f.template run<1024, 1, 1024>();
+  } else {
+    if (n <= 512) return f.template run<256, 2, 256>();
+    if (n <= 1024) return f.template run<512, 2, 512>();
+  }
   if (n <= 2048) return f.template run<1024, 2, 1024>();
   if constexpr (V == 4) {
     if (n <= 4096) return f.template run<1024, 4, 1024>();
@@ -715,6 +723,7 @@ unsigned even_grid(int64_t sets, int64_t most) {
 
 template <class T>
 struct NormLaunch {
+  static constexpr bool kThin = false;
   const NormRows &a;
   int cu_count;
   hipStream_t s;
@@ -743,6 +752,7 @@ struct NormLaunch {
 constexpr int kPartRows = 1024;   // blocks of the gradient, so rows of its partial sums, at most
 template <class T>
 struct NormGradLaunch {
+  static constexpr bool kThin = true;
   const NormGradRows &a;
   int cu_count;
   hipStream_t s;
@@ -751,10 +761,12 @@ struct NormGradLaunch {
     constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;
     constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
-    // A long row leaves a long partial sum, so half the blocks (4096 x 4096 bf16 26.7 -> 24.0 us); for shorter rows they
-    // hide more (3001 x 1111 fp16 18.0 us, with half 20.0).
-    int64_t most = (int64_t)cu_count * (W * 256 / BLOCK) / (TPR == 256 && NV * V == 16 ? 2 : 1);
+    int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);
     if (most > kPartRows) most = kPartRows;
+    // Each block leaves a row of partial sums, so long rows go to fewer blocks, of four rows if that leaves two for each
+    // CU (3001 x 2048 fp16 16.1 -> 15.1 us, 700 x 900 fp32 8.6 -> 7.5); with many rows all the blocks hide more
+    // (20000 x 2048 fp16 48 us, with half of them 53).
+    if (TPR >= 256 && most > blocks / 4) most = std::max(blocks / 4, std::min<int64_t>(most, 2 * cu_count));
     const unsigned grid = even_grid(blocks, most);
     if constexpr (TPR == 8 && NV == 1) {
       if (grid && a.d < V) {
