@@ -464,8 +464,8 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
 // ---- its gradient ------------------------------------------------------------------------------------------------
 // Block b sums dy xh over its rows per column and leaves the sums in part[b].
 // AHEAD: the next rows are read ahead, as above.  Where 128 registers do not hold everything (16 values a thread, two to a
-// register while they wait), each thread keeps its gains in LDS: a few registers spilled to memory instead cost 20 to 30 %
-// (20000 x 5000 fp16 157 us, bf16 with fewer of them 119).
+// register while they wait, and a join over a whole block), each thread keeps its gains in LDS: 9000 x 16384 fp16 167 us,
+// with some registers spilled to memory instead 239.  Rows of one wavefront need none (60000 x 1000 fp16 66 us, with 76).
 template <class T, int TPR, int NV, int BLOCK, int WAVES, bool AHEAD, bool PAST, bool ENDS>
 __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) {
   constexpr int V = 16 / sizeof(T), RPB = BLOCK / TPR, N = NV * V;
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm_grad(NormGradRows a) 
     cols.template load<PAST, ENDS>((const T *)a.dy + r * a.lddy, RPB == 1 || r < a.rows, ndy);
   };
   if constexpr (AHEAD) fetch((int64_t)blockIdx.x * RPB + sub);
-  constexpr bool GAIN_LDS = sizeof(T) == 2 && NV == 2;
+  constexpr bool GAIN_LDS = sizeof(T) == 2 && NV == 2 && TPR > 64;
   __shared__ float4 gain_lds[GAIN_LDS ? N / 4 * BLOCK : 1];
   float g[N], dg[N];
   cols.template gain<T>(a.gain, a.gain_f32, g);
