@@ -729,7 +729,8 @@ struct NormLaunch {
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 && BLOCK < 1024 ? 6 : 4;   // wavefronts a SIMD
+    // Wavefronts a SIMD, as many as need no scratch; a block of 1024 brings four at a time (six: 10000 x 5000 fp32 64 -> 92 us).
+    constexpr int V = 16 / sizeof(T), W = NV * V <= 4 ? 8 : NV * V <= 8 && BLOCK < 1024 ? 6 : 4;
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR), most = (int64_t)cu_count * (W * 256 / BLOCK);
     constexpr bool ENDS = !(V == 4 && NV == 4);   // no registers left for it there
     const unsigned grid = even_grid(blocks, most);
@@ -758,7 +759,7 @@ struct NormGradLaunch {
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;
+    constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;   // two vectors in five: 400000 x 128 fp32 100 -> 106 us
     constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
     int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);
