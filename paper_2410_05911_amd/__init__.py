@@ -816,6 +816,12 @@ class Trainer:
                 out[k] = v
         return out
 
+    def _counts(self) -> list:
+        """Values of each tensor that the library updates, in the order of TrainGrads: they follow from the model, and the
+        library reads and writes that many."""
+        L, N, d, n = self.L, self.n_layers, self.d, self.n
+        return [L * d] + [N * d * d] * 4 + [4 * N * d * d] * 2 + [6 * N] + [N * d] * 4 + [4 * N * d] + [N * d] * 5 + [d, 1, L * n, n]
+
     def grad(self, params: dict, y, xs=None, stream=None):
         """One step on the words y [B, n] (xs: transmitted +-1 words, None = all-zero codeword).
         Returns (loss one-element tensor, gradients dict shaped like params, without pos)."""
@@ -857,10 +863,11 @@ class Trainer:
         flat = [self._flat(d) for d in (params, state["m"], state["v"], grads)]
         device = params["embed"].get_device()
         _on_current_gpu(device)
+        counts = self._counts()
         for d in flat:
-            for f in fields:
-                if d[f].dtype != torch.float32 or d[f].numel() != flat[0][f].numel() or d[f].get_device() != device:
-                    raise ValueError(f"{f} must be float32, {flat[0][f].numel()} values on cuda:{device}")
+            for f, count in zip(fields, counts):
+                if d[f].dtype != torch.float32 or d[f].numel() != count or d[f].get_device() != device:
+                    raise ValueError(f"{f} must be float32, {count} values on cuda:{device}")
             lists.append(TrainGrads(*[_ptr(d[f]) for f in fields]))
         step = _step_tensor(state["step"], device)
         norm = None if max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
