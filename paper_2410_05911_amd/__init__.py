@@ -447,28 +447,49 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
 class TensorList:
     """A list of contiguous CUDA tensors (float32, bfloat16, float16; one device) as the library takes it.  A program that
     uses the same tensors again and again keeps the list; the calls below take any sequence of tensors too.  The list
-    keeps the tensors, whose memory must stay where it is (no resize_ or set_ on them)."""
+    stands for the memory that the tensors have when it is made, and keeps that memory: a tensor that is given other
+    memory later (`t.data = ...`, `module.to(...)`, `set_`) needs a new list, and `resize_` must not move it.  (Adam
+    looks after its own lists.)"""
 
-    def __init__(self, tensors):
+    def __init__(self, tensors, *, _keep: bool = True):
         self.tensors = list(tensors)
+        self._keep = _keep
+        self._read()
+        size = C.c_size_t()
+        _check(lib().aecct_update_workspace_size(len(self), C.byref(size)), "aecct_update_workspace_size")
+        self.workspace_bytes = size.value
+
+    def _read(self):
+        """Takes the tensors' addresses, and (not for the list of a single call) holds on to the memory there: the tensor
+        objects alone do not, their storage can be exchanged."""
         n = len(self.tensors)
-        self.array = (Tensor * n)()
-        self.device = self.tensors[0].get_device() if n else None
+        array = (Tensor * n)()
+        device = self.tensors[0].get_device() if n else None
         for i, t in enumerate(self.tensors):
             if not t.is_contiguous():
                 raise ValueError(f"tensor {i} must be contiguous")
-            if t.get_device() != self.device or self.device < 0:
+            if t.get_device() != device or device < 0:
                 raise ValueError("the tensors must be on one GPU")
-            self.array[i] = Tensor(t.data_ptr(), t.numel(), _dtype_code(t))
-        size = C.c_size_t()
-        _check(lib().aecct_update_workspace_size(n, C.byref(size)), "aecct_update_workspace_size")
-        self.workspace_bytes = size.value
+            array[i] = Tensor(t.data_ptr(), t.numel(), _dtype_code(t))
+        self.array, self.device = array, device
+        if self._keep:
+            self._addresses = [t.data_ptr() for t in self.tensors]
+            self._memory = [t.untyped_storage() for t in self.tensors]
+
+    def _follow(self):
+        """Takes the addresses anew if a tensor has moved since."""
+        if [t.data_ptr() for t in self.tensors] != self._addresses:
+            self._read()
 
     def __len__(self):
         return len(self.tensors)
 
 
-def _list(tensors):
+def _list(tensors):   # for one call
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors, _keep=False)
+
+
+def _kept_list(tensors):
     return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
 
 
@@ -544,15 +565,16 @@ class Adam:
     """Adam over a list of float32 tensors (Section 6), updated in place: moments m and v (zeros, or the given float32
     tensors), the number of updates made in `step` (one int64 value on the GPU), decoupled weight decay, gradients
     clipped to max_norm over the whole list (None: not; 0: not, but measured), and optional 16-bit `copies` of the parameters.
-    lr: a number, or one float32 value on the GPU that captured graphs read at each replay."""
+    lr: a number, or one float32 value on the GPU that captured graphs read at each replay.  Parameters and copies that have
+    been given other memory since (`p.data = ...`, `module.to(...)`) are updated where they are; the moments stay."""
 
     def __init__(self, params, lr=1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, max_norm=None,
                  m=None, v=None, step=None, copies=None):
         import torch
-        self.params = _list(params)
-        self.m = _list(m if m is not None else [torch.zeros_like(p) for p in self.params.tensors])
-        self.v = _list(v if v is not None else [torch.zeros_like(p) for p in self.params.tensors])
-        self.copies = None if copies is None else _list(copies)
+        self.params = _kept_list(params)
+        self.m = _kept_list(m if m is not None else [torch.zeros_like(p) for p in self.params.tensors])
+        self.v = _kept_list(v if v is not None else [torch.zeros_like(p) for p in self.params.tensors])
+        self.copies = None if copies is None else _kept_list(copies)
         for what, t in (("m", self.m), ("v", self.v), ("copies", self.copies)):
             if t is not None and len(t) != len(self.params):
                 raise ValueError(f"{what} must hold {len(self.params)} tensors")
@@ -570,7 +592,10 @@ class Adam:
         g = _list(grads)
         if len(g) != len(self.params):
             raise ValueError(f"grads must hold {len(self.params)} tensors")
-        device = _one_gpu(self.params, g) if len(g) else self.device
+        self.params._follow()
+        if self.copies is not None:
+            self.copies._follow()
+        device = _one_gpu(self.params, self.m, self.v, self.copies, g) if len(g) else self.device
         opt = _adam_options(self.lr if lr is None else lr, self.betas, self.eps, self.weight_decay, self.max_norm)
         norm = None if self.max_norm is None else torch.empty(1, dtype=torch.float32, device=device)
         ws = torch.empty(g.workspace_bytes, dtype=torch.uint8, device=device)
