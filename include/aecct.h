@@ -432,7 +432,7 @@ typedef enum aecct_code {
  *   h = x + res,   rho = 1 / sqrt(mean(h^2) + eps),   y = h rho gain,   codes and alpha of y.
  * x, res, h and y are of one type; y and the codes are taken of the unrounded h, the codes of the unrounded y.
  * A row with a NaN or an infinity gives what the formulas give (rho = NaN, or 0): its alphas are NaN where
- * a value they span is NaN, and int8 codes of NaN are 0.  Where squares leave fp32's range the row is
+ * a value they span is NaN; such an alpha's codes are 0 in int8 and NaN in e4m3.  Where squares leave fp32's range the row is
  * summed again, scaled by a power of two.
  */
 typedef struct aecct_rms_norm_args {

@@ -225,17 +225,22 @@ __device__ __forceinline__ float tail_of(float A, const float *h, const float *g
 struct CodeScale {
   float up, q, q1;   // up: a power of two that keeps A and q normal numbers
 };
-__device__ __forceinline__ CodeScale code_scale(float A, float E, float most) {
+__device__ __forceinline__ CodeScale code_scale(float alpha, float A, float E, float most) {
   CodeScale s;
   s.up = A < 0x1p-60f ? 0x1p60f : A > 0x1p60f ? 0x1p-60f : 1.0f;
   const float b = A * s.up, r = __builtin_amdgcn_rcpf(b), t = E > kNoTail ? E * s.up : 0.0f;
-  s.q = A == 0.0f ? 0.0f : most * r;
-  s.q1 = A == 0.0f || !(b <= 3e38f) ? 0.0f : fmaf(-s.q, t, fmaf(-s.q, b, most)) * r;
+  s.q = most * r;
+  s.q1 = b <= 3e38f ? fmaf(-s.q, t, fmaf(-s.q, b, most)) * r : 0.0f;
+  if (!(alpha > 0)) {   // codes 0, or NaN where alpha is: of every value, also where rho alone is 0 or NaN
+    s.q = alpha;
+    s.q1 = 0;
+  }
   return s;
 }
 template <int V>
-__device__ __forceinline__ void codes_of(int code, float A, float E, const float *h, const float *g, uint32_t (&w)[V / 4]) {
-  const CodeScale s = code_scale(A, E, code == 1 ? 127.0f : 448.0f);
+__device__ __forceinline__ void codes_of(int code, float alpha, float A, float E, const float *h, const float *g,
+                                         uint32_t (&w)[V / 4]) {
+  const CodeScale s = code_scale(alpha, A, E, code == 1 ? 127.0f : 448.0f);
   float v[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -250,7 +255,7 @@ __device__ __forceinline__ void codes_of(int code, float A, float E, const float
     }
   }
   if (code == 1) {
-    const uint32_t keep = A == A ? 0xffffffffu : 0u;
+    const uint32_t keep = alpha == alpha ? 0xffffffffu : 0u;
     uint32_t b[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] = quant_bits(v[i], 1.0f);
@@ -295,12 +300,13 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
       B = lanes_join<Max>(m[j], a.group / V);
       F = lanes_join<Largest>(tail_of<V>(B, h + j * V, g + j * V), a.group / V);
     }
+    const float alpha = B * rho;
     uint32_t w[V / 4];
-    codes_of<V>(a.code, B, F, h + j * V, g + j * V, w);
+    codes_of<V>(a.code, alpha, B, F, h + j * V, g + j * V, w);
     uint8_t *to = a.codes + r * a.ldcodes + c;
     if (live && cols.full(j)) __builtin_memcpy(to, w, V);
     if (live && cols.last && j == cols.jt) store_codes<V>(to, cols.tail, w);
-    if (live && c < a.d && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = B * rho;
+    if (live && c < a.d && c % a.group == 0) a.alpha[r * a.alphas + c / a.group] = alpha;
   }
 }
 
