@@ -78,6 +78,9 @@ __device__ __forceinline__ float near_rho(float ss, float inv_d, float eps) {
 }
 __device__ __forceinline__ bool in_range(float s) { return s >= 1e-24f && s <= 1e37f; }
 
+// rho in [2^k, 2^(k + 1)); -1 for 0, infinity and NaN, which the scaling leaves what they are
+__device__ __forceinline__ int exponent_of(float rho) { return __builtin_amdgcn_frexp_expf(rho) - 1; }
+
 // A row's rho = 1 / sqrt(mean(h^2) + eps) where the plain fp32 sum of squares is out of range: h is scaled by a power of
 // two first, `unit`, and by a second that takes rho into [1, 2), so that products with h stay in range; h rho is
 // unchanged and the rho of the row as it was is rho unit.
@@ -91,7 +94,7 @@ __device__ __forceinline__ float far_rho_of(float ss, float up, float inv_d, flo
   } else {
     rho = __builtin_amdgcn_rsqf(fmaf(ss, inv_d, eps * up * up));
   }
-  const int k = rho > 0 && rho < __builtin_inff() ? __builtin_amdgcn_frexp_expf(rho) - 1 : 0;
+  const int k = exponent_of(rho);
   more = ldexpf(1.0f, e + k);
   return ldexpf(rho, -k);
 }
@@ -112,6 +115,18 @@ __device__ __forceinline__ float far_rho(float ss, float (&h)[N], float inv_d, f
   for (int i = 0; i < N; ++i) h[i] *= more;
   unit = up * more;
   return rho;
+}
+
+// Products h gain below this are taken of h 2^k instead, and rho 2^-k, with k such that rho 2^-k lies in [2^-100, 2^-99):
+// |h rho| is at most 2^8, so h 2^k cannot overflow, and wherever |h gain rho| is not below fp32's smallest number, h 2^k gain
+// is above 2^-51 and its rounding error a normal number too.
+constexpr float kTiny = 0x1p-60f;
+template <int N>
+__device__ __forceinline__ float lift(float *h, float rho) {   // scales h, returns rho for it
+  const int k = 100 + exponent_of(rho);
+#pragma unroll
+  for (int i = 0; i < N; ++i) h[i] = ldexpf(h[i], k);
+  return ldexpf(rho, -k);
 }
 
 // Where a thread's columns lie: vector j starts at column col(j).  A row of d = V k + tail values ends in a vector of
@@ -196,7 +211,9 @@ __device__ __forceinline__ int row_of_block() {
 // ---- codes -----------------------------------------------------------------------------------------------------
 // code = round(p Q / A) with p = h gain and A = max |p|: rho is a factor of both y and alpha and drops out.  Everything is
 // taken with its rounding error beside it, p + e and A + E, and the quotient as (p + e)(q + q1), q a near Q / A and q1
-// what it lacks: a code then differs from the exact one only where the quotient is within 2^-24 of a tie.
+// what it lacks: a code then differs from the exact one only where the quotient is within 2^-24 of a tie.  A row, or a group
+// of its columns, whose products h gain are tiny is scaled first (kTiny), since neither they nor their errors need be
+// numbers of fp32.
 constexpr float kNoTail = -3e38f;
 // max |p| of each vector of a thread's values
 template <int V, int NV>
@@ -223,11 +240,11 @@ __device__ __forceinline__ float tail_of(float A, const float *h, const float *g
   return E;
 }
 struct CodeScale {
-  float up, q, q1;   // up: a power of two that keeps A and q normal numbers
+  float up, q, q1;   // up: a power of two that keeps q1 a normal number
 };
 __device__ __forceinline__ CodeScale code_scale(float alpha, float A, float E, float most) {
   CodeScale s;
-  s.up = A < 0x1p-60f ? 0x1p60f : A > 0x1p60f ? 0x1p-60f : 1.0f;
+  s.up = A > 0x1p60f ? 0x1p-60f : 1.0f;
   const float b = A * s.up, r = __builtin_amdgcn_rcpf(b), t = E > kNoTail ? E * s.up : 0.0f;
   s.q = most * r;
   s.q1 = b <= 3e38f ? fmaf(-s.q, t, fmaf(-s.q, b, most)) * r : 0.0f;
@@ -281,10 +298,10 @@ __device__ __forceinline__ void store_codes(uint8_t *to, int n, const uint32_t (
 }
 
 // ---- the norm ---------------------------------------------------------------------------------------------------
-// y and the codes of a row's columns from `off` on, those that cols holds.
+// y and the codes of a row's columns from `off` on, those that cols holds.  h is used up.
 template <class T, int V, int TPR, int NV>
 __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, TPR, NV> &cols, int off, int64_t r, bool live,
-                                           const float (&h)[NV * V], const float (&g)[NV * V], const float (&m)[NV], float A,
+                                           float (&h)[NV * V], const float (&g)[NV * V], const float (&m)[NV], float A,
                                            float E, float rho) {
   if (a.y)
     cols.store((T *)a.y + r * a.ldy + off, live, a.past_out, [&](int j, float (&v)[V]) {
@@ -294,13 +311,18 @@ __device__ __forceinline__ void write_norm(const NormRows &a, const Columns<V, T
   if (!a.code) return;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int c = off + cols.col(j);
-    float B = A, F = E;
+    const int c = off + cols.col(j), lanes = a.group / V;
+    float B = A, F = E, rho_j = rho;
     if (a.alphas > 1) {
-      B = lanes_join<Max>(m[j], a.group / V);
-      F = lanes_join<Largest>(tail_of<V>(B, h + j * V, g + j * V), a.group / V);
+      B = lanes_join<Max>(m[j], lanes);
+      if (B < kTiny) {   // the row's own maximum is not
+        float t[1];
+        rho_j = lift<V>(h + j * V, rho);
+        B = lanes_join<Max>(vector_max<V, 1>(h + j * V, g + j * V, t), lanes);
+      }
+      F = lanes_join<Largest>(tail_of<V>(B, h + j * V, g + j * V), lanes);
     }
-    const float alpha = B * rho;
+    const float alpha = B * rho_j;
     uint32_t w[V / 4];
     codes_of<V>(a.code, alpha, B, F, h + j * V, g + j * V, w);
     uint8_t *to = a.codes + r * a.ldcodes + c;
@@ -368,11 +390,16 @@ __global__ __launch_bounds__(BLOCK, WAVES) void k_rms_norm(NormRows a) {
     row_join<Max, TPR>(ss, A, lds);
     if (ENDS) store_h();   // behind the join: h may lie on an input, whose row's last lane reads columns of its neighbour's
     float rho = near_rho(ss, inv_d, a.eps);
-    if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
+    if (!in_range(ss) || !(A >= kTiny && A <= 1e37f)) {
       float unit, none = 0;
       rho = far_rho<TPR>(ss, h, inv_d, a.eps, unit, lds);
       A = vector_max<V, NV>(h, g, m);
       row_join<Max, TPR>(none, A, lds);
+      if (A < kTiny) {   // tiny gains
+        rho = lift<NV * V>(h, rho);
+        A = vector_max<V, NV>(h, g, m);
+        row_join<Max, TPR>(none, A, lds);
+      }
     }
     float E = kNoTail;
     if (a.code && a.alphas == 1) {
@@ -443,11 +470,15 @@ __global__ __launch_bounds__(kWideThreads) void k_rms_norm_wide(NormRows a) {
     };
     sums(1.0f, 1.0f);
     float rho = near_rho(ss, inv_d, a.eps), up = 1.0f, more = 1.0f;
-    if (!in_range(ss) || !(A >= 0x1p-60f && A <= 1e37f)) {
+    if (!in_range(ss) || !(A >= kTiny && A <= 1e37f)) {
       up = far_up(ss);
       sums(up, 1.0f);
       rho = far_rho_of(ss, up, inv_d, a.eps, more);
       sums(up, more);
+      if (A < kTiny) {
+        rho = lift<1>(&more, rho);
+        sums(up, more);
+      }
     }
     for (int off = 0; off < a.d; off += kWideStep) {
       const Cols cols(a.d - off, threadIdx.x);

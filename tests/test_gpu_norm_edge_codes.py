@@ -1,4 +1,5 @@
-"""The row norm's 8-bit codes in rows with NaN, infinities and zeros against the formulas in 64 bits.
+"""The row norm's 8-bit codes where products h gain leave fp32's normal range, and in rows with NaN, infinities and zeros,
+against the formulas in 64 bits.
 
 With u = 2^-24: alpha is off by 64 u and half of fp32's smallest number, 2^-150; a code is the nearest to the exact quotient
 h gain Q / max |h gain|, or that quotient is within u of a tie.  An alpha of 0 has codes 0; where alpha is NaN, int8
@@ -56,6 +57,43 @@ def _gain(d, exponent, columns, seed):
     g = 1 + 0.3 * torch.randn(d, dtype=torch.float64, generator=torch.Generator().manual_seed(seed))
     g[columns] *= 2.0 ** exponent
     return g.float().cuda()
+
+
+EXPONENTS = [-55, -70, -100, -120, -126, -133, -140, -145, -149]
+
+
+@pytest.mark.parametrize("code", list(CODES))
+@pytest.mark.parametrize("d,group", [(100, 32), (256, 64), (300, 128), (1000, 32), (2500, 64), (6000, 128), (9001, 32), (20000, 64)])
+def test_groups_of_tiny_products_beside_ordinary_ones(P, d, group, code):
+    """Each other group's gains far down, to the smallest numbers, for rows of every size."""
+    for type in (torch.float32, torch.bfloat16):
+        for scale, eps in ((1.0, 1e-5), (1e-4, 1e-5), (1e-11, 0.0), (1e17, 1e-5), (1e-20, 0.0), (1e25, 1e-5)):
+            x = (torch.randn(9, d, device="cuda", generator=torch.Generator("cuda").manual_seed(d)) * scale).to(type)
+            for e in EXPONENTS:
+                columns = (torch.arange(d) // group) % 2 == 1
+                _check(P, x, _gain(d, e, columns, d), eps, code, group, (d, group, type, scale, e))
+
+
+@pytest.mark.parametrize("code", list(CODES))
+@pytest.mark.parametrize("d", [3, 20, 60, 128, 250, 900, 1500, 3000, 6000, 16384, 20000])
+def test_rows_of_tiny_products(P, d, code):
+    for type in (torch.float32, torch.float16):
+        for scale, eps in ((1.0, 1e-5), (1e-4, 1e-5), (100.0, 0.0)):
+            x = (torch.randn(9, d, device="cuda", generator=torch.Generator("cuda").manual_seed(d)) * scale).to(type)
+            for e in EXPONENTS:
+                _check(P, x, _gain(d, e, torch.ones(d, dtype=torch.bool), d), eps, code, 0, (d, type, scale, e))
+
+
+@pytest.mark.parametrize("code", list(CODES))
+def test_a_group_of_a_few_smallest_numbers(P, code):
+    """h = 5 times the smallest number and gain 1.25: h gain = 6.25 of it, which fp32 has not; beside a group of ones."""
+    x = torch.ones(3, 64, device="cuda")
+    x[:, 32:] = 5 * 2.0 ** -149
+    x[1, 40] = -5 * 2.0 ** -149
+    x[2, 41] = 2.0 ** -149
+    _check(P, x, torch.full((64,), 1.25, device="cuda"), 1e-5, code, 32, "smallest")
+    x[:, :32] = 1e-3                      # rho of about 250: alpha is not among the smallest numbers
+    _check(P, x, torch.full((64,), 1.25, device="cuda"), 1e-5, code, 32, "smallest, larger alpha")
 
 
 @pytest.mark.parametrize("code", list(CODES))
