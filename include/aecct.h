@@ -410,8 +410,9 @@ void aecct_train_destroy(aecct_trainer *tr);
  * and Eq. 2 codes, its gradient, the norm of many gradient tensors with clipping, and the Adam update
  * (Section 6).  They take no model: every pointer is device memory of the current HIP device.
  * They enqueue on stream, and neither allocate nor synchronise, so a HIP graph may capture them; the
- * same call gives the same bits.  Calls on different streams are safe if their outputs and workspaces
- * differ; a workspace needs no clearing and holds nothing between calls.
+ * same call gives the same bits (a list's norm, and what it scales, at the same addresses: which tensors lie back to back decides the
+ * order of its fp64 sum).  Calls on different streams are safe if their outputs and workspaces differ; a workspace
+ * needs no clearing, holds nothing between calls and overlaps no tensor of its call (INVALID_ARG).
  * ---------------------------------------------------------------------------------------- */
 
 /* Types of values in device memory.  Sums, norms and moments are taken in fp32 or fp64; a 16-bit output is

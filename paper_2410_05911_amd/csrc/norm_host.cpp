@@ -124,6 +124,10 @@ aecct_status aecct_rms_norm_grad(const aecct_rms_norm_grad_args *a, void *worksp
     (void)aecct_rms_norm_grad_workspace_size(a->rows, a->d, &need);
     if (workspace_bytes < need) return AECCT_ERR_WORKSPACE_TOO_SMALL;
     if (!workspace) return AECCT_ERR_INVALID_ARG;
+    const Rows ws{workspace, 1, (int64_t)need, 0};
+    if (overlap(ws, dh) || overlap(ws, dgain)) return AECCT_ERR_INVALID_ARG;
+    for (int i = 0; i < 4; ++i)
+      if (overlap(ws, in[i])) return AECCT_ERR_INVALID_ARG;
     part = (float *)align_up((size_t)(uintptr_t)workspace);
   }
   int dev = 0, cus = 0;

@@ -168,13 +168,17 @@ aecct_status aecct_update_workspace_size(int32_t n, size_t *bytes) {
 aecct_status aecct_grad_norm(const aecct_tensor *grads, int32_t n, float *norm, void *workspace, size_t workspace_bytes,
                              void *stream) {
   if (!list_ok(grads, n) || !norm) return AECCT_ERR_INVALID_ARG;
-  const uintptr_t at = (uintptr_t)norm;
+  const uintptr_t at = (uintptr_t)norm, ws = (uintptr_t)workspace, ws_end = ws + need_bytes(n);
+  bool on_norm = false, on_ws = at < ws_end && ws < at + sizeof(float);
   for (int i = 0; i < n; ++i) {
     Span x;
-    if (span_of(grads[i], false, x) && x.begin < at + sizeof(float) && at < x.end) return AECCT_ERR_INVALID_ARG;
+    if (!span_of(grads[i], false, x)) continue;
+    on_norm = on_norm || (x.begin < at + sizeof(float) && at < x.end);
+    on_ws = on_ws || (x.begin < ws_end && ws < x.end);
   }
+  if (on_norm) return AECCT_ERR_INVALID_ARG;
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
-  if (!workspace) return AECCT_ERR_INVALID_ARG;
+  if (!workspace || on_ws) return AECCT_ERR_INVALID_ARG;
   const Work w = work_of(workspace);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
@@ -190,10 +194,11 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    Spans v(2 * (size_t)n + 1);
+    Spans v(2 * (size_t)n + 2);
     v.add(out, n, true);
     v.add(grads, n, false, out);
     v.add(norm, sizeof(float));
+    v.add(workspace, need_bytes(n));
     if (v.conflict()) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
@@ -240,7 +245,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    Spans spans(5 * (size_t)n + 3);
+    Spans spans(5 * (size_t)n + 4);
     spans.add(params, n, true);
     spans.add(m, n, true);
     spans.add(v, n, true);
@@ -249,6 +254,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
     spans.add(step, sizeof(int64_t));
     if (norm) spans.add(norm, sizeof(float));
     if (opt->lr_device) spans.add(opt->lr_device, sizeof(float), false);
+    spans.add(workspace, need_bytes(n));
     if (spans.conflict()) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
