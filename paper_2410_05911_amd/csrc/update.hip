@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void k_adam(AdamTable<N> t, const double 
     for (int i = 0; i < 4; ++i) {
       const float x = f.of(g[i]);
       m[i] = fmaf(b1, m[i], c1 * x);
-      v[i] = fmaf(b2, v[i], c2 * (x * x));
+      v[i] = fmaf(b2, v[i], c2 * x * x);   // x * x alone would leave fp32's range first
       p[i] -= fmaf(decay, p[i], size * m[i] / fmaf(sqrtf(v[i]), root, eps));
     }
     const int n = left >= 4 ? 4 : (int)left;
