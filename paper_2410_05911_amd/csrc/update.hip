@@ -164,8 +164,9 @@ __global__ __launch_bounds__(kThreads) void k_norm(const double *part, int parts
   if (threadIdx.x == 0) *norm = (float)n;
 }
 
-// min(1, max_norm / norm), and 1 for a norm that is not finite.  A factor below fp32's normal range (a norm past it) is
-// taken in two, the first a power of two.
+// min(1, max_norm / norm), and 1 for a norm that is not finite.  A factor near or below the end of fp32's normal range is
+// taken in two, the first a power of two, the second normal for every factor above 2^-275: no value is left of the largest
+// gradient below that.
 struct Factor {
   float up = 1.0f, f = 1.0f;
   __device__ __forceinline__ float of(float g) const { return g * up * f; }
@@ -174,8 +175,9 @@ __device__ __forceinline__ Factor clip_factor(double norm, double max_norm) {
   Factor r;
   if (norm > max_norm && norm <= 1.7976931348623157e308) {
     const double f = max_norm / norm;
-    r.up = f < 0x1p-100 ? 0x1p-64f : 1.0f;
-    r.f = (float)(f < 0x1p-100 ? f * 0x1p64 : f);
+    const int k = f < 0x1p-190 ? 149 : f < 0x1p-100 ? 64 : 0;
+    r.up = ldexpf(1.0f, -k);
+    r.f = (float)ldexp(f, k);
   }
   return r;
 }

@@ -35,3 +35,16 @@ def test_second_moment_of_large_gradients(P, type, size, beta2):
     for got, want, bound, what in ((p[0], p2, pb, "param"), (m[0], m2, mb, "m"), (v[0], v2, vb, "v")):
         assert got.isfinite().all(), what
         _near(got, want, bound, what)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-10, 1e-18, 1e-21, 1e-25, 1e-33, 1e-38, 1e-42, 1e-45, 1e-60])
+def test_clipping_by_factors_far_below_one(P, type, max_norm):
+    """The largest gradients clipped to norms down to the smallest numbers, and small ones beside them."""
+    g = [(torch.linspace(0.1, 1.0, 300, device="cuda") * 3e38).to(TYPES[type]), torch.tensor([1e30, -1e10, 1.0, 1e-30, 1e-45, 0.0], device="cuda")]
+    want = _norm64(g)
+    keep = [t.clone() for t in g]
+    P.grad_clip(g, max_norm)
+    for a, k in zip(g, keep):
+        x = k.double() * (max_norm / want)
+        _near(a, x, (2.1 * U + HALF[a.dtype]) * x.abs() + TINY[a.dtype], max_norm)
