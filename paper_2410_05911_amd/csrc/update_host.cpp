@@ -69,6 +69,12 @@ struct Spans {
     if (!std::is_sorted(v.begin() + old, v.end(), before)) std::sort(v.begin() + old, v.end(), before);
     if (old && old < v.size() && before(v[old], v[old - 1])) std::inplace_merge(v.begin(), v.begin() + old, v.end(), before);
   }
+  bool meets(const void *p, size_t bytes) const {   // whether any span of the lists shares a byte with these
+    const uintptr_t begin = (uintptr_t)p, end = begin + bytes;
+    bool any = false;
+    for (const Span &s : v) any |= s.begin < end && begin < s.end;
+    return any;
+  }
   bool conflict() const {
     uintptr_t any = 0, written = 0;   // the furthest ends so far
     for (const Span &s : v) {
@@ -194,12 +200,11 @@ aecct_status aecct_grad_clip(const aecct_tensor *grads, const aecct_tensor *out,
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    Spans v(2 * (size_t)n + 2);
+    Spans v(2 * (size_t)n + 1);
     v.add(out, n, true);
     v.add(grads, n, false, out);
     v.add(norm, sizeof(float));
-    v.add(workspace, need_bytes(n));
-    if (v.conflict()) return AECCT_ERR_INVALID_ARG;
+    if (v.conflict() || v.meets(workspace, need_bytes(n))) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
   }
@@ -245,7 +250,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
   if (workspace_bytes < need_bytes(n)) return AECCT_ERR_WORKSPACE_TOO_SMALL;
   if (!workspace) return AECCT_ERR_INVALID_ARG;
   try {
-    Spans spans(5 * (size_t)n + 4);
+    Spans spans(5 * (size_t)n + 3);
     spans.add(params, n, true);
     spans.add(m, n, true);
     spans.add(v, n, true);
@@ -254,8 +259,7 @@ aecct_status aecct_adam_step(const aecct_tensor *params, const aecct_tensor *m, 
     spans.add(step, sizeof(int64_t));
     if (norm) spans.add(norm, sizeof(float));
     if (opt->lr_device) spans.add(opt->lr_device, sizeof(float), false);
-    spans.add(workspace, need_bytes(n));
-    if (spans.conflict()) return AECCT_ERR_INVALID_ARG;
+    if (spans.conflict() || spans.meets(workspace, need_bytes(n))) return AECCT_ERR_INVALID_ARG;
   } catch (const std::bad_alloc &) {
     return AECCT_ERR_OUT_OF_MEMORY;
   }
