@@ -473,12 +473,16 @@ class TensorList:
             array[i] = Tensor(t.data_ptr(), t.numel(), _dtype_code(t))
         self.array, self.device = array, device
         if self._keep:
-            self._addresses = [t.data_ptr() for t in self.tensors]
+            self._addresses = self._places()
             self._memory = [t.untyped_storage() for t in self.tensors]
+
+    def _places(self):
+        import torch
+        return list(map(torch.Tensor.data_ptr, self.tensors))
 
     def _follow(self):
         """Takes the addresses anew if a tensor has moved since."""
-        if [t.data_ptr() for t in self.tensors] != self._addresses:
+        if self._places() != self._addresses:
             self._read()
 
     def __len__(self):
