@@ -410,8 +410,8 @@ void aecct_train_destroy(aecct_trainer *tr);
  * and Eq. 2 codes, its gradient, the norm of many gradient tensors with clipping, and the Adam update
  * (Section 6).  They take no model: every pointer is device memory of the current HIP device.
  * They enqueue on stream, and neither allocate nor synchronise, so a HIP graph may capture them; the
- * same call gives the same bits (a list's norm, and what it scales, at the same addresses: which tensors lie back to back decides the
- * order of its fp64 sum).  Calls on different streams are safe if their outputs and workspaces differ; a workspace
+ * same call gives the same bits (a list's norm, and what it scales, at the same addresses: which tensors lie
+ * back to back decides the order of its fp64 sum).  Calls on different streams are safe if their outputs and workspaces differ; a workspace
  * needs no clearing, holds nothing between calls and overlaps no tensor of its call (INVALID_ARG).
  * ---------------------------------------------------------------------------------------- */
 
@@ -432,6 +432,7 @@ typedef enum aecct_code {
  * Root-mean-square norm of `rows` rows of d values, ld* values apart:
  *   h = x + res,   rho = 1 / sqrt(mean(h^2) + eps),   y = h rho gain,   codes and alpha of y.
  * x, res, h and y are of one type; y and the codes are taken of the unrounded h, the codes of the unrounded y.
+ * y is (h gain) rho, both products in fp32.
  * A row with a NaN or an infinity gives what the formulas give (rho = NaN, or 0): its alphas are NaN where
  * a value they span is NaN; such an alpha's codes are 0 in int8 and NaN in e4m3.  Where squares leave fp32's range the row is
  * summed again, scaled by a power of two.
@@ -464,7 +465,7 @@ aecct_status aecct_rms_norm(const aecct_rms_norm_args *a, void *stream);
  * rounding to codes passes it straight through, alpha's dependence ignored, as in the training step), dres the
  * gradient that reaches h past the norm along the residual:
  *   xh = h rho,  c = mean(dy gain xh),  dh = rho (dy gain - xh c) + dres,  dgain = sum over rows of dy xh.
- * dh is the gradient of x and of res alike.
+ * dh is the gradient of x and of res alike.  Products of dy, gain and h are taken in fp32.
  */
 typedef struct aecct_rms_norm_grad_args {
   int64_t rows, d;

@@ -347,7 +347,8 @@ def rms_norm(x, gain=None, res=None, eps: float = 1e-5, *, y=None, h=None, codes
     """Root-mean-square norm of rows with the residual's addition: h = x + res, y = h / sqrt(mean(h^2) + eps) * gain, and
     y's 8-bit codes (Eq. 2) with their alphas, one for a row or for `group` (32, 64 or 128) columns.
 
-    x, res: CUDA tensors [..., d] of one type (float32, bfloat16, float16); gain [d] float32 or that type.  code_type:
+    x, res: CUDA tensors [..., d] of one type (float32, bfloat16, float16), contiguous or of two dimensions with contiguous
+    rows; gain [d] float32 or that type.  Autograd does not record the call: rms_norm_grad is its gradient.  code_type:
     None, torch.int8 (value = code * alpha / 127) or torch.float8_e4m3fn (value = code * alpha / 448).  y, h, codes,
     alpha: outputs to write to, else new tensors (h or y may be x or res itself).
     Returns (y, h, codes, alpha), None where there is no such output: y without with_y, h without res."""
@@ -529,7 +530,8 @@ def grad_norm(grads, stream=None):
 
 def grad_clip(grads, max_norm: float, out=None, stream=None):
     """Scales every gradient by min(1, max_norm / norm), in place or into the tensors of `out`; returns the norm before
-    clipping.  Where any value is not finite, none is scaled."""
+    clipping.  Where any value is not finite, none is scaled.  A max_norm of 0 makes every value 0.  Autograd does not see
+    the write (no version counter moves)."""
     import torch
     if stream is not None:
         with _on_stream(stream):
@@ -570,7 +572,8 @@ class Adam:
     tensors), the number of updates made in `step` (one int64 value on the GPU), decoupled weight decay, gradients
     clipped to max_norm over the whole list (None: not; 0: not, but measured), and optional 16-bit `copies` of the parameters.
     lr: a number, or one float32 value on the GPU that captured graphs read at each replay.  Parameters and copies that have
-    been given other memory since (`p.data = ...`, `module.to(...)`) are updated where they are; the moments stay."""
+    been given other memory since (`p.data = ...`, `module.to(...)`) are updated where they are; the moments stay.  Autograd
+    does not see the update (no version counter moves): finish a backward pass before the step that follows it."""
 
     def __init__(self, params, lr=1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0, max_norm=None,
                  m=None, v=None, step=None, copies=None):

@@ -722,8 +722,10 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dgain(const float *part, int 
 // values a thread where a row fits a wavefront or less, so two vectors in fp32 (one: 49152 x 128 14.8 -> 14.3 us with two)
 // and one in 16 bits (with two the gradient of 100000 x 200 26 -> 37 us, of 100000 x 512 55 -> 77).  Long rows have two
 // vectors a thread in the norm (with one 16384 x 8192 bf16 to codes 173 -> 221 us, 2000 x 8192 23 -> 25) and one in the
-// gradient (F::kThin), which holds more of each: 777 x 5003 fp16 18.5 -> 15.8 us, 2000 x 8192 bf16 25.7 -> 23.3,
-// 4096 x 2048 fp32 21.9 -> 20.5, 16384 x 4096 bf16 the same.
+// gradient (F::kThin), which holds more of each.  That pays for few rows and for widths that fill their threads: with two
+// 777 x 5003 fp16 18.4 us, with one 15.9, 2000 x 8192 bf16 25.9 and 23.4, 20000 x 8192 193 and 177, 4096 x 2048 fp32 22.0
+// and 20.7, 16384 x 4096 bf16 73.9 and 69.2; many rows a little wider than a power of two lose: 20000 x 5003 bf16 136 and
+// 147, 20000 x 2100 57 and 67.
 template <int V, class F>
 hipError_t by_width(int d, const F &f) {
   const int n = (d + V - 1) / V;   // vectors a row
@@ -796,7 +798,9 @@ struct NormGradLaunch {
   hipStream_t s;
   template <int TPR, int NV, int BLOCK>
   hipError_t run() const {
-    constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;   // two vectors in five: 400000 x 128 fp32 100 -> 106 us
+    // Wavefronts a SIMD; with two vectors in five 400000 x 128 fp32 takes 106 us, not 100.  Blocks of 512 and 1024 threads bring
+    // two and four at a time, so of five they get four.
+    constexpr int V = 16 / sizeof(T), W = NV == 1 ? 5 : 4;
     constexpr bool AHEAD = !(V == 4 && NV == 4);   // fp32 does not shrink while it waits: no registers left
     const int64_t blocks = (a.rows + BLOCK / TPR - 1) / (BLOCK / TPR);
     int64_t most = (int64_t)cu_count * (W * 256 / BLOCK);

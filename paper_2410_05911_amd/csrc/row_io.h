@@ -60,9 +60,9 @@ template <class T, int V, bool NT = false>
 __device__ __forceinline__ void load_raw(const T *p, Raw<T, V> &r) {
   copy_in<(int)sizeof(r.w), NT>(p, r.w);
 }
-// Waits for the loads issued so far.  Behind a branch that few threads take it keeps the wait inside: otherwise the
+// Waits for the loads issued so far, and with them the stores, which the same counter counts.  Behind a branch that few threads take it keeps the wait inside: otherwise the
 // registers that it loaded may still be written where the paths meet, and every wavefront waits there, also for what it
-// wanted to load ahead (gradient of 100000 x 200 bf16 35 -> 26 us).  0x0f70: no memory load left, the other counters as they are.
+// wanted to load ahead (gradient of 100000 x 200 bf16 35 -> 26 us).  0x0f70: no load or store to memory left, the other counters as they are.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // `bytes` < 4 W bytes from p into the W words, the rest 0, as loads of 16, 8, 4 and 2 bytes at most once each.  (Value by
