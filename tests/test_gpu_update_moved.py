@@ -18,8 +18,8 @@ def P():
 def test_adam_updates_parameters_where_they_are(P, how):
     """Two updates with the memory exchanged between them, against the same updates without: bit for bit, and what the
     parameter's first memory holds now stays as it is."""
-    p0 = [torch.randn(1000, device="cuda"), torch.randn(7, 11, device="cuda")]
-    g = [torch.randn_like(t) for t in p0]
+    gen = torch.Generator("cuda").manual_seed(1)
+    p0, g = ([torch.randn(s, device="cuda", generator=gen) for s in ((1000,), (7, 11))] for _ in range(2))
     twin_p, p = [t.clone() for t in p0], [t.clone() for t in p0]
     twin_c, c = ([torch.zeros_like(t, dtype=torch.bfloat16) for t in p0] for _ in range(2))
     twin = P.Adam(twin_p, lr=1e-2, max_norm=1.0, copies=twin_c)

@@ -27,7 +27,7 @@ def test_second_moment_of_large_gradients(P, type, size, beta2):
     if (1 - beta2) * size * size * 1.1 > 3.4e38:
         size = math.sqrt(3e38 / (1 - beta2) / 1.2)
     g = [(torch.linspace(0.25, 1.0, 5003, device="cuda") * size * (1 - 2 * (torch.arange(5003, device="cuda") % 2))).to(TYPES[type])]
-    p, m, v = ([t] for t in (torch.randn(5003, device="cuda"), torch.zeros(5003, device="cuda"), torch.zeros(5003, device="cuda")))
+    p, m, v = ([t] for t in (torch.randn(5003, device="cuda", generator=torch.Generator("cuda").manual_seed(1)), torch.zeros(5003, device="cuda"), torch.zeros(5003, device="cuda")))
     before = [t[0].clone() for t in (p, m, v)]
     opt = P.Adam(p, 1e-3, (0.9, beta2), m=m, v=v)
     opt.step(g)
