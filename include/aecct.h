@@ -543,6 +543,91 @@ aecct_status aecct_train_update(const aecct_trainer *tr, const aecct_train_grads
                                 const aecct_train_grads *v, const aecct_train_grads *grads, const aecct_adam_options *opt,
                                 int64_t *step, float *norm, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators around the attention and feed-forward blocks: linear maps with an epilogue, dropout and cross
+ * attention, with their gradients.  Like the operators above they take no model, enqueue on stream, neither allocate
+ * nor synchronise, take outputs that overlap nothing else of the call but where said, and workspaces that hold
+ * nothing between calls; the same call gives the same bits.
+ * ---------------------------------------------------------------------------------------- */
+
+typedef enum aecct_activation {
+  AECCT_ACT_NONE = 0,
+  AECCT_ACT_RELU = 1,
+  AECCT_ACT_GELU = 2,   /* z Phi(z), Phi the normal distribution */
+  AECCT_ACT_SILU = 3    /* z / (1 + e^-z) */
+} aecct_activation;
+
+/*
+ * Linear map with an epilogue: z = x W + bias, y = act(z) + res.
+ * On codes (Eq. 3): z = (x W) alpha / Q scale + bias, with the codes and alphas of aecct_rms_norm (one alpha a row) and
+ * weights in 8 bits with one scale an output: int8 sums are exact, e4m3 sums fp32.
+ * Sums are taken in fp32; z and y are each rounded once (y is taken of the unrounded z).
+ */
+typedef struct aecct_linear_map_args {
+  int64_t rows, in, out;       /* rows >= 0 (0: nothing is written), 1 <= in, out <= 2^20 (int8: in <= 131071) */
+  int32_t type;                /* aecct_dtype of x and w; not read for codes */
+  int32_t code_type;           /* aecct_code of x and w, or NONE */
+  int32_t y_type;              /* aecct_dtype of res, z and y; without codes: the same as type */
+  int32_t act;                 /* aecct_activation */
+  int32_t w_turned;            /* 0: w [in][out]; 1: w [out][in] */
+  const void *x;   int64_t ldx;      /* [rows][in] */
+  const void *w;   int64_t ldw;      /* its rows ldw values apart */
+  const float *alpha;                /* fp32 [rows], with codes; else NULL */
+  const float *scale;                /* fp32 [out], with codes; else NULL */
+  const float *bias;                 /* fp32 [out], or NULL */
+  const void *res; int64_t ldres;    /* [rows][out], or NULL */
+  void *z;         int64_t ldz;      /* [rows][out] out, or NULL */
+  void *y;         int64_t ldy;      /* [rows][out] out; may be res itself */
+} aecct_linear_map_args;
+/* Inputs may be rows of any stride >= 0 (w: its width at least), outputs of strides >= out.  The workspace may be NULL
+ * where its size is 0 (host call; reads sizes and types only).  Errors: INVALID_ARG, UNSUPPORTED (sizes beyond the above,
+ * more than 2^22 tiles of 64 x 64 outputs), WORKSPACE_TOO_SMALL, DEVICE. */
+aecct_status aecct_linear_map_workspace_size(const aecct_linear_map_args *a, size_t *bytes);
+aecct_status aecct_linear_map(const aecct_linear_map_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient: dz = dy act'(z),  dx = dz W^T,  dw = x^T dz,  dbias = sum of dz over the rows.  (res has the gradient dy.)
+ * z as aecct_linear_map wrote it; with 16-bit types dz is rounded to the type before the products (not for dbias), as the
+ * matrix instructions take it.  relu'(0) = 0.
+ */
+typedef struct aecct_linear_map_grad_args {
+  int64_t rows, in, out;
+  int32_t type;                /* aecct_dtype of x, w, dy, z and dx */
+  int32_t act;
+  int32_t w_turned;
+  int32_t dw_type;             /* AECCT_F32, or the same as type */
+  const void *x;  int64_t ldx;       /* [rows][in]; read for dw only */
+  const void *w;  int64_t ldw;       /* read for dx only */
+  const void *dy; int64_t lddy;      /* [rows][out] */
+  const void *z;  int64_t ldz;       /* [rows][out]; NULL with act NONE */
+  void *dx;       int64_t lddx;      /* [rows][in] out, or NULL */
+  void *dw;       int64_t lddw;      /* [in][out] out (zeros for rows = 0), or NULL */
+  float *dbias;                      /* fp32 [out] out (zeros for rows = 0), or NULL */
+} aecct_linear_map_grad_args;
+/* The workspace's size goes by which outputs are asked for.  Strides and errors as above. */
+aecct_status aecct_linear_map_grad_workspace_size(const aecct_linear_map_grad_args *a, size_t *bytes);
+aecct_status aecct_linear_map_grad(const aecct_linear_map_grad_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Dropout without a stored mask: y = x / (1 - p) + res where a value is kept, res (or 0) where it is dropped.  Value i of
+ * the tensor (i = row d + column) is dropped where word i % 4 of the block that Philox4x32 with 7 rounds makes of the
+ * counter (i / 4, offset) and the key seed, both of two words, low word first, is below p 2^32 (rounded down).  The
+ * gradient is the same call on dy with the same p, seed and offset, without res.
+ */
+typedef struct aecct_dropout_args {
+  int64_t rows, d;             /* rows >= 0, d >= 1, at most 2^35 values */
+  int32_t type;                /* aecct_dtype of x, res and y */
+  double p;                    /* 0 <= p < 1 */
+  uint64_t seed, offset;
+  const int64_t *offset_device;      /* device [1], or NULL: read in place of offset, so that a captured graph's replays
+                                        can differ */
+  const void *x;   int64_t ldx;
+  const void *res; int64_t ldres;    /* or NULL: 0 */
+  void *y;         int64_t ldy;      /* may be x or res itself */
+} aecct_dropout_args;
+/* Strides as above.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
+aecct_status aecct_dropout(const aecct_dropout_args *a, void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *aecct_status_string(aecct_status status);
 

@@ -22,6 +22,7 @@ LAYERED_ATTN_AUTO, LAYERED_ATTN_UNFUSED, LAYERED_ATTN_LDS_F32, LAYERED_ATTN_LDS_
 ACT_SCALE_TOKEN, ACT_SCALE_WORD = 0, 1
 F32, BF16, F16 = range(3)
 CODE_NONE, CODE_I8, CODE_E4M3 = range(3)
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 LIN_Q, LIN_K, LIN_V, LIN_O, LIN_FF1, LIN_FF2 = range(6)
 
 _vp = C.c_void_p
@@ -81,6 +82,26 @@ class RmsNormGradArgs(C.Structure):
     _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("type", C.c_int32), ("gain_type", C.c_int32), ("eps", C.c_float),
                 ("h", _vp), ("ldh", C.c_int64), ("dy", _vp), ("lddy", C.c_int64), ("dres", _vp), ("lddres", C.c_int64),
                 ("gain", _vp), ("dh", _vp), ("lddh", C.c_int64), ("dgain", _vp)]
+
+
+class LinearMapArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("code_type", C.c_int32),
+                ("y_type", C.c_int32), ("act", C.c_int32), ("w_turned", C.c_int32), ("x", _vp), ("ldx", C.c_int64), ("w", _vp),
+                ("ldw", C.c_int64), ("alpha", _vp), ("scale", _vp), ("bias", _vp), ("res", _vp), ("ldres", C.c_int64),
+                ("z", _vp), ("ldz", C.c_int64), ("y", _vp), ("ldy", C.c_int64)]
+
+
+class LinearMapGradArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
+                ("w_turned", C.c_int32), ("dw_type", C.c_int32), ("x", _vp), ("ldx", C.c_int64), ("w", _vp), ("ldw", C.c_int64),
+                ("dy", _vp), ("lddy", C.c_int64), ("z", _vp), ("ldz", C.c_int64), ("dx", _vp), ("lddx", C.c_int64),
+                ("dw", _vp), ("lddw", C.c_int64), ("dbias", _vp)]
+
+
+class DropoutArgs(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int64), ("type", C.c_int32), ("p", C.c_double), ("seed", C.c_uint64),
+                ("offset", C.c_uint64), ("offset_device", _vp), ("x", _vp), ("ldx", C.c_int64), ("res", _vp),
+                ("ldres", C.c_int64), ("y", _vp), ("ldy", C.c_int64)]
 
 
 class Tensor(C.Structure):
@@ -166,6 +187,13 @@ def lib():
         L.aecct_rms_norm_grad_workspace_size.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
         L.aecct_rms_norm_grad.restype = C.c_int
         L.aecct_rms_norm_grad.argtypes = [C.POINTER(RmsNormGradArgs), _vp, C.c_size_t, _vp]
+        for f, a in (("aecct_linear_map", LinearMapArgs), ("aecct_linear_map_grad", LinearMapGradArgs)):
+            getattr(L, f).restype = C.c_int
+            getattr(L, f).argtypes = [C.POINTER(a), _vp, C.c_size_t, _vp]
+            getattr(L, f + "_workspace_size").restype = C.c_int
+            getattr(L, f + "_workspace_size").argtypes = [C.POINTER(a), C.POINTER(C.c_size_t)]
+        L.aecct_dropout.restype = C.c_int
+        L.aecct_dropout.argtypes = [C.POINTER(DropoutArgs), _vp]
         _tp = C.POINTER(Tensor)
         L.aecct_update_workspace_size.restype = C.c_int
         L.aecct_update_workspace_size.argtypes = [C.c_int32, C.POINTER(C.c_size_t)]
@@ -443,6 +471,172 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
     a = RmsNormGradArgs(rows, d, _dtype_code(h), gain_type, eps, ph, ldh, pdy, lddy, pres, lddres, pgain, pdh, lddh, pdgain)
     _check(lib().aecct_rms_norm_grad(C.byref(a), pws, need, _current_stream(index)), "aecct_rms_norm_grad")
     return dh, dgain
+
+
+def _with_workspace(call: str, args, device: int):
+    """Sizes the call's workspace, takes it from torch (so on its current stream), and makes the call."""
+    import torch
+    size = C.c_size_t()
+    _check(getattr(lib(), call + "_workspace_size")(C.byref(args), C.byref(size)), call + "_workspace_size")
+    ws = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+    _check(getattr(lib(), call)(C.byref(args), ws.data_ptr() if ws is not None else None, size.value, _current_stream(device)),
+           call)
+
+
+def _act_code(act) -> int:
+    code = ACTIVATIONS.get(act or "none")
+    if code is None:
+        raise ValueError(f"unknown activation {act!r}: " + ", ".join(ACTIVATIONS))
+    return code
+
+
+def _vector_of(t, n: int, index: int, what):
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous() or t.get_device() != index or str(t.dtype) != "torch.float32":
+        raise ValueError(f"{what} must be {n} contiguous float32 values on cuda:{index}")
+    return t.data_ptr()
+
+
+def _map_of(w, dtype, index: int):
+    """(address, stride, turned) of the weights [in, out] of a map, in rows or (turned) in columns."""
+    if w.dim() != 2 or w.dtype != dtype or w.get_device() != index or w.numel() == 0:
+        raise ValueError(f"w must be {dtype} [in, out] on cuda:{index}")
+    (inputs, outputs), (a, b) = w.shape, w.stride()
+    if b == 1 or outputs == 1:
+        return w.data_ptr(), a if inputs > 1 else outputs, 0
+    if a == 1 or inputs == 1:
+        return w.data_ptr(), b, 1
+    raise ValueError("w must have contiguous rows, or contiguous columns (a transposed view)")
+
+
+def linear(x, w, bias=None, res=None, act="none", *, alpha=None, scale=None, y=None, z=None, y_type=None, with_z: bool = False,
+           stream=None):
+    """Linear map with an epilogue: z = x w + bias, y = act(z) + res, in one pass.
+
+    x: CUDA tensor [..., in], w [in, out] of the same type (float32, bfloat16, float16), contiguous or of two dimensions with
+    contiguous rows; w may also be a transposed view.  bias [out] float32; res [..., out]; act: "none", "relu", "gelu" or
+    "silu".  On codes (Eq. 3), x and w are int8 or float8_e4m3fn, x and alpha as rms_norm returned them (one alpha a row),
+    scale [out] float32 is the weights', and y_type (float32 without it) is the type of res, z and y.
+    y, z: outputs to write to, else new tensors; y may be res itself.  Autograd does not record the call: linear_grad is
+    its gradient.  Returns (y, z), z (what the activation was taken of) None without with_z."""
+    import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return linear(x, w, bias, res, act, alpha=alpha, scale=scale, y=y, z=z, y_type=y_type, with_z=with_z)
+    if x.dim() < 1 or w.dim() != 2 or x.shape[-1] != w.shape[0]:
+        raise ValueError("x must be [..., in] and w [in, out]")
+    index = x.get_device()
+    _on_current_gpu(index)
+    inputs, outputs = w.shape
+    shape, out_shape = x.shape, x.shape[:-1] + (outputs,)
+    rows = x.numel() // inputs if inputs else 0
+    code = CODE_I8 if x.dtype == torch.int8 else CODE_E4M3 if x.dtype == torch.float8_e4m3fn else CODE_NONE
+    if code == CODE_NONE:
+        type = _dtype_code(x)
+        if alpha is not None or scale is not None:
+            raise ValueError("alpha and scale go with codes")
+        if y_type is not None and y_type != x.dtype:
+            raise ValueError("without codes y is of x's type")
+        y_type = x.dtype
+    else:
+        type = F32
+        if alpha is None or scale is None:
+            raise ValueError("codes need alpha and scale")
+        y_type = torch.float32 if y_type is None else y_type
+    pw, ldw, turned = _map_of(w, x.dtype, index)
+    px, ldx = _rows_of(x, shape, x.dtype, index, "x")
+    pres, ldres = _rows_of(res, out_shape, y_type, index, "res")
+    if y is None:
+        y = torch.empty(out_shape, dtype=y_type, device=x.device)
+    if z is None and with_z:
+        z = torch.empty(out_shape, dtype=y_type, device=x.device)
+    py, ldy = _rows_of(y, out_shape, y_type, index, "y")
+    pz, ldz = _rows_of(z, out_shape, y_type, index, "z")
+    a = LinearMapArgs(rows, inputs, outputs, type, code, _dtype_code(y), _act_code(act), turned, px, ldx, pw, ldw,
+                      _vector_of(alpha, rows, index, "alpha"), _vector_of(scale, outputs, index, "scale"),
+                      _vector_of(bias, outputs, index, "bias"), pres, ldres, pz, ldz, py, ldy)
+    _with_workspace("aecct_linear_map", a, index)
+    return y, z
+
+
+def linear_grad(x, w, dy, z=None, act="none", *, dx=None, dw=None, dbias=None, dw_type=None, with_dx: bool = True,
+                with_dw: bool = True, with_dbias: bool = True, stream=None):
+    """Gradient of linear: x and w as it read them, z as it returned it (with an activation), dy the gradient of y (which
+    is res's too).  Returns (dx, dw, dbias): dw [in, out] contiguous, of w's type or float32 (dw_type); dbias float32;
+    None for what is not asked for.  dx, dw, dbias: outputs to write to, else new tensors."""
+    import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return linear_grad(x, w, dy, z, act, dx=dx, dw=dw, dbias=dbias, dw_type=dw_type, with_dx=with_dx, with_dw=with_dw,
+                               with_dbias=with_dbias)
+    if x.dim() < 1 or w.dim() != 2 or x.shape[-1] != w.shape[0]:
+        raise ValueError("x must be [..., in] and w [in, out]")
+    index = x.get_device()
+    _on_current_gpu(index)
+    inputs, outputs = w.shape
+    shape, out_shape, dtype = x.shape, x.shape[:-1] + (outputs,), x.dtype
+    rows = x.numel() // inputs if inputs else 0
+    code = _act_code(act)
+    if (z is not None) != (code != 0):
+        raise ValueError("z is what the activation was taken of: needed with one, and not without")
+    type = _dtype_code(x)
+    pw, ldw, turned = _map_of(w, dtype, index)
+    px, ldx = _rows_of(x, shape, dtype, index, "x")
+    pdy, lddy = _rows_of(dy, out_shape, dtype, index, "dy")
+    pz, ldz = _rows_of(z, out_shape, dtype, index, "z")
+    if dx is None and with_dx:
+        dx = torch.empty(shape, dtype=dtype, device=x.device)
+    if dw is None and with_dw:
+        dw = torch.empty((inputs, outputs), dtype=dw_type or dtype, device=x.device)
+    if dbias is None and with_dbias:
+        dbias = torch.empty(outputs, dtype=torch.float32, device=x.device)
+    if dx is None and dw is None and dbias is None:
+        raise ValueError("no gradient is asked for")
+    pdx, lddx = _rows_of(dx, shape, dtype, index, "dx")
+    dw_dtype = dtype if dw is None else dw.dtype
+    if dw_dtype not in (dtype, torch.float32) or (dw_type is not None and dw is not None and dw.dtype != dw_type):
+        raise ValueError(f"dw must be {dw_type or dtype}" + ("" if dw_type else " or float32"))
+    pdw, lddw = _rows_of(dw, w.shape, dw_dtype, index, "dw")
+    a = LinearMapGradArgs(rows, inputs, outputs, type, code, turned, F32 if dw is None else _dtype_code(dw), px, ldx, pw, ldw,
+                          pdy, lddy, pz, ldz, pdx, lddx, pdw, lddw, _vector_of(dbias, outputs, index, "dbias"))
+    _with_workspace("aecct_linear_map_grad", a, index)
+    return dx, dw, dbias
+
+
+def dropout(x, p: float, seed: int, offset=0, res=None, *, y=None, stream=None):
+    """Dropout whose mask is never stored: y = x / (1 - p) + res where a value is kept, res (or 0) where it is dropped.
+
+    x, res: CUDA tensors [..., d] of one type (float32, bfloat16, float16), contiguous or of two dimensions with contiguous
+    rows.  Which values are kept follows from seed and offset (whole numbers of 64 bits: say the run's, and the step's and
+    layer's) and the value's place in the tensor alone; offset may be one int64 value on the GPU, which captured graphs
+    read at each replay.  y: output to write to (may be x or res itself), else a new tensor.  Autograd does not record the
+    call: its gradient is dropout(dy, p, seed, offset)."""
+    import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return dropout(x, p, seed, offset, res, y=y)
+    shape = x.shape
+    if not shape or shape[-1] < 1:
+        raise ValueError("x must be [..., d] with d >= 1")
+    d, dtype = shape[-1], x.dtype
+    index = x.get_device()
+    _on_current_gpu(index)
+    offset_device = None
+    if hasattr(offset, "data_ptr"):
+        if offset.dtype != torch.int64 or offset.numel() != 1 or offset.get_device() != index:
+            raise ValueError(f"offset must be a number or one int64 value on cuda:{index}")
+        offset_device, offset = offset.data_ptr(), 0
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be whole numbers of 64 bits")
+    px, ldx = _rows_of(x, shape, dtype, index, "x")
+    pres, ldres = _rows_of(res, shape, dtype, index, "res")
+    if y is None:
+        y = torch.empty(shape, dtype=dtype, device=x.device)
+    py, ldy = _rows_of(y, shape, dtype, index, "y")
+    a = DropoutArgs(x.numel() // d, d, _dtype_code(x), p, seed, offset, offset_device, px, ldx, pres, ldres, py, ldy)
+    _check(lib().aecct_dropout(C.byref(a), _current_stream(index)), "aecct_dropout")
+    return y
 
 
 class TensorList:

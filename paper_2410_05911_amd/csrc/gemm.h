@@ -1,0 +1,283 @@
+// The product of two factors, a block of BM x BN outputs a workgroup: tiles of 128 bytes of k of both factors go through LDS
+// twice over (one is read by the matrix instructions while the next one is on its way), each wavefront sums 32 x 32
+// blocks of the outputs in its registers.
+//
+// The first factor of a matrix instruction is b and the second a: a lane then holds one row m of the output and groups
+// of four consecutive columns n, and reads and writes the epilogue's tensors four values at a time.
+#pragma once
+
+#include <cmath>
+
+#include "../../include/aecct.h"
+#include "linear.h"
+#include "mfma.h"
+
+namespace aecct {
+
+// ---- activations, in fp32
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
+  if (act == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  if (act == kActSilu) return z / (1.0f + expf(-z));
+  return z;
+}
+
+// ---- four values of a stored type, at any address aligned to one
+__device__ __forceinline__ void load4(int type, const void *p, int64_t at, int n, float (&f)[4]) {
+  if (type == 0) load_part<float, 4>((const float *)p + at, n, f);
+  else if (type == 1) load_part<bf16_t, 4>((const bf16_t *)p + at, n, f);
+  else load_part<f16_t, 4>((const f16_t *)p + at, n, f);
+}
+__device__ __forceinline__ void store4(int type, void *p, int64_t at, int n, const float (&f)[4]) {
+  if (type == 0) store_part<float, 4>((float *)p + at, n, f);
+  else if (type == 1) store_part<bf16_t, 4>((bf16_t *)p + at, n, f);
+  else store_part<f16_t, 4>((f16_t *)p + at, n, f);
+}
+
+// The epilogue of values (m, n0 .. n0 + count), count <= 4.
+__device__ __forceinline__ void finish4(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[4]) {
+  if (e.alpha) {
+    const float r = e.alpha[m] * e.per_q;
+    float s[4];
+    load_part<float, 4>(e.scale + n0, count, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = v[i] * r * s[i];
+  }
+  if (e.bias) {
+    float b[4];
+    load_part<float, 4>(e.bias + n0, count, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += b[i];
+  }
+  if (e.z) store4(e.type, e.z, m * e.ldz + n0, count, v);
+  if (e.act != kActNone) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = activate(v[i], e.act);
+  }
+  if (e.res) {
+    float r[4];
+    load4(e.type, e.res, m * e.ldres + n0, count, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += r[i];
+  }
+  store4(e.type, e.y, m * e.ldy + n0, count, v);
+}
+
+// ---- staging: 16-byte pieces of a factor's tile, slot by slot
+// The first `n` values at p, the others 0.
+template <class T>
+__device__ __forceinline__ u32x4 some_values(const char *p, int n) {
+  unsigned __int128 v = 0;
+#pragma unroll 1
+  for (int i = n - 1; i >= 0; --i) {
+    if constexpr (sizeof(T) == 4) v = v << 32 | *(const uint32_t *)(p + 4 * i);
+    if constexpr (sizeof(T) == 2) v = v << 16 | *(const uint16_t *)(p + 2 * i);
+    if constexpr (sizeof(T) == 1) v = v << 8 | *(const uint8_t *)(p + i);
+  }
+  return __builtin_bit_cast(u32x4, v);
+}
+__device__ __forceinline__ u32x4 any16(const char *p) {   // at any address
+  u32x4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+// A tile of ROWS rows from row0 on: where slot `slot` of its LDS lies in the factor.
+template <class T, bool ACROSS, int ROWS>
+struct Tile {
+  static constexpr int E = 16 / (int)sizeof(T), KT = 128 / (int)sizeof(T), PITCH = ROWS * (int)sizeof(T);
+  static constexpr int SLOTS = ROWS * 8;
+  // The row (first of them) and the k (first of them) that the slot holds, relative to the tile.
+  static __device__ __forceinline__ void place(int slot, int &row, int &k) {
+    if constexpr (ACROSS) {
+      constexpr int PER = PITCH / 16;
+      k = slot / PER;
+      row = ((slot % PER) ^ (line_swap<T, PITCH>(k) >> 4)) * E;
+    } else {
+      row = slot >> 3;
+      k = ((slot & 7) ^ (row & 7)) * E;
+    }
+  }
+  // The slot's values: zeros past `k_end`, anything for rows past `rows`.  k_all: the factor's k, where its memory ends.
+  static __device__ __forceinline__ u32x4 fetch(const char *p, int64_t ld, int64_t rows, int64_t k_all, int64_t row0, int64_t k0,
+                                                int64_t k_end, int slot) {
+    int r, c;
+    place(slot, r, c);
+    const int64_t k = k0 + c;
+    if constexpr (ACROSS) {
+      const int64_t row = row0 + r;
+      if (k >= k_end || row >= rows) return u32x4{0, 0, 0, 0};
+      const int64_t at = k * ld + row, left = (k_all - 1) * ld + rows - at;   // values to the end of the memory
+      return left >= E ? any16(p + at * (int64_t)sizeof(T)) : some_values<T>(p + at * (int64_t)sizeof(T), (int)left);
+    } else {
+      if (k >= k_end) return u32x4{0, 0, 0, 0};
+      const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
+      const char *const q = p + (row * ld + k) * (int64_t)sizeof(T);
+      return k + E <= k_end ? any16(q) : some_values<T>(q, (int)(k_end - k));
+    }
+  }
+  static __device__ __forceinline__ u32x4 frag(const char *tile, int row0, int chunk) {
+    if constexpr (ACROSS) return frag_n<T, PITCH>(tile, row0, chunk);
+    else return frag_k<T>(tile, row0 + (threadIdx.x & 31), chunk);
+  }
+};
+
+// Tiles in an order that keeps the blocks of one XCD (every eighth block) on neighbouring tiles: bands of 8 rows of tiles,
+// column by column.
+__device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, int64_t &im, int64_t &in) {
+  const int64_t all = tm * tn, share = all / 8;
+  const int64_t at = block < share * 8 ? (block % 8) * share + block / 8 : block;
+  const int64_t band = at / (8 * tn), first = band * 8, height = tm - first < 8 ? tm - first : 8, rest = at - band * 8 * tn;
+  im = first + rest % height;
+  in = rest / height;
+}
+
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
+  typedef Tile<T, AA, BM> TA;
+  typedef Tile<T, BA, BN> TB;
+  constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT;
+  constexpr int CA = TA::SLOTS / NT, CB = TB::SLOTS / NT, BYTES = (BM + BN) * 128;
+  static_assert(TA::SLOTS % NT == 0 && TB::SLOTS % NT == 0, "whole slots");
+  __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
+  const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
+  const int split = (int)(blockIdx.x / (tm * tn));
+  int64_t im, in;
+  tile_of(blockIdx.x % (tm * tn), tm, tn, im, in);
+  const int64_t m0 = im * BM, n0 = in * BN;
+  // Whole tiles of k to each split; only the last one has a ragged end.
+  const int64_t kt = (g.k + KT - 1) / KT, k0 = kt * split / g.splits * KT, k1 = min(g.k, kt * (split + 1) / g.splits * KT);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
+  const char *const pa = (const char *)g.a.p, *const pb = (const char *)g.b.p;
+
+  typename Product<T>::Acc acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+
+  u32x4 ra[CA], rb[CB];
+  if (k0 < k1) {
+#pragma unroll
+    for (int i = 0; i < CA; ++i) ra[i] = TA::fetch(pa, g.a.ld, g.m, g.k, m0, k0, k1, threadIdx.x + i * NT);
+#pragma unroll
+    for (int i = 0; i < CB; ++i) rb[i] = TB::fetch(pb, g.b.ld, g.n, g.k, n0, k0, k1, threadIdx.x + i * NT);
+  }
+  int buf = 0;
+  for (int64_t k = k0; k < k1; k += KT, buf ^= 1) {
+    char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
+#pragma unroll
+    for (int i = 0; i < CA; ++i) *(u32x4 *)(la + (threadIdx.x + i * NT) * 16) = ra[i];
+#pragma unroll
+    for (int i = 0; i < CB; ++i) *(u32x4 *)(lb + (threadIdx.x + i * NT) * 16) = rb[i];
+    __syncthreads();   // also: no wavefront reads the other buffer any more when the next round writes it
+    if (k + KT < k1) {
+#pragma unroll
+      for (int i = 0; i < CA; ++i) ra[i] = TA::fetch(pa, g.a.ld, g.m, g.k, m0, k + KT, k1, threadIdx.x + i * NT);
+#pragma unroll
+      for (int i = 0; i < CB; ++i) rb[i] = TB::fetch(pb, g.b.ld, g.n, g.k, n0, k + KT, k1, threadIdx.x + i * NT);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; s += 2) {
+      u32x4 a0[FM], a1[FM];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        a0[i] = TA::frag(la, wm + i * 32, 2 * s + h);
+        a1[i] = TA::frag(la, wm + i * 32, 2 * s + 2 + h);
+      }
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        const u32x4 b0 = TB::frag(lb, wn + j * 32, 2 * s + h), b1 = TB::frag(lb, wn + j * 32, 2 * s + 2 + h);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) step2<T>(acc[i][j], b0, b1, a0[i], a1[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int64_t m = m0 + wm + i * 32 + (lane & 31);
+    if (m >= g.m) continue;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t n = n0 + wn + j * 32 + 8 * q + 4 * h;
+        if (n >= g.n) continue;
+        const int count = g.n - n < 4 ? (int)(g.n - n) : 4;
+        if (g.part) {
+          // int32 sums travel as their bits
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const auto sum = acc[i][j][4 * q + r];
+            v[r] = __builtin_bit_cast(float, sum);
+          }
+          store_part<float, 4>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
+        } else {
+          float v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][4 * q + r];
+          finish4(g.e, m, n, count, v);
+        }
+      }
+    }
+  }
+}
+
+// The splits' sums of four outputs a thread, in the order of the splits, and the epilogue.
+template <bool INT>
+__global__ __launch_bounds__(256) void k_join(Gemm g) {
+  const int64_t per = (g.n + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= g.m * per) return;
+  const int64_t m = at / per, n = at % per * 4;
+  const int count = g.n - n < 4 ? (int)(g.n - n) : 4;
+  float v[4] = {0, 0, 0, 0};
+  int32_t w[4] = {0, 0, 0, 0};
+  for (int s = 0; s < g.splits; ++s) {
+    float p[4];
+    load_part<float, 4>((const float *)g.part + ((int64_t)s * g.m + m) * g.n + n, count, p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (INT) w[i] += __builtin_bit_cast(int32_t, p[i]);
+      else v[i] += p[i];
+    }
+  }
+  if constexpr (INT) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)w[i];
+  }
+  finish4(g.e, m, n, count, v);
+}
+
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+hipError_t launch_tile(const Gemm &g, hipStream_t s) {
+  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
+  k_gemm<T, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess || !g.part) return err;
+  const int64_t join = (g.m * ((g.n + 3) / 4) + 255) / 256;
+  k_join<__is_same(T, int8_t)><<<dim3((unsigned)join), dim3(256), 0, s>>>(g);
+  return hipGetLastError();
+}
+
+// The tiles that plan_gemm chooses from.
+constexpr int kTileSide[2][2] = {{64, 64}, {128, 128}};
+template <class T, bool AA, bool BA>
+hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {
+  if (p.tile == 0) return launch_tile<T, AA, BA, 64, 64, 2, 2>(g, s);
+  return launch_tile<T, AA, BA, 128, 128, 2, 2>(g, s);
+}
+// Codes are never a gradient's factor, so a of theirs lies along k.
+template <class T>
+hipError_t launch_type(const Gemm &g, const GemmPlan &p, hipStream_t s) {
+  if constexpr (sizeof(T) > 1) {
+    if (g.a.across && g.b.across) return launch_layout<T, true, true>(g, p, s);
+  }
+  if (g.a.across) return hipErrorInvalidValue;
+  return g.b.across ? launch_layout<T, false, true>(g, p, s) : launch_layout<T, false, false>(g, p, s);
+}
+
+}  // namespace aecct

@@ -1,0 +1,117 @@
+// Linear maps: which tile and how many splits a product takes, and what its gradient needs besides products.
+#include "gemm.h"
+
+namespace aecct {
+
+GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b) {
+  GemmPlan p{1, 1, 0};
+  auto tiles = [&](int t) { return (m + kTileSide[t][0] - 1) / kTileSide[t][0] * ((n + kTileSide[t][1] - 1) / kTileSide[t][1]); };
+  if (tiles(1) < 192) p.tile = 0;
+  const int64_t size = type == AECCT_F32 ? 4 : type < kCodeType ? 2 : 1, t = tiles(p.tile), kt = (k * size + 127) / 128;
+  if (t < 256) {
+    int64_t s = (512 + t - 1) / t;
+    if (s > kt / 4) s = kt / 4;
+    if (s > 64) s = 64;
+    p.splits = s > 1 ? (int)s : 1;
+  }
+  if (p.splits > 1) p.part_bytes = (size_t)(p.splits * m * n * 4);
+  return p;
+}
+
+hipError_t launch_gemm(int type, const Gemm &g, const GemmPlan &plan, hipStream_t s) {
+  if (g.m == 0 || g.n == 0) return hipSuccess;
+  switch (type) {
+    case AECCT_F32: return launch_gemm_f32(g, plan, s);
+    case AECCT_BF16: return launch_gemm_bf16(g, plan, s);
+    case AECCT_F16: return launch_gemm_f16(g, plan, s);
+    case kCodeType + AECCT_CODE_I8: return launch_gemm_i8(g, plan, s);
+    case kCodeType + AECCT_CODE_E4M3: return launch_gemm_e4m3(g, plan, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+namespace {
+
+// act'(z).  Where a factor is 0 the other may be infinite: such a product's limit is 0.
+__device__ __forceinline__ float slope(float z, int act) {
+  if (act == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+  if (act == kActGelu) {
+    const float density = expf(-0.5f * z * z) * 0.39894228040143268f;
+    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + (density == 0.0f ? 0.0f : z * density);
+  }
+  const float p = 1.0f / (1.0f + expf(-z)), q = 1.0f / (1.0f + expf(z));   // q = 1 - p
+  if (p == 0.0f || q == 0.0f) return p;
+  return p * (1.0f + z * q);
+}
+
+constexpr int kSlopeColumns = 128;   // 16 threads of 8 values a row, 16 rows at once
+
+template <class T>
+__global__ __launch_bounds__(256) void k_slope(Slope a) {
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * kSlopeColumns + c * 8;
+  const int count = a.n - n0 < 8 ? (int)(a.n - n0) : 8;
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (count > 0) {
+    for (int64_t row = (int64_t)blockIdx.y * 16 + r; row < a.rows; row += (int64_t)gridDim.y * 16) {
+      float d[8];
+      load_part<T, 8>((const T *)a.dy + row * a.lddy + n0, count, d);
+      if (a.z) {
+        float z[8];
+        load_part<T, 8>((const T *)a.z + row * a.ldz + n0, count, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] *= slope(z[i], a.act);
+        if (a.dz) store_part<T, 8>((T *)a.dz + row * a.lddz + n0, count, d);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += d[i];
+    }
+  }
+  if (!a.part) return;
+  __shared__ float s[16][kSlopeColumns + 4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[r][c * 8 + i] = sum[i];
+  __syncthreads();
+  if (threadIdx.x < kSlopeColumns) {
+    const int64_t n = (int64_t)blockIdx.x * kSlopeColumns + threadIdx.x;
+    float t = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += s[i][threadIdx.x];
+    if (n < a.n) a.part[(int64_t)blockIdx.y * a.n + n] = t;
+  }
+}
+
+__global__ __launch_bounds__(256) void k_column_sum(const float *part, int64_t blocks, int64_t n, float *out) {
+  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (c >= n) return;
+  float t = 0;
+  for (int64_t b = 0; b < blocks; ++b) t += part[b * n + c];
+  out[c] = t;
+}
+
+}  // namespace
+
+int64_t slope_blocks(int64_t rows, int64_t n) {
+  const int64_t across = (n + kSlopeColumns - 1) / kSlopeColumns;
+  int64_t b = (1024 + across - 1) / across;
+  const int64_t most = (rows + 63) / 64;
+  if (b > most) b = most;
+  return b < 1 ? 1 : b;
+}
+
+hipError_t launch_slope(int type, const Slope &a, hipStream_t s) {
+  const int64_t blocks = slope_blocks(a.rows, a.n);
+  const dim3 grid((unsigned)((a.n + kSlopeColumns - 1) / kSlopeColumns), (unsigned)blocks);
+  switch (type) {
+    case AECCT_F32: k_slope<float><<<grid, 256, 0, s>>>(a); break;
+    case AECCT_BF16: k_slope<bf16_t><<<grid, 256, 0, s>>>(a); break;
+    case AECCT_F16: k_slope<f16_t><<<grid, 256, 0, s>>>(a); break;
+    default: return hipErrorInvalidValue;
+  }
+  hipError_t err = hipGetLastError();
+  if (err != hipSuccess || !a.part) return err;
+  k_column_sum<<<dim3((unsigned)((a.n + 255) / 256)), 256, 0, s>>>(a.part, blocks, a.n, a.dbias);
+  return hipGetLastError();
+}
+
+}  // namespace aecct

@@ -1,0 +1,6 @@
+// The products of gemm.h for factors of one type.
+#include "gemm.h"
+
+namespace aecct {
+hipError_t launch_gemm_f32(const Gemm &g, const GemmPlan &plan, hipStream_t s) { return launch_type<float>(g, plan, s); }
+}  // namespace aecct
