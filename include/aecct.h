@@ -628,6 +628,60 @@ typedef struct aecct_dropout_args {
 /* Strides as above.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE. */
 aecct_status aecct_dropout(const aecct_dropout_args *a, void *stream);
 
+/* A tensor [batch][length][heads][d], strides in values (a head's d values lie one after the other). */
+typedef struct aecct_heads {
+  void *data;
+  int64_t batch, row, head;
+} aecct_heads;
+
+/*
+ * Cross attention: queries attend to keys and values of another length, heads / kv_heads heads share a key head
+ * (head i reads key head i / (heads / kv_heads)):
+ *   o = softmax over the keys j < lengths[b] with mask[i][j] of (scale q_i k_j), times v;  lse = the logarithm of the softmax's sum
+ *   (natural, of the scaled scores).
+ * A query that may attend nothing has o = 0 and lse = -infinity.  Keys past the length are never read, whatever lies there.  A key
+ * that the mask alone leaves out for some queries counts with the weight 0, so its values have to be finite.
+ * Scores, softmax and sums are taken in fp32; with 16-bit types the weights are rounded to the type before the product with v.
+ */
+typedef struct aecct_cross_attention_args {
+  int64_t batch, queries, keys;      /* each >= 0 (no batch or queries: nothing is written) */
+  int32_t heads, kv_heads, d;        /* kv_heads divides heads; 1 <= d <= 256 */
+  int32_t type;                      /* aecct_dtype of q, k, v and o */
+  float scale;                       /* > 0, finite */
+  aecct_heads q, k, v;               /* [batch][queries][heads][d], [batch][keys][kv_heads][d] twice; strides >= 0 */
+  const int32_t *lengths;            /* device [batch], taken between 0 and keys; or NULL: all keys */
+  const uint8_t *mask;               /* device [queries][ldmask], nonzero: may attend; or NULL; of all sequences and heads */
+  int64_t ldmask;
+  aecct_heads o;                     /* [batch][queries][heads][d] out; its values lie apart */
+  float *lse;                        /* fp32 [batch][heads][queries] out, or NULL */
+} aecct_cross_attention_args;
+/* The workspace's size (host call) goes by sizes, type and whether there is a mask.  Errors: INVALID_ARG, UNSUPPORTED (d > 256, more
+ * than 2^24 blocks of 32 queries or 128 keys), WORKSPACE_TOO_SMALL, DEVICE. */
+aecct_status aecct_cross_attention_workspace_size(const aecct_cross_attention_args *a, size_t *bytes);
+aecct_status aecct_cross_attention(const aecct_cross_attention_args *a, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient, from the o and lse that it wrote: with p = exp(scale q k^T - lse) where a pair counts, D = sum of dout o over d,
+ *   ds = p (dout v^T - D),  dq = scale ds k,  dk = scale sum of ds q,  dv = sum of p dout (over the queries, and the heads of a key head).
+ * dk and dv are 0 for keys past the length.  With 16-bit types p and ds are rounded to the type before the products.
+ */
+typedef struct aecct_cross_attention_grad_args {
+  int64_t batch, queries, keys;
+  int32_t heads, kv_heads, d;
+  int32_t type;
+  float scale;
+  aecct_heads q, k, v, o, dout;      /* dout: as o */
+  const float *lse;                  /* fp32 [batch][heads][queries] */
+  const int32_t *lengths;
+  const uint8_t *mask;
+  int64_t ldmask;
+  aecct_heads dq;                    /* out, or data NULL; as q */
+  aecct_heads dk, dv;                /* out, or both with data NULL; as k */
+} aecct_cross_attention_grad_args;
+aecct_status aecct_cross_attention_grad_workspace_size(const aecct_cross_attention_grad_args *a, size_t *bytes);
+aecct_status aecct_cross_attention_grad(const aecct_cross_attention_grad_args *a, void *workspace, size_t workspace_bytes,
+                                        void *stream);
+
 /* Human-readable name of a status code (static string). */
 const char *aecct_status_string(aecct_status status);
 

@@ -104,6 +104,23 @@ class DropoutArgs(C.Structure):
                 ("ldres", C.c_int64), ("y", _vp), ("ldy", C.c_int64)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("data", _vp), ("batch", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class CrossAttentionArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("queries", C.c_int64), ("keys", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("d", C.c_int32), ("type", C.c_int32), ("scale", C.c_float), ("q", Heads), ("k", Heads), ("v", Heads),
+                ("lengths", _vp), ("mask", _vp), ("ldmask", C.c_int64), ("o", Heads), ("lse", _vp)]
+
+
+class CrossAttentionGradArgs(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("queries", C.c_int64), ("keys", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("d", C.c_int32), ("type", C.c_int32), ("scale", C.c_float), ("q", Heads), ("k", Heads), ("v", Heads),
+                ("o", Heads), ("dout", Heads), ("lse", _vp), ("lengths", _vp), ("mask", _vp), ("ldmask", C.c_int64),
+                ("dq", Heads), ("dk", Heads), ("dv", Heads)]
+
+
 class Tensor(C.Structure):
     _fields_ = [("data", _vp), ("count", C.c_int64), ("type", C.c_int32)]
 
@@ -187,7 +204,8 @@ def lib():
         L.aecct_rms_norm_grad_workspace_size.argtypes = [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]
         L.aecct_rms_norm_grad.restype = C.c_int
         L.aecct_rms_norm_grad.argtypes = [C.POINTER(RmsNormGradArgs), _vp, C.c_size_t, _vp]
-        for f, a in (("aecct_linear_map", LinearMapArgs), ("aecct_linear_map_grad", LinearMapGradArgs)):
+        for f, a in (("aecct_linear_map", LinearMapArgs), ("aecct_linear_map_grad", LinearMapGradArgs),
+                     ("aecct_cross_attention", CrossAttentionArgs), ("aecct_cross_attention_grad", CrossAttentionGradArgs)):
             getattr(L, f).restype = C.c_int
             getattr(L, f).argtypes = [C.POINTER(a), _vp, C.c_size_t, _vp]
             getattr(L, f + "_workspace_size").restype = C.c_int
@@ -637,6 +655,102 @@ def dropout(x, p: float, seed: int, offset=0, res=None, *, y=None, stream=None):
     a = DropoutArgs(x.numel() // d, d, _dtype_code(x), p, seed, offset, offset_device, px, ldx, pres, ldres, py, ldy)
     _check(lib().aecct_dropout(C.byref(a), _current_stream(index)), "aecct_dropout")
     return y
+
+
+def _heads_of(t, shape, dtype, index: int, what):
+    if t is None:
+        return Heads()
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)} on cuda:{index}")
+    batch, row, head, one = t.stride()
+    if one != 1 and shape[3] > 1:
+        raise ValueError(f"{what}: a head's values must be contiguous")
+    return Heads(t.data_ptr(), batch, row, head)
+
+
+def _attention_of(q, k, v, lengths, mask, scale):
+    """What cross attention and its gradient have in common: (device, sizes, q, k, v, lengths, mask, ldmask)."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("q must be [batch, queries, heads, d] and k [batch, keys, kv_heads, d]")
+    index = q.get_device()
+    _on_current_gpu(index)
+    batch, queries, heads, d = q.shape
+    keys, kv_heads = k.shape[1], k.shape[2]
+    if not kv_heads or not heads or heads % kv_heads:
+        raise ValueError("kv_heads must divide heads")
+    if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != (batch,) or not lengths.is_contiguous() or
+                                lengths.get_device() != index):
+        raise ValueError(f"lengths must be {batch} contiguous int32 values on cuda:{index}")
+    ldmask = 0
+    if mask is not None:
+        if mask.dtype != torch.bool or mask.shape != (queries, keys) or mask.get_device() != index or \
+                (keys > 1 and mask.stride(1) != 1):
+            raise ValueError(f"mask must be bool [{queries}, {keys}] on cuda:{index} with contiguous rows")
+        ldmask = mask.stride(0)
+    sizes = (batch, queries, keys, heads, kv_heads, d, _dtype_code(q), d ** -0.5 if scale is None else scale)
+    return index, sizes, [_heads_of(t, s, q.dtype, index, what) for t, s, what in
+                          ((q, q.shape, "q"), (k, k.shape, "k"), (v, k.shape, "v"))], \
+        None if lengths is None else lengths.data_ptr(), None if mask is None else mask.data_ptr(), ldmask
+
+
+def cross_attention(q, k, v, lengths=None, mask=None, scale=None, *, o=None, lse=None, with_lse: bool = False, stream=None):
+    """Attention of queries to the keys and values of other states, of a length of their own.
+
+    q [batch, queries, heads, d], k and v [batch, keys, kv_heads, d]: CUDA tensors of one type (float32, bfloat16, float16) and any
+    strides but the last; kv_heads divides heads, which share key heads in order; d <= 256.  lengths: int32 [batch], the keys of
+    each sequence (what lies past them is never read).  mask: bool [queries, keys], True where a query may attend, the same for
+    all sequences and heads (a code's Tanner graph, say); values that it leaves out have to be finite.  scale: 1 / sqrt(d) if
+    None.  A query that may attend nothing gives 0, and the logarithm -inf.
+    o, lse: outputs to write to, else new tensors.  Autograd does not record the call: cross_attention_grad is its gradient.
+    Returns (o, lse), lse float32 [batch, heads, queries] the logarithm of each softmax's sum (None without with_lse)."""
+    import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return cross_attention(q, k, v, lengths, mask, scale, o=o, lse=lse, with_lse=with_lse)
+    index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse_shape = (sizes[0], sizes[3], sizes[1])
+    if lse is None and with_lse:
+        lse = torch.empty(lse_shape, dtype=torch.float32, device=q.device)
+    elif lse is not None and lse.shape != lse_shape:
+        raise ValueError(f"lse must be {lse_shape}")
+    a = CrossAttentionArgs(*sizes, hq, hk, hv, plengths, pmask, ldmask, _heads_of(o, q.shape, q.dtype, index, "o"),
+                           _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"))
+    _with_workspace("aecct_cross_attention", a, index)
+    return o, lse
+
+
+def cross_attention_grad(q, k, v, o, lse, dout, lengths=None, mask=None, scale=None, *, dq=None, dk=None, dv=None,
+                         with_dq: bool = True, with_dkv: bool = True, stream=None):
+    """Gradient of cross_attention: q, k, v, lengths, mask and scale as it read them, o and lse as it returned them, dout the
+    gradient of o.  Returns (dq, dk, dv), None for what is not asked for (dk and dv go together); dk and dv are 0 past the
+    lengths.  dq, dk, dv: outputs to write to, else new tensors."""
+    import torch
+    if stream is not None:
+        with _on_stream(stream):
+            return cross_attention_grad(q, k, v, o, lse, dout, lengths, mask, scale, dq=dq, dk=dk, dv=dv, with_dq=with_dq,
+                                        with_dkv=with_dkv)
+    index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
+    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+    if dq is None and with_dq:
+        dq = new(q)
+    if dk is None and (with_dkv or dv is not None):
+        dk = new(k)
+    if dv is None and dk is not None:
+        dv = new(v)
+    if dq is None and dk is None:
+        raise ValueError("no gradient is asked for")
+    if lse.shape != (sizes[0], sizes[3], sizes[1]):
+        raise ValueError(f"lse must be {(sizes[0], sizes[3], sizes[1])}")
+    a = CrossAttentionGradArgs(*sizes, hq, hk, hv, _heads_of(o, q.shape, q.dtype, index, "o"),
+                               _heads_of(dout, q.shape, q.dtype, index, "dout"),
+                               _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"), plengths, pmask, ldmask,
+                               _heads_of(dq, q.shape, q.dtype, index, "dq"), _heads_of(dk, k.shape, q.dtype, index, "dk"),
+                               _heads_of(dv, k.shape, q.dtype, index, "dv"))
+    _with_workspace("aecct_cross_attention_grad", a, index)
+    return dq, dk, dv
 
 
 class TensorList:

@@ -16,7 +16,8 @@ LIB = os.path.join(HERE, "libaecct.so")
 SOURCES = ["host.cpp", "host_fused.cpp", "aap.cpp", "kernels_layered.hip", "kernel_fused.hip", "arith_check.hip", "spe.hip",
            "train.hip", "train_host.cpp", "norm.hip", "norm_host.cpp", "update.hip", "update_host.cpp",
            "linear.hip", "linear_f32.hip", "linear_bf16.hip", "linear_f16.hip", "linear_i8.hip", "linear_e4m3.hip", "linear_host.cpp",
-           "dropout.hip", "dropout_host.cpp"]
+           "dropout.hip", "dropout_host.cpp", "attention.hip", "attention_grad.hip",
+           "attention_host.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-Wall", "-Wno-unused-function",

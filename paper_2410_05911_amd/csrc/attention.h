@@ -1,0 +1,58 @@
+// Cross attention and its gradient: what attention_host.cpp hands to the kernels.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include <hip/hip_runtime.h>
+
+namespace aecct {
+
+// [batch][length][heads][d], strides in values (d's is 1), none negative.
+struct Heads {
+  const void *p;
+  int64_t batch, row, head;
+};
+// The queries of the heads that share a key head are the rows of one problem: row r is query r % queries of head
+// key head * (heads / kv_heads) + r / queries.  A pair is a sequence and a key head.
+struct Attention {
+  int64_t batch, queries, keys;
+  int heads, kv_heads, d;
+  float scale;
+  Heads q, k, v, o;            // o: out; in the gradient an input
+  const int32_t *lengths;      // [batch], or null
+  const uint8_t *mask;         // [queries][ldmask], or null
+  int64_t ldmask;
+  uint32_t *words;             // the mask packed, 32 keys a word: [queries][words_of(keys)]
+  uint8_t *flags;              // of 32 rows and 64 keys: 0 none, 1 some, 2 all allowed: [tiles of rows][tiles of keys]
+  float *lse;                  // [batch][heads][queries]; in the gradient an input
+  int splits;
+  float *part_o, *part_ml;     // [splits][pairs][rows][d_of(d)], [splits][pairs][rows][2]
+};
+struct AttentionPlan {
+  bool few;                    // 32 rows a block, its wavefronts share the keys; else 128 rows
+  int splits;
+  size_t words, flags, part_o, part_ml;   // bytes
+};
+__host__ __device__ inline int64_t words_of(int64_t keys) { return (keys + 63) / 64 * 2; }
+__host__ __device__ inline int d_of(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t keys, int heads, int kv_heads, int d, bool masked);
+hipError_t launch_mask(const Attention &a, hipStream_t s);
+hipError_t launch_attention(int type, const Attention &a, const AttentionPlan &p, hipStream_t s);
+
+struct AttentionGrad {
+  Attention a;
+  Heads dout, dq, dk, dv;      // dq, dk, dv: out
+  float *rows;                 // [pairs][rows][2]: lse log2(e), and the sum of dout o
+  int splits;                  // of the rows, for dk and dv
+  float *part;                 // [splits][2][pairs][keys][d_of(d)], or null
+};
+struct AttentionGradPlan {
+  int splits;
+  size_t words, flags, rows, part;        // bytes
+};
+AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, int64_t keys, int heads, int kv_heads, int d,
+                                      bool masked);
+hipError_t launch_attention_grad(int type, const AttentionGrad &a, hipStream_t s);
+
+}  // namespace aecct

@@ -1,0 +1,138 @@
+// Tiles of keys and queries in LDS, and the products of attention on them, for the forward pass and the gradient.
+//
+// A tile is 32 rows (or several times 32) of RB bytes, d values padded by zeros to 32, 64, 128 or 256.  The 16-byte chunks of a row
+// are exchanged by the row's number, so that the reads of one chunk of 32 rows and those of 4 rows' columns fall on
+// different banks alike.
+#pragma once
+
+#include "../../include/aecct.h"
+#include "attention.h"
+#include "gemm_stage.h"
+#include "mfma.h"
+
+namespace aecct {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+template <int RB>
+__device__ __forceinline__ int exchange(int row) {
+  return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
+}
+// Chunk `chunk` of row `row`: of a product along d.
+template <int RB>
+__device__ __forceinline__ u32x4 row_chunk(const char *tile, int row, int chunk) {
+  return *(const u32x4 *)(tile + row * RB + ((chunk << 4) ^ exchange<RB>(row)));
+}
+// Columns d0 + lane % 32 of 16-bit rows 16 t + {4 h .. + 3, 8 + 4 h .. + 3}: the order in which a lane's registers 8 t .. 8 t + 7 hold
+// the rows of a 32 x 32 result, which is the other factor.
+template <int RB>
+__device__ __forceinline__ u32x4 column_chunk(const char *tile, int row0, int t, int d0) {
+  const int lane = threadIdx.x & 63, l = lane & 15, row = row0 + 16 * t + 4 * (lane >> 5) + (l >> 2);
+  const int col = (d0 + (lane & 16) + (l & 3) * 4) * 2;
+  return pair64(columns16(tile + row * RB + (col ^ exchange<RB>(row))),
+                columns16(tile + (row + 8) * RB + (col ^ exchange<RB>(row + 8))));
+}
+// The row of a 32 x 32 result that register i of a lane in half h holds.
+__device__ __forceinline__ int row_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// acc[f] += the tile's columns (32 f + 0..31) times p, over the 32 rows from row0 on; p a result's registers.
+template <class T, int RB, int FD>
+__device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile, int row0, const float (&p)[16]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const u32x4 b = {pack2(p[8 * t], p[8 * t + 1], T()), pack2(p[8 * t + 2], p[8 * t + 3], T()),
+                       pack2(p[8 * t + 4], p[8 * t + 5], T()), pack2(p[8 * t + 6], p[8 * t + 7], T())};
+#pragma unroll
+      for (int f = 0; f < FD; ++f) step<T>(acc[f], column_chunk<RB>(tile, row0, t, 32 * f), b);
+    }
+  } else {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = row0 + row_of(i, h);
+#pragma unroll
+      for (int f = 0; f < FD; ++f) {
+        const float v = *(const float *)(tile + row * RB + (((32 * f + (lane & 31)) * 4) ^ exchange<RB>(row)));
+        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], acc[f], 0, 0, 0);
+      }
+    }
+  }
+}
+// The product of the tile's 32 rows from row0 on with a lane's row held in registers (chunks 2 s + h).
+template <class T, int RB>
+__device__ __forceinline__ f32x16 times_rows(const char *tile, int row0, const u32x4 (&r)[RB / 32]) {
+  const int lane = threadIdx.x & 63;
+  f32x16 s;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = 0;
+#pragma unroll
+  for (int c = 0; c < RB / 32; ++c) step<T>(s, row_chunk<RB>(tile, row0 + (lane & 31), 2 * c + (lane >> 5)), r[c]);
+  return s;
+}
+
+// Both halves' values of x: theirs is the same in lanes l and l + 32.
+__device__ __forceinline__ void both_halves(float x, float &low, float &high) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t a = r[0], b = r[1];
+  low = __builtin_bit_cast(float, a);
+  high = __builtin_bit_cast(float, b);
+}
+__device__ __forceinline__ float max_halves(float x) {
+  float a, b;
+  both_halves(x, a, b);
+  return fmaxf(a, b);
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  float a, b;
+  both_halves(x, a, b);
+  return a + b;
+}
+
+// 16 bytes of a row of d values from chunk `chunk` on, zeros behind its end; `end` is where the tensor's memory ends.
+template <class T>
+__device__ __forceinline__ u32x4 row_piece(const char *row, int chunk, int d, const char *end) {
+  constexpr int E = 16 / (int)sizeof(T);
+  const int n = d - chunk * E;
+  if (n <= 0) return u32x4{0, 0, 0, 0};
+  const char *const p = row + chunk * 16;
+  if (n >= E) return any16(p);
+  if (p + 16 > end) return some_values<T>(p, n);
+  u32x4 v = any16(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      if (i >= n) v[i] = 0;
+    } else {
+      v[i] = 2 * i + 1 < n ? v[i] : 2 * i < n ? v[i] & 0xffffu : 0u;
+    }
+  }
+  return v;
+}
+__device__ __forceinline__ const char *end_of(const Heads &t, int64_t batch, int64_t length, int64_t heads, int d, int size) {
+  return (const char *)t.p + ((batch - 1) * t.batch + (length - 1) * t.row + (heads - 1) * t.head + d) * size;
+}
+
+// Blocks in an order that keeps those of one XCD (every eighth) on neighbouring numbers, which share their keys.
+__device__ __forceinline__ int64_t near_block(int64_t block, int64_t blocks) {
+  const int64_t share = blocks / 8;
+  return block < share * 8 ? (block % 8) * share + block / 8 : block;
+}
+
+// Whether any of `count` tiles of rows from `first` on may attend any of `keys` keys from key0 on.
+__device__ __forceinline__ bool any_flag(const uint8_t *flags, int64_t first, int count, int64_t row_tiles, int64_t key0, int keys,
+                                         int64_t flag_tiles) {
+  int any = 0;
+  for (int i = 0; i < count && first + i < row_tiles; ++i)
+    for (int64_t c = key0 / 64; c * 64 < key0 + keys && c < flag_tiles; ++c) any |= flags[(first + i) * flag_tiles + c];
+  return any != 0;
+}
+
+template <class T>
+__device__ __forceinline__ void store_values4(T *p, int n, float a, float b, float c, float d) {
+  const float v[4] = {a, b, c, d};
+  store_part<T, 4>(p, n, v);
+}
+
+}  // namespace aecct
