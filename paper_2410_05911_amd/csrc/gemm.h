@@ -65,8 +65,26 @@ __device__ __forceinline__ void finish4(const Epilogue &e, int64_t m, int64_t n0
 }
 
 // ---- staging: 16-byte pieces of a factor's tile, slot by slot
-// A tile of ROWS rows from row0 on: where slot `slot` of its LDS lies in the factor.
-template <class T, bool ACROSS, int ROWS>
+// E values of the stored type S at p as the product's type T: all of them, or the first n.
+template <class T, class S>
+__device__ __forceinline__ u32x4 piece(const char *p) {
+  if constexpr (__is_same(S, e4m3_t)) {
+    uint32_t v[2];
+    __builtin_memcpy(v, p, 8);
+    return widen(v[0], v[1]);
+  } else {
+    return any16(p);
+  }
+}
+template <class T, class S>
+__device__ __forceinline__ u32x4 piece(const char *p, int n) {
+  const u32x4 v = some_values<S>(p, n);
+  if constexpr (__is_same(S, e4m3_t)) return widen(v[0], v[1]);
+  return v;
+}
+
+// A tile of ROWS rows from row0 on, of values stored as S and multiplied as T: where slot `slot` of its LDS lies in the factor.
+template <class T, class S, bool ACROSS, int ROWS>
 struct Tile {
   static constexpr int E = 16 / (int)sizeof(T), KT = 128 / (int)sizeof(T), PITCH = ROWS * (int)sizeof(T);
   static constexpr int SLOTS = ROWS * 8;
@@ -91,12 +109,12 @@ struct Tile {
       const int64_t row = row0 + r;
       if (k >= k_end || row >= rows) return u32x4{0, 0, 0, 0};
       const int64_t at = k * ld + row, left = (k_all - 1) * ld + rows - at;   // values to the end of the memory
-      return left >= E ? any16(p + at * (int64_t)sizeof(T)) : some_values<T>(p + at * (int64_t)sizeof(T), (int)left);
+      return left >= E ? piece<T, S>(p + at * (int64_t)sizeof(S)) : piece<T, S>(p + at * (int64_t)sizeof(S), (int)left);
     } else {
       if (k >= k_end) return u32x4{0, 0, 0, 0};
       const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
-      const char *const q = p + (row * ld + k) * (int64_t)sizeof(T);
-      return k + E <= k_end ? any16(q) : some_values<T>(q, (int)(k_end - k));
+      const char *const q = p + (row * ld + k) * (int64_t)sizeof(S);
+      return k + E <= k_end ? piece<T, S>(q) : piece<T, S>(q, (int)(k_end - k));
     }
   }
   static __device__ __forceinline__ u32x4 frag(const char *tile, int row0, int chunk) {
@@ -115,10 +133,10 @@ __device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, i
   in = rest / height;
 }
 
-template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
-  typedef Tile<T, AA, BM> TA;
-  typedef Tile<T, BA, BN> TB;
+  typedef Tile<T, S, AA, BM> TA;
+  typedef Tile<T, S, BA, BN> TB;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT;
   constexpr int CA = TA::SLOTS / NT, CB = TB::SLOTS / NT, BYTES = (BM + BN) * 128;
   static_assert(TA::SLOTS % NT == 0 && TB::SLOTS % NT == 0, "whole slots");
@@ -164,18 +182,15 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
       for (int i = 0; i < CB; ++i) rb[i] = TB::fetch(pb, g.b.ld, g.n, g.k, n0, k + KT, k1, threadIdx.x + i * NT);
     }
 #pragma unroll
-    for (int s = 0; s < 4; s += 2) {
-      u32x4 a0[FM], a1[FM];
+    for (int s = 0; s < 4; ++s) {
+      u32x4 fa[FM];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        a0[i] = TA::frag(la, wm + i * 32, 2 * s + h);
-        a1[i] = TA::frag(la, wm + i * 32, 2 * s + 2 + h);
-      }
+      for (int i = 0; i < FM; ++i) fa[i] = TA::frag(la, wm + i * 32, 2 * s + h);
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
-        const u32x4 b0 = TB::frag(lb, wn + j * 32, 2 * s + h), b1 = TB::frag(lb, wn + j * 32, 2 * s + 2 + h);
+        const u32x4 fb = TB::frag(lb, wn + j * 32, 2 * s + h);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) step2<T>(acc[i][j], b0, b1, a0[i], a1[i]);
+        for (int i = 0; i < FM; ++i) step<T>(acc[i][j], fb, fa[i]);
       }
     }
   }
@@ -235,10 +250,10 @@ __global__ __launch_bounds__(256) void k_join(Gemm g) {
   finish4(g.e, m, n, count, v);
 }
 
-template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
 hipError_t launch_tile(const Gemm &g, hipStream_t s) {
   const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
-  k_gemm<T, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
+  k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || !g.part) return err;
   const int64_t join = (g.m * ((g.n + 3) / 4) + 255) / 256;
@@ -248,19 +263,19 @@ hipError_t launch_tile(const Gemm &g, hipStream_t s) {
 
 // The tiles that plan_gemm chooses from.
 constexpr int kTileSide[2][2] = {{64, 64}, {128, 128}};
-template <class T, bool AA, bool BA>
+template <class T, class S, bool AA, bool BA>
 hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {
-  if (p.tile == 0) return launch_tile<T, AA, BA, 64, 64, 2, 2>(g, s);
-  return launch_tile<T, AA, BA, 128, 128, 2, 2>(g, s);
+  if (p.tile == 0) return launch_tile<T, S, AA, BA, 64, 64, 2, 2>(g, s);
+  return launch_tile<T, S, AA, BA, 128, 128, 2, 2>(g, s);
 }
 // Codes are never a gradient's factor, so a of theirs lies along k.
-template <class T>
+template <class T, class S = T>
 hipError_t launch_type(const Gemm &g, const GemmPlan &p, hipStream_t s) {
-  if constexpr (sizeof(T) > 1) {
-    if (g.a.across && g.b.across) return launch_layout<T, true, true>(g, p, s);
+  if constexpr (sizeof(S) > 1) {
+    if (g.a.across && g.b.across) return launch_layout<T, S, true, true>(g, p, s);
   }
   if (g.a.across) return hipErrorInvalidValue;
-  return g.b.across ? launch_layout<T, false, true>(g, p, s) : launch_layout<T, false, false>(g, p, s);
+  return g.b.across ? launch_layout<T, S, false, true>(g, p, s) : launch_layout<T, S, false, false>(g, p, s);
 }
 
 }  // namespace aecct
