@@ -23,45 +23,48 @@ __device__ __forceinline__ float activate(float z, int act) {
   return z;
 }
 
-// ---- four values of a stored type, at any address aligned to one
-__device__ __forceinline__ void load4(int type, const void *p, int64_t at, int n, float (&f)[4]) {
-  if (type == 0) load_part<float, 4>((const float *)p + at, n, f);
-  else if (type == 1) load_part<bf16_t, 4>((const bf16_t *)p + at, n, f);
-  else load_part<f16_t, 4>((const f16_t *)p + at, n, f);
+// ---- V values of a stored type, at any address aligned to one
+template <int V>
+__device__ __forceinline__ void load_values(int type, const void *p, int64_t at, int n, float (&f)[V]) {
+  if (type == 0) load_part<float, V>((const float *)p + at, n, f);
+  else if (type == 1) load_part<bf16_t, V>((const bf16_t *)p + at, n, f);
+  else load_part<f16_t, V>((const f16_t *)p + at, n, f);
 }
-__device__ __forceinline__ void store4(int type, void *p, int64_t at, int n, const float (&f)[4]) {
-  if (type == 0) store_part<float, 4>((float *)p + at, n, f);
-  else if (type == 1) store_part<bf16_t, 4>((bf16_t *)p + at, n, f);
-  else store_part<f16_t, 4>((f16_t *)p + at, n, f);
+template <int V>
+__device__ __forceinline__ void store_values(int type, void *p, int64_t at, int n, const float (&f)[V]) {
+  if (type == 0) store_part<float, V>((float *)p + at, n, f);
+  else if (type == 1) store_part<bf16_t, V>((bf16_t *)p + at, n, f);
+  else store_part<f16_t, V>((f16_t *)p + at, n, f);
 }
 
-// The epilogue of values (m, n0 .. n0 + count), count <= 4.
-__device__ __forceinline__ void finish4(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[4]) {
+// The epilogue of values (m, n0 .. n0 + count), count <= V.
+template <int V>
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[V]) {
   if (e.alpha) {
     const float r = e.alpha[m] * e.per_q;
-    float s[4];
-    load_part<float, 4>(e.scale + n0, count, s);
+    float s[V];
+    load_part<float, V>(e.scale + n0, count, s);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = v[i] * r * s[i];
+    for (int i = 0; i < V; ++i) v[i] = v[i] * r * s[i];
   }
   if (e.bias) {
-    float b[4];
-    load_part<float, 4>(e.bias + n0, count, b);
+    float b[V];
+    load_part<float, V>(e.bias + n0, count, b);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += b[i];
+    for (int i = 0; i < V; ++i) v[i] += b[i];
   }
-  if (e.z) store4(e.type, e.z, m * e.ldz + n0, count, v);
+  if (e.z) store_values<V>(e.type, e.z, m * e.ldz + n0, count, v);
   if (e.act != kActNone) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = activate(v[i], e.act);
+    for (int i = 0; i < V; ++i) v[i] = activate(v[i], e.act);
   }
   if (e.res) {
-    float r[4];
-    load4(e.type, e.res, m * e.ldres + n0, count, r);
+    float r[V];
+    load_values<V>(e.type, e.res, m * e.ldres + n0, count, r);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += r[i];
+    for (int i = 0; i < V; ++i) v[i] += r[i];
   }
-  store4(e.type, e.y, m * e.ldy + n0, count, v);
+  store_values<V>(e.type, e.y, m * e.ldy + n0, count, v);
 }
 
 // ---- staging: 16-byte pieces of a factor's tile, slot by slot
@@ -123,6 +126,12 @@ struct Tile {
   }
 };
 
+// Orders a wavefront's LDS accesses before and after among its lanes (they run in order; the compiler must not move them).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Tiles in an order that keeps the blocks of one XCD (every eighth block) on neighbouring tiles: bands of 8 rows of tiles,
 // column by column.
 __device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, int64_t &im, int64_t &in) {
@@ -131,6 +140,52 @@ __device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, i
   const int64_t band = at / (8 * tn), first = band * 8, height = tm - first < 8 ? tm - first : 8, rest = at - band * 8 * tn;
   im = first + rest % height;
   in = rest / height;
+}
+
+// A wavefront's FM x FN sums from (m0, n0) on through the epilogue: 32 rows at a time go through LDS, so that a lane then has eight
+// neighbouring columns and neighbouring lanes a row's (stored as they lie in registers, in pieces of 16 or 8 bytes 32 rows apart,
+// 49152 x 128 -> 512 in fp32 took 89 us).  All wavefronts of the block are done with the tiles in LDS before.
+template <class T, int FM, int FN>
+__device__ __forceinline__ void finish_block(const Gemm &g, typename Product<T>::Acc (&acc)[FM][FN], char *lds, int split, int64_t m0,
+                                             int64_t n0) {
+  constexpr int LD = FN * 32 + 4, PER = FN * 4, STEP = 64 / PER;   // lanes a row, rows at once
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  float *const strip = (float *)lds + (threadIdx.x >> 6) * (32 * LD);
+  const int c = lane % PER * 8;
+  const int64_t n = n0 + c;
+  const int count = g.n - n < 8 ? (int)(g.n - n) : 8;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const auto sum = acc[i][j][4 * q + r];
+          v[r] = g.part ? __builtin_bit_cast(float, sum) : (float)sum;   // int32 partial sums travel as their bits
+        }
+        *(f32x4 *)(strip + (lane & 31) * LD + j * 32 + 8 * q + 4 * h) = v;
+      }
+    wave_sync();
+#pragma unroll 1
+    for (int row = lane / PER; row < 32; row += STEP) {
+      const int64_t m = m0 + i * 32 + row;
+      if (m >= g.m || count <= 0) continue;
+      float v[8];
+      const f32x4 lo = *(const f32x4 *)(strip + row * LD + c), hi = *(const f32x4 *)(strip + row * LD + c + 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        v[r] = lo[r];
+        v[4 + r] = hi[r];
+      }
+      if (g.part) store_part<float, 8>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
+      else finish<8>(g.e, m, n, count, v);
+    }
+    wave_sync();
+  }
 }
 
 template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
@@ -194,35 +249,106 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
       }
     }
   }
+  finish_block<T, FM, FN>(g, acc, lds, split, m0 + wm, n0 + wn);
+}
+
+// The same product where both factors' rows begin at 16-byte addresses and are whole 16-byte pieces: the pieces go from memory to LDS
+// without passing through registers, by buffer loads whose out-of-range offsets give the zeros of a ragged end.
+template <class T, bool ACROSS, int ROWS, int NT>
+struct Direct {
+  typedef Tile<T, T, ACROSS, ROWS> Place;
+  static constexpr int COUNT = Place::SLOTS / NT;
+  static constexpr uint32_t OUT = 0x80000000u;   // offsets from here on are out of range
+  uint32_t at[COUNT];
+  const char *p;
+  int64_t step;
+  __device__ __forceinline__ void init(const Factor &f, int64_t rows, int64_t row0, int64_t k0) {
+    p = (const char *)f.p + (ACROSS ? k0 * f.ld + row0 : row0 * f.ld + k0) * (int64_t)sizeof(T);
+    step = (ACROSS ? Place::KT * f.ld : Place::KT) * (int64_t)sizeof(T);
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int64_t m = m0 + wm + i * 32 + (lane & 31);
-    if (m >= g.m) continue;
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t n = n0 + wn + j * 32 + 8 * q + 4 * h;
-        if (n >= g.n) continue;
-        const int count = g.n - n < 4 ? (int)(g.n - n) : 4;
-        if (g.part) {
-          // int32 sums travel as their bits
-          float v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const auto sum = acc[i][j][4 * q + r];
-            v[r] = __builtin_bit_cast(float, sum);
-          }
-          store_part<float, 4>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
-        } else {
-          float v[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][j][4 * q + r];
-          finish4(g.e, m, n, count, v);
-        }
+    for (int i = 0; i < COUNT; ++i) {
+      int r, k;
+      Place::place(threadIdx.x + i * NT, r, k);
+      if constexpr (ACROSS) {
+        at[i] = row0 + r < rows ? (uint32_t)((k * f.ld + r) * (int64_t)sizeof(T)) : OUT;
+      } else {
+        const int64_t row = row0 + r < rows ? r : rows - 1 - row0;
+        at[i] = (uint32_t)((row * f.ld + k) * (int64_t)sizeof(T));
       }
     }
   }
+  // The next tile into LDS; `left` of its k are there.
+  __device__ __forceinline__ void load(char *lds, int64_t left) {
+    const BufferOf r(p, OUT);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      uint32_t offset = at[i];
+      if (left < Place::KT) {
+        int row, k;
+        Place::place(threadIdx.x + i * NT, row, k);
+        if (k >= left) offset = OUT;
+      }
+      r.to_lds(lds + (i * NT + wave * 64) * 16, offset);
+    }
+    p += step;
+  }
+};
+
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
+  typedef Tile<T, T, AA, BM> TA;
+  typedef Tile<T, T, BA, BN> TB;
+  constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT, BYTES = (BM + BN) * 128;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
+  const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
+  const int split = (int)(blockIdx.x / (tm * tn));
+  int64_t im, in;
+  tile_of(blockIdx.x % (tm * tn), tm, tn, im, in);
+  const int64_t m0 = im * BM, n0 = in * BN;
+  const int64_t kt = (g.k + KT - 1) / KT, k0 = kt * split / g.splits * KT, k1 = min(g.k, kt * (split + 1) / g.splits * KT);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
+  Direct<T, AA, BM, NT> da;
+  Direct<T, BA, BN, NT> db;
+  da.init(g.a, g.m, m0, k0);
+  db.init(g.b, g.n, n0, k0);
+
+  typename Product<T>::Acc acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  if (k0 < k1) {
+    da.load(lds, k1 - k0);
+    db.load(lds + BM * 128, k1 - k0);
+  }
+  int buf = 0;
+  for (int64_t k = k0; k < k1; k += KT, buf ^= 1) {
+    wait_loads();
+    __syncthreads();   // the tile is there, and nobody reads the other one any more
+    const char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
+    if (k + KT < k1) {
+      char *const next = lds + (buf ^ 1) * BYTES;
+      da.load(next, k1 - k - KT);
+      db.load(next + BM * 128, k1 - k - KT);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      u32x4 fa[FM], fb[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[i] = TA::frag(la, wm + i * 32, 2 * s + h);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = TB::frag(lb, wn + j * 32, 2 * s + h);
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) step<T>(acc[i][j], fb[j], fa[i]);
+    }
+  }
+  finish_block<T, FM, FN>(g, acc, lds, split, m0 + wm, n0 + wn);
 }
 
 // The splits' sums of four outputs a thread, in the order of the splits, and the epilogue.
@@ -247,24 +373,50 @@ __global__ __launch_bounds__(256) void k_join(Gemm g) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = (float)w[i];
   }
-  finish4(g.e, m, n, count, v);
+  finish<4>(g.e, m, n, count, v);
 }
 
-template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
-hipError_t launch_tile(const Gemm &g, hipStream_t s) {
-  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
-  k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
-  hipError_t err = hipGetLastError();
+template <class T>
+hipError_t join(const Gemm &g, hipStream_t s) {
+  const hipError_t err = hipGetLastError();
   if (err != hipSuccess || !g.part) return err;
   const int64_t join = (g.m * ((g.n + 3) / 4) + 255) / 256;
   k_join<__is_same(T, int8_t)><<<dim3((unsigned)join), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
+template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
+hipError_t launch_tile(const Gemm &g, hipStream_t s) {
+  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
+  k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
+  return join<T>(g, s);
+}
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+hipError_t launch_direct(const Gemm &g, hipStream_t s) {
+  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
+  k_gemm_direct<T, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
+  return join<T>(g, s);
+}
+
+// Whether k_gemm_direct takes a factor of `rows` rows: whole pieces at 16-byte addresses, offsets in a tile of 256 rows within 2^31.
+template <class T>
+bool direct_ok(const Factor &f, int64_t rows, int64_t k) {
+  constexpr int64_t E = 16 / sizeof(T);
+  return (uintptr_t)f.p % 16 == 0 && f.ld % E == 0 && (f.across ? rows : k) % E == 0 && f.ld < ((int64_t)1 << 22) / (int64_t)sizeof(T);
+}
 
 // The tiles that plan_gemm chooses from.
-constexpr int kTileSide[2][2] = {{64, 64}, {128, 128}};
+constexpr int kTileSide[3][2] = {{64, 64}, {128, 128}, {256, 256}};
 template <class T, class S, bool AA, bool BA>
 hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {
+  if constexpr (__is_same(T, S)) {
+    if (direct_ok<T>(g.a, g.m, g.k) && direct_ok<T>(g.b, g.n, g.k)) {
+      if constexpr (sizeof(T) < 4) {
+        if (p.tile == 2) return launch_direct<T, AA, BA, 256, 256, 2, 4>(g, s);
+      }
+      if (p.tile >= 1) return launch_direct<T, AA, BA, 128, 128, 2, 2>(g, s);
+      return launch_direct<T, AA, BA, 64, 64, 2, 2>(g, s);
+    }
+  }
   if (p.tile == 0) return launch_tile<T, S, AA, BA, 64, 64, 2, 2>(g, s);
   return launch_tile<T, S, AA, BA, 128, 128, 2, 2>(g, s);
 }

@@ -7,6 +7,7 @@ GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, boo
   GemmPlan p{1, 1, 0};
   auto tiles = [&](int t) { return (m + kTileSide[t][0] - 1) / kTileSide[t][0] * ((n + kTileSide[t][1] - 1) / kTileSide[t][1]); };
   if (tiles(1) < 192) p.tile = 0;
+  else if (tiles(2) >= 256) p.tile = 2;
   const int64_t size = type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2, t = tiles(p.tile), kt = (k * size + 127) / 128;
   if (t > 0 && t < 256) {
     int64_t s = (512 + t - 1) / t;
