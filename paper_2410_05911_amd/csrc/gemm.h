@@ -16,10 +16,29 @@
 namespace aecct {
 
 // ---- activations, in fp32
-__device__ __forceinline__ float activate(float z, int act) {
+// The normal distribution Phi(z) and e = e^(-z^2 / 2), to 1e-7: Abramowitz and Stegun 7.1.26 for its tail, 1 - erf(x) = e^(-x^2) times a
+// polynomial in 1 / (1 + 0.3275911 x).  A third of erff's instructions (16384 x 8192 outputs in bf16: 1097 -> 1000 us for the map);
+// fp32 outputs take erff.
+__device__ __forceinline__ float normal(float z, float &e) {
+  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
+  float p = fmaf(t, 1.061405429f, -1.453152027f);
+  p = fmaf(t, p, 1.421413741f);
+  p = fmaf(t, p, -0.284496736f);
+  p = fmaf(t, p, 0.254829592f);
+  const float tail = 0.5f * (p * t) * e;
+  return z > 0.0f ? 1.0f - tail : tail;
+}
+__device__ __forceinline__ float logistic(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+}
+__device__ __forceinline__ float activate(float z, int act, bool f32) {
   if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
-  if (act == kActGelu) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-  if (act == kActSilu) return z / (1.0f + expf(-z));
+  if (act == kActGelu) {
+    float e;
+    return z * (f32 ? 0.5f * (1.0f + erff(z * 0.70710678118654752f)) : normal(z, e));
+  }
+  if (act == kActSilu) return z * logistic(z);
   return z;
 }
 
@@ -56,7 +75,7 @@ __device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0,
   if (e.z) store_values<V>(e.type, e.z, m * e.ldz + n0, count, v);
   if (e.act != kActNone) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = activate(v[i], e.act);
+    for (int i = 0; i < V; ++i) v[i] = activate(v[i], e.act, e.type == AECCT_F32);
   }
   if (e.res) {
     float r[V];
@@ -132,11 +151,14 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Tiles in an order that keeps the blocks of one XCD (every eighth block) on neighbouring tiles: bands of 8 rows of tiles,
-// column by column.
+// Blocks in an order that keeps those of one XCD (every eighth block) on neighbouring numbers.
+__device__ __forceinline__ int64_t near_tile(int64_t block, int64_t all) {
+  const int64_t share = all / 8;
+  return block < share * 8 ? (block % 8) * share + block / 8 : block;
+}
+// Tiles in such an order, bands of 8 rows of tiles, column by column.
 __device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, int64_t &im, int64_t &in) {
-  const int64_t all = tm * tn, share = all / 8;
-  const int64_t at = block < share * 8 ? (block % 8) * share + block / 8 : block;
+  const int64_t at = near_tile(block, tm * tn);
   const int64_t band = at / (8 * tn), first = band * 8, height = tm - first < 8 ? tm - first : 8, rest = at - band * 8 * tn;
   im = first + rest % height;
   in = rest / height;
@@ -188,12 +210,50 @@ __device__ __forceinline__ void finish_block(const Gemm &g, typename Product<T>:
   }
 }
 
+// A factor's tiles on their way through registers: a thread's slots as 32-bit offsets from the tile's begin, where the tile is whole
+// (values past a row's end may be read, not past the memory's: rows that are not there give outputs that are not there).
+template <class T, class S, bool ACROSS, int ROWS, int NT>
+struct Through {
+  typedef Tile<T, S, ACROSS, ROWS> Place;
+  static constexpr int COUNT = Place::SLOTS / NT;
+  uint32_t at[COUNT];
+  const Factor &f;
+  int64_t rows, k_all, row0;
+  bool near;
+  __device__ __forceinline__ Through(const Factor &f, int64_t rows, int64_t k_all, int64_t row0)
+      : f(f), rows(rows), k_all(k_all), row0(row0) {
+    near = f.ld < ((int64_t)1 << 30) / (ROWS > Place::KT ? ROWS : Place::KT) / (int64_t)sizeof(S);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+      int r, k;
+      Place::place(threadIdx.x + i * NT, r, k);
+      if constexpr (!ACROSS) r = row0 + r < rows ? r : (int)(rows - 1 - row0);
+      at[i] = (uint32_t)((ACROSS ? k * f.ld + r : r * f.ld + k) * (int64_t)sizeof(S));
+    }
+  }
+  // The tile of k0, of which k_end is the end.
+  __device__ __forceinline__ void load(u32x4 (&v)[COUNT], int64_t k0, int64_t k_end) const {
+    bool whole = near && k0 + Place::KT <= k_end;
+    if constexpr (ACROSS) whole = whole && (k0 + Place::KT - 1) * f.ld + row0 + ROWS <= (k_all - 1) * f.ld + rows;
+    if (whole) {
+      const char *const p = (const char *)f.p + (ACROSS ? k0 * f.ld + row0 : row0 * f.ld + k0) * (int64_t)sizeof(S);
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) v[i] = piece<T, S>(p + at[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+        v[i] = Place::fetch((const char *)f.p, f.ld, rows, k_all, row0, k0, k_end, threadIdx.x + i * NT);
+    }
+  }
+};
+
 template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
   typedef Tile<T, S, AA, BM> TA;
   typedef Tile<T, S, BA, BN> TB;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT;
   constexpr int CA = TA::SLOTS / NT, CB = TB::SLOTS / NT, BYTES = (BM + BN) * 128;
+  constexpr int AHEAD = CA + CB <= 4 ? 3 : 1;   // tiles on their way in registers
   static_assert(TA::SLOTS % NT == 0 && TB::SLOTS % NT == 0, "whole slots");
   __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
   const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
@@ -205,7 +265,8 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
   const int64_t kt = (g.k + KT - 1) / KT, k0 = kt * split / g.splits * KT, k1 = min(g.k, kt * (split + 1) / g.splits * KT);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
-  const char *const pa = (const char *)g.a.p, *const pb = (const char *)g.b.p;
+  const Through<T, S, AA, BM, NT> ta(g.a, g.m, g.k, m0);
+  const Through<T, S, BA, BN, NT> tb(g.b, g.n, g.k, n0);
 
   typename Product<T>::Acc acc[FM][FN];
 #pragma unroll
@@ -215,27 +276,29 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
 
-  u32x4 ra[CA], rb[CB];
-  if (k0 < k1) {
+  u32x4 ra[AHEAD][CA], rb[AHEAD][CB];
 #pragma unroll
-    for (int i = 0; i < CA; ++i) ra[i] = TA::fetch(pa, g.a.ld, g.m, g.k, m0, k0, k1, threadIdx.x + i * NT);
-#pragma unroll
-    for (int i = 0; i < CB; ++i) rb[i] = TB::fetch(pb, g.b.ld, g.n, g.k, n0, k0, k1, threadIdx.x + i * NT);
+  for (int d = 0; d < AHEAD; ++d) {
+    if (k0 + d * KT < k1) {
+      ta.load(ra[d], k0 + d * KT, k1);
+      tb.load(rb[d], k0 + d * KT, k1);
+    }
   }
   int buf = 0;
-  for (int64_t k = k0; k < k1; k += KT, buf ^= 1) {
-    char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
+  for (int64_t k = k0; k < k1;) {
 #pragma unroll
-    for (int i = 0; i < CA; ++i) *(u32x4 *)(la + (threadIdx.x + i * NT) * 16) = ra[i];
+    for (int d = 0; d < AHEAD; ++d) {
+      if (k >= k1) break;
+      char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
 #pragma unroll
-    for (int i = 0; i < CB; ++i) *(u32x4 *)(lb + (threadIdx.x + i * NT) * 16) = rb[i];
-    __syncthreads();   // also: no wavefront reads the other buffer any more when the next round writes it
-    if (k + KT < k1) {
+      for (int i = 0; i < CA; ++i) *(u32x4 *)(la + (threadIdx.x + i * NT) * 16) = ra[d][i];
 #pragma unroll
-      for (int i = 0; i < CA; ++i) ra[i] = TA::fetch(pa, g.a.ld, g.m, g.k, m0, k + KT, k1, threadIdx.x + i * NT);
-#pragma unroll
-      for (int i = 0; i < CB; ++i) rb[i] = TB::fetch(pb, g.b.ld, g.n, g.k, n0, k + KT, k1, threadIdx.x + i * NT);
-    }
+      for (int i = 0; i < CB; ++i) *(u32x4 *)(lb + (threadIdx.x + i * NT) * 16) = rb[d][i];
+      __syncthreads();   // also: no wavefront reads the other buffer any more when the next round writes it
+      if (k + AHEAD * KT < k1) {
+        ta.load(ra[d], k + AHEAD * KT, k1);
+        tb.load(rb[d], k + AHEAD * KT, k1);
+      }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       u32x4 fa[FM];
@@ -247,6 +310,9 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
 #pragma unroll
         for (int i = 0; i < FM; ++i) step<T>(acc[i][j], fb, fa[i]);
       }
+    }
+      k += KT;
+      buf ^= 1;
     }
   }
   finish_block<T, FM, FN>(g, acc, lds, split, m0 + wm, n0 + wn);
@@ -295,12 +361,14 @@ struct Direct {
   }
 };
 
-template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+// STAGES tiles of LDS: while one is multiplied, STAGES - 2 lie ready or are on their way beside the one being asked for.
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
   typedef Tile<T, T, AA, BM> TA;
   typedef Tile<T, T, BA, BN> TB;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT, BYTES = (BM + BN) * 128;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
+  constexpr int STRIPS = WM * WN * 32 * (FN * 32 + 4) * 4;   // what finish_block takes
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * BYTES > STRIPS ? STAGES * BYTES : STRIPS];
   const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
   const int split = (int)(blockIdx.x / (tm * tn));
   int64_t im, in;
@@ -321,31 +389,57 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
-  if (k0 < k1) {
-    da.load(lds, k1 - k0);
-    db.load(lds + BM * 128, k1 - k0);
-  }
-  int buf = 0;
-  for (int64_t k = k0; k < k1; k += KT, buf ^= 1) {
-    wait_loads();
-    __syncthreads();   // the tile is there, and nobody reads the other one any more
-    const char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
-    if (k + KT < k1) {
-      char *const next = lds + (buf ^ 1) * BYTES;
-      da.load(next, k1 - k - KT);
-      db.load(next + BM * 128, k1 - k - KT);
+  constexpr int AHEAD = STAGES > 1 ? STAGES - 1 : 1;   // one stage: for a k of one tile
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    if (k0 + i * KT < k1) {
+      da.load(lds + i * BYTES, k1 - k0 - i * KT);
+      db.load(lds + i * BYTES + BM * 128, k1 - k0 - i * KT);
     }
+  }
+  int buf = 0, free = AHEAD;
+  for (int64_t k = k0; k < k1; k += KT) {
+    // Loads come back in order: the tile is there when only those of the tiles after it are left.
+    if (k + (AHEAD - 1) * KT < k1) wait_loads_but<(AHEAD - 1) * (Direct<T, AA, BM, NT>::COUNT + Direct<T, BA, BN, NT>::COUNT)>();
+    else wait_loads();
+    barrier();   // the tile is there for all, and nobody reads the one before it any more
+    const char *const la = lds + buf * BYTES, *const lb = la + BM * 128;
+    if (k + AHEAD * KT < k1) {
+      da.load(lds + free * BYTES, k1 - k - AHEAD * KT);
+      db.load(lds + free * BYTES + BM * 128, k1 - k - AHEAD * KT);
+    }
+    buf = buf + 1 == STAGES ? 0 : buf + 1;
+    free = free + 1 == STAGES ? 0 : free + 1;
+    u32x4 fa[2][FM], fb[2][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) fa[0][i] = TA::frag(la, wm + i * 32, h);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[0][j] = TB::frag(lb, wn + j * 32, h);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      u32x4 fa[FM], fb[FN];
+      if (s < 3) {
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = TA::frag(la, wm + i * 32, 2 * s + h);
+        for (int i = 0; i < FM; ++i) fa[(s + 1) & 1][i] = TA::frag(la, wm + i * 32, 2 * s + 2 + h);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = TB::frag(lb, wn + j * 32, 2 * s + h);
+        for (int j = 0; j < FN; ++j) fb[(s + 1) & 1][j] = TB::frag(lb, wn + j * 32, 2 * s + 2 + h);
+      }
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int i = 0; i < FM; ++i) step<T>(acc[i][j], fb[j], fa[i]);
+        for (int i = 0; i < FM; ++i) step<T>(acc[i][j], fb[s & 1][j], fa[s & 1][i]);
+    }
+    if constexpr (sizeof(T) < 4) {
+      constexpr int READS = (AA ? 2 : 1) * FM + (BA ? 2 : 1) * FN, EACH = (READS + FM * FN - 1) / (FM * FN);
+      __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+      for (int s = 0; s < 3; ++s) {
+#pragma unroll
+        for (int i = 0; i < FM * FN; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        }
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, FM * FN, 0);
     }
   }
   finish_block<T, FM, FN>(g, acc, lds, split, m0 + wm, n0 + wn);
@@ -376,6 +470,185 @@ __global__ __launch_bounds__(256) void k_join(Gemm g) {
   finish<4>(g.e, m, n, count, v);
 }
 
+// ---- few rows: the weights are read once, by vector instructions
+constexpr int kFewRows = 4;
+
+// V values of the stored type S as the type they are summed in.
+template <class S, class A, int V>
+__device__ __forceinline__ void numbers(const char *p, int n, A (&f)[V]) {
+  constexpr int W = V * (int)sizeof(S) / 4;
+  uint32_t w[W];
+  if (n >= V) {
+    __builtin_memcpy(w, p, V * sizeof(S));
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; j += 4) {
+      const u32x4 x = some_values<S>(p + 4 * j, min(n - j * 4 / (int)sizeof(S), 16 / (int)sizeof(S)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j + i < W) w[j + i] = x[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if constexpr (sizeof(S) == 4) f[i] = __builtin_bit_cast(float, w[i]);
+    else if constexpr (__is_same(S, bf16_t)) f[i] = __builtin_bit_cast(float, i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    else if constexpr (__is_same(S, f16_t)) f[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
+    else if constexpr (__is_same(S, int8_t)) f[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+    else f[i] = e4m3_value(w[i / 4], i % 4);
+  }
+}
+template <class S>
+struct SumOf {
+  typedef float type;
+};
+template <>
+struct SumOf<int8_t> {
+  typedef int32_t type;
+};
+template <class S, class A>
+__device__ __forceinline__ A number(const S *p) {
+  if constexpr (__is_same(S, e4m3_t)) return e4m3_value(p->bits, 0);
+  else return (A)*p;
+}
+template <class A>
+__device__ __forceinline__ A add_product(A a, A x, A w) {
+  if constexpr (__is_same(A, float)) return fmaf(x, w, a);
+  else return a + x * w;
+}
+
+// Weights across k: a block takes 8 C columns, C threads a line of them and 1024 / C lines at once.  No split of k, so no second launch:
+// one row of 4096 x 4096 bf16 16.8 us by 64 x 64 tiles in 8 splits.
+template <class S, int R, int C>
+__global__ __launch_bounds__(1024) void k_few_across(Gemm g) {
+  constexpr int LINES = 1024 / C;
+  typedef typename SumOf<S>::type A;
+  const int64_t n0 = near_tile(blockIdx.x, gridDim.x) * (8 * C) + threadIdx.x % C * 8;
+  const int count = g.n - n0 < 8 ? (int)(g.n - n0) : 8, line = threadIdx.x / C;
+  A acc[R][8];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[r][i] = 0;
+  const S *const px = (const S *)g.a.p;
+  const char *const pw = (const char *)g.b.p + n0 * (int64_t)sizeof(S);
+  auto add = [&](int64_t k, const A (&w)[8]) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      A x[1];
+      if (r < g.m) x[0] = number<S, A>(px + r * g.a.ld + k);
+      else x[0] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[r][i] = add_product(acc[r][i], x[0], w[i]);
+    }
+  };
+  if (count == 8) {
+    constexpr int AT = sizeof(S) == 4 ? 4 : 8;
+    int64_t k = line;
+    for (; k + (AT - 1) * LINES < g.k; k += AT * LINES) {
+      A w[AT][8];
+#pragma unroll
+      for (int j = 0; j < AT; ++j) numbers<S, A, 8>(pw + (k + j * LINES) * g.b.ld * (int64_t)sizeof(S), 8, w[j]);
+#pragma unroll
+      for (int j = 0; j < AT; ++j) add(k + j * LINES, w[j]);
+    }
+    for (; k < g.k; k += LINES) {
+      A w[8];
+      numbers<S, A, 8>(pw + k * g.b.ld * (int64_t)sizeof(S), 8, w);
+      add(k, w);
+    }
+  } else if (count > 0) {
+    for (int64_t k = line; k < g.k; k += LINES) {
+      A w[8];
+      numbers<S, A, 8>(pw + k * g.b.ld * (int64_t)sizeof(S), count, w);
+      add(k, w);
+    }
+  }
+  __shared__ A part[16][R][8 * C];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      A v = acc[r][i];
+#pragma unroll
+      for (int x = C; x < 64; x *= 2) v += __shfl_xor(v, x);
+      if ((threadIdx.x & 63) < C) part[threadIdx.x >> 6][r][threadIdx.x % C * 8 + i] = v;
+    }
+  __syncthreads();
+  const int r = threadIdx.x / C;
+  if (r >= R || r >= g.m || count <= 0) return;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    A t = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) t += part[w][r][threadIdx.x % C * 8 + i];
+    v[i] = (float)t;
+  }
+  finish<8>(g.e, r, n0, count, v);
+}
+
+// Weights along k: a wavefront takes two columns.
+template <class S, int R>
+__global__ __launch_bounds__(256) void k_few_along(Gemm g) {
+  typedef typename SumOf<S>::type A;
+  constexpr int E = 16 / (int)sizeof(S);
+  const int lane = threadIdx.x & 63;
+  const int64_t n0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 2;
+  if (n0 >= g.n) return;
+  const int64_t n1 = n0 + 1 < g.n ? n0 + 1 : n0;
+  const char *const px = (const char *)g.a.p, *const p0 = (const char *)g.b.p + n0 * g.b.ld * (int64_t)sizeof(S),
+             *const p1 = (const char *)g.b.p + n1 * g.b.ld * (int64_t)sizeof(S);
+  A acc[R][2];
+#pragma unroll
+  for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = 0;
+  for (int64_t k = lane * E; k < g.k; k += 64 * E) {
+    const int n = g.k - k < E ? (int)(g.k - k) : E;
+    A w0[E], w1[E], x[E];
+    numbers<S, A, E>(p0 + k * (int64_t)sizeof(S), n, w0);
+    numbers<S, A, E>(p1 + k * (int64_t)sizeof(S), n, w1);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= g.m) break;
+      numbers<S, A, E>(px + (r * g.a.ld + k) * (int64_t)sizeof(S), n, x);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        acc[r][0] = add_product(acc[r][0], x[i], w0[i]);
+        acc[r][1] = add_product(acc[r][1], x[i], w1[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      A v = acc[r][c];
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) v += __shfl_xor(v, x);
+      acc[r][c] = v;
+    }
+  if (lane == 0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (r >= g.m) break;
+      float v[4] = {(float)acc[r][0], (float)acc[r][1], 0, 0};
+      finish<4>(g.e, r, n0, g.n - n0 < 2 ? 1 : 2, v);
+    }
+  }
+}
+template <class S, int R>
+hipError_t launch_few_rows(const Gemm &g, hipStream_t s) {
+  // 16 columns a block where 32 would leave compute units idle.
+  if (g.b.across && g.n < 32 * 256) k_few_across<S, R, 2><<<dim3((unsigned)((g.n + 15) / 16)), 1024, 0, s>>>(g);
+  else if (g.b.across) k_few_across<S, R, 4><<<dim3((unsigned)((g.n + 31) / 32)), 1024, 0, s>>>(g);
+  else k_few_along<S, R><<<dim3((unsigned)((g.n + 7) / 8)), 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+template <class S>
+hipError_t launch_few(const Gemm &g, hipStream_t s) {
+  return g.m == 1 ? launch_few_rows<S, 1>(g, s) : g.m == 2 ? launch_few_rows<S, 2>(g, s) : launch_few_rows<S, 4>(g, s);
+}
+
 template <class T>
 hipError_t join(const Gemm &g, hipStream_t s) {
   const hipError_t err = hipGetLastError();
@@ -390,10 +663,10 @@ hipError_t launch_tile(const Gemm &g, hipStream_t s) {
   k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
   return join<T>(g, s);
 }
-template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN>
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
 hipError_t launch_direct(const Gemm &g, hipStream_t s) {
   const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
-  k_gemm_direct<T, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
+  k_gemm_direct<T, AA, BA, BM, BN, WM, WN, STAGES><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
   return join<T>(g, s);
 }
 
@@ -411,10 +684,11 @@ hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {
   if constexpr (__is_same(T, S)) {
     if (direct_ok<T>(g.a, g.m, g.k) && direct_ok<T>(g.b, g.n, g.k)) {
       if constexpr (sizeof(T) < 4) {
-        if (p.tile == 2) return launch_direct<T, AA, BA, 256, 256, 2, 4>(g, s);
+        if (p.tile == 2) return launch_direct<T, AA, BA, 256, 256, 2, 4, 2>(g, s);
       }
-      if (p.tile >= 1) return launch_direct<T, AA, BA, 128, 128, 2, 2>(g, s);
-      return launch_direct<T, AA, BA, 64, 64, 2, 2>(g, s);
+      if (p.tile >= 1 && !AA && g.k * (int64_t)sizeof(T) <= 128) return launch_direct<T, AA, BA, 128, 128, 2, 2, 1>(g, s);
+      if (p.tile >= 1) return launch_direct<T, AA, BA, 128, 128, 2, 2, 2>(g, s);
+      return launch_direct<T, AA, BA, 64, 64, 2, 2, 4>(g, s);
     }
   }
   if (p.tile == 0) return launch_tile<T, S, AA, BA, 64, 64, 2, 2>(g, s);
@@ -427,6 +701,7 @@ hipError_t launch_type(const Gemm &g, const GemmPlan &p, hipStream_t s) {
     if (g.a.across && g.b.across) return launch_layout<T, S, true, true>(g, p, s);
   }
   if (g.a.across) return hipErrorInvalidValue;
+  if (g.m <= kFewRows) return launch_few<S>(g, s);
   return g.b.across ? launch_layout<T, S, false, true>(g, p, s) : launch_layout<T, S, false, false>(g, p, s);
 }
 

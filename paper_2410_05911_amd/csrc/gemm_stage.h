@@ -23,6 +23,19 @@ __device__ __forceinline__ u32x4 any16(const char *p) {   // at any address
   return v;
 }
 
+// Waits until at most N of the loads issued so far are not there yet.
+template <int N>
+__device__ __forceinline__ void wait_loads_but() {
+  static_assert(N < 64, "the counter's bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+}
+// A block's barrier behind which its LDS accesses are done, that leaves loads from memory on their way.
+__device__ __forceinline__ void barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Loads that go to LDS without passing through registers: 16 bytes a lane from byte `offset` of a buffer (zeros from `size` on) to
 // the wavefront's place `lds` + 16 lane.  Written as assembly because the compiler waits for such loads before any read of LDS,
 // whichever part of it that reads; here wait_loads() says when they have to be there.  (They write no registers.  One

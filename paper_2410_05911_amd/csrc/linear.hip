@@ -5,9 +5,10 @@ namespace aecct {
 
 GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b) {
   GemmPlan p{1, 1, 0};
+  if (m <= kFewRows && !across_a) return p;
   auto tiles = [&](int t) { return (m + kTileSide[t][0] - 1) / kTileSide[t][0] * ((n + kTileSide[t][1] - 1) / kTileSide[t][1]); };
   if (tiles(1) < 192) p.tile = 0;
-  else if (tiles(2) >= 256) p.tile = 2;
+  else if (tiles(2) >= 256 && k * (type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2) >= 1024) p.tile = 2;
   const int64_t size = type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2, t = tiles(p.tile), kt = (k * size + 127) / 128;
   if (t > 0 && t < 256) {
     int64_t s = (512 + t - 1) / t;
@@ -34,13 +35,14 @@ hipError_t launch_gemm(int type, const Gemm &g, const GemmPlan &plan, hipStream_
 namespace {
 
 // act'(z).  Where a factor is 0 the other may be infinite: such a product's limit is 0.
-__device__ __forceinline__ float slope(float z, int act) {
+__device__ __forceinline__ float slope(float z, int act, bool f32) {
   if (act == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
   if (act == kActGelu) {
-    const float density = expf(-0.5f * z * z) * 0.39894228040143268f;
-    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + (density == 0.0f ? 0.0f : z * density);
+    float e;
+    const float phi = normal(z, e), density = e * 0.39894228040143268f;
+    return (f32 ? 0.5f * (1.0f + erff(z * 0.70710678118654752f)) : phi) + (density == 0.0f ? 0.0f : z * density);
   }
-  const float p = 1.0f / (1.0f + expf(-z)), q = 1.0f / (1.0f + expf(z));   // q = 1 - p
+  const float p = logistic(z), q = logistic(-z);   // q = 1 - p
   if (p == 0.0f || q == 0.0f) return p;
   return p * (1.0f + z * q);
 }
@@ -61,7 +63,7 @@ __global__ __launch_bounds__(256) void k_slope(Slope a) {
         float z[8];
         load_part<T, 8>((const T *)a.z + row * a.ldz + n0, count, z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] *= slope(z[i], a.act);
+        for (int i = 0; i < 8; ++i) d[i] *= slope(z[i], a.act, sizeof(T) == 4);
         if (a.dz) store_part<T, 8>((T *)a.dz + row * a.lddz + n0, count, d);
       }
 #pragma unroll
@@ -82,12 +84,20 @@ __global__ __launch_bounds__(256) void k_slope(Slope a) {
   }
 }
 
+// 16 columns a block, 16 threads each.
 __global__ __launch_bounds__(256) void k_column_sum(const float *part, int64_t blocks, int64_t n, float *out) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= n) return;
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int64_t at = (int64_t)blockIdx.x * 16 + c;
   float t = 0;
-  for (int64_t b = 0; b < blocks; ++b) t += part[b * n + c];
-  out[c] = t;
+  if (at < n)
+    for (int64_t b = r; b < blocks; b += 16) t += part[b * n + at];
+  __shared__ float s[16][17];
+  s[r][c] = t;
+  __syncthreads();
+  if (r || at >= n) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) t += s[i][c];
+  out[at] = t;
 }
 
 }  // namespace
@@ -95,7 +105,7 @@ __global__ __launch_bounds__(256) void k_column_sum(const float *part, int64_t b
 int64_t slope_blocks(int64_t rows, int64_t n) {
   const int64_t across = (n + kSlopeColumns - 1) / kSlopeColumns;
   int64_t b = (1024 + across - 1) / across;
-  const int64_t most = (rows + 63) / 64;
+  const int64_t most = (rows + 15) / 16;
   if (b > most) b = most;
   return b < 1 ? 1 : b;
 }
@@ -111,7 +121,7 @@ hipError_t launch_slope(int type, const Slope &a, hipStream_t s) {
   }
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || !a.part) return err;
-  k_column_sum<<<dim3((unsigned)((a.n + 255) / 256)), 256, 0, s>>>(a.part, blocks, a.n, a.dbias);
+  k_column_sum<<<dim3((unsigned)((a.n + 15) / 16)), 256, 0, s>>>(a.part, blocks, a.n, a.dbias);
   return hipGetLastError();
 }
 

@@ -62,6 +62,14 @@ __device__ __forceinline__ u32x4 widen(uint32_t low, uint32_t high) {
                __builtin_bit_cast(uint32_t, d)};
 }
 
+// Value `i` of four e4m3 values.
+__device__ __forceinline__ float e4m3_value(uint32_t w, int i) {
+  typedef float two __attribute__((ext_vector_type(2)));
+  const two v = i < 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  const float low = v[0], high = v[1];
+  return i % 2 ? high : low;
+}
+
 // ---- tiles in LDS
 // "Along k": a row of the tile is 128 bytes of k, its chunk c at place c ^ (row & 7), so that a wavefront's reads of one
 // chunk of 32 rows fall on different banks.
