@@ -580,7 +580,7 @@ typedef struct aecct_linear_map_args {
   void *y;         int64_t ldy;      /* [rows][out] out; may be res itself */
 } aecct_linear_map_args;
 /* Inputs may be rows of any stride >= 0 (w: its width at least), outputs of strides >= out.  The workspace may be NULL
- * where its size is 0 (host call; reads sizes and types only).  Errors: INVALID_ARG, UNSUPPORTED (sizes beyond the above,
+ * where its size is 0 (host call; reads no address).  Errors: INVALID_ARG, UNSUPPORTED (sizes beyond the above,
  * more than 2^22 tiles of 64 x 64 outputs), WORKSPACE_TOO_SMALL, DEVICE. */
 aecct_status aecct_linear_map_workspace_size(const aecct_linear_map_args *a, size_t *bytes);
 aecct_status aecct_linear_map(const aecct_linear_map_args *a, void *workspace, size_t workspace_bytes, void *stream);

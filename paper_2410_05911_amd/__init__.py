@@ -491,14 +491,42 @@ def rms_norm_grad(h, dy, gain=None, dres=None, eps: float = 1e-5, *, dh=None, dg
     return dh, dgain
 
 
-def _with_workspace(call: str, args, device: int):
-    """Sizes the call's workspace, takes it from torch (so on its current stream), and makes the call."""
+@functools.lru_cache(maxsize=None)
+def _entry(call: str):
+    return getattr(lib(), call), getattr(lib(), call + "_workspace_size")
+
+
+_SIZES: dict = {}
+
+
+def _with_workspace(call: str, args, index: int, like, key):
+    """Takes the call's workspace from torch (so on its current stream) and makes the call.  Workspace sizes go by `key`."""
+    f, size_of = _entry(call)
+    need = _SIZES.get(key)
+    if need is None:
+        size = C.c_size_t()
+        _check(size_of(C.byref(args), C.byref(size)), call + "_workspace_size")
+        if len(_SIZES) >= 4096:
+            _SIZES.clear()
+        need = _SIZES[key] = size.value
+    ws = None
+    if need:
+        ws = like.new_empty(need, dtype=_uint8())
+        _check(f(C.byref(args), ws.data_ptr(), need, _current_stream(index)), call)
+    else:
+        _check(f(C.byref(args), None, 0, _current_stream(index)), call)
+
+
+@functools.lru_cache(maxsize=None)
+def _uint8():
     import torch
-    size = C.c_size_t()
-    _check(getattr(lib(), call + "_workspace_size")(C.byref(args), C.byref(size)), call + "_workspace_size")
-    ws = torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
-    _check(getattr(lib(), call)(C.byref(args), ws.data_ptr() if ws is not None else None, size.value, _current_stream(device)),
-           call)
+    return torch.uint8
+
+
+@functools.lru_cache(maxsize=None)
+def _float32():
+    import torch
+    return torch.float32
 
 
 def _act_code(act) -> int:
@@ -511,14 +539,14 @@ def _act_code(act) -> int:
 def _vector_of(t, n: int, index: int, what):
     if t is None:
         return None
-    if t.numel() != n or not t.is_contiguous() or t.get_device() != index or str(t.dtype) != "torch.float32":
+    if t.numel() != n or not t.is_contiguous() or t.get_device() != index or t.dtype is not _float32():
         raise ValueError(f"{what} must be {n} contiguous float32 values on cuda:{index}")
     return t.data_ptr()
 
 
 def _map_of(w, dtype, index: int):
     """(address, stride, turned) of the weights [in, out] of a map, in rows or (turned) in columns."""
-    if w.dim() != 2 or w.dtype != dtype or w.get_device() != index or w.numel() == 0:
+    if w.dim() != 2 or w.dtype is not dtype or w.get_device() != index or w.numel() == 0:
         raise ValueError(f"w must be {dtype} [in, out] on cuda:{index}")
     (inputs, outputs), (a, b) = w.shape, w.stride()
     if b == 1 or outputs == 1:
@@ -547,34 +575,38 @@ def linear(x, w, bias=None, res=None, act="none", *, alpha=None, scale=None, y=N
     index = x.get_device()
     _on_current_gpu(index)
     inputs, outputs = w.shape
-    shape, out_shape = x.shape, x.shape[:-1] + (outputs,)
+    shape, dtype = x.shape, x.dtype
+    out_shape = shape[:-1] + (outputs,)
     rows = x.numel() // inputs if inputs else 0
-    code = CODE_I8 if x.dtype == torch.int8 else CODE_E4M3 if x.dtype == torch.float8_e4m3fn else CODE_NONE
-    if code == CODE_NONE:
-        type = _dtype_code(x)
-        if alpha is not None or scale is not None:
-            raise ValueError("alpha and scale go with codes")
-        if y_type is not None and y_type != x.dtype:
-            raise ValueError("without codes y is of x's type")
-        y_type = x.dtype
-    else:
-        type = F32
+    type, code = _DTYPES.get(dtype), CODE_NONE
+    if type is None:
+        code = CODE_I8 if dtype is torch.int8 else CODE_E4M3 if dtype is torch.float8_e4m3fn else CODE_NONE
+        type = F32 if code else _dtype_code(x)
+    if code:
         if alpha is None or scale is None:
             raise ValueError("codes need alpha and scale")
         y_type = torch.float32 if y_type is None else y_type
-    pw, ldw, turned = _map_of(w, x.dtype, index)
-    px, ldx = _rows_of(x, shape, x.dtype, index, "x")
-    pres, ldres = _rows_of(res, out_shape, y_type, index, "res")
+    else:
+        if alpha is not None or scale is not None:
+            raise ValueError("alpha and scale go with codes")
+        if y_type is not None and y_type != dtype:
+            raise ValueError("without codes y is of x's type")
+        y_type = dtype
+    pw, ldw, turned = _map_of(w, dtype, index)
+    px, ldx = _rows_of(x, shape, dtype, index, "x")
+    pres, ldres = (None, 0) if res is None else _rows_of(res, out_shape, y_type, index, "res")
     if y is None:
-        y = torch.empty(out_shape, dtype=y_type, device=x.device)
+        y = x.new_empty(out_shape, dtype=y_type)
+        py, ldy = y.data_ptr(), outputs
+    else:
+        py, ldy = _rows_of(y, out_shape, y_type, index, "y")
     if z is None and with_z:
-        z = torch.empty(out_shape, dtype=y_type, device=x.device)
-    py, ldy = _rows_of(y, out_shape, y_type, index, "y")
-    pz, ldz = _rows_of(z, out_shape, y_type, index, "z")
+        z = x.new_empty(out_shape, dtype=y_type)
+    pz, ldz = (None, 0) if z is None else _rows_of(z, out_shape, y_type, index, "z")
     a = LinearMapArgs(rows, inputs, outputs, type, code, _dtype_code(y), _act_code(act), turned, px, ldx, pw, ldw,
                       _vector_of(alpha, rows, index, "alpha"), _vector_of(scale, outputs, index, "scale"),
                       _vector_of(bias, outputs, index, "bias"), pres, ldres, pz, ldz, py, ldy)
-    _with_workspace("aecct_linear_map", a, index)
+    _with_workspace("aecct_linear_map", a, index, x, ("linear", rows, inputs, outputs, type, code, turned, ldw))
     return y, z
 
 
@@ -604,11 +636,11 @@ def linear_grad(x, w, dy, z=None, act="none", *, dx=None, dw=None, dbias=None, d
     pdy, lddy = _rows_of(dy, out_shape, dtype, index, "dy")
     pz, ldz = _rows_of(z, out_shape, dtype, index, "z")
     if dx is None and with_dx:
-        dx = torch.empty(shape, dtype=dtype, device=x.device)
+        dx = x.new_empty(shape)
     if dw is None and with_dw:
-        dw = torch.empty((inputs, outputs), dtype=dw_type or dtype, device=x.device)
+        dw = x.new_empty((inputs, outputs), dtype=dw_type or dtype)
     if dbias is None and with_dbias:
-        dbias = torch.empty(outputs, dtype=torch.float32, device=x.device)
+        dbias = x.new_empty(outputs, dtype=torch.float32)
     if dx is None and dw is None and dbias is None:
         raise ValueError("no gradient is asked for")
     pdx, lddx = _rows_of(dx, shape, dtype, index, "dx")
@@ -618,7 +650,8 @@ def linear_grad(x, w, dy, z=None, act="none", *, dx=None, dw=None, dbias=None, d
     pdw, lddw = _rows_of(dw, w.shape, dw_dtype, index, "dw")
     a = LinearMapGradArgs(rows, inputs, outputs, type, code, turned, F32 if dw is None else _dtype_code(dw), px, ldx, pw, ldw,
                           pdy, lddy, pz, ldz, pdx, lddx, pdw, lddw, _vector_of(dbias, outputs, index, "dbias"))
-    _with_workspace("aecct_linear_map_grad", a, index)
+    _with_workspace("aecct_linear_map_grad", a, index, x, ("linear_grad", rows, inputs, outputs, type, code, turned, ldw, dx is None,
+                                                            dw is None, dbias is None))
     return dx, dw, dbias
 
 
@@ -650,8 +683,10 @@ def dropout(x, p: float, seed: int, offset=0, res=None, *, y=None, stream=None):
     px, ldx = _rows_of(x, shape, dtype, index, "x")
     pres, ldres = _rows_of(res, shape, dtype, index, "res")
     if y is None:
-        y = torch.empty(shape, dtype=dtype, device=x.device)
-    py, ldy = _rows_of(y, shape, dtype, index, "y")
+        y = x.new_empty(shape)
+        py, ldy = y.data_ptr(), d
+    else:
+        py, ldy = _rows_of(y, shape, dtype, index, "y")
     a = DropoutArgs(x.numel() // d, d, _dtype_code(x), p, seed, offset, offset_device, px, ldx, pres, ldres, py, ldy)
     _check(lib().aecct_dropout(C.byref(a), _current_stream(index)), "aecct_dropout")
     return y
@@ -710,15 +745,15 @@ def cross_attention(q, k, v, lengths=None, mask=None, scale=None, *, o=None, lse
             return cross_attention(q, k, v, lengths, mask, scale, o=o, lse=lse, with_lse=with_lse)
     index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        o = q.new_empty(q.shape)
     lse_shape = (sizes[0], sizes[3], sizes[1])
     if lse is None and with_lse:
-        lse = torch.empty(lse_shape, dtype=torch.float32, device=q.device)
+        lse = q.new_empty(lse_shape, dtype=_float32())
     elif lse is not None and lse.shape != lse_shape:
         raise ValueError(f"lse must be {lse_shape}")
     a = CrossAttentionArgs(*sizes, hq, hk, hv, plengths, pmask, ldmask, _heads_of(o, q.shape, q.dtype, index, "o"),
                            _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"))
-    _with_workspace("aecct_cross_attention", a, index)
+    _with_workspace("aecct_cross_attention", a, index, q, ("attention", *sizes[:7], pmask is None))
     return o, lse
 
 
@@ -733,13 +768,12 @@ def cross_attention_grad(q, k, v, o, lse, dout, lengths=None, mask=None, scale=N
             return cross_attention_grad(q, k, v, o, lse, dout, lengths, mask, scale, dq=dq, dk=dk, dv=dv, with_dq=with_dq,
                                         with_dkv=with_dkv)
     index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
-    new = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
     if dq is None and with_dq:
-        dq = new(q)
+        dq = q.new_empty(q.shape)
     if dk is None and (with_dkv or dv is not None):
-        dk = new(k)
+        dk = k.new_empty(k.shape)
     if dv is None and dk is not None:
-        dv = new(v)
+        dv = v.new_empty(v.shape)
     if dq is None and dk is None:
         raise ValueError("no gradient is asked for")
     if lse.shape != (sizes[0], sizes[3], sizes[1]):
@@ -749,7 +783,7 @@ def cross_attention_grad(q, k, v, o, lse, dout, lengths=None, mask=None, scale=N
                                _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"), plengths, pmask, ldmask,
                                _heads_of(dq, q.shape, q.dtype, index, "dq"), _heads_of(dk, k.shape, q.dtype, index, "dk"),
                                _heads_of(dv, k.shape, q.dtype, index, "dv"))
-    _with_workspace("aecct_cross_attention_grad", a, index)
+    _with_workspace("aecct_cross_attention_grad", a, index, q, ("attention_grad", *sizes[:7], pmask is None))
     return dq, dk, dv
 
 

@@ -151,18 +151,35 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Blocks in an order that keeps those of one XCD (every eighth block) on neighbouring numbers.
-__device__ __forceinline__ int64_t near_tile(int64_t block, int64_t all) {
-  const int64_t share = all / 8;
-  return block < share * 8 ? (block % 8) * share + block / 8 : block;
+// Blocks in an order that keeps those of one XCD (every eighth block) on neighbouring numbers.  (Numbers of blocks and tiles are 32-bit:
+// a 64-bit division takes 150 instructions, and several of them a microsecond of a small product.)
+__device__ __forceinline__ uint32_t near_tile(uint32_t block, uint32_t all) {
+  const uint32_t share = all / 8;
+  return block < share * 8 ? block % 8 * share + block / 8 : block;
 }
 // Tiles in such an order, bands of 8 rows of tiles, column by column.
-__device__ __forceinline__ void tile_of(int64_t block, int64_t tm, int64_t tn, int64_t &im, int64_t &in) {
-  const int64_t at = near_tile(block, tm * tn);
-  const int64_t band = at / (8 * tn), first = band * 8, height = tm - first < 8 ? tm - first : 8, rest = at - band * 8 * tn;
-  im = first + rest % height;
+__device__ __forceinline__ void tile_of(uint32_t block, uint32_t tm, uint32_t tn, uint32_t &im, uint32_t &in) {
+  const uint32_t at = near_tile(block, tm * tn);
+  const uint32_t band = at / (8 * tn), first = band * 8, height = min(tm - first, 8u), rest = at - band * 8 * tn;
   in = rest / height;
+  im = first + rest - in * height;
 }
+// A block's tile and its share of k: whole tiles of k to each split; only the last one has a ragged end.
+struct Share {
+  int m0, n0, k0, k1, split;
+  template <int BM, int BN, int KT>
+  static __device__ __forceinline__ Share of(const Gemm &g) {
+    const uint32_t tm = (uint32_t)(g.m + BM - 1) / BM, tn = (uint32_t)(g.n + BN - 1) / BN, tiles = tm * tn;
+    const uint32_t split = g.splits > 1 ? blockIdx.x / tiles : 0, kt = (uint32_t)(g.k + KT - 1) / KT;
+    uint32_t im, in, first = 0, last = kt;
+    tile_of(blockIdx.x - split * tiles, tm, tn, im, in);
+    if (g.splits > 1) {
+      first = kt * split / (uint32_t)g.splits;
+      last = kt * (split + 1) / (uint32_t)g.splits;
+    }
+    return {(int)(im * BM), (int)(in * BN), (int)(first * KT), min(g.k, (int)(last * KT)), (int)split};
+  }
+};
 
 // A wavefront's FM x FN sums from (m0, n0) on through the epilogue: 32 rows at a time go through LDS, so that a lane then has eight
 // neighbouring columns and neighbouring lanes a row's (stored as they lie in registers, in pieces of 16 or 8 bytes 32 rows apart,
@@ -256,13 +273,8 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
   constexpr int AHEAD = CA + CB <= 4 ? 3 : 1;   // tiles on their way in registers
   static_assert(TA::SLOTS % NT == 0 && TB::SLOTS % NT == 0, "whole slots");
   __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
-  const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
-  const int split = (int)(blockIdx.x / (tm * tn));
-  int64_t im, in;
-  tile_of(blockIdx.x % (tm * tn), tm, tn, im, in);
-  const int64_t m0 = im * BM, n0 = in * BN;
-  // Whole tiles of k to each split; only the last one has a ragged end.
-  const int64_t kt = (g.k + KT - 1) / KT, k0 = kt * split / g.splits * KT, k1 = min(g.k, kt * (split + 1) / g.splits * KT);
+  const Share at = Share::of<BM, BN, KT>(g);
+  const int m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1, split = at.split;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
   const Through<T, S, AA, BM, NT> ta(g.a, g.m, g.k, m0);
@@ -285,7 +297,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
     }
   }
   int buf = 0;
-  for (int64_t k = k0; k < k1;) {
+  for (int k = k0; k < k1;) {
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d) {
       if (k >= k1) break;
@@ -344,7 +356,7 @@ struct Direct {
     }
   }
   // The next tile into LDS; `left` of its k are there.
-  __device__ __forceinline__ void load(char *lds, int64_t left) {
+  __device__ __forceinline__ void load(char *lds, int left) {
     const BufferOf r(p, OUT);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
@@ -369,12 +381,8 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
   constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT, BYTES = (BM + BN) * 128;
   constexpr int STRIPS = WM * WN * 32 * (FN * 32 + 4) * 4;   // what finish_block takes
   __shared__ __attribute__((aligned(16))) char lds[STAGES * BYTES > STRIPS ? STAGES * BYTES : STRIPS];
-  const int64_t tm = (g.m + BM - 1) / BM, tn = (g.n + BN - 1) / BN;
-  const int split = (int)(blockIdx.x / (tm * tn));
-  int64_t im, in;
-  tile_of(blockIdx.x % (tm * tn), tm, tn, im, in);
-  const int64_t m0 = im * BM, n0 = in * BN;
-  const int64_t kt = (g.k + KT - 1) / KT, k0 = kt * split / g.splits * KT, k1 = min(g.k, kt * (split + 1) / g.splits * KT);
+  const Share at = Share::of<BM, BN, KT>(g);
+  const int m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1, split = at.split;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
   Direct<T, AA, BM, NT> da;
@@ -398,7 +406,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
     }
   }
   int buf = 0, free = AHEAD;
-  for (int64_t k = k0; k < k1; k += KT) {
+  for (int k = k0; k < k1; k += KT) {
     // Loads come back in order: the tile is there when only those of the tiles after it are left.
     if (k + (AHEAD - 1) * KT < k1) wait_loads_but<(AHEAD - 1) * (Direct<T, AA, BM, NT>::COUNT + Direct<T, BA, BN, NT>::COUNT)>();
     else wait_loads();
@@ -448,19 +456,25 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
 // The splits' sums of four outputs a thread, in the order of the splits, and the epilogue.
 template <bool INT>
 __global__ __launch_bounds__(256) void k_join(Gemm g) {
-  const int64_t per = (g.n + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= g.m * per) return;
-  const int64_t m = at / per, n = at % per * 4;
+  const uint32_t per = (uint32_t)(g.n + 3) / 4, at = blockIdx.x * 256 + threadIdx.x;
+  const int m = (int)(at / per), n = (int)(at % per) * 4;
+  if (m >= g.m) return;
   const int count = g.n - n < 4 ? (int)(g.n - n) : 4;
   float v[4] = {0, 0, 0, 0};
   int32_t w[4] = {0, 0, 0, 0};
-  for (int s = 0; s < g.splits; ++s) {
-    float p[4];
-    load_part<float, 4>((const float *)g.part + ((int64_t)s * g.m + m) * g.n + n, count, p);
+  const float *const part = (const float *)g.part + (int64_t)m * g.n + n;
+  for (int s = 0; s < g.splits; s += 8) {
+    float p[8][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (INT) w[i] += __builtin_bit_cast(int32_t, p[i]);
-      else v[i] += p[i];
+    for (int j = 0; j < 8; ++j) load_part<float, 4>(part + (int64_t)min(s + j, g.splits - 1) * g.m * g.n, count, p[j]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (s + j >= g.splits) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (INT) w[i] += __builtin_bit_cast(int32_t, p[j][i]);
+        else v[i] += p[j][i];
+      }
     }
   }
   if constexpr (INT) {
@@ -470,17 +484,28 @@ __global__ __launch_bounds__(256) void k_join(Gemm g) {
   finish<4>(g.e, m, n, count, v);
 }
 
+template <class T>
+hipError_t join(const Gemm &g, hipStream_t s) {
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || !g.part) return err;
+  const int64_t join = ((int64_t)g.m * ((g.n + 3) / 4) + 255) / 256;
+  k_join<__is_same(T, int8_t)><<<dim3((unsigned)join), dim3(256), 0, s>>>(g);
+  return hipGetLastError();
+}
 // ---- few rows: the weights are read once, by vector instructions
-constexpr int kFewRows = 4;
+constexpr int kFewRows = 4, kFewRound = 256;   // k of a split at least
 
-// V values of the stored type S as the type they are summed in.
-template <class S, class A, int V>
-__device__ __forceinline__ void numbers(const char *p, int n, A (&f)[V]) {
-  constexpr int W = V * (int)sizeof(S) / 4;
+// V values of the stored type S: as they lie in memory (the first n), and as the type they are summed in.
+template <class S, int V>
+struct Stored {
+  static constexpr int W = V * (int)sizeof(S) / 4;
   uint32_t w[W];
-  if (n >= V) {
-    __builtin_memcpy(w, p, V * sizeof(S));
-  } else {
+  __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(w, p, V * sizeof(S)); }
+  __device__ __forceinline__ void load(const char *p, int n) {
+    if (n >= V) {
+      load(p);
+      return;
+    }
 #pragma unroll
     for (int j = 0; j < W; j += 4) {
       const u32x4 x = some_values<S>(p + 4 * j, min(n - j * 4 / (int)sizeof(S), 16 / (int)sizeof(S)));
@@ -489,15 +514,18 @@ __device__ __forceinline__ void numbers(const char *p, int n, A (&f)[V]) {
         if (j + i < W) w[j + i] = x[i];
     }
   }
+  template <class A>
+  __device__ __forceinline__ void numbers(A (&f)[V]) const {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    if constexpr (sizeof(S) == 4) f[i] = __builtin_bit_cast(float, w[i]);
-    else if constexpr (__is_same(S, bf16_t)) f[i] = __builtin_bit_cast(float, i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
-    else if constexpr (__is_same(S, f16_t)) f[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
-    else if constexpr (__is_same(S, int8_t)) f[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
-    else f[i] = e4m3_value(w[i / 4], i % 4);
+    for (int i = 0; i < V; ++i) {
+      if constexpr (sizeof(S) == 4) f[i] = __builtin_bit_cast(float, w[i]);
+      else if constexpr (__is_same(S, bf16_t)) f[i] = __builtin_bit_cast(float, i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+      else if constexpr (__is_same(S, f16_t)) f[i] = (float)__builtin_bit_cast(f16_t, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
+      else if constexpr (__is_same(S, int8_t)) f[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+      else f[i] = e4m3_value(w[i / 4], i % 4);
+    }
   }
-}
+};
 template <class S>
 struct SumOf {
   typedef float type;
@@ -511,20 +539,27 @@ __device__ __forceinline__ A number(const S *p) {
   if constexpr (__is_same(S, e4m3_t)) return e4m3_value(p->bits, 0);
   else return (A)*p;
 }
+__device__ __forceinline__ uint64_t mul_wide(int a, uint32_t b) { return (uint64_t)(uint32_t)a * b; }
 template <class A>
 __device__ __forceinline__ A add_product(A a, A x, A w) {
   if constexpr (__is_same(A, float)) return fmaf(x, w, a);
   else return a + x * w;
 }
 
-// Weights across k: a block takes 8 C columns, C threads a line of them and 1024 / C lines at once.  No split of k, so no second launch:
-// one row of 4096 x 4096 bf16 16.8 us by 64 x 64 tiles in 8 splits.
-template <class S, int R, int C>
-__global__ __launch_bounds__(1024) void k_few_across(Gemm g) {
-  constexpr int LINES = 1024 / C;
+// Weights across k: a block takes 64 columns, so whole lines of 128 bytes in 16 bits, eight threads a line of them and 32 lines at once;
+// x goes through LDS as numbers.  k is split over blocks: a compute unit alone gets about 30 GB/s (one row of 4096 x 4096 bf16 in
+// blocks that sum all of k: 64 columns each 18 us, 32 columns 15, 16 columns, a quarter of a line, 13).
+template <class S, int R, int NT>
+__global__ __launch_bounds__(NT) void k_few_across(Gemm g) {
   typedef typename SumOf<S>::type A;
-  const int64_t n0 = near_tile(blockIdx.x, gridDim.x) * (8 * C) + threadIdx.x % C * 8;
-  const int count = g.n - n0 < 8 ? (int)(g.n - n0) : 8, line = threadIdx.x / C;
+  constexpr int LINES = NT / 8, AT = 8, ROUND = LINES * AT;   // loads on their way, k of a round
+  __shared__ __attribute__((aligned(16))) A sx[ROUND][R];
+  const uint32_t tn = (uint32_t)(g.n + 63) / 64, at = near_tile(blockIdx.x, gridDim.x);
+  const int split = (int)(at / tn), line = threadIdx.x >> 3, col = (threadIdx.x & 7) * 8;
+  const int n0 = (int)(at - split * tn) * 64 + col, count = min(g.n - n0, 8);
+  const uint32_t rounds = (uint32_t)(g.k + ROUND - 1) / ROUND;
+  const int begin = (int)(rounds * split / (uint32_t)g.splits) * ROUND,
+            end = min(g.k, (int)(rounds * (split + 1) / (uint32_t)g.splits) * ROUND);
   A acc[R][8];
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -532,60 +567,60 @@ __global__ __launch_bounds__(1024) void k_few_across(Gemm g) {
     for (int i = 0; i < 8; ++i) acc[r][i] = 0;
   const S *const px = (const S *)g.a.p;
   const char *const pw = (const char *)g.b.p + n0 * (int64_t)sizeof(S);
-  auto add = [&](int64_t k, const A (&w)[8]) {
+  const uint32_t step = (uint32_t)(g.b.ld * (int64_t)sizeof(S));   // below 2^32: few_ok
+  for (int k0 = begin; k0 < end; k0 += ROUND) {
+    Stored<S, 8> w[AT];
+    if (count == 8) {
+      // Lines past the end are the last one again: no branch, so that all loads are on their way before one is waited for.
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      A x[1];
-      if (r < g.m) x[0] = number<S, A>(px + r * g.a.ld + k);
-      else x[0] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[r][i] = add_product(acc[r][i], x[0], w[i]);
+      for (int j = 0; j < AT; ++j) w[j].load(pw + mul_wide(min(k0 + line + j * LINES, end - 1), step));
     }
-  };
-  if (count == 8) {
-    constexpr int AT = sizeof(S) == 4 ? 4 : 8;
-    int64_t k = line;
-    for (; k + (AT - 1) * LINES < g.k; k += AT * LINES) {
-      A w[AT][8];
+    __builtin_amdgcn_sched_barrier(0);
+    if (k0 != begin) __syncthreads();
+    for (int i = threadIdx.x; i < ROUND && k0 + i < end; i += NT) {
 #pragma unroll
-      for (int j = 0; j < AT; ++j) numbers<S, A, 8>(pw + (k + j * LINES) * g.b.ld * (int64_t)sizeof(S), 8, w[j]);
+      for (int r = 0; r < R; ++r) sx[i][r] = r < g.m ? number<S, A>(px + r * g.a.ld + k0 + i) : (A)0;
+    }
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < AT; ++j) add(k + j * LINES, w[j]);
-    }
-    for (; k < g.k; k += LINES) {
-      A w[8];
-      numbers<S, A, 8>(pw + k * g.b.ld * (int64_t)sizeof(S), 8, w);
-      add(k, w);
-    }
-  } else if (count > 0) {
-    for (int64_t k = line; k < g.k; k += LINES) {
-      A w[8];
-      numbers<S, A, 8>(pw + k * g.b.ld * (int64_t)sizeof(S), count, w);
-      add(k, w);
+    for (int j = 0; j < AT; ++j) {
+      const int k = k0 + line + j * LINES;
+      if (k >= end) break;
+      if (count < 8) w[j].load(pw + mul_wide(k, step), count);
+      A f[8];
+      w[j].numbers(f);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const A x = sx[line + j * LINES][r];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[r][i] = add_product(acc[r][i], x, f[i]);
+      }
     }
   }
-  __shared__ A part[16][R][8 * C];
+  // The lines' sums: eight of them in a wavefront by exchanges, then over the wavefronts.
+  __shared__ A part[NT / 64][R][64];
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       A v = acc[r][i];
 #pragma unroll
-      for (int x = C; x < 64; x *= 2) v += __shfl_xor(v, x);
-      if ((threadIdx.x & 63) < C) part[threadIdx.x >> 6][r][threadIdx.x % C * 8 + i] = v;
+      for (int x = 8; x < 64; x *= 2) v += __shfl_xor(v, x);
+      if ((threadIdx.x & 63) < 8) part[threadIdx.x >> 6][r][col + i] = v;
     }
   __syncthreads();
-  const int r = threadIdx.x / C;
+  const int r = threadIdx.x >> 3;
   if (r >= R || r >= g.m || count <= 0) return;
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    A t = 0;
+    A t = part[0][r][col + i];
 #pragma unroll
-    for (int w = 0; w < 16; ++w) t += part[w][r][threadIdx.x % C * 8 + i];
-    v[i] = (float)t;
+    for (int w = 1; w < NT / 64; ++w) t += part[w][r][col + i];
+    v[i] = g.part ? __builtin_bit_cast(float, t) : (float)t;
   }
-  finish<8>(g.e, r, n0, count, v);
+  if (g.part) store_part<float, 8>((float *)g.part + ((int64_t)split * g.m + r) * g.n + n0, count, v);
+  else finish<8>(g.e, r, n0, count, v);
 }
 
 // Weights along k: a wavefront takes two columns.
@@ -594,23 +629,27 @@ __global__ __launch_bounds__(256) void k_few_along(Gemm g) {
   typedef typename SumOf<S>::type A;
   constexpr int E = 16 / (int)sizeof(S);
   const int lane = threadIdx.x & 63;
-  const int64_t n0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 2;
+  const int n0 = ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)) * 2;
   if (n0 >= g.n) return;
   const int64_t n1 = n0 + 1 < g.n ? n0 + 1 : n0;
-  const char *const px = (const char *)g.a.p, *const p0 = (const char *)g.b.p + n0 * g.b.ld * (int64_t)sizeof(S),
+  const char *const px = (const char *)g.a.p, *const p0 = (const char *)g.b.p + (int64_t)n0 * g.b.ld * (int64_t)sizeof(S),
              *const p1 = (const char *)g.b.p + n1 * g.b.ld * (int64_t)sizeof(S);
   A acc[R][2];
 #pragma unroll
   for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = 0;
-  for (int64_t k = lane * E; k < g.k; k += 64 * E) {
-    const int n = g.k - k < E ? (int)(g.k - k) : E;
+  for (int k = lane * E; k < g.k; k += 64 * E) {
+    const int n = min(g.k - k, E);
+    Stored<S, E> v0, v1, v;
+    v0.load(p0 + k * (int64_t)sizeof(S), n);
+    v1.load(p1 + k * (int64_t)sizeof(S), n);
     A w0[E], w1[E], x[E];
-    numbers<S, A, E>(p0 + k * (int64_t)sizeof(S), n, w0);
-    numbers<S, A, E>(p1 + k * (int64_t)sizeof(S), n, w1);
+    v0.numbers(w0);
+    v1.numbers(w1);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (r >= g.m) break;
-      numbers<S, A, E>(px + (r * g.a.ld + k) * (int64_t)sizeof(S), n, x);
+      v.load(px + (r * g.a.ld + k) * (int64_t)sizeof(S), n);
+      v.numbers(x);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         acc[r][0] = add_product(acc[r][0], x[i], w0[i]);
@@ -638,41 +677,36 @@ __global__ __launch_bounds__(256) void k_few_along(Gemm g) {
 }
 template <class S, int R>
 hipError_t launch_few_rows(const Gemm &g, hipStream_t s) {
-  // 16 columns a block where 32 would leave compute units idle.
-  if (g.b.across && g.n < 32 * 256) k_few_across<S, R, 2><<<dim3((unsigned)((g.n + 15) / 16)), 1024, 0, s>>>(g);
-  else if (g.b.across) k_few_across<S, R, 4><<<dim3((unsigned)((g.n + 31) / 32)), 1024, 0, s>>>(g);
-  else k_few_along<S, R><<<dim3((unsigned)((g.n + 7) / 8)), 256, 0, s>>>(g);
-  return hipGetLastError();
+  if (!g.b.across) {
+    k_few_along<S, R><<<dim3((unsigned)((g.n + 7) / 8)), 256, 0, s>>>(g);
+    return hipGetLastError();
+  }
+  // Blocks that sum all of k need its lines on their way at once: 1024 x 1024 bf16 8.1 us in blocks of 256 threads, 5 in those of 1024.
+  if (g.splits == 1) k_few_across<S, R, 1024><<<dim3((unsigned)((g.n + 63) / 64)), 1024, 0, s>>>(g);
+  else k_few_across<S, R, 256><<<dim3((unsigned)((g.n + 63) / 64 * g.splits)), 256, 0, s>>>(g);
+  return join<S>(g, s);
 }
 template <class S>
 hipError_t launch_few(const Gemm &g, hipStream_t s) {
   return g.m == 1 ? launch_few_rows<S, 1>(g, s) : g.m == 2 ? launch_few_rows<S, 2>(g, s) : launch_few_rows<S, 4>(g, s);
 }
 
-template <class T>
-hipError_t join(const Gemm &g, hipStream_t s) {
-  const hipError_t err = hipGetLastError();
-  if (err != hipSuccess || !g.part) return err;
-  const int64_t join = (g.m * ((g.n + 3) / 4) + 255) / 256;
-  k_join<__is_same(T, int8_t)><<<dim3((unsigned)join), dim3(256), 0, s>>>(g);
-  return hipGetLastError();
-}
 template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
 hipError_t launch_tile(const Gemm &g, hipStream_t s) {
-  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
+  const int64_t blocks = (int64_t)((g.m + BM - 1) / BM) * ((g.n + BN - 1) / BN) * g.splits;
   k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
   return join<T>(g, s);
 }
 template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
 hipError_t launch_direct(const Gemm &g, hipStream_t s) {
-  const int64_t blocks = (g.m + BM - 1) / BM * ((g.n + BN - 1) / BN) * g.splits;
+  const int64_t blocks = (int64_t)((g.m + BM - 1) / BM) * ((g.n + BN - 1) / BN) * g.splits;
   k_gemm_direct<T, AA, BA, BM, BN, WM, WN, STAGES><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
   return join<T>(g, s);
 }
 
 // Whether k_gemm_direct takes a factor of `rows` rows: whole pieces at 16-byte addresses, offsets in a tile of 256 rows within 2^31.
 template <class T>
-bool direct_ok(const Factor &f, int64_t rows, int64_t k) {
+bool direct_ok(const Factor &f, int rows, int k) {
   constexpr int64_t E = 16 / sizeof(T);
   return (uintptr_t)f.p % 16 == 0 && f.ld % E == 0 && (f.across ? rows : k) % E == 0 && f.ld < ((int64_t)1 << 22) / (int64_t)sizeof(T);
 }
@@ -701,7 +735,7 @@ hipError_t launch_type(const Gemm &g, const GemmPlan &p, hipStream_t s) {
     if (g.a.across && g.b.across) return launch_layout<T, S, true, true>(g, p, s);
   }
   if (g.a.across) return hipErrorInvalidValue;
-  if (g.m <= kFewRows) return launch_few<S>(g, s);
+  if (g.m <= kFewRows && p.few) return launch_few<S>(g, s);
   return g.b.across ? launch_layout<T, S, false, true>(g, p, s) : launch_layout<T, S, false, false>(g, p, s);
 }
 

@@ -29,7 +29,7 @@ struct Epilogue {
   int64_t ldres, ldz, ldy;
 };
 struct Gemm {
-  int64_t m, n, k;
+  int m, n, k;                         // at most 2^28; offsets in memory take 64 bits
   Factor a, b;
   Epilogue e;
   void *part;                          // fp32 (int8 factors: int32) [splits][m][n], or null: one split
@@ -38,11 +38,12 @@ struct Gemm {
 // type: aecct_dtype, or 16 + aecct_code for codes.
 constexpr int kCodeType = 16;
 struct GemmPlan {
-  int tile;                            // which tile
+  bool few;                            // few rows by vector instructions
+  int tile;                            // else: which tile
   int splits;
   size_t part_bytes;
 };
-GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b);
+GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b, int64_t ldb);
 hipError_t launch_gemm(int type, const Gemm &g, const GemmPlan &plan, hipStream_t s);
 hipError_t launch_gemm_f32(const Gemm &g, const GemmPlan &plan, hipStream_t s);
 hipError_t launch_gemm_bf16(const Gemm &g, const GemmPlan &plan, hipStream_t s);

@@ -3,13 +3,24 @@
 
 namespace aecct {
 
-GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b) {
-  GemmPlan p{1, 1, 0};
-  if (m <= kFewRows && !across_a) return p;
+GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b, int64_t ldb) {
+  GemmPlan p{false, 1, 1, 0};
+  const int64_t size = type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2;   // of a value in LDS
+  if (m <= kFewRows && !across_a && ldb < (int64_t)1 << 30) {
+    p.few = true;
+    const int64_t t = (n + 63) / 64, rounds = (k + kFewRound - 1) / kFewRound;
+    // Weights of less than 4 MB are read in less time than a second launch takes.
+    if (across_b && m > 0 && t < 512 && n * k * size >= ((int64_t)4 << 20)) {
+      p.splits = (int)(1024 / t < rounds ? 1024 / t : rounds);
+      if (p.splits > 16) p.splits = 16;
+      if (p.splits > 1) p.part_bytes = (size_t)(p.splits * m * n * 4);
+    }
+    return p;
+  }
   auto tiles = [&](int t) { return (m + kTileSide[t][0] - 1) / kTileSide[t][0] * ((n + kTileSide[t][1] - 1) / kTileSide[t][1]); };
   if (tiles(1) < 192) p.tile = 0;
-  else if (tiles(2) >= 256 && k * (type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2) >= 1024) p.tile = 2;
-  const int64_t size = type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2, t = tiles(p.tile), kt = (k * size + 127) / 128;
+  else if (tiles(2) >= 256 && k * size >= 1024) p.tile = 2;
+  const int64_t t = tiles(p.tile), kt = (k * size + 127) / 128;
   if (t > 0 && t < 256) {
     int64_t s = (512 + t - 1) / t;
     if (s > kt / 4) s = kt / 4;

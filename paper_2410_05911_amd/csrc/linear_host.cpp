@@ -44,7 +44,7 @@ aecct_status check_linear(const aecct_linear_map_args *a) {
 }
 int kind(const aecct_linear_map_args *a) { return a->code_type == AECCT_CODE_NONE ? a->type : aecct::kCodeType + a->code_type; }
 aecct::GemmPlan plan(const aecct_linear_map_args *a) {
-  return aecct::plan_gemm(kind(a), a->rows, a->out, a->in, false, !a->w_turned);
+  return aecct::plan_gemm(kind(a), a->rows, a->out, a->in, false, !a->w_turned, a->ldw);
 }
 
 aecct_status check_grad(const aecct_linear_map_grad_args *a) {
@@ -60,8 +60,8 @@ struct GradWork {
 };
 GradWork grad_work(const aecct_linear_map_grad_args *a) {
   GradWork w{};
-  w.dx = aecct::plan_gemm(a->type, a->rows, a->in, a->out, false, a->w_turned);
-  w.dw = aecct::plan_gemm(a->type, a->in, a->out, a->rows, true, true);
+  w.dx = aecct::plan_gemm(a->type, a->rows, a->in, a->out, false, a->w_turned, a->ldw);
+  w.dw = aecct::plan_gemm(a->type, a->in, a->out, a->rows, true, true, 0);
   w.lddz = (a->out + 63) / 64 * 64;
   w.dz = a->act != AECCT_ACT_NONE ? align_up((size_t)(a->rows * w.lddz * type_size(a->type))) : 0;
   const size_t p = a->dx ? w.dx.part_bytes : 0, q = a->dw ? w.dw.part_bytes : 0;
@@ -121,7 +121,7 @@ aecct_status aecct_linear_map(const aecct_linear_map_args *a, void *workspace, s
     part = (void *)align_up((size_t)(uintptr_t)workspace);
   }
   const float q = a->code_type == AECCT_CODE_I8 ? 127.0f : 448.0f;
-  const aecct::Gemm g{a->rows, a->out, a->in, {a->x, a->ldx, false}, {a->w, a->ldw, !a->w_turned},
+  const aecct::Gemm g{(int)a->rows, (int)a->out, (int)a->in, {a->x, a->ldx, false}, {a->w, a->ldw, !a->w_turned},
                       {a->alpha, a->scale, a->bias, 1.0f / q, a->act, a->y_type, a->res, a->z, a->y, a->ldres, a->ldz, a->ldy},
                       part, p.splits};
   return aecct::launch_gemm(kind(a), g, p, (hipStream_t)stream) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
@@ -184,13 +184,13 @@ aecct_status aecct_linear_map_grad(const aecct_linear_map_grad_args *a, void *wo
   const void *const d = need_dz ? (const void *)dz : a->dy;
   const int64_t ldd = need_dz ? w.lddz : a->lddy;
   if (a->dx && a->rows) {
-    const aecct::Gemm g{a->rows, a->in, a->out, {d, ldd, false}, {a->w, a->ldw, a->w_turned != 0},
+    const aecct::Gemm g{(int)a->rows, (int)a->in, (int)a->out, {d, ldd, false}, {a->w, a->ldw, a->w_turned != 0},
                         {nullptr, nullptr, nullptr, 0.0f, 0, a->type, nullptr, nullptr, a->dx, 0, 0, a->lddx},
                         w.dx.part_bytes ? part : nullptr, w.dx.splits};
     if (aecct::launch_gemm(a->type, g, w.dx, s) != hipSuccess) return AECCT_ERR_DEVICE;
   }
   if (a->dw) {
-    const aecct::Gemm g{a->in, a->out, a->rows, {a->x, a->ldx, true}, {d, ldd, true},
+    const aecct::Gemm g{(int)a->in, (int)a->out, (int)a->rows, {a->x, a->ldx, true}, {d, ldd, true},
                         {nullptr, nullptr, nullptr, 0.0f, 0, a->dw_type, nullptr, nullptr, a->dw, 0, 0, a->lddw},
                         w.dw.part_bytes ? part : nullptr, w.dw.splits};
     if (aecct::launch_gemm(a->type, g, w.dw, s) != hipSuccess) return AECCT_ERR_DEVICE;

@@ -35,7 +35,7 @@ def _set(a, kw):
 
 
 def _linear(P, **kw):
-    a = P.LinearMapArgs(rows=4, in_=4096, out=32, type=P.F32, code_type=P.CODE_NONE, y_type=P.F32, act=0, w_turned=0, x=BASE,
+    a = P.LinearMapArgs(rows=8, in_=4096, out=32, type=P.F32, code_type=P.CODE_NONE, y_type=P.F32, act=0, w_turned=0, x=BASE,
                         ldx=4096, w=BASE + G, ldw=32, y=BASE + 2 * G, ldy=32)
     return _set(a, kw)
 
