@@ -14,34 +14,37 @@ namespace {
 template <class T>
 __device__ constexpr float weight_shift() { return __is_same(T, f16_t) ? 10.0f : 0.0f; }
 
-template <class T, int DP, int WQ, int WK, bool MASK>
-__global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
+// How far a row's scores (times log2(e)) may pass its reference before the sums are scaled down to a new one: weights stay below 2^8,
+// in fp16 with its factor below 2^15.  Most tiles then leave the sums alone.
+template <class T>
+__device__ constexpr float slack() { return __is_same(T, f16_t) ? 5.0f : 8.0f; }
+
+// WQ wavefronts take 32 rows each and share the tiles of keys, or (WQ = 1) WK wavefronts the same 32 rows and different keys.
+// DIRECT: keys and values go from memory to LDS past the registers, a tile ahead where two fit.
+template <class T, int DP, int WQ, int WK, bool MASK, bool DIRECT>
+__global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention(Attention a) {
   constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = WQ * WK * 64;
   constexpr int SUB = WK == 1 && RB <= 256 ? 2 : 1, KT = 32 * SUB * WK;   // keys of a tile
-  constexpr int PER = KT * RB / 16 / NT, CH = RB / 16;                    // pieces a thread and a row
-  static_assert(KT * RB / 16 % NT == 0, "whole pieces");
-  __shared__ __attribute__((aligned(16))) char lds[2 * KT * RB];
-  char *const lk = lds, *const lv = lds + KT * RB;
+  constexpr int STAGES = DIRECT && 4 * KT * RB <= 131072 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * KT * RB];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wq = WK == 1 ? wave : 0, wk = WK == 1 ? 0 : wave;
-  const int group = a.heads / a.kv_heads;
-  const int64_t rows = group * a.queries, row_blocks = (rows + 32 * WQ - 1) / (32 * WQ);
-  const int64_t at = near_block(blockIdx.x, gridDim.x);
-  const int64_t row_block = at % row_blocks, rest = at / row_blocks, pairs = a.batch * a.kv_heads;
-  const int64_t pair = rest / a.splits;
-  const int split = (int)(rest % a.splits);
-  const int64_t b = pair / a.kv_heads;
-  const int kh = (int)(pair % a.kv_heads);
-  int64_t length = a.keys;
-  if (a.lengths) {
-    const int64_t l = a.lengths[b];
-    length = l < 0 ? 0 : l < length ? l : length;
-  }
+  const uint32_t group = a.heads / a.kv_heads, queries = (uint32_t)a.queries, rows = group * queries;
+  const uint32_t row_blocks = (rows + 32 * WQ - 1) / (32 * WQ), pairs = (uint32_t)a.batch * a.kv_heads;
+  const uint32_t at = near_block(blockIdx.x, gridDim.x), rest = at / row_blocks, row_block = at - rest * row_blocks;
+  const uint32_t pair = a.splits > 1 ? rest / (uint32_t)a.splits : rest, split = rest - pair * (uint32_t)a.splits * (a.splits > 1);
+  const uint32_t b = pair / (uint32_t)a.kv_heads, kh = pair - b * a.kv_heads;
+  const int length = length_of(a, b);
   // This block's tiles of keys.
-  const int64_t tiles = (length + KT - 1) / KT, t0 = tiles * split / a.splits, t1 = tiles * (split + 1) / a.splits;
+  const int tiles = (length + KT - 1) / KT;
+  int t0 = 0, t1 = tiles;
+  if (a.splits > 1) {
+    t0 = (int)((uint32_t)tiles * split / (uint32_t)a.splits);
+    t1 = (int)((uint32_t)tiles * (split + 1) / (uint32_t)a.splits);
+  }
   // This lane's row.
-  const int64_t r = row_block * (32 * WQ) + wq * 32 + (lane & 31), rc = r < rows ? r : rows - 1;
-  const int64_t head = kh * group + rc / a.queries, query = rc % a.queries;
+  const uint32_t r = row_block * (32 * WQ) + wq * 32 + (lane & 31), rc = min(r, rows - 1);
+  const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * (32 * WQ) + wq * 32 >= rows;   // the whole wavefront's rows are past the last
   u32x4 q[RB / 32];
   {
@@ -50,16 +53,13 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
 #pragma unroll
     for (int c = 0; c < RB / 32; ++c) q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
   }
-  const char *const pk = (const char *)a.k.p + (b * a.k.batch + kh * a.k.head) * (int64_t)sizeof(T);
-  const char *const pv = (const char *)a.v.p + (b * a.v.batch + kh * a.v.head) * (int64_t)sizeof(T);
-  const char *const ek = end_of(a.k, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-  const char *const ev = end_of(a.v, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-  const int64_t words = words_of(a.keys), flag_tiles = words / 2;
-  const uint8_t *const flags = MASK ? a.flags + (row_block * WQ + wq) * flag_tiles : nullptr;
+  Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
+  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
+  const uint32_t *const mask = MASK ? a.words + (int64_t)query * words + wk * SUB : nullptr;
   // Tiles of keys that none of the block's rows may attend are passed over: 64 tiles are looked up at once.
   uint64_t want = 0;
-  int64_t want0 = t0 - 64;
-  auto from = [&](int64_t t) {   // the first tile to be done from t on
+  int want0 = t0 - 64;
+  auto from = [&](int t) {   // the first tile to be done from t on
     if constexpr (!MASK) return t;
     while (t < t1) {
       if (t - want0 >= 64) {
@@ -78,40 +78,63 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
   for (int f = 0; f < FD; ++f)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[f][i] = 0;
-  float m = -INFINITY, sum = 0;
+  float m = -INFINITY, sum = 0;   // the row's reference, and its sum of 2^(score - reference)
   const float to2 = a.scale * kLog2e;
 
-  u32x4 ck[PER], cv[PER];
-  auto load = [&](int64_t t) {
+  int t = from(t0), buf = 0;
+  uint32_t w[SUB] = {}, w_next[SUB] = {};   // what the lane's row may attend of the tile
+  auto look = [&](int t, uint32_t (&w)[SUB]) {
+    if constexpr (MASK) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      const int64_t key = t * KT + row;
-      ck[i] = cv[i] = u32x4{0, 0, 0, 0};
-      if (key < length) {   // keys past the length are never read: their weights are 0, and 0 times what lies there may be NaN
-        ck[i] = row_piece<T>(pk + key * a.k.row * (int64_t)sizeof(T), chunk, a.d, ek);
-        cv[i] = row_piece<T>(pv + key * a.v.row * (int64_t)sizeof(T), chunk, a.d, ev);
-      }
+      for (int u = 0; u < SUB; ++u) w[u] = t * (KT / 32) + wk * SUB + u < words ? mask[t * (KT / 32) + u] : 0;
     }
   };
-  int64_t t = from(t0);
-  if (t < t1) load(t);
-  while (t < t1) {
-    const int64_t next = from(t + 1);
-    __syncthreads();   // the tile before has been read
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      const int to = row * RB + ((chunk << 4) ^ exchange<RB>(row));
-      *(u32x4 *)(lk + to) = ck[i];
-      *(u32x4 *)(lv + to) = cv[i];
+  if (t < t1) {
+    if constexpr (!DIRECT || STAGES == 2) {
+      keys.load(lds, t);
+      values.load(lds + KT * RB, t);
     }
-    __syncthreads();
-    if (next < t1) load(next);
-    const int64_t key0 = t * KT + wk * 32 * SUB;
-    int flag = 2;
-    if constexpr (MASK) flag = !idle && key0 < length ? flags[key0 / 64] : 0;
-    if (!idle && key0 < length && flag != 0) {
+    look(t, w_next);
+  }
+  while (t < t1) {
+    const int next = from(t + 1);
+    char *const lk = lds + buf * 2 * KT * RB, *const lv = lk + KT * RB;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) w[u] = w_next[u];
+    if constexpr (DIRECT && STAGES == 2) {
+      wait_loads();
+      barrier();         // the tile is there for all, and nobody reads the other one any more
+      if (next < t1) {
+        keys.load(lds + (buf ^ 1) * 2 * KT * RB, next);
+        values.load(lds + (buf ^ 1) * 2 * KT * RB + KT * RB, next);
+      }
+      buf ^= 1;
+    } else if constexpr (DIRECT) {
+      barrier();         // the tile before has been read
+      keys.load(lk, t);
+      values.load(lv, t);
+      wait_loads();
+      barrier();
+    } else {
+      barrier();
+      keys.store(lk);
+      values.store(lv);
+      barrier();
+      if (next < t1) {
+        keys.load(nullptr, next);
+        values.load(nullptr, next);
+      }
+    }
+    if (next < t1) look(next, w_next);
+    const int key0 = t * KT + wk * 32 * SUB;
+    bool none = idle || key0 >= length;
+    if constexpr (MASK) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) any |= w[u];
+      none = none || !__any(any != 0);
+    }
+    if (!none) {
       float s[SUB][16];
       float top = -INFINITY;
 #pragma unroll
@@ -119,47 +142,49 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
         const f32x16 x = times_rows<T, RB>(lk, (wk * SUB + u) * 32, q);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[u][i] = x[i];
-        const int64_t k0 = key0 + u * 32;
-        if (k0 + 32 > length) {
+      }
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const int k0 = key0 + u * 32;
+        if constexpr (MASK) {
+          uint32_t in = w[u];
+          if (k0 + 32 > length) in = length > k0 ? in & ((1u << (length - k0)) - 1) : 0;
+          in >>= 4 * h;
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(in >> row_of(i, 0) & 1)) s[u][i] = -INFINITY;
+        } else if (k0 + 32 > length) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (k0 + row_of(i, h) >= length) s[u][i] = -INFINITY;
         }
-        if constexpr (MASK) {
-          if (flag == 1) {
-            const uint32_t w = a.words[query * words + k0 / 32] >> (4 * h);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!(w >> row_of(i, 0) & 1)) s[u][i] = -INFINITY;
-          }
-        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
       }
-      top = fmaxf(m, max_halves(top) * to2);
-      // A row that has met no key it may attend keeps the maximum -inf; its weights are 2^-inf = 0.
-      const float base = top == -INFINITY ? 0.0f : top;
-      if (__any(top != m)) {
-        const float down = __builtin_amdgcn_exp2f(m - base);
+      top = max_halves(top) * to2;
+      if (__any(top > m + slack<T>())) {
+        const float now = top > m + slack<T>() ? top : m;
+        // A row that has met no key it may attend keeps the reference -inf; its weights are 2^-inf = 0.
+        const float down = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+        m = now;
         sum *= down;
 #pragma unroll
         for (int f = 0; f < FD; ++f)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[f][i] *= down;
       }
-      m = top;
-      const float lift = base - weight_shift<T>();
-      float part = 0;
+      const float lift = (m == -INFINITY ? 0.0f : m) - weight_shift<T>();
+      float part[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], to2, -lift));
-          part += s[u][i];
+          part[i & 3] += s[u][i];
         }
         add_columns<T, RB, FD>(acc, lv, (wk * SUB + u) * 32, s[u]);
       }
-      sum += part;
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
     }
     t = next;
   }
@@ -168,7 +193,7 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
   if constexpr (WK > 1) {
     // The wavefronts' shares of the keys are joined through LDS.
     constexpr int LD = DP;
-    static_assert(2 * KT * RB >= WK * 32 * LD * 4, "the sums fit where the tiles were");
+    static_assert(STAGES * 2 * KT * RB >= WK * 32 * LD * 4, "the sums fit where the tiles were");
     __shared__ float ml[WK][32][2];
     __syncthreads();
     if (h == 0) {
@@ -215,7 +240,7 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
 
   if (r >= rows) return;
   if (a.splits > 1) {
-    const int64_t at_row = ((int64_t)split * pairs + pair) * rows + r;
+    const int64_t at_row = (int64_t)(split * pairs + pair) * rows + r;
     if (h == 0 && wk == 0) {
       a.part_ml[at_row * 2] = m;
       a.part_ml[at_row * 2 + 1] = sum;
@@ -232,7 +257,7 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
   }
   const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
   if (a.lse && h == 0 && wk == 0)
-    a.lse[(b * a.heads + head) * a.queries + query] = sum == 0.0f ? -INFINITY : (m + (__log2f(sum) - weight_shift<T>())) * kLn2;
+    a.lse[(int64_t)(b * a.heads + head) * queries + query] = sum == 0.0f ? -INFINITY : (m + (__log2f(sum) - weight_shift<T>())) * kLn2;
   T *const o = (T *)a.o.p + b * a.o.batch + query * a.o.row + head * a.o.head;
 #pragma unroll
   for (int f = 0; f < FD; ++f) {
@@ -248,10 +273,9 @@ __global__ __launch_bounds__(WQ *WK * 64) void k_attention(Attention a) {
 // The splits' sums of four columns of a row a thread, in the order of the splits.
 template <class T>
 __global__ __launch_bounds__(256) void k_join_attention(Attention a, int dp) {
-  const int group = a.heads / a.kv_heads, per = dp / 4;
-  const int64_t rows = group * a.queries, pairs = a.batch * a.kv_heads, all = pairs * rows;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / per;
-  const int c = (int)(at % per) * 4;
+  const uint32_t group = a.heads / a.kv_heads, per = dp / 4, queries = (uint32_t)a.queries, rows = group * queries;
+  const int64_t all = (int64_t)a.batch * a.kv_heads * rows;
+  const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = at / per, c = (at - row * per) * 4;
   if (row >= all) return;
   float m = -INFINITY, sum = 0;
   for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(s * all + row) * 2]);
@@ -264,13 +288,13 @@ __global__ __launch_bounds__(256) void k_join_attention(Attention a, int dp) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += o[i] * down;
   }
-  const int64_t pair = row / rows, r = row % rows, b = pair / a.kv_heads;
-  const int64_t head = pair % a.kv_heads * group + r / a.queries, query = r % a.queries;
+  const uint32_t pair = row / rows, r = row - pair * rows, b = pair / (uint32_t)a.kv_heads;
+  const uint32_t head = (pair - b * a.kv_heads) * group + r / queries, query = r % queries;
   const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
   if (a.lse && c == 0)
-    a.lse[(b * a.heads + head) * a.queries + query] = sum == 0.0f ? -INFINITY : (m + (__log2f(sum) - weight_shift<T>())) * kLn2;
-  if (c < a.d)
-    store_values4<T>((T *)a.o.p + b * a.o.batch + query * a.o.row + head * a.o.head + c, a.d - c, v[0] * over, v[1] * over,
+    a.lse[(int64_t)(b * a.heads + head) * queries + query] = sum == 0.0f ? -INFINITY : (m + (__log2f(sum) - weight_shift<T>())) * kLn2;
+  if ((int)c < a.d)
+    store_values4<T>((T *)a.o.p + b * a.o.batch + query * a.o.row + head * a.o.head + c, a.d - (int)c, v[0] * over, v[1] * over,
                      v[2] * over, v[3] * over);
 }
 
@@ -283,16 +307,16 @@ __device__ __forceinline__ uint32_t nonzero4(uint32_t w) {
 // keys; bits past the last key are 0 in the words, and do not count in the flags.
 __global__ __launch_bounds__(64) void k_pack_mask(Attention a) {
   const int lane = threadIdx.x, h = lane >> 5;
-  const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries, words = words_of(a.keys), tiles = words / 2;
-  const int64_t per = (tiles + 1) / 2, rt = blockIdx.x / per, t = blockIdx.x % per * 2 + h;
-  const int64_t r = rt * 32 + (lane & 31);
+  const uint32_t queries = (uint32_t)a.queries, rows = (uint32_t)(a.heads / a.kv_heads) * queries;
+  const uint32_t words = (uint32_t)words_of(a.keys), tiles = words / 2, per = (tiles + 1) / 2;
+  const uint32_t rt = blockIdx.x / per, t = (blockIdx.x - rt * per) * 2 + h, r = rt * 32 + (lane & 31);
   const bool live = r < rows && t < tiles;
   uint64_t w = 0, full = ~(uint64_t)0;
   if (live) {
-    const int64_t k0 = t * 64;
+    const int64_t k0 = (int64_t)t * 64;
     const int n = a.keys - k0 < 64 ? (int)(a.keys - k0) : 64;
     if (n < 64) full = ((uint64_t)1 << n) - 1;
-    const uint8_t *const p = a.mask + (r % a.queries) * a.ldmask + k0;
+    const uint8_t *const p = a.mask + (int64_t)(r % queries) * a.ldmask + k0;
     if (n == 64) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -306,12 +330,12 @@ __global__ __launch_bounds__(64) void k_pack_mask(Attention a) {
     } else {
       for (int i = 0; i < n; ++i) w |= (uint64_t)(p[i] != 0) << i;
     }
-    if (r < a.queries) *(uint64_t *)(a.words + r * words + t * 2) = w;
+    if (r < queries) *(uint64_t *)(a.words + (int64_t)r * words + t * 2) = w;
   }
   const uint64_t any = __ballot(live && w != 0), gap = __ballot(live && w != full);
   if ((lane & 31) == 0 && t < tiles) {
     const uint32_t x = (uint32_t)(any >> (32 * h)), y = (uint32_t)(gap >> (32 * h));
-    a.flags[rt * tiles + t] = x == 0 ? 0 : y == 0 ? 2 : 1;
+    a.flags[(int64_t)rt * tiles + t] = x == 0 ? 0 : y == 0 ? 2 : 1;
   }
 }
 
@@ -319,8 +343,11 @@ template <class T, int DP, int WQ, int WK>
 hipError_t launch_shape(const Attention &a, hipStream_t s) {
   const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries;
   const int64_t blocks = (rows + 32 * WQ - 1) / (32 * WQ) * a.batch * a.kv_heads * a.splits;
-  if (a.mask) k_attention<T, DP, WQ, WK, true><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
-  else k_attention<T, DP, WQ, WK, false><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
+  const bool direct = direct_ok<T>(a.k, a) && direct_ok<T>(a.v, a);
+  if (a.mask && direct) k_attention<T, DP, WQ, WK, true, true><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
+  else if (a.mask) k_attention<T, DP, WQ, WK, true, false><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
+  else if (direct) k_attention<T, DP, WQ, WK, false, true><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
+  else k_attention<T, DP, WQ, WK, false, false><<<dim3((unsigned)blocks), WQ * WK * 64, 0, s>>>(a);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess || a.splits == 1) return err;
   const int64_t threads = rows * a.batch * a.kv_heads * (DP / 4);

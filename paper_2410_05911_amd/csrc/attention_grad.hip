@@ -62,12 +62,6 @@ __global__ __launch_bounds__(256) void k_attention_rows(AttentionGrad g) {
   }
 }
 
-__device__ __forceinline__ int64_t length_of(const Attention &a, int64_t b) {
-  if (!a.lengths) return a.keys;
-  const int64_t l = a.lengths[b];
-  return l < 0 ? 0 : l < a.keys ? l : a.keys;
-}
-
 // dq: a wavefront takes 32 rows, tiles of 32 keys pass through LDS.
 template <class T, int DP, bool MASK>
 __global__ __launch_bounds__(256) void k_attention_dq(AttentionGrad g) {

@@ -13,7 +13,7 @@ namespace {
 using aecct::overlap;
 using aecct::Span;
 
-constexpr int64_t kMaxCount = (int64_t)1 << 31, kMaxSpan = (int64_t)1 << 56;   // no byte offset overflows
+constexpr int64_t kMaxCount = (int64_t)1 << 30, kMaxSpan = (int64_t)1 << 56;   // no byte offset overflows
 constexpr int64_t kMaxThreads = ((int64_t)1 << 32) - 512;                      // of a grid
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }

@@ -115,17 +115,91 @@ __device__ __forceinline__ const char *end_of(const Heads &t, int64_t batch, int
 }
 
 // Blocks in an order that keeps those of one XCD (every eighth) on neighbouring numbers, which share their keys.
-__device__ __forceinline__ int64_t near_block(int64_t block, int64_t blocks) {
-  const int64_t share = blocks / 8;
-  return block < share * 8 ? (block % 8) * share + block / 8 : block;
+__device__ __forceinline__ uint32_t near_block(uint32_t block, uint32_t blocks) {
+  const uint32_t share = blocks / 8;
+  return block < share * 8 ? block % 8 * share + block / 8 : block;
+}
+__device__ __forceinline__ int length_of(const Attention &a, uint32_t b) {
+  if (!a.lengths) return (int)a.keys;
+  const int l = a.lengths[b];
+  return max(0, min(l, (int)a.keys));
 }
 
+// Whether a tensor's rows are whole 16-byte pieces at 16-byte addresses, and the offsets in a tile of 256 rows within 2^31.
+template <class T>
+bool direct_ok(const Heads &t, const Attention &a) {
+  constexpr int64_t E = 16 / sizeof(T);
+  return (uintptr_t)t.p % 16 == 0 && a.d % E == 0 && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
+         t.row < ((int64_t)1 << 22) / (int64_t)sizeof(T);
+}
+// Tiles of KT keys (or values) of one pair, on their way to LDS: DIRECT by loads whose out-of-range offsets give the zeros behind d and
+// past the length, else through registers.  What lies past the length is never read: its weights are 0, and 0 times it may be NaN.
+template <class T, int RB, int KT, int NT, bool DIRECT>
+struct Keys {
+  static constexpr int CH = RB / 16, PER = (KT * CH + NT - 1) / NT, E = 16 / (int)sizeof(T);
+  static constexpr uint32_t OUT = 0x80000000u;
+  const char *p, *end;
+  int64_t stride;              // bytes of a row
+  int length, d;
+  uint32_t at[DIRECT ? PER : 1];
+  u32x4 v[DIRECT ? 1 : PER];
+  static __device__ __forceinline__ void place(int i, int &row, int &chunk) {
+    const int slot = threadIdx.x + i * NT;
+    row = slot / CH;
+    chunk = (((slot % CH) << 4) ^ exchange<RB>(row)) >> 4;
+  }
+  __device__ __forceinline__ Keys(const Heads &t, const Attention &a, uint32_t b, uint32_t kh, int length)
+      : p((const char *)t.p + (b * t.batch + kh * t.head) * (int64_t)sizeof(T)),
+        end(end_of(t, a.batch, a.keys, a.kv_heads, a.d, sizeof(T))), stride(t.row * (int64_t)sizeof(T)), length(length), d(a.d) {
+    if constexpr (DIRECT) {
+      static_assert(KT * CH % NT == 0, "whole pieces");
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        int row, chunk;
+        place(i, row, chunk);
+        at[i] = chunk * E < d ? (uint32_t)(row * stride + chunk * 16) : OUT;
+      }
+    }
+  }
+  __device__ __forceinline__ void load(char *lds, int t) {
+    if constexpr (DIRECT) {
+      const BufferOf r(p + (int64_t)t * KT * stride, OUT);
+      const int left = length - t * KT, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        uint32_t offset = at[i];
+        if (left < KT) {
+          int row, chunk;
+          place(i, row, chunk);
+          if (row >= left) offset = OUT;
+        }
+        r.to_lds(lds + (i * NT + wave * 64) * 16, offset);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        int row, chunk;
+        place(i, row, chunk);
+        const int64_t key = (int64_t)t * KT + row;
+        v[i] = u32x4{0, 0, 0, 0};
+        if (row < KT && key < length) v[i] = row_piece<T>(p + key * stride, chunk, d, end);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char *lds) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int slot = threadIdx.x + i * NT;
+      if (PER * NT == KT * CH || slot < KT * CH) *(u32x4 *)(lds + slot * 16) = v[i];
+    }
+  }
+};
+
 // Whether any of `count` tiles of rows from `first` on may attend any of `keys` keys from key0 on.
-__device__ __forceinline__ bool any_flag(const uint8_t *flags, int64_t first, int count, int64_t row_tiles, int64_t key0, int keys,
-                                         int64_t flag_tiles) {
+__device__ __forceinline__ bool any_flag(const uint8_t *flags, int first, int count, int row_tiles, int key0, int keys, int flag_tiles) {
   int any = 0;
   for (int i = 0; i < count && first + i < row_tiles; ++i)
-    for (int64_t c = key0 / 64; c * 64 < key0 + keys && c < flag_tiles; ++c) any |= flags[(first + i) * flag_tiles + c];
+    for (int c = key0 / 64; c * 64 < key0 + keys && c < flag_tiles; ++c) any |= flags[(int64_t)(first + i) * flag_tiles + c];
   return any != 0;
 }
 
