@@ -40,64 +40,95 @@ struct Scaled {
   __device__ __forceinline__ float out() const { return __is_same(T, f16_t) ? 1.0f / by : 1.0f; }
 };
 
-// lse log2(e) (a row that attends nothing: infinity, so that its weights are 0) and D, a wavefront a row.
+// What a row of p and ds is taken from: lse log2(e) (a row that attends nothing: infinity, so that its weights are 0) and D.
+__device__ __forceinline__ void row_terms(float lse, float sum, float &l2, float &dd) {
+  l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  dd = lse == -INFINITY ? 0.0f : sum;
+}
+// The sum of the products of two pieces of 16 bytes.
+template <class T>
+__device__ __forceinline__ float dot(u32x4 x, u32x4 y, float sum) {
+  Raw<T, 16 / sizeof(T)> a, b;
+  float f[16 / sizeof(T)], g[16 / sizeof(T)];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a.w[i] = x[i];
+    b.w[i] = y[i];
+  }
+  unpack<T, 16 / sizeof(T)>(a, f);
+  unpack<T, 16 / sizeof(T)>(b, g);
+#pragma unroll
+  for (int i = 0; i < (int)(16 / sizeof(T)); ++i) sum = fmaf(f[i], g[i], sum);
+  return sum;
+}
+// The rows' terms where dq, which takes them along, is not asked for: 16 lanes a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_attention_rows(AttentionGrad g) {
   const Attention &a = g.a;
-  const int lane = threadIdx.x & 63, group = a.heads / a.kv_heads;
-  const int64_t rows = group * a.queries, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows * a.batch * a.kv_heads) return;
-  const int64_t pair = row / rows, r = row % rows, b = pair / a.kv_heads;
-  const int64_t head = pair % a.kv_heads * group + r / a.queries, query = r % a.queries;
-  const T *const o = (const T *)a.o.p + b * a.o.batch + query * a.o.row + head * a.o.head;
-  const T *const d = (const T *)g.dout.p + b * g.dout.batch + query * g.dout.row + head * g.dout.head;
+  const uint32_t group = a.heads / a.kv_heads, queries = (uint32_t)a.queries, rows = group * queries;
+  const uint32_t row = blockIdx.x * 16 + (threadIdx.x >> 4), pair = row / rows, r = row - pair * rows, b = pair / (uint32_t)a.kv_heads;
+  if (b >= a.batch) return;
+  const uint32_t head = (pair - b * a.kv_heads) * group + r / queries, query = r % queries;
+  const char *const o = (const char *)a.o.p + (b * a.o.batch + query * a.o.row + head * a.o.head) * (int64_t)sizeof(T);
+  const char *const d = (const char *)g.dout.p + (b * g.dout.batch + query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T);
+  const char *const eo = end_of(a.o, a.batch, a.queries, a.heads, a.d, sizeof(T));
+  const char *const ed = end_of(g.dout, a.batch, a.queries, a.heads, a.d, sizeof(T));
   float sum = 0;
-  for (int c = lane; c < a.d; c += 64) sum = fmaf((float)o[c], (float)d[c], sum);
+  for (int c = threadIdx.x & 15; c * (int)(16 / sizeof(T)) < a.d; c += 16)
+    sum = dot<T>(row_piece<T>(o, c, a.d, eo), row_piece<T>(d, c, a.d, ed), sum);
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) sum += __shfl_xor(sum, i);
-  if (lane == 0) {
-    const float lse = a.lse[(b * a.heads + head) * a.queries + query];
-    g.rows[row * 2] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    g.rows[row * 2 + 1] = lse == -INFINITY ? 0.0f : sum;
+  for (int i = 1; i < 16; i *= 2) sum += __shfl_xor(sum, i);
+  if ((threadIdx.x & 15) == 0) {
+    float l2, dd;
+    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum, l2, dd);
+    g.rows[(int64_t)row * 2] = l2;
+    g.rows[(int64_t)row * 2 + 1] = dd;
   }
 }
 
-// dq: a wavefront takes 32 rows, tiles of 32 keys pass through LDS.
-template <class T, int DP, bool MASK>
-__global__ __launch_bounds__(256) void k_attention_dq(AttentionGrad g) {
-  constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = 256, KT = 32, CH = RB / 16, PER = (KT * CH + NT - 1) / NT;
+// dq: a wavefront takes 32 rows, tiles of keys pass through LDS.  It leaves the rows' terms for dk and dv.
+template <class T, int DP, bool MASK, bool DIRECT>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(AttentionGrad g) {
+  constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = 256, SUB = RB <= 256 ? 2 : 1, KT = 32 * SUB;
+  constexpr int STAGES = DIRECT && 4 * KT * RB <= 131072 ? 2 : 1;
   const Attention &a = g.a;
-  __shared__ __attribute__((aligned(16))) char lds[2 * KT * RB];
-  char *const lk = lds, *const lv = lds + KT * RB;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5, group = a.heads / a.kv_heads;
-  const int64_t rows = group * a.queries, row_blocks = (rows + 127) / 128;
-  const int64_t at = near_block(blockIdx.x, gridDim.x), row_block = at % row_blocks, pair = at / row_blocks, b = pair / a.kv_heads;
-  const int kh = (int)(pair % a.kv_heads);
-  const int64_t length = length_of(a, b), t1 = (length + KT - 1) / KT;
-  const int64_t r = row_block * 128 + wave * 32 + (lane & 31), rc = r < rows ? r : rows - 1;
-  const int64_t head = kh * group + rc / a.queries, query = rc % a.queries;
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * KT * RB];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  const uint32_t group = a.heads / a.kv_heads, queries = (uint32_t)a.queries, rows = group * queries, row_blocks = (rows + 127) / 128;
+  const uint32_t at = near_block(blockIdx.x, gridDim.x), pair = at / row_blocks, row_block = at - pair * row_blocks;
+  const uint32_t b = pair / (uint32_t)a.kv_heads, kh = pair - b * a.kv_heads;
+  const int length = length_of(a, b), t1 = (length + KT - 1) / KT;
+  const uint32_t r = row_block * 128 + wave * 32 + (lane & 31), rc = min(r, rows - 1);
+  const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * 128 + wave * 32 >= rows;
   u32x4 q[RB / 32], dout[RB / 32];
+  float dd = 0, l2;
   {
     const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
     const char *const pd = (const char *)g.dout.p + (b * g.dout.batch + query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T);
+    const char *const po = (const char *)a.o.p + (b * a.o.batch + query * a.o.row + head * a.o.head) * (int64_t)sizeof(T);
     const char *const end = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
     const char *const endd = end_of(g.dout, a.batch, a.queries, a.heads, a.d, sizeof(T));
+    const char *const endo = end_of(a.o, a.batch, a.queries, a.heads, a.d, sizeof(T));
 #pragma unroll
     for (int c = 0; c < RB / 32; ++c) {
       q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
       dout[c] = row_piece<T>(pd, 2 * c + h, a.d, endd);
+      dd = dot<T>(row_piece<T>(po, 2 * c + h, a.d, endo), dout[c], dd);
+    }
+    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l2, dd);
+    if (h == 0 && r < rows) {
+      g.rows[((int64_t)pair * rows + r) * 2] = l2;
+      g.rows[((int64_t)pair * rows + r) * 2 + 1] = dd;
     }
   }
-  const float l2 = g.rows[(pair * rows + rc) * 2], dd = g.rows[(pair * rows + rc) * 2 + 1], to2 = a.scale * kLog2e;
-  const char *const pk = (const char *)a.k.p + (b * a.k.batch + kh * a.k.head) * (int64_t)sizeof(T);
-  const char *const pv = (const char *)a.v.p + (b * a.v.batch + kh * a.v.head) * (int64_t)sizeof(T);
-  const char *const ek = end_of(a.k, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-  const char *const ev = end_of(a.v, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-  const int64_t words = words_of(a.keys), flag_tiles = words / 2;
+  const float to2 = a.scale * kLog2e;
+  Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
+  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
+  const uint32_t *const mask = MASK ? a.words + (int64_t)query * words : nullptr;
   uint64_t want = 0;
-  int64_t want0 = -64;
-  auto from = [&](int64_t t) {
+  int want0 = -64;
+  auto from = [&](int t) {
     if constexpr (!MASK) return t;
     while (t < t1) {
       if (t - want0 >= 64) {
@@ -116,53 +147,67 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionGrad g) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[f][i] = 0;
   Scaled<T, FD> scaled;
-  u32x4 ck[PER], cv[PER];
-  auto load = [&](int64_t t) {
+  uint32_t w[SUB] = {}, w_next[SUB] = {};
+  auto look = [&](int t, uint32_t (&w)[SUB]) {
+    if constexpr (MASK) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      const int64_t key = t * KT + row;
-      ck[i] = cv[i] = u32x4{0, 0, 0, 0};
-      if (row < KT && key < length) {
-        ck[i] = row_piece<T>(pk + key * a.k.row * (int64_t)sizeof(T), chunk, a.d, ek);
-        cv[i] = row_piece<T>(pv + key * a.v.row * (int64_t)sizeof(T), chunk, a.d, ev);
-      }
+      for (int u = 0; u < SUB; ++u) w[u] = t * SUB + u < words ? mask[t * SUB + u] : 0;
     }
   };
-  int64_t t = from(0);
-  if (t < t1) load(t);
-  while (t < t1) {
-    const int64_t next = from(t + 1);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      if (row >= KT) continue;
-      const int to = row * RB + ((chunk << 4) ^ exchange<RB>(row));
-      *(u32x4 *)(lk + to) = ck[i];
-      *(u32x4 *)(lv + to) = cv[i];
+  int t = from(0), buf = 0;
+  if (t < t1) {
+    if constexpr (!DIRECT || STAGES == 2) {
+      keys.load(lds, t);
+      values.load(lds + KT * RB, t);
     }
-    __syncthreads();
-    if (next < t1) load(next);
-    const int64_t k0 = t * KT;
-    int flag = 2;
-    if constexpr (MASK) flag = !idle ? a.flags[(row_block * 4 + wave) * flag_tiles + k0 / 64] : 0;
-    if (!idle && flag != 0) {
-      const f32x16 s = times_rows<T, RB>(lk, 0, q), dp = times_rows<T, RB>(lv, 0, dout);
-      uint32_t w = ~0u;
-      if (k0 + 32 > length) w = (1u << (length - k0)) - 1;
-      if constexpr (MASK) {
-        if (flag == 1) w &= a.words[query * words + k0 / 32];
+    look(t, w_next);
+  }
+  while (t < t1) {
+    const int next = from(t + 1);
+    char *const lk = lds + buf * 2 * KT * RB, *const lv = lk + KT * RB;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) w[u] = w_next[u];
+    if constexpr (DIRECT && STAGES == 2) {
+      wait_loads();
+      barrier();
+      if (next < t1) {
+        keys.load(lds + (buf ^ 1) * 2 * KT * RB, next);
+        values.load(lds + (buf ^ 1) * 2 * KT * RB + KT * RB, next);
       }
-      w >>= 4 * h;
+      buf ^= 1;
+    } else if constexpr (DIRECT) {
+      barrier();
+      keys.load(lk, t);
+      values.load(lv, t);
+      wait_loads();
+      barrier();
+    } else {
+      barrier();
+      keys.store(lk);
+      values.store(lv);
+      barrier();
+      if (next < t1) {
+        keys.load(nullptr, next);
+        values.load(nullptr, next);
+      }
+    }
+    if (next < t1) look(next, w_next);
+#pragma unroll
+    for (int u = 0; u < SUB; ++u) {
+      const int k0 = t * KT + u * 32;
+      uint32_t in = MASK ? w[u] : ~0u;
+      if (k0 + 32 > length) in = length > k0 ? in & ((1u << (length - k0)) - 1) : 0;
+      if (idle || !__any(in != 0)) continue;
+      const f32x16 s = times_rows<T, RB>(lk, u * 32, q), dp = times_rows<T, RB>(lv, u * 32, dout);
+      in >>= 4 * h;
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = __builtin_amdgcn_exp2f(fmaf(s[i], to2, -l2));
-        ds[i] = w >> row_of(i, 0) & 1 ? p * (dp[i] - dd) : 0.0f;
+        ds[i] = in >> row_of(i, 0) & 1 ? p * (dp[i] - dd) : 0.0f;
       }
       scaled.apply(ds, acc);
-      add_columns<T, RB, FD>(acc, lk, 0, ds);
+      add_columns<T, RB, FD>(acc, lk, u * 32, ds);
     }
     t = next;
   }
@@ -178,25 +223,80 @@ __global__ __launch_bounds__(256) void k_attention_dq(AttentionGrad g) {
     }
 }
 
+// Tiles of 32 rows (queries of the heads of a key head) of one pair on their way to LDS, as Keys.
+template <class T, int RB, bool DIRECT>
+struct RowsOf {
+  static constexpr int NT = 256, CH = RB / 16, PER = (32 * CH + NT - 1) / NT, E = 16 / (int)sizeof(T);
+  static constexpr uint32_t OUT = 0x80000000u;
+  const char *p, *end;
+  int64_t row_stride, head_stride;
+  uint32_t rows, queries;
+  int d;
+  u32x4 v[DIRECT ? 1 : PER];
+  __device__ __forceinline__ RowsOf(const Heads &t, const Attention &a, uint32_t b, uint32_t kh)
+      : p((const char *)t.p + (b * t.batch + kh * (a.heads / a.kv_heads) * t.head) * (int64_t)sizeof(T)),
+        end(end_of(t, a.batch, a.queries, a.heads, a.d, sizeof(T))), row_stride(t.row * (int64_t)sizeof(T)),
+        head_stride(t.head * (int64_t)sizeof(T)), rows((uint32_t)(a.heads / a.kv_heads) * (uint32_t)a.queries),
+        queries((uint32_t)a.queries), d(a.d) {}
+  __device__ __forceinline__ void load(char *lds, int t) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const BufferOf buffer(p, OUT);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = (((slot % CH) << 4) ^ exchange<RB>(row)) >> 4;
+      const uint32_t r = t * 32 + row, head = r / queries, query = r - head * queries;
+      const bool there = r < rows && row < 32;
+      if constexpr (DIRECT) {
+        // The last wavefronts of a tile of less than 256 pieces have none.
+        if (32 * CH >= NT || wave * 64 < 32 * CH) {
+          const uint32_t at = query * (uint32_t)row_stride + head * (uint32_t)head_stride + chunk * 16;
+          buffer.to_lds(lds + (i * NT + wave * 64) * 16, there && chunk * E < d ? at : OUT);
+        }
+      } else {
+        v[i] = u32x4{0, 0, 0, 0};
+        if (there) v[i] = row_piece<T>(p + query * row_stride + head * head_stride, chunk, d, end);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char *lds) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int slot = threadIdx.x + i * NT;
+      if (slot < 32 * CH) *(u32x4 *)(lds + slot * 16) = v[i];
+    }
+  }
+};
+// Whether RowsOf takes a tensor past the registers: whole 16-byte pieces, and a sequence's offsets within 2^31.
+template <class T>
+bool direct_rows(const Heads &t, const Attention &a) {
+  constexpr int64_t E = 16 / sizeof(T);
+  return (uintptr_t)t.p % 16 == 0 && a.d % E == 0 && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
+         t.row * (a.queries - 1) + t.head * a.heads + a.d < ((int64_t)1 << 31) / (int64_t)sizeof(T);
+}
+
 // dk and dv (DK, DV: which of them): a wavefront takes 32 keys, tiles of 32 rows pass through LDS.
-template <class T, int DP, bool MASK, bool DK, bool DV>
-__global__ __launch_bounds__(256) void k_attention_dkv(AttentionGrad g) {
-  constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = 256, RT = 32, CH = RB / 16, PER = (RT * CH + NT - 1) / NT;
+template <class T, int DP, bool MASK, bool DK, bool DV, bool DIRECT>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1) void k_attention_dkv(AttentionGrad g) {
+  constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, RT = 32, STAGES = DIRECT ? 2 : 1;
   const Attention &a = g.a;
-  __shared__ __attribute__((aligned(16))) char lds[2 * RT * RB];
-  __shared__ __attribute__((aligned(16))) float rl[32], rd[32];
-  __shared__ __attribute__((aligned(16))) uint32_t rw[4][32];
-  char *const lq = lds, *const ld = lds + RT * RB;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5, group = a.heads / a.kv_heads;
-  const int64_t rows = group * a.queries, key_blocks = (a.keys + 127) / 128, pairs = a.batch * a.kv_heads;
-  const int64_t at = near_block(blockIdx.x, gridDim.x), key_block = at % key_blocks, rest = at / key_blocks;
-  const int64_t pair = rest / g.splits, b = pair / a.kv_heads;
-  const int split = (int)(rest % g.splits), kh = (int)(pair % a.kv_heads);
-  const int64_t length = length_of(a, b), key = key_block * 128 + wave * 32 + (lane & 31), key0 = key_block * 128 + wave * 32;
-  const int64_t tiles = (rows + RT - 1) / RT, t0 = tiles * split / g.splits;
-  // A block whose keys are all past the length has nothing to sum.
-  const int64_t t1 = key_block * 128 < length ? tiles * (split + 1) / g.splits : t0;
-  const bool idle = key0 >= length;
+  __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * RT * RB];
+  __shared__ __attribute__((aligned(16))) float rl[2][32], rd[2][32];
+  __shared__ __attribute__((aligned(16))) uint32_t rw[2][4][32];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
+  const uint32_t group = a.heads / a.kv_heads, queries = (uint32_t)a.queries, rows = group * queries;
+  const uint32_t key_blocks = (uint32_t)((a.keys + 127) / 128), pairs = (uint32_t)a.batch * a.kv_heads;
+  const uint32_t at = near_block(blockIdx.x, gridDim.x), rest = at / key_blocks, key_block = at - rest * key_blocks;
+  const uint32_t pair = g.splits > 1 ? rest / (uint32_t)g.splits : rest, split = g.splits > 1 ? rest - pair * g.splits : 0;
+  const uint32_t b = pair / (uint32_t)a.kv_heads, kh = pair - b * a.kv_heads;
+  const int length = length_of(a, b), key0 = key_block * 128 + wave * 32, key = key0 + (lane & 31);
+  const int tiles = (int)((rows + RT - 1) / RT);
+  int t0 = 0, t1 = tiles;
+  if (g.splits > 1) {
+    t0 = (int)((uint32_t)tiles * split / (uint32_t)g.splits);
+    t1 = (int)((uint32_t)tiles * (split + 1) / (uint32_t)g.splits);
+  }
+  if ((int)(key_block * 128) >= length) t1 = t0;   // a block whose keys are all past the length has nothing to sum
+  const bool idle = key0 >= length, mine = key < length;
   const float to2 = a.scale * kLog2e;
   u32x4 k[RB / 32], v[DK ? RB / 32 : 1];
   {
@@ -207,17 +307,17 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionGrad g) {
 #pragma unroll
     for (int c = 0; c < RB / 32; ++c) {
       k[c] = u32x4{0, 0, 0, 0};
-      if (key < length) k[c] = row_piece<T>(pk, 2 * c + h, a.d, ek);
+      if (mine) k[c] = row_piece<T>(pk, 2 * c + h, a.d, ek);
       if constexpr (DK) {
         v[c] = u32x4{0, 0, 0, 0};
-        if (key < length) v[c] = row_piece<T>(pv, 2 * c + h, a.d, ev);
+        if (mine) v[c] = row_piece<T>(pv, 2 * c + h, a.d, ev);
       }
     }
   }
-  const int64_t words = words_of(a.keys), flag_tiles = words / 2;
+  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
   uint64_t want = 0;
-  int64_t want0 = t0 - 64;
-  auto from = [&](int64_t t) {
+  int want0 = t0 - 64;
+  auto from = [&](int t) {
     if constexpr (!MASK) return t;
     while (t < t1) {
       if (t - want0 >= 64) {
@@ -239,68 +339,57 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionGrad g) {
       if constexpr (DV) av[f][i] = 0;
     }
   Scaled<T, DK ? FD : 1> scaled;
-  const char *const pq = (const char *)a.q.p + b * a.q.batch * (int64_t)sizeof(T);
-  const char *const pd = (const char *)g.dout.p + b * g.dout.batch * (int64_t)sizeof(T);
-  const char *const eq = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
-  const char *const ed = end_of(g.dout, a.batch, a.queries, a.heads, a.d, sizeof(T));
-  u32x4 cq[PER], cd[PER];
+  RowsOf<T, RB, DIRECT> qs(a.q, a, b, kh), ds_(g.dout, a, b, kh);
   float nl = 0, nd = 0;
   uint32_t nw = 0;
-  auto load = [&](int64_t t) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      const int64_t r = t * RT + row;
-      cq[i] = cd[i] = u32x4{0, 0, 0, 0};
-      if (row < RT && r < rows) {
-        const int64_t head = kh * group + r / a.queries, query = r % a.queries;
-        cq[i] = row_piece<T>(pq + (query * a.q.row + head * a.q.head) * (int64_t)sizeof(T), chunk, a.d, eq);
-        cd[i] = row_piece<T>(pd + (query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T), chunk, a.d, ed);
-      }
-    }
-    if (lane < 32) {
-      const int64_t r = t * RT + lane;
-      // rows past the last have the weights 2^-inf = 0
-      nl = r < rows ? g.rows[(pair * rows + r) * 2] : INFINITY;
-      nd = r < rows ? g.rows[(pair * rows + r) * 2 + 1] : 0.0f;
-      if constexpr (MASK) nw = r < rows && key0 < a.keys ? a.words[r % a.queries * words + key0 / 32] : 0;
-    }
+  // The terms and mask words of a tile's rows, a row a lane (rows past the last have the weights 2^-inf = 0).
+  auto look = [&](int t) {
+    const uint32_t r = t * RT + (lane & 31);
+    nl = r < rows ? g.rows[((int64_t)pair * rows + r) * 2] : INFINITY;
+    nd = r < rows ? g.rows[((int64_t)pair * rows + r) * 2 + 1] : 0.0f;
+    if constexpr (MASK) nw = r < rows && key0 < a.keys ? a.words[(int64_t)(r % queries) * words + key0 / 32] : 0;
   };
-  int64_t t = from(t0);
-  if (t < t1) load(t);
-  while (t < t1) {
-    const int64_t next = from(t + 1);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int slot = threadIdx.x + i * NT, row = slot / CH, chunk = slot % CH;
-      if (row >= RT) continue;
-      const int to = row * RB + ((chunk << 4) ^ exchange<RB>(row));
-      *(u32x4 *)(lq + to) = cq[i];
-      *(u32x4 *)(ld + to) = cd[i];
+  int t = from(t0), buf = 0;
+  if (t < t1) {
+    qs.load(lds, t);
+    ds_.load(lds + RT * RB, t);
+    look(t);
+  }
+  for (int turn = 0; t < t1; turn ^= 1) {
+    const int next = from(t + 1);
+    char *const lq = lds + buf * 2 * RT * RB, *const ld = lq + RT * RB;
+    uint32_t any = nw;
+    if constexpr (DIRECT) {
+      wait_loads();
+    } else {
+      barrier();   // the tile before has been read
+      qs.store(lq);
+      ds_.store(ld);
     }
     if (lane < 32) {
       if (wave == 0) {
-        rl[lane] = nl;
-        rd[lane] = nd;
+        rl[turn][lane] = nl;
+        rd[turn][lane] = nd;
       }
-      if constexpr (MASK) rw[wave][lane] = nw;
+      if constexpr (MASK) rw[turn][wave][lane] = nw;
     }
-    __syncthreads();
-    if (next < t1) load(next);
-    bool none = idle;
-    if constexpr (MASK) none = none || a.flags[t * flag_tiles + key0 / 64] == 0;
-    if (!none) {
+    barrier();     // the tile is there for all (DIRECT: and nobody reads the other one any more)
+    if (next < t1) {
+      qs.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB, next);
+      ds_.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB + RT * RB, next);
+      look(next);
+    }
+    if constexpr (DIRECT) buf ^= 1;
+    if (!idle && (!MASK || __any(any != 0))) {
       const f32x16 s = times_rows<T, RB>(lq, 0, k);
       f32x16 dp;
       if constexpr (DK) dp = times_rows<T, RB>(ld, 0, v);
       float p[16], ds[16];
-      const bool mine = key < length;
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        const f32x4 l2 = *(const f32x4 *)(rl + row_of(i, h)), dd = *(const f32x4 *)(rd + row_of(i, h));
+        const f32x4 l2 = *(const f32x4 *)(&rl[turn][row_of(i, h)]), dd = *(const f32x4 *)(&rd[turn][row_of(i, h)]);
         u32x4 w = {~0u, ~0u, ~0u, ~0u};
-        if constexpr (MASK) w = *(const u32x4 *)(&rw[wave][row_of(i, h)]);
+        if constexpr (MASK) w = *(const u32x4 *)(&rw[turn][wave][row_of(i, h)]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bool in = mine && (!MASK || (w[j] >> (lane & 31) & 1));
@@ -320,7 +409,7 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionGrad g) {
   constexpr float down = __is_same(T, f16_t) ? 0x1p-14f : 1.0f;   // 2^-p_shift
   const float outk = a.scale * scaled.out() * down;
   if (g.part) {
-    float *const pk = g.part + (((int64_t)split * 2 * pairs + pair) * a.keys + key) * DP, *const pv = pk + pairs * a.keys * DP;
+    float *const pk = g.part + (((int64_t)split * 2 * pairs + pair) * a.keys + key) * DP, *const pv = pk + (int64_t)pairs * a.keys * DP;
 #pragma unroll
     for (int f = 0; f < FD; ++f)
 #pragma unroll
@@ -348,44 +437,47 @@ __global__ __launch_bounds__(256) void k_attention_dkv(AttentionGrad g) {
 template <class T>
 __global__ __launch_bounds__(256) void k_join_dkv(AttentionGrad g, int dp) {
   const Attention &a = g.a;
-  const int64_t pairs = a.batch * a.kv_heads, at = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 4, all = pairs * a.keys;
-  const int64_t row = at / per;
-  const int c = (int)(at % per) * 4;
+  const uint32_t per = dp / 4, keys = (uint32_t)a.keys, all = (uint32_t)a.batch * a.kv_heads * keys;
+  const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = at / per;
+  const int c = (int)(at - row * per) * 4;
   if (row >= 2 * all || c >= a.d) return;
   float v[4] = {0, 0, 0, 0};
   for (int s = 0; s < g.splits; ++s) {
-    const f32x4 x = *(const f32x4 *)(g.part + (s * 2 * all + row) * dp + c);
+    const f32x4 x = *(const f32x4 *)(g.part + ((int64_t)s * 2 * all + row) * dp + c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += x[i];
   }
   const Heads &o = row < all ? g.dk : g.dv;
-  const int64_t pk = row < all ? row : row - all, pair = pk / a.keys, key = pk % a.keys;
-  store_values4<T>((T *)o.p + pair / a.kv_heads * o.batch + key * o.row + pair % a.kv_heads * o.head + c, a.d - c, v[0], v[1], v[2], v[3]);
+  const uint32_t pk = row < all ? row : row - all, pair = pk / keys, key = pk - pair * keys, b = pair / (uint32_t)a.kv_heads;
+  store_values4<T>((T *)o.p + b * o.batch + key * o.row + (pair - b * a.kv_heads) * o.head + c, a.d - c, v[0], v[1], v[2], v[3]);
 }
 
+template <class T, int DP, bool MASK, bool DIRECT>
+void launch_dkv(const AttentionGrad &g, dim3 grid, hipStream_t s) {
+  // Rows of 256 values leave no registers for both sums beside a key and its value.
+  if constexpr (DP == 256) {
+    k_attention_dkv<T, DP, MASK, true, false, DIRECT><<<grid, 256, 0, s>>>(g);
+    k_attention_dkv<T, DP, MASK, false, true, DIRECT><<<grid, 256, 0, s>>>(g);
+  } else {
+    k_attention_dkv<T, DP, MASK, true, true, DIRECT><<<grid, 256, 0, s>>>(g);
+  }
+}
 template <class T, int DP, bool MASK>
 hipError_t launch_shape(const AttentionGrad &g, hipStream_t s) {
   const Attention &a = g.a;
   const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries, pairs = a.batch * a.kv_heads;
   hipError_t err = hipSuccess;
   if (rows) {
-    k_attention_rows<T><<<dim3((unsigned)((rows * pairs + 3) / 4)), 256, 0, s>>>(g);
+    const dim3 grid((unsigned)((rows + 127) / 128 * pairs));
+    if (!g.dq.p) k_attention_rows<T><<<dim3((unsigned)((rows * pairs + 15) / 16)), 256, 0, s>>>(g);
+    else if (direct_ok<T>(a.k, a) && direct_ok<T>(a.v, a)) k_attention_dq<T, DP, MASK, true><<<grid, 256, 0, s>>>(g);
+    else k_attention_dq<T, DP, MASK, false><<<grid, 256, 0, s>>>(g);
     if ((err = hipGetLastError()) != hipSuccess) return err;
-    if (g.dq.p) {
-      k_attention_dq<T, DP, MASK><<<dim3((unsigned)((rows + 127) / 128 * pairs)), 256, 0, s>>>(g);
-      if ((err = hipGetLastError()) != hipSuccess) return err;
-    }
   }
   if (!g.dk.p) return err;
   const dim3 grid((unsigned)((a.keys + 127) / 128 * pairs * g.splits));
-  // Rows of 256 fp32 values leave no registers for both sums beside a key and its value.
-  if constexpr (DP * sizeof(T) > 512) {
-    k_attention_dkv<T, DP, MASK, true, false><<<grid, 256, 0, s>>>(g);
-    if ((err = hipGetLastError()) != hipSuccess) return err;
-    k_attention_dkv<T, DP, MASK, false, true><<<grid, 256, 0, s>>>(g);
-  } else {
-    k_attention_dkv<T, DP, MASK, true, true><<<grid, 256, 0, s>>>(g);
-  }
+  if (direct_rows<T>(a.q, a) && direct_rows<T>(g.dout, a)) launch_dkv<T, DP, MASK, true>(g, grid, s);
+  else launch_dkv<T, DP, MASK, false>(g, grid, s);
   if ((err = hipGetLastError()) != hipSuccess || !g.part) return err;
   const int64_t threads = 2 * pairs * a.keys * (DP / 4);
   k_join_dkv<T><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, s>>>(g, DP);
