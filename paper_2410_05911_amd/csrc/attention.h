@@ -24,7 +24,7 @@ struct Attention {
   const uint8_t *mask;         // [queries][ldmask], or null
   int64_t ldmask;
   uint32_t *words;             // the mask packed, 32 keys a word: [queries][words_of(keys)]
-  uint8_t *flags;              // of 32 rows and 64 keys: 0 none, 1 some, 2 all allowed: [tiles of rows][tiles of keys]
+  uint8_t *flags;              // whether any of 32 queries may attend any of 64 keys: [tiles of queries][tiles of keys]
   float *lse;                  // [batch][heads][queries]; in the gradient an input
   int splits;
   float *part_o, *part_ml;     // [splits][pairs][rows][d_of(d)], [splits][pairs][rows][2]

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
     for (int c = 0; c < RB / 32; ++c) q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
   }
   Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
-  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
+  const int words = (int)words_of(a.keys);
   const uint32_t *const mask = MASK ? a.words + (int64_t)query * words + wk * SUB : nullptr;
   // Tiles of keys that none of the block's rows may attend are passed over: 64 tiles are looked up at once.
   uint64_t want = 0;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a.flags, row_block * WQ, WQ, (rows + 31) / 32, (t + lane) * KT, KT, flag_tiles));
+        want = __ballot(t + lane < t1 && any_flag(a, row_block * (32 * WQ), 32 * WQ, (t + lane) * KT, KT));
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -303,40 +303,39 @@ __device__ __forceinline__ uint32_t nonzero4(uint32_t w) {
   const uint32_t t = ((((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w) >> 7) & 0x01010101u;
   return (t * 0x01020408u) >> 24 & 15u;
 }
-// The mask in words of 32 keys, and what each 32 rows may attend of each 64 keys.  A wavefront takes 32 rows and two such tiles of
-// keys; bits past the last key are 0 in the words, and do not count in the flags.
+// The mask in words of 32 keys (0 past the last), and whether any of 32 queries may attend any of 64 keys.  A wavefront takes 32
+// queries and two such tiles of keys.
 __global__ __launch_bounds__(64) void k_pack_mask(Attention a) {
   const int lane = threadIdx.x, h = lane >> 5;
-  const uint32_t queries = (uint32_t)a.queries, rows = (uint32_t)(a.heads / a.kv_heads) * queries;
   const uint32_t words = (uint32_t)words_of(a.keys), tiles = words / 2, per = (tiles + 1) / 2;
-  const uint32_t rt = blockIdx.x / per, t = (blockIdx.x - rt * per) * 2 + h, r = rt * 32 + (lane & 31);
-  const bool live = r < rows && t < tiles;
-  uint64_t w = 0, full = ~(uint64_t)0;
-  if (live) {
+  const uint32_t qt = blockIdx.x / per, t = (blockIdx.x - qt * per) * 2 + h, query = qt * 32 + (lane & 31);
+  uint64_t w = 0;
+  if (query < a.queries && t < tiles) {
     const int64_t k0 = (int64_t)t * 64;
     const int n = a.keys - k0 < 64 ? (int)(a.keys - k0) : 64;
-    if (n < 64) full = ((uint64_t)1 << n) - 1;
-    const uint8_t *const p = a.mask + (int64_t)(r % queries) * a.ldmask + k0;
+    const char *const p = (const char *)a.mask + (int64_t)query * a.ldmask + k0;
+    u32x4 v[4];
     if (n == 64) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const u32x4 v = any16((const char *)p + 16 * c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t x = v[i];
-          w |= (uint64_t)nonzero4(x) << (16 * c + 4 * i);
-        }
-      }
+      for (int c = 0; c < 4; ++c) v[c] = any16(p + 16 * c);
     } else {
-      for (int i = 0; i < n; ++i) w |= (uint64_t)(p[i] != 0) << i;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (n >= 16 * c + 16) v[c] = any16(p + 16 * c);
+        else v[c] = some_values<uint8_t>(p + 16 * c, n - 16 * c);
+      }
     }
-    if (r < queries) *(uint64_t *)(a.words + (int64_t)r * words + t * 2) = w;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = v[c][i];
+        w |= (uint64_t)nonzero4(x) << (16 * c + 4 * i);
+      }
+    *(uint64_t *)(a.words + (int64_t)query * words + t * 2) = w;
   }
-  const uint64_t any = __ballot(live && w != 0), gap = __ballot(live && w != full);
-  if ((lane & 31) == 0 && t < tiles) {
-    const uint32_t x = (uint32_t)(any >> (32 * h)), y = (uint32_t)(gap >> (32 * h));
-    a.flags[(int64_t)rt * tiles + t] = x == 0 ? 0 : y == 0 ? 2 : 1;
-  }
+  const uint64_t any = __ballot(w != 0);
+  if ((lane & 31) == 0 && t < tiles) a.flags[(int64_t)qt * tiles + t] = (uint32_t)(any >> (32 * h)) != 0;
 }
 
 template <class T, int DP, int WQ, int WK>
@@ -388,7 +387,7 @@ AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t k
   p.splits = splits > 1 && blocks < 512 ? (int)splits : 1;
   if (masked) {
     p.words = (size_t)(queries * words_of(keys)) * 4;
-    p.flags = (size_t)((rows + 31) / 32 * (words_of(keys) / 2));
+    p.flags = (size_t)((queries + 31) / 32 * (words_of(keys) / 2));
   }
   if (p.splits > 1) {
     p.part_o = (size_t)(p.splits * pairs * rows * dp) * 4;
@@ -398,8 +397,8 @@ AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t k
 }
 
 hipError_t launch_mask(const Attention &a, hipStream_t s) {
-  const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries, tiles = words_of(a.keys) / 2;
-  k_pack_mask<<<dim3((unsigned)((rows + 31) / 32 * ((tiles + 1) / 2))), 64, 0, s>>>(a);
+  const int64_t tiles = words_of(a.keys) / 2;
+  k_pack_mask<<<dim3((unsigned)((a.queries + 31) / 32 * ((tiles + 1) / 2))), 64, 0, s>>>(a);
   return hipGetLastError();
 }
 

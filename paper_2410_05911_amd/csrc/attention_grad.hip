@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
   }
   const float to2 = a.scale * kLog2e;
   Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
-  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
+  const int words = (int)words_of(a.keys);
   const uint32_t *const mask = MASK ? a.words + (int64_t)query * words : nullptr;
   uint64_t want = 0;
   int want0 = -64;
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a.flags, row_block * 4, 4, (rows + 31) / 32, (t + lane) * KT, KT, flag_tiles));
+        want = __ballot(t + lane < t1 && any_flag(a, row_block * 128, 128, (t + lane) * KT, KT));
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
       }
     }
   }
-  const int words = (int)words_of(a.keys), flag_tiles = words / 2;
+  const int words = (int)words_of(a.keys);
   uint64_t want = 0;
   int want0 = t0 - 64;
   auto from = [&](int t) {
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a.flags, t + lane, 1, tiles, key_block * 128, 128, flag_tiles));
+        want = __ballot(t + lane < t1 && any_flag(a, (t + lane) * RT, RT, key_block * 128, 128));
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -505,7 +505,7 @@ AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, 
   p.splits = splits > 1 ? (int)splits : 1;
   if (masked) {
     p.words = (size_t)(queries * words_of(keys)) * 4;
-    p.flags = (size_t)((rows + 31) / 32 * (words_of(keys) / 2));
+    p.flags = (size_t)((queries + 31) / 32 * (words_of(keys) / 2));
   }
   p.rows = (size_t)(rows * pairs) * 8;
   if (p.splits > 1) p.part = (size_t)(p.splits * 2 * pairs * keys * d_of(d)) * 4;

@@ -195,11 +195,17 @@ struct Keys {
   }
 };
 
-// Whether any of `count` tiles of rows from `first` on may attend any of `keys` keys from key0 on.
-__device__ __forceinline__ bool any_flag(const uint8_t *flags, int first, int count, int row_tiles, int key0, int keys, int flag_tiles) {
+// Whether any of `count` rows from row `first` on may attend any of `keys` keys from key0 on, by the tiles of 32 queries that they
+// fall in.
+__device__ __forceinline__ bool any_flag(const Attention &a, uint32_t first, uint32_t count, int key0, int keys) {
+  const uint32_t queries = (uint32_t)a.queries, tiles = (queries + 31) / 32, key_tiles = (uint32_t)words_of(a.keys) / 2;
+  const uint32_t c0 = key0 / 64, c1 = min((uint32_t)(key0 + keys + 63) / 64, key_tiles);
+  uint32_t q = first % queries / 32, left = min((count + 31) / 32 + 2, tiles);   // one more at each end, and behind the last query
   int any = 0;
-  for (int i = 0; i < count && first + i < row_tiles; ++i)
-    for (int c = key0 / 64; c * 64 < key0 + keys && c < flag_tiles; ++c) any |= flags[(int64_t)(first + i) * flag_tiles + c];
+  for (; left > 0; --left) {
+    for (uint32_t c = c0; c < c1; ++c) any |= a.flags[(int64_t)q * key_tiles + c];
+    q = q + 1 == tiles ? 0 : q + 1;
+  }
   return any != 0;
 }
 

@@ -168,11 +168,11 @@ __device__ __forceinline__ void tile_of(uint32_t block, uint32_t tm, uint32_t tn
 struct Share {
   int m0, n0, k0, k1, split;
   template <int BM, int BN, int KT>
-  static __device__ __forceinline__ Share of(const Gemm &g) {
+  static __device__ __forceinline__ Share of(const Gemm &g, uint32_t block) {
     const uint32_t tm = (uint32_t)(g.m + BM - 1) / BM, tn = (uint32_t)(g.n + BN - 1) / BN, tiles = tm * tn;
-    const uint32_t split = g.splits > 1 ? blockIdx.x / tiles : 0, kt = (uint32_t)(g.k + KT - 1) / KT;
+    const uint32_t split = g.splits > 1 ? block / tiles : 0, kt = (uint32_t)(g.k + KT - 1) / KT;
     uint32_t im, in, first = 0, last = kt;
-    tile_of(blockIdx.x - split * tiles, tm, tn, im, in);
+    tile_of(block - split * tiles, tm, tn, im, in);
     if (g.splits > 1) {
       first = kt * split / (uint32_t)g.splits;
       last = kt * (split + 1) / (uint32_t)g.splits;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm(Gemm g) {
   constexpr int AHEAD = CA + CB <= 4 ? 3 : 1;   // tiles on their way in registers
   static_assert(TA::SLOTS % NT == 0 && TB::SLOTS % NT == 0, "whole slots");
   __shared__ __attribute__((aligned(16))) char lds[2 * BYTES];
-  const Share at = Share::of<BM, BN, KT>(g);
+  const Share at = Share::of<BM, BN, KT>(g, blockIdx.x);
   const int m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1, split = at.split;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
@@ -374,14 +374,17 @@ struct Direct {
 };
 
 // STAGES tiles of LDS: while one is multiplied, STAGES - 2 lie ready or are on their way beside the one being asked for.
+template <int BM, int BN, int WM, int WN, int STAGES>
+struct DirectShape {
+  static constexpr int BYTES = (BM + BN) * 128, STRIPS = WM * WN * 32 * (BN / WN + 4) * 4;   // a stage; what finish_block takes
+  static constexpr int LDS = STAGES * BYTES > STRIPS ? STAGES * BYTES : STRIPS;
+};
 template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
-__global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
+__device__ __forceinline__ void gemm_direct(const Gemm &g, uint32_t block, char *lds) {
   typedef Tile<T, T, AA, BM> TA;
   typedef Tile<T, T, BA, BN> TB;
   constexpr int NT = WM * WN * 64, FM = BM / WM / 32, FN = BN / WN / 32, KT = TA::KT, BYTES = (BM + BN) * 128;
-  constexpr int STRIPS = WM * WN * 32 * (FN * 32 + 4) * 4;   // what finish_block takes
-  __shared__ __attribute__((aligned(16))) char lds[STAGES * BYTES > STRIPS ? STAGES * BYTES : STRIPS];
-  const Share at = Share::of<BM, BN, KT>(g);
+  const Share at = Share::of<BM, BN, KT>(g, block);
   const int m0 = at.m0, n0 = at.n0, k0 = at.k0, k1 = at.k1, split = at.split;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const int wm = wave / WN * (FM * 32), wn = wave % WN * (FN * 32);
@@ -453,45 +456,19 @@ __global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
   finish_block<T, FM, FN>(g, acc, lds, split, m0 + wm, n0 + wn);
 }
 
-// The splits' sums of four outputs a thread, in the order of the splits, and the epilogue.
-template <bool INT>
-__global__ __launch_bounds__(256) void k_join(Gemm g) {
-  const uint32_t per = (uint32_t)(g.n + 3) / 4, at = blockIdx.x * 256 + threadIdx.x;
-  const int m = (int)(at / per), n = (int)(at % per) * 4;
-  if (m >= g.m) return;
-  const int count = g.n - n < 4 ? (int)(g.n - n) : 4;
-  float v[4] = {0, 0, 0, 0};
-  int32_t w[4] = {0, 0, 0, 0};
-  const float *const part = (const float *)g.part + (int64_t)m * g.n + n;
-  for (int s = 0; s < g.splits; s += 8) {
-    float p[8][4];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) load_part<float, 4>(part + (int64_t)min(s + j, g.splits - 1) * g.m * g.n, count, p[j]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (s + j >= g.splits) break;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (INT) w[i] += __builtin_bit_cast(int32_t, p[j][i]);
-        else v[i] += p[j][i];
-      }
-    }
-  }
-  if constexpr (INT) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)w[i];
-  }
-  finish<4>(g.e, m, n, count, v);
+template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM *WN * 64) void k_gemm_direct(Gemm g) {
+  __shared__ __attribute__((aligned(16))) char lds[DirectShape<BM, BN, WM, WN, STAGES>::LDS];
+  gemm_direct<T, AA, BA, BM, BN, WM, WN, STAGES>(g, blockIdx.x, lds);
+}
+// A gradient's two products in one launch: small ones leave compute units idle one after the other.
+template <class T, bool BA>
+__global__ __launch_bounds__(256) void k_gemm_two(Gemm g0, Gemm g1, uint32_t blocks0) {
+  __shared__ __attribute__((aligned(16))) char lds[DirectShape<64, 64, 2, 2, 4>::LDS];
+  if (blockIdx.x < blocks0) gemm_direct<T, false, BA, 64, 64, 2, 2, 4>(g0, blockIdx.x, lds);
+  else gemm_direct<T, true, true, 64, 64, 2, 2, 4>(g1, blockIdx.x - blocks0, lds);
 }
 
-template <class T>
-hipError_t join(const Gemm &g, hipStream_t s) {
-  const hipError_t err = hipGetLastError();
-  if (err != hipSuccess || !g.part) return err;
-  const int64_t join = ((int64_t)g.m * ((g.n + 3) / 4) + 255) / 256;
-  k_join<__is_same(T, int8_t)><<<dim3((unsigned)join), dim3(256), 0, s>>>(g);
-  return hipGetLastError();
-}
 // ---- few rows: the weights are read once, by vector instructions
 constexpr int kFewRows = 4, kFewRound = 256;   // k of a split at least
 
@@ -677,66 +654,87 @@ __global__ __launch_bounds__(256) void k_few_along(Gemm g) {
 }
 template <class S, int R>
 hipError_t launch_few_rows(const Gemm &g, hipStream_t s) {
-  if (!g.b.across) {
-    k_few_along<S, R><<<dim3((unsigned)((g.n + 7) / 8)), 256, 0, s>>>(g);
-    return hipGetLastError();
-  }
   // Blocks that sum all of k need its lines on their way at once: 1024 x 1024 bf16 8.1 us in blocks of 256 threads, 5 in those of 1024.
-  if (g.splits == 1) k_few_across<S, R, 1024><<<dim3((unsigned)((g.n + 63) / 64)), 1024, 0, s>>>(g);
+  if (!g.b.across) k_few_along<S, R><<<dim3((unsigned)((g.n + 7) / 8)), 256, 0, s>>>(g);
+  else if (g.splits == 1) k_few_across<S, R, 1024><<<dim3((unsigned)((g.n + 63) / 64)), 1024, 0, s>>>(g);
   else k_few_across<S, R, 256><<<dim3((unsigned)((g.n + 63) / 64 * g.splits)), 256, 0, s>>>(g);
-  return join<S>(g, s);
+  return hipGetLastError();
 }
 template <class S>
 hipError_t launch_few(const Gemm &g, hipStream_t s) {
   return g.m == 1 ? launch_few_rows<S, 1>(g, s) : g.m == 2 ? launch_few_rows<S, 2>(g, s) : launch_few_rows<S, 4>(g, s);
 }
 
+template <int BM, int BN>
+unsigned blocks_of(const Gemm &g) {
+  return (unsigned)((int64_t)((g.m + BM - 1) / BM) * ((g.n + BN - 1) / BN) * g.splits);
+}
 template <class T, class S, bool AA, bool BA, int BM, int BN, int WM, int WN>
 hipError_t launch_tile(const Gemm &g, hipStream_t s) {
-  const int64_t blocks = (int64_t)((g.m + BM - 1) / BM) * ((g.n + BN - 1) / BN) * g.splits;
-  k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
-  return join<T>(g, s);
+  k_gemm<T, S, AA, BA, BM, BN, WM, WN><<<dim3(blocks_of<BM, BN>(g)), dim3(WM * WN * 64), 0, s>>>(g);
+  return hipGetLastError();
 }
 template <class T, bool AA, bool BA, int BM, int BN, int WM, int WN, int STAGES>
 hipError_t launch_direct(const Gemm &g, hipStream_t s) {
-  const int64_t blocks = (int64_t)((g.m + BM - 1) / BM) * ((g.n + BN - 1) / BN) * g.splits;
-  k_gemm_direct<T, AA, BA, BM, BN, WM, WN, STAGES><<<dim3((unsigned)blocks), dim3(WM * WN * 64), 0, s>>>(g);
-  return join<T>(g, s);
+  k_gemm_direct<T, AA, BA, BM, BN, WM, WN, STAGES><<<dim3(blocks_of<BM, BN>(g)), dim3(WM * WN * 64), 0, s>>>(g);
+  return hipGetLastError();
 }
 
 // Whether k_gemm_direct takes a factor of `rows` rows: whole pieces at 16-byte addresses, offsets in a tile of 256 rows within 2^31.
 template <class T>
 bool direct_ok(const Factor &f, int rows, int k) {
   constexpr int64_t E = 16 / sizeof(T);
-  return (uintptr_t)f.p % 16 == 0 && f.ld % E == 0 && (f.across ? rows : k) % E == 0 && f.ld < ((int64_t)1 << 22) / (int64_t)sizeof(T);
+  return (uintptr_t)f.p % 16 == 0 && f.ld % E == 0 && (f.packed || (f.across ? rows : k) % E == 0) &&
+         f.ld < ((int64_t)1 << 22) / (int64_t)sizeof(T);
+}
+template <class T>
+bool direct_ok(const Gemm &g) {
+  return direct_ok<T>(g.a, g.m, g.k) && direct_ok<T>(g.b, g.n, g.k);
 }
 
 // The tiles that plan_gemm chooses from.
 constexpr int kTileSide[3][2] = {{64, 64}, {128, 128}, {256, 256}};
 template <class T, class S, bool AA, bool BA>
 hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {
-  if constexpr (__is_same(T, S)) {
-    if (direct_ok<T>(g.a, g.m, g.k) && direct_ok<T>(g.b, g.n, g.k)) {
-      if constexpr (sizeof(T) < 4) {
-        if (p.tile == 2) return launch_direct<T, AA, BA, 256, 256, 2, 4, 2>(g, s);
-      }
-      if (p.tile >= 1 && !AA && g.k * (int64_t)sizeof(T) <= 128) return launch_direct<T, AA, BA, 128, 128, 2, 2, 1>(g, s);
-      if (p.tile >= 1) return launch_direct<T, AA, BA, 128, 128, 2, 2, 2>(g, s);
-      return launch_direct<T, AA, BA, 64, 64, 2, 2, 4>(g, s);
+  if ((__is_same(T, S) || g.a.packed) && direct_ok<T>(g)) {
+    if constexpr (sizeof(T) < 4) {
+      if (p.tile == 2) return launch_direct<T, AA, BA, 256, 256, 2, 4, 2>(g, s);
     }
+    if constexpr (!AA) {
+      if (p.tile >= 1 && g.k * (int64_t)sizeof(T) <= 128) return launch_direct<T, AA, BA, 128, 128, 2, 2, 1>(g, s);
+    }
+    if (p.tile >= 1) return launch_direct<T, AA, BA, 128, 128, 2, 2, 2>(g, s);
+    return launch_direct<T, AA, BA, 64, 64, 2, 2, 4>(g, s);
   }
   if (p.tile == 0) return launch_tile<T, S, AA, BA, 64, 64, 2, 2>(g, s);
   return launch_tile<T, S, AA, BA, 128, 128, 2, 2>(g, s);
 }
 // Codes are never a gradient's factor, so a of theirs lies along k.
-template <class T, class S = T>
-hipError_t launch_type(const Gemm &g, const GemmPlan &p, hipStream_t s) {
+template <class T, class S>
+hipError_t launch_one(const Gemm &g, const GemmPlan &p, hipStream_t s) {
+  if (g.m == 0 || g.n == 0) return hipSuccess;
+  if (p.few) return g.a.across ? hipErrorInvalidValue : launch_few<S>(g, s);
   if constexpr (sizeof(S) > 1) {
     if (g.a.across && g.b.across) return launch_layout<T, S, true, true>(g, p, s);
   }
   if (g.a.across) return hipErrorInvalidValue;
-  if (g.m <= kFewRows && p.few) return launch_few<S>(g, s);
   return g.b.across ? launch_layout<T, S, false, true>(g, p, s) : launch_layout<T, S, false, false>(g, p, s);
+}
+template <class T, class S = T>
+hipError_t launch_type(const Gemm *g, const GemmPlan *p, int count, hipStream_t s) {
+  if constexpr (sizeof(S) > 1) {
+    if (count == 2 && !p[0].few && !p[1].few && p[0].tile == 0 && p[1].tile == 0 && g[0].m > 0 && direct_ok<T>(g[0]) && direct_ok<T>(g[1])) {
+      const unsigned first = blocks_of<64, 64>(g[0]), all = first + blocks_of<64, 64>(g[1]);
+      if (g[0].b.across) k_gemm_two<T, true><<<dim3(all), 256, 0, s>>>(g[0], g[1], first);
+      else k_gemm_two<T, false><<<dim3(all), 256, 0, s>>>(g[0], g[1], first);
+      return hipGetLastError();
+    }
+  }
+  for (int i = 0; i < count; ++i) {
+    const hipError_t err = launch_one<T, S>(g[i], p[i], s);
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 }  // namespace aecct

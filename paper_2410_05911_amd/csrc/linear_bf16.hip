@@ -2,5 +2,5 @@
 #include "gemm.h"
 
 namespace aecct {
-hipError_t launch_gemm_bf16(const Gemm &g, const GemmPlan &plan, hipStream_t s) { return launch_type<bf16_t>(g, plan, s); }
+hipError_t launch_gemm_bf16(const Gemm *g, const GemmPlan *plan, int count, hipStream_t s) { return launch_type<bf16_t>(g, plan, count, s); }
 }  // namespace aecct

@@ -43,8 +43,34 @@ aecct_status check_linear(const aecct_linear_map_args *a) {
   return a->code_type == AECCT_CODE_I8 && a->in > kMaxIntWidth ? AECCT_ERR_UNSUPPORTED : AECCT_OK;
 }
 int kind(const aecct_linear_map_args *a) { return a->code_type == AECCT_CODE_NONE ? a->type : aecct::kCodeType + a->code_type; }
-aecct::GemmPlan plan(const aecct_linear_map_args *a) {
-  return aecct::plan_gemm(kind(a), a->rows, a->out, a->in, false, !a->w_turned, a->ldw);
+// Products of fewer operations are done before a launch that copies their factors into whole pieces would pay.
+constexpr double kPackWork = 4e9;
+// A forward map's workspace: copies of ragged factors, the splits' sums.
+struct MapWork {
+  aecct::GemmPlan plan;
+  bool pack_x, pack_w;
+  int64_t ldx, ldw;
+  size_t x, w, part, total;
+};
+MapWork map_work(const aecct_linear_map_args *a) {
+  MapWork m{};
+  const int t = kind(a);
+  const int64_t lines = a->w_turned ? a->out : a->in, across = a->w_turned ? a->in : a->out;
+  const bool ragged_x = aecct::ragged(t, a->ldx, a->in), ragged_w = aecct::ragged(t, a->ldw, across),
+             pack = 2.0 * a->rows * a->in * a->out >= kPackWork;
+  m.plan = aecct::plan_gemm(t, a->rows, a->out, a->in, false, !a->w_turned, a->ldw, pack || !(ragged_x || ragged_w));
+  if (!m.plan.few && pack) {
+    m.pack_x = ragged_x;
+    m.pack_w = ragged_w;
+  }
+  m.ldx = aecct::packed_line(t, a->in);
+  m.ldw = aecct::packed_line(t, across);
+  m.x = m.pack_x ? align_up((size_t)(a->rows * m.ldx * aecct::type_bytes(t))) : 0;
+  m.w = m.pack_w ? align_up((size_t)(lines * m.ldw * aecct::type_bytes(t))) : 0;
+  m.part = align_up(m.plan.part_bytes);
+  m.total = m.x + m.w + m.part;
+  if (m.total) m.total += kAlign;
+  return m;
 }
 
 aecct_status check_grad(const aecct_linear_map_grad_args *a) {
@@ -52,22 +78,39 @@ aecct_status check_grad(const aecct_linear_map_grad_args *a) {
   if (a->act < AECCT_ACT_NONE || a->act > AECCT_ACT_SILU || (a->w_turned != 0 && a->w_turned != 1)) return AECCT_ERR_INVALID_ARG;
   return sizes_ok(a->rows, a->in, a->out);
 }
-// What a gradient's workspace holds: dz, the splits' sums of one product after the other, the column sums.
+// What a gradient's workspace holds: dz, copies of ragged factors, the splits' sums of both products, the column sums.
 struct GradWork {
   aecct::GemmPlan dx, dw;
-  int64_t lddz;
-  size_t dz, part, sums, total;
+  bool need_dz, pack_x, pack_w, pack_dy;
+  int64_t lddz, ldx, ldw;
+  size_t dz, x, w, part_dx, part_dw, sums, total;
 };
 GradWork grad_work(const aecct_linear_map_grad_args *a) {
   GradWork w{};
-  w.dx = aecct::plan_gemm(a->type, a->rows, a->in, a->out, false, a->w_turned, a->ldw);
-  w.dw = aecct::plan_gemm(a->type, a->in, a->out, a->rows, true, true, 0);
-  w.lddz = (a->out + 63) / 64 * 64;
-  w.dz = a->act != AECCT_ACT_NONE ? align_up((size_t)(a->rows * w.lddz * type_size(a->type))) : 0;
-  const size_t p = a->dx ? w.dx.part_bytes : 0, q = a->dw ? w.dw.part_bytes : 0;
-  w.part = align_up(p > q ? p : q);
+  const int t = a->type, size = aecct::type_bytes(t);
+  const int64_t lines = a->w_turned ? a->out : a->in, across = a->w_turned ? a->in : a->out;
+  w.need_dz = a->act != AECCT_ACT_NONE && (a->dx || a->dw);
+  w.lddz = aecct::packed_line(t, a->out);
+  // With a first launch for dz or the sums the copies cost little more.
+  const bool pack = w.need_dz || a->dbias || 2.0 * a->rows * a->in * a->out >= kPackWork;
+  const bool ragged_x = aecct::ragged(t, a->ldx, a->in), ragged_w = aecct::ragged(t, a->ldw, across),
+             ragged_d = !w.need_dz && aecct::ragged(t, a->lddy, a->out);
+  w.dx = aecct::plan_gemm(t, a->rows, a->in, a->out, false, a->w_turned, a->ldw, pack || !(ragged_w || ragged_d));
+  w.dw = aecct::plan_gemm(t, a->in, a->out, a->rows, true, true, 0, pack || !(ragged_x || ragged_d));
+  if (pack) {
+    w.pack_x = a->dw && ragged_x;
+    w.pack_w = a->dx && !w.dx.few && ragged_w;
+    w.pack_dy = ragged_d && (a->dw || (a->dx && !w.dx.few));
+  }
+  w.ldx = aecct::packed_line(t, a->in);
+  w.ldw = aecct::packed_line(t, across);
+  w.dz = w.need_dz || w.pack_dy ? align_up((size_t)(a->rows * w.lddz * size)) : 0;
+  w.x = w.pack_x ? align_up((size_t)(a->rows * w.ldx * size)) : 0;
+  w.w = w.pack_w ? align_up((size_t)(lines * w.ldw * size)) : 0;
+  w.part_dx = a->dx ? align_up(w.dx.part_bytes) : 0;
+  w.part_dw = a->dw ? align_up(w.dw.part_bytes) : 0;
   w.sums = a->dbias ? align_up((size_t)(aecct::slope_blocks(a->rows, a->out) * a->out) * 4) : 0;
-  w.total = w.dz + w.part + w.sums;
+  w.total = w.dz + w.x + w.w + w.part_dx + w.part_dw + w.sums;
   if (w.total) w.total += kAlign;
   return w;
 }
@@ -80,8 +123,7 @@ aecct_status aecct_linear_map_workspace_size(const aecct_linear_map_args *a, siz
   if (!bytes) return AECCT_ERR_INVALID_ARG;
   const aecct_status s = check_linear(a);
   if (s != AECCT_OK) return s;
-  const size_t part = plan(a).part_bytes;
-  *bytes = part ? kAlign + align_up(part) : 0;
+  *bytes = map_work(a).total;
   return AECCT_OK;
 }
 
@@ -108,23 +150,39 @@ aecct_status aecct_linear_map(const aecct_linear_map_args *a, void *workspace, s
   for (int i = 0; i < 6; ++i)
     for (int k = 0; k < 2; ++k)
       if (overlap(out[k], in[i]) && !(i == 5 && k == 1 && same(out[k], in[i]))) return AECCT_ERR_INVALID_ARG;
-  const aecct::GemmPlan p = plan(a);
-  void *part = nullptr;
-  if (p.part_bytes) {
-    const size_t need = kAlign + align_up(p.part_bytes);
-    if (workspace_bytes < need) return AECCT_ERR_WORKSPACE_TOO_SMALL;
+  const MapWork m = map_work(a);
+  char *ws = nullptr;
+  if (m.total) {
+    if (workspace_bytes < m.total) return AECCT_ERR_WORKSPACE_TOO_SMALL;
     if (!workspace) return AECCT_ERR_INVALID_ARG;
-    const Span ws{workspace, 1, (int64_t)need, 0};
+    const Span all{workspace, 1, (int64_t)m.total, 0};
     for (const Span &t : in)
-      if (overlap(ws, t)) return AECCT_ERR_INVALID_ARG;
-    if (overlap(ws, out[0]) || overlap(ws, out[1])) return AECCT_ERR_INVALID_ARG;
-    part = (void *)align_up((size_t)(uintptr_t)workspace);
+      if (overlap(all, t)) return AECCT_ERR_INVALID_ARG;
+    if (overlap(all, out[0]) || overlap(all, out[1])) return AECCT_ERR_INVALID_ARG;
+    ws = (char *)align_up((size_t)(uintptr_t)workspace);
+  }
+  aecct::Factor x{a->x, a->ldx, false, false}, w{a->w, a->ldw, !a->w_turned, false};
+  aecct::Prepare prepare{};
+  if (m.pack_x) {
+    prepare.pack[0] = {a->x, a->ldx, (int)a->rows, (int)a->in, ws, m.ldx};
+    x = {ws, m.ldx, false, true};
+  }
+  if (m.pack_w) {
+    prepare.pack[1] = {a->w, a->ldw, (int)lines, (int)across, ws + m.x, m.ldw};
+    w = {ws + m.x, m.ldw, !a->w_turned, true};
   }
   const float q = a->code_type == AECCT_CODE_I8 ? 127.0f : 448.0f;
-  const aecct::Gemm g{(int)a->rows, (int)a->out, (int)a->in, {a->x, a->ldx, false}, {a->w, a->ldw, !a->w_turned},
+  const aecct::Gemm g{(int)a->rows, (int)a->out, (int)a->in, x, w,
                       {a->alpha, a->scale, a->bias, 1.0f / q, a->act, a->y_type, a->res, a->z, a->y, a->ldres, a->ldz, a->ldy},
-                      part, p.splits};
-  return aecct::launch_gemm(kind(a), g, p, (hipStream_t)stream) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
+                      m.plan.part_bytes ? ws + m.x + m.w : nullptr, m.plan.splits};
+  const hipStream_t st = (hipStream_t)stream;
+  const int t = kind(a);
+  if ((m.pack_x || m.pack_w) && aecct::launch_prepare(t, prepare, st) != hipSuccess) return AECCT_ERR_DEVICE;
+  if (aecct::launch_gemm(t, &g, &m.plan, 1, st) != hipSuccess) return AECCT_ERR_DEVICE;
+  if (!g.part) return AECCT_OK;
+  aecct::Finish f{};
+  f.g[0] = g;
+  return aecct::launch_finish(t, f, st) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
 }
 
 aecct_status aecct_linear_map_grad_workspace_size(const aecct_linear_map_grad_args *a, size_t *bytes) {
@@ -161,41 +219,64 @@ aecct_status aecct_linear_map_grad(const aecct_linear_map_grad_args *a, void *wo
       if (overlap(out[i], t)) return AECCT_ERR_INVALID_ARG;
   }
   const GradWork w = grad_work(a);
-  char *dz = nullptr, *part = nullptr, *sums = nullptr;
+  char *ws = nullptr;
   if (w.total) {
     if (workspace_bytes < w.total) return AECCT_ERR_WORKSPACE_TOO_SMALL;
     if (!workspace) return AECCT_ERR_INVALID_ARG;
-    const Span ws{workspace, 1, (int64_t)w.total, 0};
+    const Span all{workspace, 1, (int64_t)w.total, 0};
     for (const Span &t : in)
-      if (overlap(ws, t)) return AECCT_ERR_INVALID_ARG;
+      if (overlap(all, t)) return AECCT_ERR_INVALID_ARG;
     for (const Span &t : out)
-      if (overlap(ws, t)) return AECCT_ERR_INVALID_ARG;
-    dz = (char *)align_up((size_t)(uintptr_t)workspace);
-    part = dz + w.dz;
-    sums = part + w.part;
+      if (overlap(all, t)) return AECCT_ERR_INVALID_ARG;
+    ws = (char *)align_up((size_t)(uintptr_t)workspace);
   }
+  char *const dz = ws, *const cx = dz + w.dz, *const cw = cx + w.x, *const part_dx = cw + w.w, *const part_dw = part_dx + w.part_dx,
+       *const sums = part_dw + w.part_dw;
   const hipStream_t s = (hipStream_t)stream;
-  const bool need_dz = sloped && (a->dx || a->dw);
-  if (need_dz || a->dbias) {
-    const aecct::Slope v{a->rows, a->out, a->act, a->dy, a->z, a->lddy, a->ldz, need_dz ? dz : nullptr, w.lddz,
-                         a->dbias ? (float *)sums : nullptr, a->dbias};
-    if (aecct::launch_slope(a->type, v, s) != hipSuccess) return AECCT_ERR_DEVICE;
+  const bool turned = a->w_turned != 0;
+  aecct::Factor x{a->x, a->ldx, true, false}, m{a->w, a->ldw, turned, false}, d{a->dy, a->lddy, false, false};
+  aecct::Prepare prepare{};
+  if (w.need_dz || a->dbias)
+    prepare.slope = {(int)a->rows, (int)a->out, a->act, a->dy, a->z, a->lddy, a->ldz, w.need_dz ? dz : nullptr, w.lddz,
+                     a->dbias ? (float *)sums : nullptr, (int)aecct::slope_blocks(a->rows, a->out)};
+  if (w.pack_x) {
+    prepare.pack[0] = {a->x, a->ldx, (int)a->rows, (int)a->in, cx, w.ldx};
+    x = {cx, w.ldx, true, true};
   }
-  const void *const d = need_dz ? (const void *)dz : a->dy;
-  const int64_t ldd = need_dz ? w.lddz : a->lddy;
+  if (w.pack_w) {
+    prepare.pack[1] = {a->w, a->ldw, (int)lines, (int)across, cw, w.ldw};
+    m = {cw, w.ldw, turned, true};
+  }
+  if (w.pack_dy) prepare.pack[2] = {a->dy, a->lddy, (int)a->rows, (int)a->out, dz, w.lddz};
+  if (w.pack_dy || w.need_dz) d = {dz, w.lddz, false, true};
+  if (aecct::launch_prepare(a->type, prepare, s) != hipSuccess) return AECCT_ERR_DEVICE;
+  aecct::Gemm g[2];
+  aecct::GemmPlan plan[2];
+  int count = 0;
   if (a->dx && a->rows) {
-    const aecct::Gemm g{(int)a->rows, (int)a->in, (int)a->out, {d, ldd, false}, {a->w, a->ldw, a->w_turned != 0},
-                        {nullptr, nullptr, nullptr, 0.0f, 0, a->type, nullptr, nullptr, a->dx, 0, 0, a->lddx},
-                        w.dx.part_bytes ? part : nullptr, w.dx.splits};
-    if (aecct::launch_gemm(a->type, g, w.dx, s) != hipSuccess) return AECCT_ERR_DEVICE;
+    plan[count] = w.dx;
+    g[count++] = {(int)a->rows, (int)a->in, (int)a->out, d, m,
+                  {nullptr, nullptr, nullptr, 0.0f, 0, a->type, nullptr, nullptr, a->dx, 0, 0, a->lddx},
+                  w.dx.part_bytes ? part_dx : nullptr, w.dx.splits};
   }
   if (a->dw) {
-    const aecct::Gemm g{(int)a->in, (int)a->out, (int)a->rows, {a->x, a->ldx, true}, {d, ldd, true},
-                        {nullptr, nullptr, nullptr, 0.0f, 0, a->dw_type, nullptr, nullptr, a->dw, 0, 0, a->lddw},
-                        w.dw.part_bytes ? part : nullptr, w.dw.splits};
-    if (aecct::launch_gemm(a->type, g, w.dw, s) != hipSuccess) return AECCT_ERR_DEVICE;
+    aecct::Factor dt = d;
+    dt.across = true;
+    plan[count] = w.dw;
+    g[count++] = {(int)a->in, (int)a->out, (int)a->rows, x, dt,
+                  {nullptr, nullptr, nullptr, 0.0f, 0, a->dw_type, nullptr, nullptr, a->dw, 0, 0, a->lddw},
+                  w.dw.part_bytes ? part_dw : nullptr, w.dw.splits};
   }
-  return AECCT_OK;
+  if (aecct::launch_gemm(a->type, g, plan, count, s) != hipSuccess) return AECCT_ERR_DEVICE;
+  aecct::Finish f{};
+  for (int i = 0; i < count; ++i) f.g[i] = g[i];
+  if (a->dbias) {
+    f.part = (const float *)sums;
+    f.blocks = (int)aecct::slope_blocks(a->rows, a->out);
+    f.n = (int)a->out;
+    f.out = a->dbias;
+  }
+  return aecct::launch_finish(a->type, f, s) == hipSuccess ? AECCT_OK : AECCT_ERR_DEVICE;
 }
 
 }  // extern "C"
