@@ -81,6 +81,20 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
   float m = -INFINITY, sum = 0;   // the row's reference, and its sum of 2^(score - reference)
   const float to2 = a.scale * kLog2e;
 
+  // Scales the sums down to a new reference where a score passes the old one by too much.
+  auto refer = [&](float top) {
+    if (!__any(top > m + slack<T>())) return;
+    const float now = top > m + slack<T>() ? top : m;
+    // A row that has met no key it may attend keeps the reference -inf; its weights are 2^-inf = 0.
+    const float down = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+    m = now;
+    sum *= down;
+#pragma unroll
+    for (int f = 0; f < FD; ++f)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[f][i] *= down;
+  };
+
   int t = from(t0), buf = 0;
   uint32_t w[SUB] = {}, w_next[SUB] = {};   // what the lane's row may attend of the tile
   auto look = [&](int t, uint32_t (&w)[SUB]) {
@@ -134,7 +148,27 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
       for (int u = 0; u < SUB; ++u) any |= w[u];
       none = none || !__any(any != 0);
     }
-    if (!none) {
+    bool dense = !none;
+    if constexpr (MASK && pairwise<T, RB>()) {
+      uint64_t in = w[0];
+      if constexpr (SUB == 2) in |= (uint64_t)w[1] << 32;
+      if (key0 + 32 * SUB > length) in = length > key0 ? in & (((uint64_t)1 << (length - key0)) - 1) : 0;
+      if (dense && !__any(__popcll(in) > kFewPairs * SUB)) {
+        dense = false;
+        while (__any(in != 0)) {
+          const int j = in ? __builtin_ctzll(in) : 0, row = wk * SUB * 32 + j;
+          const float score = sum_halves(HalfRow<RB>(lk, row, a.d).dot(q, a.d)) * to2;
+          const float s = in ? score : -INFINITY;
+          refer(s);
+          const float p = __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.0f : m));
+          sum += h == 0 ? p : 0.0f;      // both halves have it
+          // (a lane that has no pair left: no value that it may not see)
+          if (in) HalfRow<RB>(lv, row, a.d).add_to(acc, p, a.d);
+          in &= in - 1;
+        }
+      }
+    }
+    if (dense) {
       float s[SUB][16];
       float top = -INFINITY;
 #pragma unroll
@@ -162,17 +196,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
       }
       top = max_halves(top) * to2;
-      if (__any(top > m + slack<T>())) {
-        const float now = top > m + slack<T>() ? top : m;
-        // A row that has met no key it may attend keeps the reference -inf; its weights are 2^-inf = 0.
-        const float down = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
-        m = now;
-        sum *= down;
-#pragma unroll
-        for (int f = 0; f < FD; ++f)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[f][i] *= down;
-      }
+      refer(top);
       const float lift = (m == -INFINITY ? 0.0f : m) - weight_shift<T>();
       float part[4] = {0, 0, 0, 0};
 #pragma unroll

@@ -198,6 +198,19 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
       uint32_t in = MASK ? w[u] : ~0u;
       if (k0 + 32 > length) in = length > k0 ? in & ((1u << (length - k0)) - 1) : 0;
       if (idle || !__any(in != 0)) continue;
+      if constexpr (MASK && pairwise<T, RB>()) {
+        if (!__any(__popc(in) > kFewPairs)) {
+          while (__any(in != 0)) {
+            const int row = u * 32 + (in ? __builtin_ctz(in) : 0);
+            const HalfRow<RB> key(lk, row, a.d), value(lv, row, a.d);
+            const float s = sum_halves(key.dot(q, a.d)), dp = sum_halves(value.dot(dout, a.d));
+            const float ds = __builtin_amdgcn_exp2f(fmaf(s, to2, -l2)) * (dp - dd);
+            if (in) key.add_to(acc, ds, a.d);
+            in &= in - 1;
+          }
+          continue;
+        }
+      }
       const f32x16 s = times_rows<T, RB>(lk, u * 32, q), dp = times_rows<T, RB>(lv, u * 32, dout);
       in >>= 4 * h;
       float ds[16];
@@ -380,7 +393,28 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
       look(next);
     }
     if constexpr (DIRECT) buf ^= 1;
-    if (!idle && (!MASK || __any(any != 0))) {
+    bool dense = !idle && (!MASK || __any(any != 0));
+    if constexpr (MASK && DK && DV && pairwise<T, RB>()) {
+      if (dense && !__any(__popc(any) > 16)) {
+        uint32_t in = turn_bits(any);    // the rows of the tile that may attend the lane's key
+        if (!mine) in = 0;
+        if (!__any(__popc(in) > kFewPairs)) {
+          dense = false;
+          while (__any(in != 0)) {
+            const int row = in ? __builtin_ctz(in) : 0;
+            const HalfRow<RB> q(lq, row, a.d), dout(ld, row, a.d);
+            const float s = sum_halves(q.dot(k, a.d)), dp = sum_halves(dout.dot(v, a.d));
+            const float p = __builtin_amdgcn_exp2f(fmaf(s, to2, -rl[turn][row])), ds = p * (dp - rd[turn][row]);
+            if (in) {
+              dout.add_to(av, p, a.d);
+              q.add_to(ak, ds, a.d);
+            }
+            in &= in - 1;
+          }
+        }
+      }
+    }
+    if (dense) {
       const f32x16 s = times_rows<T, RB>(lq, 0, k);
       f32x16 dp;
       if constexpr (DK) dp = times_rows<T, RB>(ld, 0, v);

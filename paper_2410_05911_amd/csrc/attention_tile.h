@@ -90,6 +90,58 @@ __device__ __forceinline__ float sum_halves(float x) {
   return a + b;
 }
 
+// ---- masks that leave few pairs (a Tanner graph's): fp32 tiles go pair by pair, each lane through its own row's keys (or its key's
+// rows), where the matrix instructions would take 64 DP clocks for 32 x 32 pairs, a pair of one lane about 240 + 8 DP.
+template <class T, int RB>
+__device__ constexpr bool pairwise() { return sizeof(T) == 4 && RB <= 256; }   // more do not fit in registers
+constexpr int kFewPairs = 4;   // of a lane, for 32 keys or rows
+// The lane's half of a row of a tile: chunks 2 c + h, which are also the columns that its sums of a result's columns are for.  Read once
+// for a product and for a sum (LDS is what bounds these loops).
+template <int RB>
+struct HalfRow {
+  f32x4 x[RB / 32];
+  __device__ __forceinline__ HalfRow(const char *tile, int row, int d) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      if (8 * c >= d) break;
+      x[c] = __builtin_bit_cast(f32x4, row_chunk<RB>(tile, row, 2 * c + h));
+    }
+  }
+  // Half of the product with the row in the lane's registers.
+  __device__ __forceinline__ float dot(const u32x4 (&r)[RB / 32], int d) const {
+    float s = 0;
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      if (8 * c >= d) break;
+      const f32x4 y = __builtin_bit_cast(f32x4, r[c]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = fmaf(x[c][i], y[i], s);
+    }
+    return s;
+  }
+  template <int FD>
+  __device__ __forceinline__ void add_to(f32x16 (&acc)[FD], float w, int d) const {
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      if (8 * c >= d) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c >> 2][4 * (c & 3) + i] = fmaf(w, x[c][i], acc[c >> 2][4 * (c & 3) + i]);
+    }
+  }
+};
+// Bit k of lane r's word to bit r of lane k's, in each half of the wavefront.
+__device__ __forceinline__ uint32_t turn_bits(uint32_t x) {
+  uint32_t m = 0x0000ffffu;
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    const uint32_t y = (uint32_t)__shfl_xor((int)x, s);
+    x = threadIdx.x & s ? (x & ~m) | ((y & ~m) >> s) : (x & m) | ((y & m) << s);
+    m ^= m << (s >> 1);
+  }
+  return x;
+}
+
 // 16 bytes of a row of d values from chunk `chunk` on, zeros behind its end; `end` is where the tensor's memory ends.
 template <class T>
 __device__ __forceinline__ u32x4 row_piece(const char *row, int chunk, int d, const char *end) {
