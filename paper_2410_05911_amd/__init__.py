@@ -334,20 +334,27 @@ def _on_stream(stream):
     return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
 
 
+@functools.lru_cache(maxsize=None)
+def _raw():
+    """The current device and a device's current stream's handle, without the objects around them where torch hands them out."""
+    import torch
+    device = getattr(torch._C, "_cuda_getDevice", None) if torch.cuda.is_initialized() else None
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return device or torch.cuda.current_device, stream or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _on_current_gpu(index: int):
     """Refuses tensors of another GPU than the current one, where the library launches (index: get_device())."""
-    import torch
-    current = torch.cuda.current_device() if index >= 0 else -1
-    if index != current or index < 0:
-        raise ValueError("tensors must be on the GPU" if index < 0 else
-                         f"tensors are on cuda:{index}, the current device is cuda:{current}")
+    if index < 0:
+        raise ValueError("tensors must be on the GPU")
+    current = _raw()[0]()
+    if index != current:
+        raise ValueError(f"tensors are on cuda:{index}, the current device is cuda:{current}")
 
 
 def _current_stream(index: int) -> int:
-    """Handle of the current stream of a GPU, without a Stream object around it where torch hands it out."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
+    """Handle of the current stream of a GPU."""
+    return _raw()[1](index)
 
 
 _DTYPES: dict = {}
@@ -367,7 +374,7 @@ def _rows_of(t, shape, dtype, index: int, what):
     """(address, row stride) of a tensor of rows [..., d] of that shape, type and GPU."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)} on cuda:{index}")
     d = shape[-1]
     if t.is_contiguous():
@@ -596,7 +603,7 @@ def linear(x, w, bias=None, res=None, act="none", *, alpha=None, scale=None, y=N
     px, ldx = _rows_of(x, shape, dtype, index, "x")
     pres, ldres = (None, 0) if res is None else _rows_of(res, out_shape, y_type, index, "res")
     if y is None:
-        y = x.new_empty(out_shape, dtype=y_type)
+        y = torch.empty_like(res) if ldres == outputs and res.is_contiguous() else x.new_empty(out_shape, dtype=y_type)
         py, ldy = y.data_ptr(), outputs
     else:
         py, ldy = _rows_of(y, out_shape, y_type, index, "y")
@@ -636,7 +643,7 @@ def linear_grad(x, w, dy, z=None, act="none", *, dx=None, dw=None, dbias=None, d
     pdy, lddy = _rows_of(dy, out_shape, dtype, index, "dy")
     pz, ldz = _rows_of(z, out_shape, dtype, index, "z")
     if dx is None and with_dx:
-        dx = x.new_empty(shape)
+        dx = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
     if dw is None and with_dw:
         dw = x.new_empty((inputs, outputs), dtype=dw_type or dtype)
     if dbias is None and with_dbias:
@@ -683,7 +690,7 @@ def dropout(x, p: float, seed: int, offset=0, res=None, *, y=None, stream=None):
     px, ldx = _rows_of(x, shape, dtype, index, "x")
     pres, ldres = _rows_of(res, shape, dtype, index, "res")
     if y is None:
-        y = x.new_empty(shape)
+        y = torch.empty_like(x) if x.is_contiguous() else x.new_empty(shape)
         py, ldy = y.data_ptr(), d
     else:
         py, ldy = _rows_of(y, shape, dtype, index, "y")
@@ -695,7 +702,7 @@ def dropout(x, p: float, seed: int, offset=0, res=None, *, y=None, stream=None):
 def _heads_of(t, shape, dtype, index: int, what):
     if t is None:
         return Heads()
-    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)} on cuda:{index}")
     batch, row, head, one = t.stride()
     if one != 1 and shape[3] > 1:
@@ -745,7 +752,7 @@ def cross_attention(q, k, v, lengths=None, mask=None, scale=None, *, o=None, lse
             return cross_attention(q, k, v, lengths, mask, scale, o=o, lse=lse, with_lse=with_lse)
     index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
     if o is None:
-        o = q.new_empty(q.shape)
+        o = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     lse_shape = (sizes[0], sizes[3], sizes[1])
     if lse is None and with_lse:
         lse = q.new_empty(lse_shape, dtype=_float32())
@@ -769,11 +776,11 @@ def cross_attention_grad(q, k, v, o, lse, dout, lengths=None, mask=None, scale=N
                                         with_dkv=with_dkv)
     index, sizes, (hq, hk, hv), plengths, pmask, ldmask = _attention_of(q, k, v, lengths, mask, scale)
     if dq is None and with_dq:
-        dq = q.new_empty(q.shape)
+        dq = torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
     if dk is None and (with_dkv or dv is not None):
-        dk = k.new_empty(k.shape)
+        dk = torch.empty_like(k) if k.is_contiguous() else k.new_empty(k.shape)
     if dv is None and dk is not None:
-        dv = v.new_empty(v.shape)
+        dv = torch.empty_like(v) if v.is_contiguous() else v.new_empty(v.shape)
     if dq is None and dk is None:
         raise ValueError("no gradient is asked for")
     if lse.shape != (sizes[0], sizes[3], sizes[1]):
