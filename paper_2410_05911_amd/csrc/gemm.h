@@ -56,21 +56,30 @@ __device__ __forceinline__ void store_values(int type, void *p, int64_t at, int 
   else store_part<f16_t, V>((f16_t *)p + at, n, f);
 }
 
-// The epilogue of values (m, n0 .. n0 + count), count <= V.
+// What the epilogue takes of V columns (n0 .. n0 + count, count <= V).
 template <int V>
-__device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[V]) {
-  if (e.alpha) {
-    const float r = e.alpha[m] * e.per_q;
-    float s[V];
-    load_part<float, V>(e.scale + n0, count, s);
+struct Columns {
+  float scale[V], bias[V];
+  __device__ __forceinline__ Columns(const Epilogue &e, int64_t n0, int count) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = v[i] * r * s[i];
+    for (int i = 0; i < V; ++i) scale[i] = bias[i] = 0;
+    if (e.alpha) load_part<float, V>(e.scale + n0, count, scale);
+    if (e.bias) load_part<float, V>(e.bias + n0, count, bias);
+  }
+};
+// The epilogue of those columns' values of row m.
+template <int V>
+__device__ __forceinline__ void finish(const Epilogue &e, const Columns<V> &of, int64_t m, int64_t n0, int count, float (&v)[V]) {
+  float r[V];
+  if (e.res) load_values<V>(e.type, e.res, m * e.ldres + n0, count, r);
+  if (e.alpha) {
+    const float a = e.alpha[m] * e.per_q;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = v[i] * a * of.scale[i];
   }
   if (e.bias) {
-    float b[V];
-    load_part<float, V>(e.bias + n0, count, b);
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] += b[i];
+    for (int i = 0; i < V; ++i) v[i] += of.bias[i];
   }
   if (e.z) store_values<V>(e.type, e.z, m * e.ldz + n0, count, v);
   if (e.act != kActNone) {
@@ -78,12 +87,14 @@ __device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0,
     for (int i = 0; i < V; ++i) v[i] = activate(v[i], e.act, e.type == AECCT_F32);
   }
   if (e.res) {
-    float r[V];
-    load_values<V>(e.type, e.res, m * e.ldres + n0, count, r);
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] += r[i];
   }
   store_values<V>(e.type, e.y, m * e.ldy + n0, count, v);
+}
+template <int V>
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[V]) {
+  finish<V>(e, Columns<V>(e, n0, count), m, n0, count, v);
 }
 
 // ---- staging: 16-byte pieces of a factor's tile, slot by slot
@@ -181,18 +192,36 @@ struct Share {
   }
 };
 
-// A wavefront's FM x FN sums from (m0, n0) on through the epilogue: 32 rows at a time go through LDS, so that a lane then has eight
-// neighbouring columns and neighbouring lanes a row's (stored as they lie in registers, in pieces of 16 or 8 bytes 32 rows apart,
-// 49152 x 128 -> 512 in fp32 took 89 us).  All wavefronts of the block are done with the tiles in LDS before.
+// 32 rows of sums in LDS through the epilogue, V neighbouring columns a lane.
+template <int V, int FN, int TURNS>
+__device__ __forceinline__ void finish_strip(const Gemm &g, const float *strip, int split, int m0, int n0) {
+  constexpr int LD = FN * 32 + 4, PER = FN * 32 / V, STEP = 64 / PER;   // lanes a row, rows at once
+  const int lane = threadIdx.x & 63, c = lane % PER * V, n = n0 + c, count = min(g.n - n, V);
+  const Columns<V> columns(g.e, n, g.part ? 0 : count);
+#pragma unroll TURNS
+  for (int at = 0; at < 32; at += STEP) {
+    const int row = at + lane / PER, m = m0 + row;
+    if (m >= g.m || count <= 0) continue;
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const f32x4 x = *(const f32x4 *)(strip + row * LD + c + i);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[i + r] = x[r];
+    }
+    if (g.part) store_part<float, V>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
+    else finish<V>(g.e, columns, m, n, count, v);
+  }
+}
+// A wavefront's FM x FN sums from (m0, n0) on through the epilogue: 32 rows at a time go through LDS, so that a lane then has 16 bytes of
+// neighbouring outputs and neighbouring lanes a row's (stored as they lie in registers, in pieces of 16 or 8 bytes 32 rows apart,
+// 49152 x 128 -> 512 to fp32 took 89 us; in pieces of 16 bytes 32 apart 38).  All wavefronts of the block are done with the
+// tiles in LDS before.
 template <class T, int FM, int FN>
-__device__ __forceinline__ void finish_block(const Gemm &g, typename Product<T>::Acc (&acc)[FM][FN], char *lds, int split, int64_t m0,
-                                             int64_t n0) {
-  constexpr int LD = FN * 32 + 4, PER = FN * 4, STEP = 64 / PER;   // lanes a row, rows at once
+__device__ __forceinline__ void finish_block(const Gemm &g, typename Product<T>::Acc (&acc)[FM][FN], char *lds, int split, int m0, int n0) {
+  constexpr int LD = FN * 32 + 4;
   const int lane = threadIdx.x & 63, h = lane >> 5;
   float *const strip = (float *)lds + (threadIdx.x >> 6) * (32 * LD);
-  const int c = lane % PER * 8;
-  const int64_t n = n0 + c;
-  const int count = g.n - n < 8 ? (int)(g.n - n) : 8;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
@@ -209,20 +238,8 @@ __device__ __forceinline__ void finish_block(const Gemm &g, typename Product<T>:
         *(f32x4 *)(strip + (lane & 31) * LD + j * 32 + 8 * q + 4 * h) = v;
       }
     wave_sync();
-#pragma unroll 1
-    for (int row = lane / PER; row < 32; row += STEP) {
-      const int64_t m = m0 + i * 32 + row;
-      if (m >= g.m || count <= 0) continue;
-      float v[8];
-      const f32x4 lo = *(const f32x4 *)(strip + row * LD + c), hi = *(const f32x4 *)(strip + row * LD + c + 4);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        v[r] = lo[r];
-        v[4 + r] = hi[r];
-      }
-      if (g.part) store_part<float, 8>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
-      else finish<8>(g.e, m, n, count, v);
-    }
+    if (g.part || g.e.type == AECCT_F32) finish_strip<4, FN, 4>(g, strip, split, m0 + i * 32, n0);
+    else finish_strip<8, FN, (FM * FN <= 4 ? 4 : 2)>(g, strip, split, m0 + i * 32, n0);
     wave_sync();
   }
 }
