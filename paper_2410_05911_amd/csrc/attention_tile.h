@@ -16,6 +16,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 template <int RB>
 __device__ __forceinline__ int exchange(int row) {
+  if constexpr (RB >= 256) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
   return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
 }
 // Chunk `chunk` of row `row`: of a product along d.
@@ -93,7 +94,7 @@ __device__ __forceinline__ float sum_halves(float x) {
 // ---- masks that leave few pairs (a Tanner graph's): fp32 tiles go pair by pair, each lane through its own row's keys (or its key's
 // rows), where the matrix instructions would take 64 DP clocks for 32 x 32 pairs, a pair of one lane about 240 + 8 DP.
 template <class T, int RB>
-__device__ constexpr bool pairwise() { return sizeof(T) == 4 && RB <= 256; }   // more do not fit in registers
+__host__ __device__ constexpr bool pairwise() { return sizeof(T) == 4 && RB <= 256; }   // more do not fit in registers
 constexpr int kFewPairs = 4;   // of a lane, for 32 keys or rows
 // The lane's half of a row of a tile: chunks 2 c + h, which are also the columns that its sums of a result's columns are for.  Read once
 // for a product and for a sum (LDS is what bounds these loops).

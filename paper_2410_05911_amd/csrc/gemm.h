@@ -129,7 +129,7 @@ struct Tile {
       row = ((slot % PER) ^ (line_swap<T, PITCH>(k) >> 4)) * E;
     } else {
       row = slot >> 3;
-      k = ((slot & 7) ^ (row & 7)) * E;
+      k = ((slot & 7) ^ along_swap(row)) * E;
     }
   }
   // The slot's values: zeros past `k_end`, anything for rows past `rows`.  k_all: the factor's k, where its memory ends.

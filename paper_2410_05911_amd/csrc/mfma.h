@@ -71,9 +71,10 @@ __device__ __forceinline__ float e4m3_value(uint32_t w, int i) {
 }
 
 // ---- tiles in LDS
-// "Along k": a row of the tile is 128 bytes of k, its chunk c at place c ^ (row & 7), so that a wavefront's reads of one
-// chunk of 32 rows fall on different banks.
-__device__ __forceinline__ int along_k(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
+// "Along k": a row of the tile is 128 bytes of k, its chunk c at place c ^ (row / 2 % 8): LDS serves 16 lanes of 16 bytes at once where
+// they fall on all of its banks, and 16 rows of two to 256 bytes do.
+__device__ __forceinline__ int along_swap(int row) { return row >> 1 & 7; }
+__device__ __forceinline__ int along_k(int row, int chunk) { return row * 128 + ((chunk ^ along_swap(row)) << 4); }
 template <class T>
 __device__ __forceinline__ u32x4 frag_k(const char *tile, int row, int chunk) {
   return *(const u32x4 *)(tile + along_k(row, chunk));
