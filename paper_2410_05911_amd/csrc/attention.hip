@@ -46,13 +46,6 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
   const uint32_t r = row_block * (32 * WQ) + wq * 32 + (lane & 31), rc = min(r, rows - 1);
   const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * (32 * WQ) + wq * 32 >= rows;   // the whole wavefront's rows are past the last
-  u32x4 q[RB / 32];
-  {
-    const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
-    const char *const end = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
-#pragma unroll
-    for (int c = 0; c < RB / 32; ++c) q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
-  }
   Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
   const int words = (int)words_of(a.keys);
   const uint32_t *const mask = MASK ? a.words + (int64_t)query * words + wk * SUB : nullptr;
@@ -64,7 +57,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a, row_block * (32 * WQ), 32 * WQ, (t + lane) * KT, KT));
+        want = __ballot(any_flag<32 * WQ, KT>(a, row_block * (32 * WQ), min(t + lane, t1 - 1) * KT) && t + lane < t1);
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -109,6 +102,14 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
       values.load(lds + KT * RB, t);
     }
     look(t, w_next);
+  }
+  // (behind the first tile, which is on its way by now)
+  u32x4 q[RB / 32];
+  {
+    const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
+    const char *const end = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
   }
   while (t < t1) {
     const int next = from(t + 1);

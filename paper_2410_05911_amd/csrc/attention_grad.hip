@@ -101,27 +101,6 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
   const uint32_t r = row_block * 128 + wave * 32 + (lane & 31), rc = min(r, rows - 1);
   const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * 128 + wave * 32 >= rows;
-  u32x4 q[RB / 32], dout[RB / 32];
-  float dd = 0, l2;
-  {
-    const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
-    const char *const pd = (const char *)g.dout.p + (b * g.dout.batch + query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T);
-    const char *const po = (const char *)a.o.p + (b * a.o.batch + query * a.o.row + head * a.o.head) * (int64_t)sizeof(T);
-    const char *const end = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
-    const char *const endd = end_of(g.dout, a.batch, a.queries, a.heads, a.d, sizeof(T));
-    const char *const endo = end_of(a.o, a.batch, a.queries, a.heads, a.d, sizeof(T));
-#pragma unroll
-    for (int c = 0; c < RB / 32; ++c) {
-      q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
-      dout[c] = row_piece<T>(pd, 2 * c + h, a.d, endd);
-      dd = dot<T>(row_piece<T>(po, 2 * c + h, a.d, endo), dout[c], dd);
-    }
-    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l2, dd);
-    if (h == 0 && r < rows) {
-      g.rows[((int64_t)pair * rows + r) * 2] = l2;
-      g.rows[((int64_t)pair * rows + r) * 2 + 1] = dd;
-    }
-  }
   const float to2 = a.scale * kLog2e;
   Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
   const int words = (int)words_of(a.keys);
@@ -133,7 +112,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a, row_block * 128, 128, (t + lane) * KT, KT));
+        want = __ballot(any_flag<128, KT>(a, row_block * 128, min(t + lane, t1 - 1) * KT) && t + lane < t1);
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -161,6 +140,28 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
       values.load(lds + KT * RB, t);
     }
     look(t, w_next);
+  }
+  // (behind the first tile, which is on its way by now)
+  u32x4 q[RB / 32], dout[RB / 32];
+  float dd = 0, l2;
+  {
+    const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
+    const char *const pd = (const char *)g.dout.p + (b * g.dout.batch + query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T);
+    const char *const po = (const char *)a.o.p + (b * a.o.batch + query * a.o.row + head * a.o.head) * (int64_t)sizeof(T);
+    const char *const end = end_of(a.q, a.batch, a.queries, a.heads, a.d, sizeof(T));
+    const char *const endd = end_of(g.dout, a.batch, a.queries, a.heads, a.d, sizeof(T));
+    const char *const endo = end_of(a.o, a.batch, a.queries, a.heads, a.d, sizeof(T));
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      q[c] = row_piece<T>(p, 2 * c + h, a.d, end);
+      dout[c] = row_piece<T>(pd, 2 * c + h, a.d, endd);
+      dd = dot<T>(row_piece<T>(po, 2 * c + h, a.d, endo), dout[c], dd);
+    }
+    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l2, dd);
+    if (h == 0 && r < rows) {
+      g.rows[((int64_t)pair * rows + r) * 2] = l2;
+      g.rows[((int64_t)pair * rows + r) * 2 + 1] = dd;
+    }
   }
   while (t < t1) {
     const int next = from(t + 1);
@@ -302,40 +303,21 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
   const uint32_t pair = g.splits > 1 ? rest / (uint32_t)g.splits : rest, split = g.splits > 1 ? rest - pair * g.splits : 0;
   const uint32_t b = pair / (uint32_t)a.kv_heads, kh = pair - b * a.kv_heads;
   const int length = length_of(a, b), key0 = key_block * 128 + wave * 32, key = key0 + (lane & 31);
-  const int tiles = (int)((rows + RT - 1) / RT);
-  int t0 = 0, t1 = tiles;
-  if (g.splits > 1) {
-    t0 = (int)((uint32_t)tiles * split / (uint32_t)g.splits);
-    t1 = (int)((uint32_t)tiles * (split + 1) / (uint32_t)g.splits);
-  }
-  if ((int)(key_block * 128) >= length) t1 = t0;   // a block whose keys are all past the length has nothing to sum
+  // Every splits-th tile of rows, so that under a band each split has its share of those that a key meets.
+  const int tiles = (int)((rows + RT - 1) / RT), by = g.splits;
+  int t1 = (tiles - (int)split + by - 1) / by;
+  if ((int)(key_block * 128) >= length) t1 = 0;   // a block whose keys are all past the length has nothing to sum
   const bool idle = key0 >= length, mine = key < length;
   const float to2 = a.scale * kLog2e;
-  u32x4 k[RB / 32], v[DK ? RB / 32 : 1];
-  {
-    const char *const pk = (const char *)a.k.p + (b * a.k.batch + key * a.k.row + kh * a.k.head) * (int64_t)sizeof(T);
-    const char *const pv = (const char *)a.v.p + (b * a.v.batch + key * a.v.row + kh * a.v.head) * (int64_t)sizeof(T);
-    const char *const ek = end_of(a.k, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-    const char *const ev = end_of(a.v, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
-#pragma unroll
-    for (int c = 0; c < RB / 32; ++c) {
-      k[c] = u32x4{0, 0, 0, 0};
-      if (mine) k[c] = row_piece<T>(pk, 2 * c + h, a.d, ek);
-      if constexpr (DK) {
-        v[c] = u32x4{0, 0, 0, 0};
-        if (mine) v[c] = row_piece<T>(pv, 2 * c + h, a.d, ev);
-      }
-    }
-  }
   const int words = (int)words_of(a.keys);
   uint64_t want = 0;
-  int want0 = t0 - 64;
+  int want0 = -64;
   auto from = [&](int t) {
     if constexpr (!MASK) return t;
     while (t < t1) {
       if (t - want0 >= 64) {
         want0 = t;
-        want = __ballot(t + lane < t1 && any_flag(a, (t + lane) * RT, RT, key_block * 128, 128));
+        want = __ballot(any_flag<RT, 128>(a, (min(t + lane, t1 - 1) * by + split) * RT, key_block * 128) && t + lane < t1);
       }
       const uint64_t left = want >> (t - want0);
       if (left) return t + __builtin_ctzll(left);
@@ -357,16 +339,33 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
   uint32_t nw = 0;
   // The terms and mask words of a tile's rows, a row a lane (rows past the last have the weights 2^-inf = 0).
   auto look = [&](int t) {
-    const uint32_t r = t * RT + (lane & 31);
+    const uint32_t r = (t * by + split) * RT + (lane & 31);
     nl = r < rows ? g.rows[((int64_t)pair * rows + r) * 2] : INFINITY;
     nd = r < rows ? g.rows[((int64_t)pair * rows + r) * 2 + 1] : 0.0f;
     if constexpr (MASK) nw = r < rows && key0 < a.keys ? a.words[(int64_t)(r % queries) * words + key0 / 32] : 0;
   };
-  int t = from(t0), buf = 0;
+  int t = from(0), buf = 0;
   if (t < t1) {
-    qs.load(lds, t);
-    ds_.load(lds + RT * RB, t);
+    qs.load(lds, t * by + split);
+    ds_.load(lds + RT * RB, t * by + split);
     look(t);
+  }
+  // (behind the first tile, which is on its way by now)
+  u32x4 k[RB / 32], v[DK ? RB / 32 : 1];
+  {
+    const char *const pk = (const char *)a.k.p + (b * a.k.batch + key * a.k.row + kh * a.k.head) * (int64_t)sizeof(T);
+    const char *const pv = (const char *)a.v.p + (b * a.v.batch + key * a.v.row + kh * a.v.head) * (int64_t)sizeof(T);
+    const char *const ek = end_of(a.k, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
+    const char *const ev = end_of(a.v, a.batch, a.keys, a.kv_heads, a.d, sizeof(T));
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      k[c] = u32x4{0, 0, 0, 0};
+      if (mine) k[c] = row_piece<T>(pk, 2 * c + h, a.d, ek);
+      if constexpr (DK) {
+        v[c] = u32x4{0, 0, 0, 0};
+        if (mine) v[c] = row_piece<T>(pv, 2 * c + h, a.d, ev);
+      }
+    }
   }
   for (int turn = 0; t < t1; turn ^= 1) {
     const int next = from(t + 1);
@@ -388,8 +387,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
     }
     barrier();     // the tile is there for all (DIRECT: and nobody reads the other one any more)
     if (next < t1) {
-      qs.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB, next);
-      ds_.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB + RT * RB, next);
+      qs.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB, next * by + split);
+      ds_.load(lds + (DIRECT ? buf ^ 1 : 0) * 2 * RT * RB + RT * RB, next * by + split);
       look(next);
     }
     if constexpr (DIRECT) buf ^= 1;

@@ -248,15 +248,18 @@ struct Keys {
   }
 };
 
-// Whether any of `count` rows from row `first` on may attend any of `keys` keys from key0 on, by the tiles of 32 queries that they
-// fall in.
-__device__ __forceinline__ bool any_flag(const Attention &a, uint32_t first, uint32_t count, int key0, int keys) {
+// Whether any of ROWS rows from row `first` on may attend any of KEYS keys from key0 on, by the tiles of 32 queries that they fall in (one
+// more at each end, and behind the last query).  No branch between the loads: they are on their way together.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ bool any_flag(const Attention &a, uint32_t first, int key0) {
   const uint32_t queries = (uint32_t)a.queries, tiles = (queries + 31) / 32, key_tiles = (uint32_t)words_of(a.keys) / 2;
-  const uint32_t c0 = key0 / 64, c1 = min((uint32_t)(key0 + keys + 63) / 64, key_tiles);
-  uint32_t q = first % queries / 32, left = min((count + 31) / 32 + 2, tiles);   // one more at each end, and behind the last query
+  constexpr int C = KEYS <= 64 ? 1 : KEYS / 64;     // key0 is a multiple of KEYS
+  uint32_t q = first % queries / 32;
   int any = 0;
-  for (; left > 0; --left) {
-    for (uint32_t c = c0; c < c1; ++c) any |= a.flags[(int64_t)q * key_tiles + c];
+#pragma unroll
+  for (int i = 0; i < (ROWS + 31) / 32 + 2; ++i) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) any |= a.flags[(int64_t)q * key_tiles + min((uint32_t)key0 / 64 + c, key_tiles - 1)];
     q = q + 1 == tiles ? 0 : q + 1;
   }
   return any != 0;
