@@ -20,9 +20,10 @@ template <class T>
 __device__ constexpr float slack() { return __is_same(T, f16_t) ? 5.0f : 8.0f; }
 
 // WQ wavefronts take 32 rows each and share the tiles of keys, or (WQ = 1) WK wavefronts the same 32 rows and different keys.
-// DIRECT: keys and values go from memory to LDS past the registers, a tile ahead where two fit.
+// DIRECT: keys and values go from memory to LDS past the registers, a tile ahead where two fit.  Rows of 128 bytes are held to the
+// registers of three wavefronts a SIMD (four: they spill, 256 x 128 under a Tanner graph 26 -> 34 us), wider ones to those of two.
 template <class T, int DP, int WQ, int WK, bool MASK, bool DIRECT>
-__global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention(Attention a) {
+__global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) void k_attention(Attention a) {
   constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = WQ * WK * 64;
   constexpr int SUB = WK == 1 && RB <= 256 ? 2 : 1, KT = 32 * SUB * WK;   // keys of a tile
   constexpr int STAGES = DIRECT && 4 * KT * RB <= 131072 ? 2 : 1;
@@ -184,10 +185,12 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 256 ? 2 : 1) void k_
         if constexpr (MASK) {
           uint32_t in = w[u];
           if (k0 + 32 > length) in = length > k0 ? in & ((1u << (length - k0)) - 1) : 0;
-          in >>= 4 * h;
+          if (pairwise<T, RB>() || !__all(in == ~0u)) {   // (where pairs are taken one by one this branch costs the registers of a wavefront)
+            in >>= 4 * h;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!(in >> row_of(i, 0) & 1)) s[u][i] = -INFINITY;
+            for (int i = 0; i < 16; ++i)
+              if (!(in >> row_of(i, 0) & 1)) s[u][i] = -INFINITY;
+          }
         } else if (k0 + 32 > length) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)

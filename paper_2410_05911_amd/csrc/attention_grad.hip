@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void k_attention_rows(AttentionGrad g) {
 
 // dq: a wavefront takes 32 rows, tiles of keys pass through LDS.  It leaves the rows' terms for dk and dv.
 template <class T, int DP, bool MASK, bool DIRECT>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(AttentionGrad g) {
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) void k_attention_dq(AttentionGrad g) {
   constexpr int RB = DP * (int)sizeof(T), FD = DP / 32, NT = 256, SUB = RB <= 256 ? 2 : 1, KT = 32 * SUB;
   constexpr int STAGES = DIRECT && 4 * KT * RB <= 131072 ? 2 : 1;
   const Attention &a = g.a;
@@ -213,12 +213,13 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void k_attentio
         }
       }
       const f32x16 s = times_rows<T, RB>(lk, u * 32, q), dp = times_rows<T, RB>(lv, u * 32, dout);
-      in >>= 4 * h;
       float ds[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[i], to2, -l2));
-        ds[i] = in >> row_of(i, 0) & 1 ? p * (dp[i] - dd) : 0.0f;
+      for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], to2, -l2)) * (dp[i] - dd);
+      if (!__all(in == ~0u)) {
+        in >>= 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ds[i] = in >> row_of(i, 0) & 1 ? ds[i] : 0.0f;
       }
       scaled.apply(ds, acc);
       add_columns<T, RB, FD>(acc, lk, u * 32, ds);
@@ -421,13 +422,23 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const f32x4 l2 = *(const f32x4 *)(&rl[turn][row_of(i, h)]), dd = *(const f32x4 *)(&rd[turn][row_of(i, h)]);
-        u32x4 w = {~0u, ~0u, ~0u, ~0u};
-        if constexpr (MASK) w = *(const u32x4 *)(&rw[turn][wave][row_of(i, h)]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool in = mine && (!MASK || (w[j] >> (lane & 31) & 1));
-          p[i + j] = in ? __builtin_amdgcn_exp2f(fmaf(s[i + j], to2, p_shift<T>() - l2[j])) : 0.0f;
-          if constexpr (DK) ds[i + j] = in ? p[i + j] * (dp[i + j] - dd[j]) : 0.0f;
+          p[i + j] = __builtin_amdgcn_exp2f(fmaf(s[i + j], to2, p_shift<T>() - l2[j]));
+          if constexpr (DK) ds[i + j] = p[i + j] * (dp[i + j] - dd[j]);
+        }
+      }
+      if (!__all(mine && (!MASK || any == ~0u))) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          u32x4 w = {~0u, ~0u, ~0u, ~0u};
+          if constexpr (MASK) w = *(const u32x4 *)(&rw[turn][wave][row_of(i, h)]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool in = mine && (w[j] >> (lane & 31) & 1);
+            p[i + j] = in ? p[i + j] : 0.0f;
+            if constexpr (DK) ds[i + j] = in ? ds[i + j] : 0.0f;
+          }
         }
       }
       if constexpr (DV) add_columns<T, RB, FD>(av, ld, 0, p);
