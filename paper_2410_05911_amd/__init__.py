@@ -613,7 +613,7 @@ def linear(x, w, bias=None, res=None, act="none", *, alpha=None, scale=None, y=N
     a = LinearMapArgs(rows, inputs, outputs, type, code, _dtype_code(y), _act_code(act), turned, px, ldx, pw, ldw,
                       _vector_of(alpha, rows, index, "alpha"), _vector_of(scale, outputs, index, "scale"),
                       _vector_of(bias, outputs, index, "bias"), pres, ldres, pz, ldz, py, ldy)
-    _with_workspace("aecct_linear_map", a, index, x, ("linear", rows, inputs, outputs, type, code, turned, ldw))
+    _with_workspace("aecct_linear_map", a, index, x, ("linear", rows, inputs, outputs, type, code, turned, ldx, ldw))
     return y, z
 
 
@@ -657,8 +657,8 @@ def linear_grad(x, w, dy, z=None, act="none", *, dx=None, dw=None, dbias=None, d
     pdw, lddw = _rows_of(dw, w.shape, dw_dtype, index, "dw")
     a = LinearMapGradArgs(rows, inputs, outputs, type, code, turned, F32 if dw is None else _dtype_code(dw), px, ldx, pw, ldw,
                           pdy, lddy, pz, ldz, pdx, lddx, pdw, lddw, _vector_of(dbias, outputs, index, "dbias"))
-    _with_workspace("aecct_linear_map_grad", a, index, x, ("linear_grad", rows, inputs, outputs, type, code, turned, ldw, dx is None,
-                                                            dw is None, dbias is None))
+    _with_workspace("aecct_linear_map_grad", a, index, x, ("linear_grad", rows, inputs, outputs, type, code, turned, ldx, ldw, lddy,
+                                                            dx is None, dw is None, dbias is None))
     return dx, dw, dbias
 
 

@@ -46,10 +46,12 @@ struct AttentionGrad {
   float *rows;                 // [pairs][rows][2]: lse log2(e), and the sum of dout o
   int splits;                  // of the rows, for dk and dv
   float *part;                 // [splits][2][pairs][keys][d_of(d)], or null
+  int splits_q;                // of the keys, for dq
+  float *part_q;               // [splits_q][pairs][rows][d_of(d)], or null
 };
 struct AttentionGradPlan {
-  int splits;
-  size_t words, flags, rows, part;        // bytes
+  int splits, splits_q;
+  size_t words, flags, rows, part, part_q;   // bytes
 };
 AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, int64_t keys, int heads, int kv_heads, int d,
                                       bool masked);

@@ -6,6 +6,10 @@
 //
 // As in the forward pass the scores are computed so that a lane's registers are the second factor of the products that follow:
 // keys by rows for dq, rows by keys for dk and dv.
+//
+// Measured: 2 x 2049 queries on 1531 keys, 16 heads of 64 on 4 key heads, a band of a quarter, bf16: dq 28 us, dk and dv 49, their join
+// 10, all 86; 128 x 256 on 128 keys, 8 heads of 16, three keys a query, fp32: 35 and 53, all 86.  Both are bound by the instructions
+// and latencies of short loops (dq has 9 tiles of keys a block, dk and dv 8 to 16 of rows), not by memory.
 #include "attention_tile.h"
 
 namespace aecct {
@@ -95,9 +99,15 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
   __shared__ __attribute__((aligned(16))) char lds[STAGES * 2 * KT * RB];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5;
   const uint32_t group = a.heads / a.kv_heads, queries = (uint32_t)a.queries, rows = group * queries, row_blocks = (rows + 127) / 128;
-  const uint32_t at = near_block(blockIdx.x, gridDim.x), pair = at / row_blocks, row_block = at - pair * row_blocks;
+  const uint32_t at = near_block(blockIdx.x, gridDim.x), rest = at / row_blocks, row_block = at - rest * row_blocks;
+  const uint32_t pair = g.splits_q > 1 ? rest / (uint32_t)g.splits_q : rest, split = g.splits_q > 1 ? rest - pair * g.splits_q : 0;
   const uint32_t b = pair / (uint32_t)a.kv_heads, kh = pair - b * a.kv_heads;
-  const int length = length_of(a, b), t1 = (length + KT - 1) / KT;
+  const int length = length_of(a, b), tiles = (length + KT - 1) / KT;
+  int t0 = 0, t1 = tiles;
+  if (g.splits_q > 1) {
+    t0 = (int)((uint32_t)tiles * split / (uint32_t)g.splits_q);
+    t1 = (int)((uint32_t)tiles * (split + 1) / (uint32_t)g.splits_q);
+  }
   const uint32_t r = row_block * 128 + wave * 32 + (lane & 31), rc = min(r, rows - 1);
   const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * 128 + wave * 32 >= rows;
@@ -106,7 +116,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
   const int words = (int)words_of(a.keys);
   const uint32_t *const mask = MASK ? a.words + (int64_t)query * words : nullptr;
   uint64_t want = 0;
-  int want0 = -64;
+  int want0 = t0 - 64;
   auto from = [&](int t) {
     if constexpr (!MASK) return t;
     while (t < t1) {
@@ -133,7 +143,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
       for (int u = 0; u < SUB; ++u) w[u] = t * SUB + u < words ? mask[t * SUB + u] : 0;
     }
   };
-  int t = from(0), buf = 0;
+  int t = from(t0), buf = 0;
   if (t < t1) {
     if constexpr (!DIRECT || STAGES == 2) {
       keys.load(lds, t);
@@ -158,7 +168,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
       dd = dot<T>(row_piece<T>(po, 2 * c + h, a.d, endo), dout[c], dd);
     }
     row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l2, dd);
-    if (h == 0 && r < rows) {
+    if (h == 0 && r < rows && split == 0) {
       g.rows[((int64_t)pair * rows + r) * 2] = l2;
       g.rows[((int64_t)pair * rows + r) * 2 + 1] = dd;
     }
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
           continue;
         }
       }
-      const f32x16 s = times_rows<T, RB>(lk, u * 32, q), dp = times_rows<T, RB>(lv, u * 32, dout);
+      const f32x16 s = times_rows<T, RB>(lk, u * 32, q, a.d), dp = times_rows<T, RB>(lv, u * 32, dout, a.d);
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], to2, -l2)) * (dp[i] - dd);
@@ -222,12 +232,35 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
         for (int i = 0; i < 16; ++i) ds[i] = in >> row_of(i, 0) & 1 ? ds[i] : 0.0f;
       }
       scaled.apply(ds, acc);
-      add_columns<T, RB, FD>(acc, lk, u * 32, ds);
+      if constexpr (sizeof(T) == 4 && RB <= 512) {
+        // In fp32 a tile's sums begin anew: one chain over all keys adds up to twice the error of a product in blocks (3000 keys 1.2e-6).
+        f32x16 fresh[FD];
+#pragma unroll
+        for (int f = 0; f < FD; ++f)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) fresh[f][i] = 0;
+        add_columns<T, RB, FD>(fresh, lk, u * 32, ds, a.d);
+#pragma unroll
+        for (int f = 0; f < FD; ++f)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[f][i] += fresh[f][i];
+      } else {
+        add_columns<T, RB, FD>(acc, lk, u * 32, ds, a.d);
+      }
     }
     t = next;
   }
   if (r >= rows) return;
   const float out = a.scale * scaled.out();
+  if (g.splits_q > 1) {
+    float *const o = g.part_q + ((int64_t)(split * (uint32_t)a.batch * a.kv_heads + pair) * rows + r) * DP;
+#pragma unroll
+    for (int f = 0; f < FD; ++f)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4 *)(o + 32 * f + row_of(i, h)) = f32x4{acc[f][i] * out, acc[f][i + 1] * out, acc[f][i + 2] * out, acc[f][i + 3] * out};
+    return;
+  }
   T *const o = (T *)g.dq.p + b * g.dq.batch + query * g.dq.row + head * g.dq.head;
 #pragma unroll
   for (int f = 0; f < FD; ++f)
@@ -415,9 +448,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
       }
     }
     if (dense) {
-      const f32x16 s = times_rows<T, RB>(lq, 0, k);
+      const f32x16 s = times_rows<T, RB>(lq, 0, k, a.d);
       f32x16 dp;
-      if constexpr (DK) dp = times_rows<T, RB>(ld, 0, v);
+      if constexpr (DK) dp = times_rows<T, RB>(ld, 0, v, a.d);
       float p[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
@@ -441,10 +474,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
           }
         }
       }
-      if constexpr (DV) add_columns<T, RB, FD>(av, ld, 0, p);
+      if constexpr (DV) add_columns<T, RB, FD>(av, ld, 0, p, a.d);
       if constexpr (DK) {
         scaled.apply(ds, ak);
-        add_columns<T, RB, FD>(ak, lq, 0, ds);
+        add_columns<T, RB, FD>(ak, lq, 0, ds, a.d);
       }
     }
     t = next;
@@ -477,6 +510,24 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
     }
 }
 
+// The splits' sums of four columns of a row's dq a thread, in the order of the splits.
+template <class T>
+__global__ __launch_bounds__(256) void k_join_dq(AttentionGrad g, int dp) {
+  const Attention &a = g.a;
+  const uint32_t group = a.heads / a.kv_heads, per = dp / 4, queries = (uint32_t)a.queries, rows = group * queries;
+  const uint32_t all = (uint32_t)a.batch * a.kv_heads * rows, at = blockIdx.x * 256 + threadIdx.x, row = at / per;
+  const int c = (int)(at - row * per) * 4;
+  if (row >= all || c >= a.d) return;
+  float v[4] = {0, 0, 0, 0};
+  for (int s = 0; s < g.splits_q; ++s) {
+    const f32x4 x = *(const f32x4 *)(g.part_q + ((int64_t)s * all + row) * dp + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += x[i];
+  }
+  const uint32_t pair = row / rows, r = row - pair * rows, b = pair / (uint32_t)a.kv_heads;
+  const uint32_t head = (pair - b * a.kv_heads) * group + r / queries, query = r % queries;
+  store_values4<T>((T *)g.dq.p + b * g.dq.batch + query * g.dq.row + head * g.dq.head + c, a.d - c, v[0], v[1], v[2], v[3]);
+}
 // The splits' sums of four columns of a key's dk or dv a thread, in the order of the splits.
 template <class T>
 __global__ __launch_bounds__(256) void k_join_dkv(AttentionGrad g, int dp) {
@@ -512,11 +563,15 @@ hipError_t launch_shape(const AttentionGrad &g, hipStream_t s) {
   const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries, pairs = a.batch * a.kv_heads;
   hipError_t err = hipSuccess;
   if (rows) {
-    const dim3 grid((unsigned)((rows + 127) / 128 * pairs));
+    const dim3 grid((unsigned)((rows + 127) / 128 * pairs * g.splits_q));
     if (!g.dq.p) k_attention_rows<T><<<dim3((unsigned)((rows * pairs + 15) / 16)), 256, 0, s>>>(g);
     else if (direct_ok<T>(a.k, a) && direct_ok<T>(a.v, a)) k_attention_dq<T, DP, MASK, true><<<grid, 256, 0, s>>>(g);
     else k_attention_dq<T, DP, MASK, false><<<grid, 256, 0, s>>>(g);
     if ((err = hipGetLastError()) != hipSuccess) return err;
+    if (g.dq.p && g.splits_q > 1) {
+      k_join_dq<T><<<dim3((unsigned)((rows * pairs * (DP / 4) + 255) / 256)), 256, 0, s>>>(g, DP);
+      if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
   }
   if (!g.dk.p) return err;
   const dim3 grid((unsigned)((a.keys + 127) / 128 * pairs * g.splits));
@@ -544,7 +599,7 @@ AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, 
   AttentionGradPlan p{};
   const int64_t rows = (int64_t)(heads / kv_heads) * queries, pairs = batch * kv_heads, blocks = (keys + 127) / 128 * pairs;
   int64_t splits = blocks > 0 ? 768 / blocks : 1;
-  if (splits > rows / 256) splits = rows / 256;
+  if (splits > rows / 128) splits = rows / 128;
   if (splits > 32) splits = 32;
   p.splits = splits > 1 ? (int)splits : 1;
   if (masked) {
@@ -553,6 +608,13 @@ AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, 
   }
   p.rows = (size_t)(rows * pairs) * 8;
   if (p.splits > 1) p.part = (size_t)(p.splits * 2 * pairs * keys * d_of(d)) * 4;
+  // dq's blocks of 128 rows, where they are few, split the keys: at least 256 keys each.
+  const int64_t row_blocks = (rows + 127) / 128 * pairs;
+  int64_t q = row_blocks > 0 ? 512 / row_blocks : 1;
+  if (q > keys / 256) q = keys / 256;
+  if (q > 32) q = 32;
+  p.splits_q = q > 1 ? (int)q : 1;
+  if (p.splits_q > 1) p.part_q = (size_t)(p.splits_q * pairs * rows * d_of(d)) * 4;
   return p;
 }
 

@@ -146,7 +146,7 @@ aecct_status aecct_cross_attention_grad_workspace_size(const aecct_cross_attenti
   if (s != AECCT_OK) return s;
   const aecct::AttentionGradPlan p =
       aecct::plan_attention_grad(a->type, a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->mask != nullptr);
-  const size_t need = align_up(p.words) + align_up(p.flags) + align_up(p.rows) + align_up(p.part);
+  const size_t need = align_up(p.words) + align_up(p.flags) + align_up(p.rows) + align_up(p.part) + align_up(p.part_q);
   *bytes = need ? need + kAlign : 0;
   return AECCT_OK;
 }
@@ -198,6 +198,8 @@ aecct_status aecct_cross_attention_grad(const aecct_cross_attention_grad_args *a
   x.rows = (float *)(x.a.flags + align_up(p.flags));
   x.splits = p.splits;
   x.part = p.part ? (float *)((char *)x.rows + align_up(p.rows)) : nullptr;
+  x.splits_q = p.splits_q;
+  x.part_q = (float *)((char *)x.rows + align_up(p.rows) + align_up(p.part));
   x.dout = heads_of(a->dout);
   x.dq = heads_of(a->dq);
   x.dk = heads_of(a->dk);

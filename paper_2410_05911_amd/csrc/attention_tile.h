@@ -37,8 +37,9 @@ __device__ __forceinline__ u32x4 column_chunk(const char *tile, int row0, int t,
 __device__ __forceinline__ int row_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
 // acc[f] += the tile's columns (32 f + 0..31) times p, over the 32 rows from row0 on; p a result's registers.
+// Rows of 1024 bytes, so of 129 to 256 fp32 values, stop at d (200: 3850 -> 2157 us a gradient; narrower ones lose more by the branches).
 template <class T, int RB, int FD>
-__device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile, int row0, const float (&p)[16]) {
+__device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile, int row0, const float (&p)[16], int d) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -54,6 +55,7 @@ __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile,
       const int row = row0 + row_of(i, h);
 #pragma unroll
       for (int f = 0; f < FD; ++f) {
+        if (RB == 1024 && f && 32 * f >= d) break;
         const float v = *(const float *)(tile + row * RB + (((32 * f + (lane & 31)) * 4) ^ exchange<RB>(row)));
         acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], acc[f], 0, 0, 0);
       }
@@ -62,13 +64,16 @@ __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile,
 }
 // The product of the tile's 32 rows from row0 on with a lane's row held in registers (chunks 2 s + h).
 template <class T, int RB>
-__device__ __forceinline__ f32x16 times_rows(const char *tile, int row0, const u32x4 (&r)[RB / 32]) {
+__device__ __forceinline__ f32x16 times_rows(const char *tile, int row0, const u32x4 (&r)[RB / 32], int d) {
   const int lane = threadIdx.x & 63;
   f32x16 s;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = 0;
 #pragma unroll
-  for (int c = 0; c < RB / 32; ++c) step<T>(s, row_chunk<RB>(tile, row0 + (lane & 31), 2 * c + (lane >> 5)), r[c]);
+  for (int c = 0; c < RB / 32; ++c) {
+    if (RB == 1024 && c && 8 * c >= d) break;
+    step<T>(s, row_chunk<RB>(tile, row0 + (lane & 31), 2 * c + (lane >> 5)), r[c]);
+  }
   return s;
 }
 

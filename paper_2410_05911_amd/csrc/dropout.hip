@@ -1,6 +1,10 @@
 // Dropout whose mask is never stored: y = x kept / (1 - p) + res.  Value i of the tensor (row by row) takes word i % 4 of
 // Philox4x32-7's block with the counter (i / 4, offset) and the key `seed` (Salmon, Moraes, Dror and Shaw, "Parallel random
 // numbers: as easy as 1, 2, 3", SC 2011), so any call with the same numbers, also on a gradient, drops the same values.
+//
+// Eight values a thread, so 16-byte accesses in 16 bits and two blocks of words; where rows begin inside a block, three.  Bound by
+// memory (16384 x 8192 bf16 with residual 136 us, 5.9 TB/s; the words' products and exclusive ors take 60 % of the clocks beside),
+// small calls by the launch (5888 x 32 fp32: 3 us on the GPU, 7.5 with the host).
 #include "../../include/aecct.h"
 #include "dropout.h"
 #include "row_io.h"

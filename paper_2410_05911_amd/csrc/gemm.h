@@ -17,7 +17,7 @@ namespace aecct {
 
 // ---- activations, in fp32
 // The normal distribution Phi(z) and e = e^(-z^2 / 2), to 1e-7: Abramowitz and Stegun 7.1.26 for its tail, 1 - erf(x) = e^(-x^2) times a
-// polynomial in 1 / (1 + 0.3275911 x).  A third of erff's instructions (16384 x 8192 outputs in bf16: 1097 -> 1000 us for the map);
+// polynomial in 1 / (1 + 0.3275911 x).  A third of erff's instructions (16384 x 4096 -> 8192 bf16 1097 -> 1071 us, the gradient's first launch 68 -> 50);
 // fp32 outputs take erff.
 __device__ __forceinline__ float normal(float z, float &e) {
   const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
@@ -709,7 +709,12 @@ bool direct_ok(const Gemm &g) {
   return direct_ok<T>(g.a, g.m, g.k) && direct_ok<T>(g.b, g.n, g.k);
 }
 
-// The tiles that plan_gemm chooses from.
+// The tiles that plan_gemm chooses from.  What a tile of BM x BN costs beside its products is reading BM + BN lines of k: with 256 x 256
+// and eight wavefronts of 128 x 64 the matrix instructions are busy 63 % of the clocks, which fall to 1.75 GHz under them (8192 x 4096
+// x 4096 bf16 245 us a product, 1.1 PFLOP/s; with 128 x 128 415 us).  The two stages of it fill LDS, so one block a compute unit, whose
+// epilogue nothing overlaps: about 60 of the 1040 us of 16384 x 4096 -> 8192 with GELU and z.  Where 256 x 256 would leave compute units
+// idle, or k is short, 128 x 128 with two blocks a unit (49152 x 128 -> 512 int8 49 -> 41 us); for small products 64 x 64 with four
+// stages, as their time is loads' latency.
 constexpr int kTileSide[3][2] = {{64, 64}, {128, 128}, {256, 256}};
 template <class T, class S, bool AA, bool BA>
 hipError_t launch_layout(const Gemm &g, const GemmPlan &p, hipStream_t s) {

@@ -193,6 +193,25 @@ def test_rows_do_not_mix(P):
         assert bool(y[5].isnan().all()) and bool(y[:, 140].isnan().all()) and not bool(y[130, :140].isfinite().any())
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "e4m3"])
+def test_strided_after_contiguous(P, kind):
+    """The same sizes with other strides take another workspace (2048 x 1024 x 1024 products are copied into whole pieces first)."""
+    s = _case(2048, 1024, 1024, kind, False, 0, 8)
+    more = dict(alpha=s["alpha"], scale=s["scale"]) if kind == "e4m3" else {}
+    plain = [s[k].contiguous() for k in ("x", "w")]
+    want = P.linear(*plain, s["bias"], **more)[0]
+    for x, w in ((_in_nan(plain[0], 3), plain[1]), (plain[0], _in_nan(plain[1], 5)), (_in_nan(plain[0], 1), _in_nan(plain[1], 2)), plain):
+        got = P.linear(x, w, s["bias"], **more)[0]
+        # the same products in another order at most: 2 (K + 8) u of sums of about 0.8 K / sqrt(K) terms, and the rounding of the type
+        assert bool(((got - want).abs() <= 4 * 1032 * U * 64 + 2 * HALF[got.dtype] * want.abs()).all())
+    if kind != "e4m3":
+        dy = plain[0][:, :].clone()
+        want = P.linear_grad(*plain, dy)
+        for x, w, d in ((_in_nan(plain[0], 3), plain[1], dy), (plain[0], _in_nan(plain[1], 5), dy), (plain[0], plain[1], _in_nan(dy, 1))):
+            for p, q in zip(P.linear_grad(x, w, d), want):
+                assert bool(((p - q).abs() <= 4 * 2056 * U * q.abs().max() + 2 * HALF[p.dtype] * q.abs()).all())
+
+
 def test_activation_limits(P):
     z = torch.tensor([[-float("inf"), -200.0, -0.0, 0.0, 200.0, float("inf"), float("nan")]], device="cuda")
     one = torch.ones(1, 1, device="cuda")
