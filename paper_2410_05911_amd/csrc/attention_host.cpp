@@ -27,12 +27,12 @@ aecct_status check_sizes(int64_t batch, int64_t queries, int64_t keys, int32_t h
     return AECCT_ERR_INVALID_ARG;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return AECCT_ERR_INVALID_ARG;
   if (d > 256 || batch > kMaxCount || queries > kMaxCount || keys > kMaxCount || heads > (1 << 20)) return AECCT_ERR_UNSUPPORTED;
-  // Threads of the largest grids: 256 for 32 rows of a pair (times the splits, which only few blocks take), 64 for 32 rows and
-  // 128 keys of the mask, one for four values of the joined sums.
+  // Threads of the largest grids: 256 for 32 rows of a pair or 128 keys (times the splits, which only few blocks take), 64 for 32 rows
+  // and 128 keys of the mask, 16 for a row's terms.
   const __int128 rows = (__int128)(heads / kv_heads) * queries, pairs = (__int128)batch * kv_heads;
   const __int128 blocks = (rows + 31) / 32 * pairs, masks = (rows + 31) / 32 * ((keys + 127) / 128 + 1);
   const __int128 keyed = ((__int128)keys + 127) / 128 * pairs;
-  if (blocks > kMaxThreads / 256 || masks > kMaxThreads / 64 || keyed > kMaxThreads / 256 || rows * pairs > kMaxThreads / 64)
+  if (blocks > kMaxThreads / 256 || masks > kMaxThreads / 64 || keyed > kMaxThreads / 256 || rows * pairs > kMaxThreads / 16)
     return AECCT_ERR_UNSUPPORTED;
   return AECCT_OK;
 }
