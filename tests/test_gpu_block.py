@@ -126,3 +126,29 @@ def test_tokens_one_by_one_are_the_batch(P):
     for i in range(0, n, 20):
         one, _ = P.cross_attention(q[:, i: i + 1], k, v, lengths)
         assert bool(((one.float() - whole[:, i: i + 1].float()).abs() <= (4 * 2.0 ** -8 + 1e-3) * most).all())
+
+
+def test_calls_on_two_streams_at_once(P):
+    """Calls in flight together have workspaces of their own: split products, masks, joined sums."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()  # noqa: E731
+    mask = torch.rand(3, 2000, device="cuda", generator=g) < 0.3
+    jobs = []
+    for _ in range(2):
+        x, w, dy = new(20, 4000), new(4000, 200), new(20, 200)
+        q, k, v, dout = new(2, 3, 8, 64), new(2, 2000, 2, 64), new(2, 2000, 2, 64), new(2, 3, 8, 64)
+
+        def job(x=x, w=w, dy=dy, q=q, k=k, v=v, dout=dout):
+            o, lse = P.cross_attention(q, k, v, None, mask, with_lse=True)
+            return [P.linear(x, w)[0], *P.linear_grad(x, w, dy), o, lse, *P.cross_attention_grad(q, k, v, o, lse, dout, None, mask)]
+        jobs.append(job)
+    want = [job() for job in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[], []]
+    for _ in range(8):
+        for i, job in enumerate(jobs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(job())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for run in got[i] for a, b in zip(run, want[i]))

@@ -308,6 +308,21 @@ def test_captured_on_streams_and_the_same_bits(P, n, m):
         assert all(torch.equal(a, b) for a, b in zip(want, out)), step
 
 
+def test_wide_strides(P):
+    """Rows 2^21 values apart, which tiles take through registers: what contiguous rows give, to the last bit but for splits, whose number
+    goes by sizes alone."""
+    n, m, d = 40, 90, 32
+    far = [torch.empty(1, r, 1, 1 << 21, dtype=torch.bfloat16, device="cuda")[..., :d] for r in (n, m, m, n)]
+    for t in far:
+        t.normal_()
+    near = [t.contiguous() for t in far]
+    o, lse = P.cross_attention(*far[:3], with_lse=True)
+    want, want_lse = P.cross_attention(*near[:3], with_lse=True)
+    assert torch.equal(o, want) and torch.equal(lse, want_lse)
+    for a, b in zip(P.cross_attention_grad(*far[:3], o, lse, far[3]), P.cross_attention_grad(*near[:3], o, lse, near[3])):
+        assert torch.equal(a, b)
+
+
 def test_offsets_past_32_bits(P):
     """A cache of more than 2^32 bytes, its last sequence read: 5 sequences 2^30 bytes apart."""
     cache = torch.empty(5, 1 << 23, 1, 64, dtype=torch.bfloat16, device="cuda")

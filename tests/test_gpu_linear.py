@@ -212,6 +212,23 @@ def test_strided_after_contiguous(P, kind):
                 assert bool(((p - q).abs() <= 4 * 2056 * U * q.abs().max() + 2 * HALF[p.dtype] * q.abs()).all())
 
 
+def test_wide_strides(P):
+    """Rows 2^21 and 2^23 values apart: past what 32-bit offsets of a tile take.  The same products in the same or another order: 2 (K + 8) u
+    of sums of |x w|."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for ld in (1 << 21, 1 << 23):
+        x, w, dy = (torch.empty(r, ld, dtype=torch.bfloat16, device="cuda")[:, :c] for r, c in ((70, 96), (96, 80), (70, 80)))
+        for t in (x, w, dy):
+            t.copy_(_rand(g, *t.shape))
+        near = [t.contiguous() for t in (x, w, dy)]
+        each = near[0].double().abs() @ near[1].double().abs()
+        y, want = P.linear(x, w)[0].double(), near[0].double() @ near[1].double()
+        _near(y, want, 208 * U * each + HALF[torch.bfloat16] * want.abs(), "y")
+        assert torch.equal(P.linear(x[:2], w)[0], P.linear(near[0][:2], near[1])[0])
+        for a, b in zip(P.linear_grad(x, w, dy), P.linear_grad(*near)):
+            assert bool(((a.float() - b.float()).abs() <= 2 * HALF[a.dtype] * b.float().abs() + 416 * U * 96).all())
+
+
 def test_activation_limits(P):
     z = torch.tensor([[-float("inf"), -200.0, -0.0, 0.0, 200.0, float("inf"), float("nan")]], device="cuda")
     one = torch.ones(1, 1, device="cuda")
