@@ -6,6 +6,7 @@
 
 #include "../../include/aecct.h"
 #include "norm.h"
+#include "spans.h"
 
 namespace {
 
@@ -17,24 +18,9 @@ size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool type_ok(int32_t t) { return t == AECCT_F32 || t == AECCT_BF16 || t == AECCT_F16; }
 int64_t type_size(int32_t t) { return t == AECCT_F32 ? 4 : 2; }
 
-// `rows` rows of `width` bytes, `pitch` bytes apart.
-struct Rows {
-  const void *p;
-  int64_t rows, width, pitch;
-  uintptr_t begin() const { return (uintptr_t)p; }
-  uintptr_t end() const { return rows > 0 ? begin() + (uintptr_t)((rows - 1) * pitch + width) : begin(); }
-};
-bool same(const Rows &a, const Rows &b) { return a.p == b.p && a.width == b.width && (a.pitch == b.pitch || a.rows <= 1); }
-// Whether two regions may share a byte: their spans do, unless both are columns of rows of one pitch that lie side
-// by side.
-bool overlap(const Rows &a, const Rows &b) {
-  if (!a.p || !b.p || a.begin() >= b.end() || b.begin() >= a.end()) return false;
-  if (a.pitch != b.pitch || a.pitch <= 0) return true;
-  const uintptr_t pitch = (uintptr_t)a.pitch;
-  const uintptr_t off = b.begin() >= a.begin() ? (b.begin() - a.begin()) % pitch
-                                               : (pitch - (a.begin() - b.begin()) % pitch) % pitch;
-  return !(off >= (uintptr_t)a.width && off + (uintptr_t)b.width <= pitch);
-}
+using Rows = aecct::Span;
+using aecct::overlap;
+using aecct::same;
 
 bool stride_ok(const void *p, int64_t rows, int64_t ld, int64_t least) {
   return !p || (ld >= least && ld <= kMaxSpan / (rows > 0 ? rows : 1));

@@ -1,4 +1,4 @@
-// Regions of device memory that the entry points of rows and lists compare before a launch.
+// Regions of device memory that entry points compare before a launch.
 #pragma once
 
 #include <cstdint>
