@@ -35,7 +35,7 @@ struct AttentionPlan {
   size_t words, flags, part_o, part_ml;   // bytes
 };
 __host__ __device__ inline int64_t words_of(int64_t keys) { return (keys + 63) / 64 * 2; }
-__host__ __device__ inline int d_of(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+__host__ __device__ inline int d_of(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
 AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t keys, int heads, int kv_heads, int d, bool masked);
 hipError_t launch_mask(const Attention &a, hipStream_t s);
 hipError_t launch_attention(int type, const Attention &a, const AttentionPlan &p, hipStream_t s);

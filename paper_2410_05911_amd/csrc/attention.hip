@@ -386,7 +386,7 @@ hipError_t launch_shape(const Attention &a, hipStream_t s) {
   k_join_attention<T><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, s>>>(a, DP);
   return hipGetLastError();
 }
-// 256 fp32 values a row: tiles of four wavefronts' keys do not fit in LDS, so few rows run as many do.
+// Over 128 fp32 values a row: tiles of four wavefronts' keys do not fit in LDS, so few rows run as many do.
 template <class T, int DP>
 hipError_t launch_rows(const Attention &a, bool few, hipStream_t s) {
   if constexpr (DP * sizeof(T) <= 512) {
@@ -400,6 +400,7 @@ hipError_t launch_type(const Attention &a, bool few, hipStream_t s) {
     case 32: return launch_rows<T, 32>(a, few, s);
     case 64: return launch_rows<T, 64>(a, few, s);
     case 128: return launch_rows<T, 128>(a, few, s);
+    case 192: return launch_rows<T, 192>(a, few, s);
     default: return launch_rows<T, 256>(a, few, s);
   }
 }
@@ -411,7 +412,7 @@ AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t k
   const int dp = d_of(d);
   const int64_t rows = (int64_t)(heads / kv_heads) * queries, pairs = batch * kv_heads;
   const int64_t wide = (rows + 127) / 128 * pairs;
-  p.few = wide < 256 && !(type == AECCT_F32 && dp == 256);
+  p.few = wide < 256 && !(type == AECCT_F32 && dp > 128);
   const int64_t blocks = p.few ? (rows + 31) / 32 * pairs : wide;
   // At least 512 keys a split, about four blocks a compute unit.
   int64_t splits = blocks > 0 ? 1024 / blocks : 1;

@@ -549,8 +549,8 @@ __global__ __launch_bounds__(256) void k_join_dkv(AttentionGrad g, int dp) {
 
 template <class T, int DP, bool MASK, bool DIRECT>
 void launch_dkv(const AttentionGrad &g, dim3 grid, hipStream_t s) {
-  // Rows of 256 values leave no registers for both sums beside a key and its value.
-  if constexpr (DP == 256) {
+  // Rows of 256 values, or 192 in fp32, leave no registers for both sums beside a key and its value.
+  if constexpr (DP == 256 || DP * sizeof(T) > 512) {
     k_attention_dkv<T, DP, MASK, true, false, DIRECT><<<grid, 256, 0, s>>>(g);
     k_attention_dkv<T, DP, MASK, false, true, DIRECT><<<grid, 256, 0, s>>>(g);
   } else {
@@ -588,6 +588,7 @@ hipError_t launch_type(const AttentionGrad &g, hipStream_t s) {
     case 32: return g.a.mask ? launch_shape<T, 32, true>(g, s) : launch_shape<T, 32, false>(g, s);
     case 64: return g.a.mask ? launch_shape<T, 64, true>(g, s) : launch_shape<T, 64, false>(g, s);
     case 128: return g.a.mask ? launch_shape<T, 128, true>(g, s) : launch_shape<T, 128, false>(g, s);
+    case 192: return g.a.mask ? launch_shape<T, 192, true>(g, s) : launch_shape<T, 192, false>(g, s);
     default: return g.a.mask ? launch_shape<T, 256, true>(g, s) : launch_shape<T, 256, false>(g, s);
   }
 }

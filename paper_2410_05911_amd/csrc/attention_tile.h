@@ -1,6 +1,6 @@
 // Tiles of keys and queries in LDS, and the products of attention on them, for the forward pass and the gradient.
 //
-// A tile is 32 rows (or several times 32) of RB bytes, d values padded by zeros to 32, 64, 128 or 256.  The 16-byte chunks of a row
+// A tile is 32 rows (or several times 32) of RB bytes, d values padded by zeros to 32, 64, 128, 192 or 256.  The 16-byte chunks of a row
 // are exchanged by the row's number, so that the reads of one chunk of 32 rows and those of 4 rows' columns fall on
 // different banks alike.
 #pragma once
@@ -16,7 +16,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 template <int RB>
 __device__ __forceinline__ int exchange(int row) {
-  if constexpr (RB >= 256) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
+  static_assert(RB % 128 == 0 || RB == 64, "chunks stay in their row");
+  if constexpr (RB % 256 == 0) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
   return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
 }
 // Chunk `chunk` of row `row`: of a product along d.
