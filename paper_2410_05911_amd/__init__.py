@@ -760,7 +760,7 @@ def cross_attention(q, k, v, lengths=None, mask=None, scale=None, *, o=None, lse
         raise ValueError(f"lse must be {lse_shape}")
     a = CrossAttentionArgs(*sizes, hq, hk, hv, plengths, pmask, ldmask, _heads_of(o, q.shape, q.dtype, index, "o"),
                            _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"))
-    _with_workspace("aecct_cross_attention", a, index, q, ("attention", *sizes[:7], pmask is None))
+    _with_workspace("aecct_cross_attention", a, index, q, ("attention", *sizes[:7], pmask is None, k.stride(), v.stride()))
     return o, lse
 
 
@@ -790,7 +790,8 @@ def cross_attention_grad(q, k, v, o, lse, dout, lengths=None, mask=None, scale=N
                                _vector_of(lse, sizes[0] * sizes[1] * sizes[3], index, "lse"), plengths, pmask, ldmask,
                                _heads_of(dq, q.shape, q.dtype, index, "dq"), _heads_of(dk, k.shape, q.dtype, index, "dk"),
                                _heads_of(dv, k.shape, q.dtype, index, "dv"))
-    _with_workspace("aecct_cross_attention_grad", a, index, q, ("attention_grad", *sizes[:7], pmask is None))
+    _with_workspace("aecct_cross_attention_grad", a, index, q, ("attention_grad", *sizes[:7], pmask is None, q.stride(), k.stride(), v.stride(),
+                                                              dout.stride()))
     return dq, dk, dv
 
 

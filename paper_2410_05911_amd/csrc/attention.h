@@ -12,6 +12,7 @@ namespace aecct {
 struct Heads {
   const void *p;
   int64_t batch, row, head;
+  bool packed = false;         // zeros behind each row's d values, up to a whole 16-byte piece
 };
 // The queries of the heads that share a key head are the rows of one problem: row r is query r % queries of head
 // key head * (heads / kv_heads) + r / queries.  A pair is a sequence and a key head.
@@ -29,6 +30,25 @@ struct Attention {
   int splits;
   float *part_o, *part_ml;     // [splits][pairs][rows][d_of(d)], [splits][pairs][rows][2]
 };
+// Copies of up to four tensors [batch][length][heads][d] as [batch][length][heads][line], zeros behind d.  What lies past a sequence's
+// length is not read (lengths: or null).
+struct PackHeads {
+  Heads from;
+  int64_t batch, length;       // length 0: not asked for
+  int heads, d, line;
+  const int32_t *lengths;
+  void *to;
+};
+struct PackHeadsAll {
+  PackHeads t[4];
+};
+hipError_t launch_pack_heads(int type, const PackHeadsAll &p, hipStream_t s);
+// Whether the tiles of such a tensor go past the registers as it is (its address apart).
+inline bool ragged_heads(int size, int64_t batch, int64_t row, int64_t head, int d) {
+  const int64_t e = 16 / size;
+  return d % e != 0 || batch % e != 0 || row % e != 0 || head % e != 0;
+}
+
 struct AttentionPlan {
   bool few;                    // 32 rows a block, its wavefronts share the keys; else 128 rows
   int splits;

@@ -371,6 +371,37 @@ __global__ __launch_bounds__(64) void k_pack_mask(Attention a) {
   if ((lane & 31) == 0 && t < tiles) a.flags[(int64_t)qt * tiles + t] = (uint32_t)(any >> (32 * h)) != 0;
 }
 
+struct PackGrid {
+  uint32_t blocks[4];
+};
+// Pieces of the copies, one a thread and turn.
+template <class T>
+__global__ __launch_bounds__(256) void k_pack_heads(PackHeadsAll all, PackGrid grid) {
+  constexpr int E = 16 / (int)sizeof(T);
+  uint32_t block = blockIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (block >= grid.blocks[i]) {
+      block -= grid.blocks[i];
+      continue;
+    }
+    const PackHeads &p = all.t[i];
+    const uint32_t per = p.line / E, row_pieces = per * p.heads;
+    const uint64_t pieces = (uint64_t)p.batch * p.length * row_pieces;
+    const char *const end = end_of(p.from, p.batch, p.length, p.heads, p.d, sizeof(T));
+    for (uint64_t at = (uint64_t)block * 256 + threadIdx.x; at < pieces; at += (uint64_t)grid.blocks[i] * 256) {
+      const uint64_t row = at >> 32 ? at / row_pieces : (uint32_t)at / row_pieces;
+      const uint32_t rest = (uint32_t)(at - row * row_pieces), head = rest / per, c = rest - head * per;
+      const uint32_t b = row >> 32 ? (uint32_t)(row / p.length) : (uint32_t)row / (uint32_t)p.length;
+      const int64_t n = (int64_t)row - (int64_t)b * p.length;
+      if (p.lengths && n >= p.lengths[b]) continue;
+      const char *const from = (const char *)p.from.p + (b * p.from.batch + n * p.from.row + head * p.from.head) * (int64_t)sizeof(T);
+      *(u32x4 *)((char *)p.to + at * 16) = row_piece<T>(from, (int)c, p.d, end);
+    }
+    return;
+  }
+}
+
 template <class T, int DP, int WQ, int WK>
 hipError_t launch_shape(const Attention &a, hipStream_t s) {
   const int64_t rows = (int64_t)(a.heads / a.kv_heads) * a.queries;
@@ -433,6 +464,24 @@ AttentionPlan plan_attention(int type, int64_t batch, int64_t queries, int64_t k
 hipError_t launch_mask(const Attention &a, hipStream_t s) {
   const int64_t tiles = words_of(a.keys) / 2;
   k_pack_mask<<<dim3((unsigned)((a.queries + 31) / 32 * ((tiles + 1) / 2))), 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pack_heads(int type, const PackHeadsAll &p, hipStream_t s) {
+  PackGrid grid{};
+  uint32_t all = 0;
+  for (int i = 0; i < 4; ++i) {
+    const int64_t pieces = p.t[i].length ? p.t[i].batch * p.t[i].length * p.t[i].heads * (p.t[i].line / (16 / (type == AECCT_F32 ? 4 : 2))) : 0;
+    grid.blocks[i] = (uint32_t)(pieces < (int64_t)1 << 24 ? (pieces + 255) / 256 : 1 << 16);
+    all += grid.blocks[i];
+  }
+  if (all == 0) return hipSuccess;
+  switch (type) {
+    case AECCT_F32: k_pack_heads<float><<<dim3(all), 256, 0, s>>>(p, grid); break;
+    case AECCT_BF16: k_pack_heads<bf16_t><<<dim3(all), 256, 0, s>>>(p, grid); break;
+    case AECCT_F16: k_pack_heads<f16_t><<<dim3(all), 256, 0, s>>>(p, grid); break;
+    default: return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
 

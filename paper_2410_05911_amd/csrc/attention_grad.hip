@@ -318,7 +318,7 @@ struct RowsOf {
 template <class T>
 bool direct_rows(const Heads &t, const Attention &a) {
   constexpr int64_t E = 16 / sizeof(T);
-  return (uintptr_t)t.p % 16 == 0 && a.d % E == 0 && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
+  return (uintptr_t)t.p % 16 == 0 && (t.packed || a.d % E == 0) && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
          t.row * (a.queries - 1) + t.head * a.heads + a.d < ((int64_t)1 << 31) / (int64_t)sizeof(T);
 }
 

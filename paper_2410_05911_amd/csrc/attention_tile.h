@@ -188,7 +188,7 @@ __device__ __forceinline__ int length_of(const Attention &a, uint32_t b) {
 template <class T>
 bool direct_ok(const Heads &t, const Attention &a) {
   constexpr int64_t E = 16 / sizeof(T);
-  return (uintptr_t)t.p % 16 == 0 && a.d % E == 0 && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
+  return (uintptr_t)t.p % 16 == 0 && (t.packed || a.d % E == 0) && t.batch % E == 0 && t.row % E == 0 && t.head % E == 0 &&
          t.row < ((int64_t)1 << 22) / (int64_t)sizeof(T);
 }
 // Tiles of KT keys (or values) of one pair, on their way to LDS: DIRECT by loads whose out-of-range offsets give the zeros behind d and

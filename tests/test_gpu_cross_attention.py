@@ -115,6 +115,7 @@ SHAPES = [  # batch, queries, keys, heads, kv_heads, d
     (1, 1, 1, 1, 1, 1), (2, 1, 33, 4, 2, 16), (3, 5, 64, 2, 2, 17), (7, 33, 31, 6, 2, 32), (2, 65, 129, 4, 1, 33), (1, 128, 100, 2, 2, 64),
     (2, 3, 1100, 8, 2, 64), (7, 130, 200, 4, 2, 128), (3, 40, 257, 2, 1, 100), (2, 70, 90, 2, 2, 256), (1, 1, 2100, 4, 1, 129),
     (2, 45, 150, 4, 2, 192), (1, 150, 330, 2, 1, 161), (2, 2, 700, 2, 2, 193),
+    (2, 500, 700, 4, 2, 177), (3, 2, 9000, 2, 1, 99),       # copied into whole pieces first
     (2, 300, 65, 3, 3, 8)]
 
 
