@@ -41,27 +41,32 @@ aecct_status check_sizes(int64_t batch, int64_t queries, int64_t keys, int32_t h
 struct Box {
   int64_t batch, length, heads, d;
 };
+struct Dim {
+  int64_t n, stride;
+};
+// The dimensions longer than one, in the order of their strides.
+int dims_of(const aecct_heads &t, const Box &n, Dim (&dims)[3]) {
+  int count = 0;
+  for (const Dim &x : {Dim{n.heads, t.head}, Dim{n.length, t.row}, Dim{n.batch, t.batch}}) {
+    if (x.n <= 1) continue;
+    int i = count++;
+    for (; i > 0 && dims[i - 1].stride > x.stride; --i) dims[i] = dims[i - 1];
+    dims[i] = x;
+  }
+  return count;
+}
 bool strides_ok(const aecct_heads &t, const Box &n, bool out) {
   if (!t.data || n.batch == 0 || n.length == 0) return true;
   if (t.batch < 0 || t.row < 0 || t.head < 0) return false;
   if (t.batch > kMaxSpan / n.batch || t.row > kMaxSpan / n.length || t.head > kMaxSpan / n.heads) return false;
   if (!out) return true;
-  // An output's values lie apart: the strides of its dimensions longer than one, in rising order, each step over all of the one before.
-  struct Dim {
-    int64_t n, stride;
-  } dims[3] = {{n.batch, t.batch}, {n.length, t.row}, {n.heads, t.head}};
-  for (int i = 0; i < 3; ++i)
-    for (int k = i + 1; k < 3; ++k)
-      if (dims[k].stride < dims[i].stride) {
-        const Dim s = dims[i];
-        dims[i] = dims[k];
-        dims[k] = s;
-      }
+  // An output's values lie apart: each step of a dimension goes over all of the ones inside it.
+  Dim dims[3];
+  const int count = dims_of(t, n, dims);
   int64_t reach = n.d;
-  for (const Dim &x : dims) {
-    if (x.n <= 1) continue;
-    if (x.stride < reach) return false;
-    reach = (x.n - 1) * x.stride + reach;
+  for (int i = 0; i < count; ++i) {
+    if (dims[i].stride < reach) return false;
+    reach += (dims[i].n - 1) * dims[i].stride;
   }
   return true;
 }
@@ -69,17 +74,26 @@ Span span_of(const aecct_heads &t, const Box &n, int64_t size) {
   if (!t.data || n.batch == 0 || n.length == 0) return {nullptr, 0, 0, 0};
   return {t.data, 1, ((n.batch - 1) * t.batch + (n.length - 1) * t.row + (n.heads - 1) * t.head + n.d) * size, 0};
 }
-// Whether two tensors of one box may share a byte: their spans do, unless they lie side by side in rows of one pitch (equal
-// strides, and apart by less than the smallest of them: as q, k and v of one projection do).
+// Whether two outputs of one box may share a byte: their spans do, unless their strides are equal and they lie side by side at some
+// dimension (as k and v of one projection do, or heads in turn): inside it one ends before the other begins, and each step
+// of it and of those around it goes over both.
 bool mix(const aecct_heads &s, const Span &x, const aecct_heads &t, const Span &y, const Box &n, int64_t size) {
   if (!overlap(x, y)) return false;
-  if (s.batch != t.batch || s.row != t.row || s.head != t.head) return true;
-  const Span &first = x.begin() <= y.begin() ? x : y, &second = x.begin() <= y.begin() ? y : x;
-  const int64_t width = ((n.heads - 1) * s.head + n.d) * size, pitch = (n.length > 1 ? s.row : s.batch) * size;
-  if (n.length <= 1 && n.batch <= 1) return true;
-  if (n.length > 1 && n.batch > 1 && s.batch < (n.length - 1) * s.row) return true;
-  const int64_t off = (int64_t)(second.begin() - first.begin());
-  return !(off >= width && off + width <= pitch);
+  Dim dims[3], others[3];
+  const int count = dims_of(s, n, dims);
+  (void)dims_of(t, n, others);
+  for (int i = 0; i < count; ++i)
+    if (dims[i].n != others[i].n || dims[i].stride != others[i].stride) return true;
+  const int64_t off = (int64_t)(x.begin() <= y.begin() ? y.begin() - x.begin() : x.begin() - y.begin());
+  int64_t reach = n.d * size;              // of one of them
+  for (int at = 0; at < count && off >= reach; ++at) {
+    int64_t both = off + reach;
+    int i = at;
+    for (; i < count && dims[i].stride * size >= both; ++i) both += (dims[i].n - 1) * dims[i].stride * size;
+    if (i == count) return false;
+    reach += (dims[at].n - 1) * dims[at].stride * size;
+  }
+  return true;
 }
 
 // Attention of at least this many operations, or on this many bytes of keys, first has tensors whose rows are no whole 16-byte pieces

@@ -192,3 +192,44 @@ def test_attention_grad_sizes(P):
     for kw in (dict(queries=0), dict(keys=0)):
         assert _need(P, name, _attention_grad(P, **kw))[0] == P.OK
     assert _need(P, name, _attention_grad(P, d=300))[0] == P.ERR_UNSUPPORTED
+
+
+def _taken(n, strides, d, first):
+    """The places (in values) of a [batch][length][heads][d] tensor."""
+    b, r, h = strides
+    return [first + i * b + j * r + k * h + c for i in range(n[0]) for j in range(n[1]) for k in range(n[2]) for c in range(d)]
+
+
+def _grad_into(P, n, strides, d, off):
+    """The status of a gradient whose dk and dv are `off` values apart, with no workspace: refused before or because of that."""
+    heads = lambda at: P.Heads(at, *strides)  # noqa: E731
+    a = _attention_grad(P, batch=n[0], keys=n[1], heads=n[2], kv_heads=n[2], d=d, lengths=None, mask=None)
+    a.q, a.o, a.dout, a.dq = (_heads(P, i, 3, n[2]) for i in (0, 3, 7, 8))
+    a.k, a.v = _heads(P, 1, n[1], n[2]), _heads(P, 2, n[1], n[2])
+    a.dk, a.dv = heads(BASE + 9 * G), heads(BASE + 9 * G + 4 * off)
+    return _call(P, "aecct_cross_attention_grad", a, ws_bytes=0)
+
+
+@pytest.mark.parametrize("n", [(2, 2, 1), (2, 3, 2), (1, 3, 2), (3, 1, 2), (2, 1, 1), (2, 2, 2), (1, 1, 3)])
+def test_dk_and_dv_that_share_values_are_refused(P, n):
+    """Every small layout of dk whose values lie apart, and dv at every offset: what shares a value is refused; what lies side by side in
+    rows, heads or sequences of one step is not."""
+    d, seen = 2, [0, 0]
+    for b in (4, 6, 8, 12, 14, 15, 16, 20, 24):
+        for r in (2, 4, 5, 6, 8, 10, 12, 24):
+            for h in (2, 4, 5, 8):
+                dk = _taken(n, (b, r, h), d, 0)
+                if len(set(dk)) < len(dk) or _grad_into(P, n, (b, r, h), d, 1 << 20) != P.ERR_WORKSPACE_TOO_SMALL:
+                    continue
+                for off in range(0, 60):
+                    share = bool(set(dk) & set(_taken(n, (b, r, h), d, off)))
+                    got = _grad_into(P, n, (b, r, h), d, off)
+                    assert got == P.ERR_INVALID_ARG or (got == P.ERR_WORKSPACE_TOO_SMALL and not share), (n, (b, r, h), off)
+                    seen[got == P.ERR_INVALID_ARG] += 1
+    assert min(seen) > 0
+    # two sequences of two keys, dv 5 values behind dk in rows 10 apart: sequences 20 apart have room for both, 14 apart do not
+    assert _grad_into(P, (2, 2, 1), (20, 10, 4), 4, 5) == P.ERR_WORKSPACE_TOO_SMALL
+    assert _grad_into(P, (2, 2, 1), (14, 10, 4), 4, 5) == P.ERR_INVALID_ARG
+    # [keys][batch][2][heads][d] and [batch][keys][heads][2][d]
+    assert _grad_into(P, (3, 5, 2), (16, 48, 4), 4, 8) == P.ERR_WORKSPACE_TOO_SMALL
+    assert _grad_into(P, (3, 5, 2), (80, 16, 8), 4, 4) == P.ERR_WORKSPACE_TOO_SMALL
