@@ -655,8 +655,10 @@ typedef struct aecct_cross_attention_args {
   aecct_heads o;                     /* [batch][queries][heads][d] out; its values lie apart */
   float *lse;                        /* fp32 [batch][heads][queries] out, or NULL */
 } aecct_cross_attention_args;
-/* The workspace's size (host call) goes by sizes, strides, type and whether there is a mask; it reads no address.  Errors: INVALID_ARG, UNSUPPORTED (d > 256, a
- * length past 2^30, more than 2^28 queries over sequences and heads, or 2^31 keys over sequences and key heads), WORKSPACE_TOO_SMALL, DEVICE. */
+/* The workspace's size (host call) goes by sizes, strides, type and whether there is a mask; it reads no address.  Errors: INVALID_ARG,
+ * UNSUPPORTED (d > 256; batch, queries or keys past 2^30; heads past 2^20; more than 2^28 - 32 queries over sequences and heads, or
+ * 2^24 - 2 blocks, over sequences and key heads, of 32 queries of the heads that share one or of 128 keys; with a mask more than 2^26 - 8
+ * blocks of 32 queries on 128 keys, these counted with 128 keys more), WORKSPACE_TOO_SMALL, DEVICE. */
 aecct_status aecct_cross_attention_workspace_size(const aecct_cross_attention_args *a, size_t *bytes);
 aecct_status aecct_cross_attention(const aecct_cross_attention_args *a, void *workspace, size_t workspace_bytes, void *stream);
 

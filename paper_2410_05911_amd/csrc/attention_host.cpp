@@ -22,15 +22,15 @@ bool type_ok(int32_t t) { return t == AECCT_F32 || t == AECCT_BF16 || t == AECCT
 int64_t type_size(int32_t t) { return t == AECCT_F32 ? 4 : 2; }
 
 aecct_status check_sizes(int64_t batch, int64_t queries, int64_t keys, int32_t heads, int32_t kv_heads, int32_t d, int32_t type,
-                         float scale) {
+                         float scale, bool masked) {
   if (batch < 0 || queries < 0 || keys < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || d < 1 || !type_ok(type))
     return AECCT_ERR_INVALID_ARG;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return AECCT_ERR_INVALID_ARG;
   if (d > 256 || batch > kMaxCount || queries > kMaxCount || keys > kMaxCount || heads > (1 << 20)) return AECCT_ERR_UNSUPPORTED;
-  // Threads of the largest grids: 256 for 32 rows of a pair or 128 keys (times the splits, which only few blocks take), 64 for 32 rows
-  // and 128 keys of the mask, 16 for a row's terms.
+  // Threads of the largest grids: 256 for 32 rows of a pair or 128 keys (times the splits, which only few blocks take), 16 for a row's
+  // terms, and with a mask, which all heads share, 64 for 32 queries and 128 keys.
   const __int128 rows = (__int128)(heads / kv_heads) * queries, pairs = (__int128)batch * kv_heads;
-  const __int128 blocks = (rows + 31) / 32 * pairs, masks = (rows + 31) / 32 * ((keys + 127) / 128 + 1);
+  const __int128 blocks = (rows + 31) / 32 * pairs, masks = masked ? ((__int128)queries + 31) / 32 * ((keys + 127) / 128 + 1) : 0;
   const __int128 keyed = ((__int128)keys + 127) / 128 * pairs;
   if (blocks > kMaxThreads / 256 || masks > kMaxThreads / 64 || keyed > kMaxThreads / 256 || rows * pairs > kMaxThreads / 16)
     return AECCT_ERR_UNSUPPORTED;
@@ -127,7 +127,7 @@ extern "C" {
 
 aecct_status aecct_cross_attention_workspace_size(const aecct_cross_attention_args *a, size_t *bytes) {
   if (!a || !bytes) return AECCT_ERR_INVALID_ARG;
-  const aecct_status s = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale);
+  const aecct_status s = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale, a->mask);
   if (s != AECCT_OK) return s;
   const aecct::AttentionPlan p =
       aecct::plan_attention(a->type, a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->mask != nullptr);
@@ -142,7 +142,7 @@ aecct_status aecct_cross_attention_workspace_size(const aecct_cross_attention_ar
 
 aecct_status aecct_cross_attention(const aecct_cross_attention_args *a, void *workspace, size_t workspace_bytes, void *stream) {
   if (!a) return AECCT_ERR_INVALID_ARG;
-  const aecct_status st = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale);
+  const aecct_status st = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale, a->mask);
   if (st != AECCT_OK) return st;
   if (a->batch == 0 || a->queries == 0) return AECCT_OK;
   if (!a->q.data || !a->o.data || (a->keys && (!a->k.data || !a->v.data))) return AECCT_ERR_INVALID_ARG;
@@ -190,7 +190,7 @@ aecct_status aecct_cross_attention(const aecct_cross_attention_args *a, void *wo
 
 aecct_status aecct_cross_attention_grad_workspace_size(const aecct_cross_attention_grad_args *a, size_t *bytes) {
   if (!a || !bytes) return AECCT_ERR_INVALID_ARG;
-  const aecct_status s = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale);
+  const aecct_status s = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale, a->mask);
   if (s != AECCT_OK) return s;
   const aecct::AttentionGradPlan p =
       aecct::plan_attention_grad(a->type, a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->mask != nullptr);
@@ -207,7 +207,7 @@ aecct_status aecct_cross_attention_grad_workspace_size(const aecct_cross_attenti
 aecct_status aecct_cross_attention_grad(const aecct_cross_attention_grad_args *a, void *workspace, size_t workspace_bytes,
                                         void *stream) {
   if (!a) return AECCT_ERR_INVALID_ARG;
-  const aecct_status st = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale);
+  const aecct_status st = check_sizes(a->batch, a->queries, a->keys, a->heads, a->kv_heads, a->d, a->type, a->scale, a->mask);
   if (st != AECCT_OK) return st;
   if (a->batch == 0) return AECCT_OK;
   const bool some_q = a->queries > 0, some_k = a->keys > 0;

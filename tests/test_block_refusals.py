@@ -233,3 +233,25 @@ def test_dk_and_dv_that_share_values_are_refused(P, n):
     # [keys][batch][2][heads][d] and [batch][keys][heads][2][d]
     assert _grad_into(P, (3, 5, 2), (16, 48, 4), 4, 8) == P.ERR_WORKSPACE_TOO_SMALL
     assert _grad_into(P, (3, 5, 2), (80, 16, 8), 4, 4) == P.ERR_WORKSPACE_TOO_SMALL
+
+
+def test_attention_limits(P):
+    """Each limit that the header names, from both sides: the last size that is taken and the first that is not."""
+    def need(grad, **kw):
+        a = _attention_grad(P, lengths=None, **kw) if grad else _attention(P, lengths=None, **kw)
+        return _need(P, "aecct_cross_attention_grad" if grad else "aecct_cross_attention", a)[0]
+    one = dict(batch=1, heads=1, kv_heads=1)
+    last_mask = ((1 << 26) - 8) // 1025 * 32       # queries on 131072 keys
+    for kw, taken in ((dict(one, heads=32, kv_heads=2, queries=131072, keys=131072, mask=None), True),
+                      (dict(one, heads=32, kv_heads=2, queries=131072, keys=131072), True),
+                      (dict(one, heads=64, kv_heads=1, queries=131072, keys=131072), True),
+                      (dict(one, queries=last_mask, keys=131072), True), (dict(one, queries=last_mask + 1, keys=131072), False),
+                      (dict(one, queries=last_mask + 1, keys=131072, mask=None), True),
+                      (dict(one, queries=(1 << 28) - 32, keys=1, mask=None), True),
+                      (dict(one, queries=(1 << 28) - 31, keys=1, mask=None), False),
+                      (dict(one, batch=(1 << 24) - 2, queries=1, keys=1), True), (dict(one, batch=(1 << 24) - 1, queries=1, keys=1), False),
+                      (dict(one, batch=1 << 23, queries=1, keys=129), False), (dict(one, keys=1 << 30, queries=1, mask=None), True),
+                      (dict(one, keys=(1 << 30) + 1, queries=1, mask=None), False),
+                      (dict(one, heads=1 << 20, queries=1, keys=1), True), (dict(one, heads=(1 << 20) + 1, queries=1, keys=1), False)):
+        for grad in (False, True):
+            assert need(grad, **kw) == (P.OK if taken else P.ERR_UNSUPPORTED), (grad, kw)
