@@ -38,8 +38,8 @@ __device__ __forceinline__ void barrier() {
 
 // Loads that go to LDS without passing through registers: 16 bytes a lane from byte `offset` of a buffer (zeros from `size` on) to
 // the wavefront's place `lds` + 16 lane.  Written as assembly because the compiler waits for such loads before any read of LDS,
-// whichever part of it that reads; here wait_loads() says when they have to be there.  (They write no registers.  One
-// instruction has to lie between the write of m0 and its use.)
+// whichever part of it that reads; here wait_loads() says when they have to be there.  (They write no vector registers;
+// m0 is the wavefront's place.  One instruction has to lie between the write of m0 and its use.)
 struct BufferOf {
   u32x4 r;
   __device__ __forceinline__ BufferOf(const void *p, uint32_t size) {
@@ -49,7 +49,7 @@ struct BufferOf {
   }
   __device__ __forceinline__ void to_lds(char *lds, uint32_t offset) const {
     const uint32_t at = (uint32_t)(uintptr_t)AECCT_LDS(char, lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(r) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(r) : "memory", "m0");
   }
 };
 
