@@ -561,7 +561,7 @@ __global__ __launch_bounds__(NT) void k_few_across(Gemm g) {
     for (int i = 0; i < 8; ++i) acc[r][i] = 0;
   const S *const px = (const S *)g.a.p;
   const char *const pw = (const char *)g.b.p + n0 * (int64_t)sizeof(S);
-  const uint32_t step = (uint32_t)(g.b.ld * (int64_t)sizeof(S));   // below 2^32: few_ok
+  const uint32_t step = (uint32_t)(g.b.ld * (int64_t)sizeof(S));   // below 2^32: plan_gemm takes few rows with ldb < 2^30 only
   for (int k0 = begin; k0 < end; k0 += ROUND) {
     Stored<S, 8> w[AT];
     if (count == 8) {
