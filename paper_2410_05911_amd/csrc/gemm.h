@@ -16,29 +16,38 @@
 namespace aecct {
 
 // ---- activations, in fp32
-// The normal distribution Phi(z) and e = e^(-z^2 / 2), to 1e-7: Abramowitz and Stegun 7.1.26 for its tail, 1 - erf(x) = e^(-x^2) times a
-// polynomial in 1 / (1 + 0.3275911 x).  A third of erff's instructions (16384 x 4096 -> 8192 bf16 1097 -> 1071 us, the gradient's first launch 68 -> 50);
-// fp32 outputs take erff.
-__device__ __forceinline__ float normal(float z, float &e) {
-  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+// The normal distribution Phi(z) and e = e^(-z^2 / 2).  Its tail, half of erfc(x) at x = |z| / sqrt(2), is e times a polynomial in
+// 1 / (1 + 0.412 x) whose coefficients are fitted here for the smallest error against the larger of 1.4e-7 and 2^-14 of erfc(x), x to 9.6:
+// Phi is off by at most 2.3e-7, and by an eighth of fp16's half step where it is small (with one coefficient less, fitted for the
+// first alone, GELU at -4 was off by 2 half steps of fp16 and below -7 by several of bf16).  A third of erfc's instructions
+// (16384 x 4096 -> 8192 bf16 with erff 1097 us, so 1071); fp32 outputs take erfcf and expf.
+__device__ __forceinline__ float normal(float z, float &e, bool f32) {
+  if (f32) {
+    e = expf(-0.5f * z * z);
+    return 0.5f * erfcf(z * -0.70710678118654752f);
+  }
+  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.412f, x, 1.0f));
   e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
-  float p = fmaf(t, 1.061405429f, -1.453152027f);
-  p = fmaf(t, p, 1.421413741f);
-  p = fmaf(t, p, -0.284496736f);
-  p = fmaf(t, p, 0.254829592f);
+  float p = fmaf(t, -0.17485723f, 0.55085403f);
+  p = fmaf(t, p, -0.1636966f);
+  p = fmaf(t, p, 0.3475389f);
+  p = fmaf(t, p, 0.20564933f);
+  p = fmaf(t, p, 0.23451155f);
   const float tail = 0.5f * (p * t) * e;
   return z > 0.0f ? 1.0f - tail : tail;
 }
-__device__ __forceinline__ float logistic(float z) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+// 1 / (1 + e^-z) and q = 1 - that, each from e^-|z|, so that the smaller one keeps its bits and does not vanish before e^-|z| does.
+__device__ __forceinline__ float logistic(float z, float &q, bool f32) {
+  const float e = f32 ? expf(-fabsf(z)) : __builtin_amdgcn_exp2f(fabsf(z) * -1.4426950408889634f);
+  const float large = f32 ? 1.0f / (1.0f + e) : __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+  q = z < 0.0f ? large : small;
+  return z < 0.0f ? small : large;
 }
 __device__ __forceinline__ float activate(float z, int act, bool f32) {
+  float other;
   if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
-  if (act == kActGelu) {
-    float e;
-    return z * (f32 ? 0.5f * (1.0f + erff(z * 0.70710678118654752f)) : normal(z, e));
-  }
-  if (act == kActSilu) return z * logistic(z);
+  if (act == kActGelu) return z * normal(z, other, f32);
+  if (act == kActSilu) return z * logistic(z, other, f32);
   return z;
 }
 

@@ -54,10 +54,11 @@ __device__ __forceinline__ float slope(float z, int act, bool f32) {
   if (act == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
   if (act == kActGelu) {
     float e;
-    const float phi = normal(z, e), density = e * 0.39894228040143268f;
-    return (f32 ? 0.5f * (1.0f + erff(z * 0.70710678118654752f)) : phi) + (density == 0.0f ? 0.0f : z * density);
+    const float phi = normal(z, e, f32), density = e * 0.39894228040143268f;
+    return phi + (density == 0.0f ? 0.0f : z * density);
   }
-  const float p = logistic(z), q = logistic(-z);   // q = 1 - p
+  float q;
+  const float p = logistic(z, q, f32);
   if (p == 0.0f || q == 0.0f) return p;
   return p * (1.0f + z * q);
 }

@@ -295,3 +295,41 @@ def test_refusals(P):
             call()
     with pytest.raises(P.AecctError):    # y overlaps x
         P.linear(x, torch.zeros(8, 8, device="cuda"), y=x)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("kind", ["fp32", "bf16", "fp16"])
+def test_activation_tails(P, act, kind):
+    """Activations and slopes relative to their own size, where they are small too.  z is exact: one product with 1.
+
+    Conditions: z Phi(z) moves by a share of at most (z^2 + 2) a where z moves by a share a, z / (1 + e^-z) by (|z| + 1) a.  fp32 takes erfc
+    at z / sqrt(2) (off by 2 u for the factor and its product, which moves erfc's share by z^2 + 1 times that), e^x within 2 u of
+    its value, and a few products: 4 (z^2 + 8) u.  16-bit types: the same, and 2^-14 for the fitted tail.  Then the type's
+    half step.  Slopes are sums Phi + z phi, or products p (1 + z q), whose parts are off by such shares."""
+    t = TYPES[kind]
+    z = torch.linspace(-12.5, 12.5, 40001, device="cuda").to(t).unique()
+    one = torch.ones(1, 1, device="cuda", dtype=t)
+    y, got = P.linear(z[:, None], one, act=act, with_z=True)
+    assert torch.equal(got[:, 0], z)
+    zz = z.double()
+    fit = 0 if kind == "fp32" or act == "silu" else 2.0 ** -14
+    share = 4 * (zz * zz + 8) * U + fit
+    p = 0.5 * torch.erfc(-zz * 0.5 ** 0.5) if act == "gelu" else torch.sigmoid(zz)     # (ndtr on the GPU is 0 or 2^-54 off in the tail)
+    want = zz * p
+    _near(y[:, 0], want, (share + HALF[t]) * want.abs() + TINY[t], "y")
+    across = torch.ones(1, z.numel(), device="cuda", dtype=t)
+    _, _, dbias = P.linear_grad(one, across, across, z[None], act, with_dx=False, with_dw=False)      # of one row: the slopes, in fp32
+    inner = zz * torch.exp(-0.5 * zz * zz) / (2 * torch.pi) ** 0.5 if act == "gelu" else zz * p * torch.sigmoid(-zz)
+    _near(dbias, p + inner, share * (p + inner.abs()) + TINY[torch.float32], "slope")
+
+
+def test_silu_far_below(P):
+    """e^z is a normal number to z = -87.3; 4 (|z| + 8) u as above, the slopes' two parts each."""
+    z = torch.linspace(-87, -80, 50, device="cuda")
+    y, _ = P.linear(z[:, None], torch.ones(1, 1, device="cuda"), act="silu")
+    zz = z.double()
+    _near(y[:, 0], zz * torch.sigmoid(zz), 4 * (zz.abs() + 8) * U * (zz * torch.sigmoid(zz)).abs(), "y")
+    one = torch.ones(1, 50, device="cuda")
+    _, _, dbias = P.linear_grad(one[:, :1], one, one, z[None], "silu", with_dx=False, with_dw=False)
+    p = torch.sigmoid(zz)
+    _near(dbias, p * (1 + zz * torch.sigmoid(-zz)), 4 * (zz.abs() + 8) * U * p * (1 + zz.abs()), "slope")
