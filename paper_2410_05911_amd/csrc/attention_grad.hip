@@ -213,8 +213,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
         if (!__any(__popc(in) > kFewPairs)) {
           while (__any(in != 0)) {
             const int row = u * 32 + (in ? __builtin_ctz(in) : 0);
-            const HalfRow<RB> key(lk, row, a.d), value(lv, row, a.d);
-            const float s = sum_halves(key.dot(q, a.d)), dp = sum_halves(value.dot(dout, a.d));
+            const float dp = sum_halves(HalfRow<RB>(lv, row, a.d).dot(dout, a.d));
+            const HalfRow<RB> key(lk, row, a.d);
+            const float s = sum_halves(key.dot(q, a.d));
             const float ds = __builtin_amdgcn_exp2f(fmaf(s, to2, -l2)) * (dp - dd);
             if (in) key.add_to(acc, ds, a.d);
             in &= in - 1;
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
     }
     if constexpr (DIRECT) buf ^= 1;
     bool dense = !idle && (!MASK || __any(any != 0));
-    if constexpr (MASK && DK && DV && pairwise<T, RB>()) {
+    if constexpr (MASK && DK && DV && pairwise<T, RB>() && RB <= 128) {
       if (dense && !__any(__popc(any) > 16)) {
         uint32_t in = turn_bits(any);    // the rows of the tile that may attend the lane's key
         if (!mine) in = 0;

@@ -20,6 +20,15 @@ __device__ __forceinline__ int exchange(int row) {
   if constexpr (RB % 256 == 0) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
   return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
 }
+// The lane, for LDS addresses.  In fp32 rows of 33 to 64 values take it as a new value each time: the addresses of a tile, the same for
+// every tile, are then computed where they are used instead of being kept over the loop, for which 60 to 160 registers a lane
+// were spilled under a mask (128 x 256 on 128 keys, 8 heads of 64, a band: 163 -> 104 us, its gradient 527 -> 311).
+template <class T, int RB>
+__device__ __forceinline__ int lane_of() {
+  int lane = threadIdx.x & 63;
+  if constexpr (sizeof(T) == 4 && RB == 256) asm volatile("" : "+v"(lane));
+  return lane;
+}
 // Chunk `chunk` of row `row`: of a product along d.
 template <int RB>
 __device__ __forceinline__ u32x4 row_chunk(const char *tile, int row, int chunk) {
@@ -50,7 +59,7 @@ __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile,
       for (int f = 0; f < FD; ++f) step<T>(acc[f], column_chunk<RB>(tile, row0, t, 32 * f), b);
     }
   } else {
-    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int lane = lane_of<T, RB>(), h = lane >> 5;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int row = row0 + row_of(i, h);
@@ -66,7 +75,7 @@ __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile,
 // The product of the tile's 32 rows from row0 on with a lane's row held in registers (chunks 2 s + h).
 template <class T, int RB>
 __device__ __forceinline__ f32x16 times_rows(const char *tile, int row0, const u32x4 (&r)[RB / 32], int d) {
-  const int lane = threadIdx.x & 63;
+  const int lane = lane_of<T, RB>();
   f32x16 s;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = 0;
@@ -98,9 +107,11 @@ __device__ __forceinline__ float sum_halves(float x) {
 }
 
 // ---- masks that leave few pairs (a Tanner graph's): fp32 tiles go pair by pair, each lane through its own row's keys (or its key's
-// rows), where the matrix instructions would take 64 DP clocks for 32 x 32 pairs, a pair of one lane about 240 + 8 DP.
+// rows), where the matrix instructions would take 64 DP clocks for 32 x 32 pairs, a pair of one lane about 240 + 8 DP.  To 64 values a
+// row, in dk and dv to 32: a key, its value and both sums leave no registers there (128 x 256 on 128 keys, 8 heads of 64, a Tanner
+// graph: the gradient with pairs in dk and dv too 500 us and more, without 299).
 template <class T, int RB>
-__host__ __device__ constexpr bool pairwise() { return sizeof(T) == 4 && RB <= 256; }   // more do not fit in registers
+__host__ __device__ constexpr bool pairwise() { return sizeof(T) == 4 && RB <= 256; }
 constexpr int kFewPairs = 4;   // of a lane, for 32 keys or rows
 // The lane's half of a row of a tile: chunks 2 c + h, which are also the columns that its sums of a result's columns are for.  Read once
 // for a product and for a sum (LDS is what bounds these loops).
@@ -108,7 +119,7 @@ template <int RB>
 struct HalfRow {
   f32x4 x[RB / 32];
   __device__ __forceinline__ HalfRow(const char *tile, int row, int d) {
-    const int h = (threadIdx.x & 63) >> 5;
+    const int h = lane_of<float, RB>() >> 5;
 #pragma unroll
     for (int c = 0; c < RB / 32; ++c) {
       if (8 * c >= d) break;
