@@ -63,7 +63,7 @@ hipError_t launch_attention(int type, const Attention &a, const AttentionPlan &p
 struct AttentionGrad {
   Attention a;
   Heads dout, dq, dk, dv;      // dq, dk, dv: out
-  float *rows;                 // [pairs][rows][2]: lse log2(e), and the sum of dout o
+  float *rows;                 // [pairs][rows][2]: lse (16-bit types: times log2(e)), and the sum of dout o
   int splits;                  // of the rows, for dk and dv
   float *part;                 // [splits][2][pairs][keys][d_of(d)], or null
   int splits_q;                // of the keys, for dq

@@ -44,10 +44,20 @@ struct Scaled {
   __device__ __forceinline__ float out() const { return __is_same(T, f16_t) ? 1.0f / by : 1.0f; }
 };
 
-// What a row of p and ds is taken from: lse log2(e) (a row that attends nothing: infinity, so that its weights are 0) and D.
-__device__ __forceinline__ void row_terms(float lse, float sum, float &l2, float &dd) {
-  l2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+// What a row of p and ds is taken from: lse, in 16-bit types times log2(e) (a row that attends nothing: infinity, so that its weights
+// are 0) and D.
+template <class T>
+__device__ __forceinline__ void row_terms(float lse, float sum, float &l, float &dd) {
+  l = lse == -INFINITY ? INFINITY : sizeof(T) == 4 ? lse : lse * kLog2e;
   dd = lse == -INFINITY ? 0.0f : sum;
+}
+// p of a score s, times 2^shift.  In fp32 the score's distance from lse is taken before it is multiplied by log2(e): it is small where p is
+// not, while lse log2(e) alone, rounded, moves a row's p by up to 2^-24 of |lse log2(e)| (2 queries on 24 keys of 64 values: dv off by
+// 2.6e-7 of its norm, so 2.1e-7; what is left is the scores' own sums).
+template <class T>
+__device__ __forceinline__ float weight(float s, float scale, float l, float shift) {
+  if constexpr (sizeof(T) == 4) return __builtin_amdgcn_exp2f(fmaf(s, scale, -l) * kLog2e);
+  else return __builtin_amdgcn_exp2f(fmaf(s, scale * kLog2e, shift - l));
 }
 // The sum of the products of two pieces of 16 bytes.
 template <class T>
@@ -83,9 +93,9 @@ __global__ __launch_bounds__(256) void k_attention_rows(AttentionGrad g) {
 #pragma unroll
   for (int i = 1; i < 16; i *= 2) sum += __shfl_xor(sum, i);
   if ((threadIdx.x & 15) == 0) {
-    float l2, dd;
-    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum, l2, dd);
-    g.rows[(int64_t)row * 2] = l2;
+    float l, dd;
+    row_terms<T>(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum, l, dd);
+    g.rows[(int64_t)row * 2] = l;
     g.rows[(int64_t)row * 2 + 1] = dd;
   }
 }
@@ -111,7 +121,6 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
   const uint32_t r = row_block * 128 + wave * 32 + (lane & 31), rc = min(r, rows - 1);
   const uint32_t head = kh * group + rc / queries, query = rc % queries;
   const bool idle = row_block * 128 + wave * 32 >= rows;
-  const float to2 = a.scale * kLog2e;
   Keys<T, RB, KT, NT, DIRECT> keys(a.k, a, b, kh, length), values(a.v, a, b, kh, length);
   const int words = (int)words_of(a.keys);
   const uint32_t *const mask = MASK ? a.words + (int64_t)query * words : nullptr;
@@ -153,7 +162,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
   }
   // (behind the first tile, which is on its way by now)
   u32x4 q[RB / 32], dout[RB / 32];
-  float dd = 0, l2;
+  float dd = 0, l;
   {
     const char *const p = (const char *)a.q.p + (b * a.q.batch + query * a.q.row + head * a.q.head) * (int64_t)sizeof(T);
     const char *const pd = (const char *)g.dout.p + (b * g.dout.batch + query * g.dout.row + head * g.dout.head) * (int64_t)sizeof(T);
@@ -167,9 +176,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
       dout[c] = row_piece<T>(pd, 2 * c + h, a.d, endd);
       dd = dot<T>(row_piece<T>(po, 2 * c + h, a.d, endo), dout[c], dd);
     }
-    row_terms(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l2, dd);
+    row_terms<T>(a.lse[(int64_t)(b * a.heads + head) * queries + query], sum_halves(dd), l, dd);
     if (h == 0 && r < rows && split == 0) {
-      g.rows[((int64_t)pair * rows + r) * 2] = l2;
+      g.rows[((int64_t)pair * rows + r) * 2] = l;
       g.rows[((int64_t)pair * rows + r) * 2 + 1] = dd;
     }
   }
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
             const float dp = sum_halves(HalfRow<RB>(lv, row, a.d).dot(dout, a.d));
             const HalfRow<RB> key(lk, row, a.d);
             const float s = sum_halves(key.dot(q, a.d));
-            const float ds = __builtin_amdgcn_exp2f(fmaf(s, to2, -l2)) * (dp - dd);
+            const float ds = weight<T>(s, a.scale, l, 0.0f) * (dp - dd);
             if (in) key.add_to(acc, ds, a.d);
             in &= in - 1;
           }
@@ -226,7 +235,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
       const f32x16 s = times_rows<T, RB>(lk, u * 32, q, a.d), dp = times_rows<T, RB>(lv, u * 32, dout, a.d);
       float ds[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(s[i], to2, -l2)) * (dp[i] - dd);
+      for (int i = 0; i < 16; ++i) ds[i] = weight<T>(s[i], a.scale, l, 0.0f) * (dp[i] - dd);
       if (!__all(in == ~0u)) {
         in >>= 4 * h;
 #pragma unroll
@@ -343,7 +352,6 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
   int t1 = (tiles - (int)split + by - 1) / by;
   if ((int)(key_block * 128) >= length) t1 = 0;   // a block whose keys are all past the length has nothing to sum
   const bool idle = key0 >= length, mine = key < length;
-  const float to2 = a.scale * kLog2e;
   const int words = (int)words_of(a.keys);
   uint64_t want = 0;
   int want0 = -64;
@@ -438,7 +446,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
             const int row = in ? __builtin_ctz(in) : 0;
             const HalfRow<RB> q(lq, row, a.d), dout(ld, row, a.d);
             const float s = sum_halves(q.dot(k, a.d)), dp = sum_halves(dout.dot(v, a.d));
-            const float p = __builtin_amdgcn_exp2f(fmaf(s, to2, -rl[turn][row])), ds = p * (dp - rd[turn][row]);
+            const float p = weight<T>(s, a.scale, rl[turn][row], 0.0f), ds = p * (dp - rd[turn][row]);
             if (in) {
               dout.add_to(av, p, a.d);
               q.add_to(ak, ds, a.d);
@@ -455,10 +463,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
       float p[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        const f32x4 l2 = *(const f32x4 *)(&rl[turn][row_of(i, h)]), dd = *(const f32x4 *)(&rd[turn][row_of(i, h)]);
+        const f32x4 l = *(const f32x4 *)(&rl[turn][row_of(i, h)]), dd = *(const f32x4 *)(&rd[turn][row_of(i, h)]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          p[i + j] = __builtin_amdgcn_exp2f(fmaf(s[i + j], to2, p_shift<T>() - l2[j]));
+          p[i + j] = weight<T>(s[i + j], a.scale, l[j], p_shift<T>());
           if constexpr (DK) ds[i + j] = p[i + j] * (dp[i + j] - dd[j]);
         }
       }

@@ -361,3 +361,37 @@ def test_refusals(P):
     with pytest.raises(P.AecctError) as e:
         P.cross_attention(wide, wide, wide)
     assert e.value.status == P.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("d,few", [(16, False), (16, True), (64, False), (64, True), (100, False), (250, False)])
+def test_weights_of_the_gradient_in_fp32(P, d, few):
+    """Single weights, from scores that are exact in fp32 (small whole numbers, a scale of 1) up to 48 and more below and above: with dout of one
+    1 and o = 0, dv of a key is its p, and with v of one key only dq is p k.  p = e^t, t = s - lse the distance from the lse that is
+    given: t is rounded once, its product with log2(e) is off by 2 u more, e^x by 2 u of its value, and a product or a sum with zeros
+    by u: (3 |t| + 6) u."""
+    b, m = 20, 70
+    g = torch.Generator(device="cuda").manual_seed(31)
+    k = torch.randint(-3, 4, (b, m, 1, d), device="cuda", generator=g).float()
+    q = torch.randint(-2, 3, (b, 1, 1, d), device="cuda", generator=g).float()
+    q[:, :, :, 8:] = 0
+    k[:, 3, :, :8] = 3 * q[:, 0, :, :8].sign()
+    mask = None
+    if few:
+        mask = torch.zeros(1, m, dtype=torch.bool, device="cuda")
+        mask[0, [3, 20, 41, 69]] = True
+    o, lse = P.cross_attention(q, k, k, None, mask, 1.0, with_lse=True)
+    score = (q.double() * k.double()).sum(-1)[..., 0]
+    t = score - lse.double()[:, 0]
+    p = torch.exp(t) if mask is None else torch.exp(t) * mask
+    bound = (3 * t.abs() + 6) * U * p + TINY[torch.float32]
+    dout = torch.zeros_like(q)
+    dout[..., 0] = 1
+    none = torch.zeros_like(q)
+    for at in (3, 20, 41):
+        v = torch.zeros_like(k)
+        v[:, at, 0, 0] = 1
+        dq, dk, dv = P.cross_attention_grad(q, k, v, none, lse, dout, None, mask, 1.0)
+        _near(dv[:, :, 0, 0], p, bound, "dv")
+        assert not dv[..., 1:].any()
+        _near(dq[:, 0, 0], p[:, at, None] * k[:, at, 0].double(), bound[:, at, None] * k[:, at, 0].double().abs(), "dq")
+        _near(dk[:, at, 0], p[:, at, None] * q[:, 0, 0].double(), bound[:, at, None] * q[:, 0, 0].double().abs(), "dk")
