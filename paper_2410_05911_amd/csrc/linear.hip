@@ -5,6 +5,32 @@
 
 namespace aecct {
 
+namespace {
+
+// fp32: the matrix instructions' time is nearly all there is, so what counts is the blocks of the fullest compute unit.  Microseconds by
+// what was measured (512 x 512 x 512 to 4096 x 4096 x 4096, 26 x 6912 -> 4096, 7717 x 5144 -> 128): a tile of k of 128 x 128 outputs
+// 2.0, of 64 x 64 0.6 beside others and 0.7 alone; joining splits 4 and what their sums take at 6.5 TB/s.  (With the rule for 16 bits 288
+// blocks of 128 x 128 took two rounds: 2048 x 2048 -> 2304 257 us, k split in five 183; 1280 x 4096 -> 3840 504 and 334; 672 x 6352 ->
+// 1024 122 and 94.)
+void plan_f32(GemmPlan &p, int64_t m, int64_t n, int64_t tiles64, int64_t tiles128, int64_t kt) {
+  double best = 0;
+  for (int tile = 0; tile < 2; ++tile)
+    for (int64_t s = 1; s <= 64; ++s) {
+      const int64_t blocks = (tile ? tiles128 : tiles64) * s, rounds = (blocks + 255) / 256;
+      if (s > 1 && (kt / s < 4 || rounds > 8)) break;
+      const double each = tile ? 2.0 : rounds > 1 ? 0.6 : 0.7;
+      const double time = (double)(rounds * ((kt + s - 1) / s)) * each + (s > 1 ? 4 + (double)(s * m * n) * 8 / 6.5e6 : 0);
+      if ((tile == 0 && s == 1) || time < best) {
+        best = time;
+        p.tile = tile;
+        p.splits = (int)s;
+      }
+    }
+  if (p.splits > 1) p.part_bytes = (size_t)(p.splits * m * n * 4);
+}
+
+}  // namespace
+
 GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, bool across_b, int64_t ldb, bool whole) {
   GemmPlan p{false, 1, 1, 0};
   const int64_t size = type == AECCT_F32 ? 4 : type == kCodeType + AECCT_CODE_I8 ? 1 : 2;   // of a value in LDS
@@ -20,6 +46,10 @@ GemmPlan plan_gemm(int type, int64_t m, int64_t n, int64_t k, bool across_a, boo
     return p;
   }
   auto tiles = [&](int t) { return (m + kTileSide[t][0] - 1) / kTileSide[t][0] * ((n + kTileSide[t][1] - 1) / kTileSide[t][1]); };
+  if (type == AECCT_F32) {
+    plan_f32(p, m, n, tiles(0), tiles(1), (k + 31) / 32);
+    return p;
+  }
   if (tiles(1) < 192) p.tile = 0;
   else if (tiles(2) >= 256 && k * size >= 1024) p.tile = 2;
   const int64_t t = tiles(p.tile), kt = (k * size + 127) / 128;
