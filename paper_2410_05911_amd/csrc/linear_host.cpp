@@ -43,8 +43,13 @@ aecct_status check_linear(const aecct_linear_map_args *a) {
   return a->code_type == AECCT_CODE_I8 && a->in > kMaxIntWidth ? AECCT_ERR_UNSUPPORTED : AECCT_OK;
 }
 int kind(const aecct_linear_map_args *a) { return a->code_type == AECCT_CODE_NONE ? a->type : aecct::kCodeType + a->code_type; }
-// Products of fewer operations are done before a launch that copies their factors into whole pieces would pay.
-constexpr double kPackWork = 4e9;
+// Factors that are no whole 16-byte pieces are copied into such where that pays: where the product takes longer than the launch that copies
+// them, and each copied value enters so many products that its reading and writing is less than what the product gains.  A map in 16
+// or 8 bits, from 300 products a value on (bf16 1295 x 7731 -> 1082, 580 a value, 114 -> 88 us; 9987 x 4929 -> 187, 184 a value, copied
+// 77, as it lies 64), in fp32 from 2000 on (2001 x 1001 -> 2601, 1130 a value, copied 124 us, as it lies 119; 6081 x 2480 -> 4735, 6081 a
+// value, 1143 and 1180).  A gradient, which reads a factor across its lines, from 160 on (7717 x 5137 -> 128, 126 a value, fp32 279 and 231, bf16 94 and 75; 1001 x 777 ->
+// 1333, 330 a value, fp32 77 and 92, bf16 25.5 and 39).
+constexpr double kPackWork = 4e9, kPackMap = 300, kPackMap32 = 2000, kPackGrad = 160;
 // A forward map's workspace: copies of ragged factors, the splits' sums.
 struct MapWork {
   aecct::GemmPlan plan;
@@ -57,7 +62,10 @@ MapWork map_work(const aecct_linear_map_args *a) {
   const int t = kind(a);
   const int64_t lines = a->w_turned ? a->out : a->in, across = a->w_turned ? a->in : a->out;
   const bool ragged_x = aecct::ragged(t, a->ldx, a->in), ragged_w = aecct::ragged(t, a->ldw, across),
-             pack = 2.0 * a->rows * a->in * a->out >= kPackWork;
+             pack = 2.0 * a->rows * a->in * a->out >= kPackWork &&
+                    (double)a->rows * a->in * a->out >=
+                        (t == AECCT_F32 ? kPackMap32 : kPackMap) *
+                            ((ragged_x ? (double)a->rows * a->in : 0) + (ragged_w ? (double)a->in * a->out : 0));
   m.plan = aecct::plan_gemm(t, a->rows, a->out, a->in, false, !a->w_turned, a->ldw, pack || !(ragged_x || ragged_w));
   if (!m.plan.few && pack) {
     m.pack_x = ragged_x;
@@ -91,10 +99,13 @@ GradWork grad_work(const aecct_linear_map_grad_args *a) {
   const int64_t lines = a->w_turned ? a->out : a->in, across = a->w_turned ? a->in : a->out;
   w.need_dz = a->act != AECCT_ACT_NONE && (a->dx || a->dw);
   w.lddz = aecct::packed_line(t, a->out);
-  // With a first launch for dz or the sums the copies cost little more.
-  const bool pack = w.need_dz || a->dbias || 2.0 * a->rows * a->in * a->out >= kPackWork;
   const bool ragged_x = aecct::ragged(t, a->ldx, a->in), ragged_w = aecct::ragged(t, a->ldw, across),
              ragged_d = !w.need_dz && aecct::ragged(t, a->lddy, a->out);
+  const double values = (a->dw && ragged_x ? (double)a->rows * a->in : 0) + (a->dx && ragged_w ? (double)a->in * a->out : 0) +
+                        (ragged_d ? (double)a->rows * a->out : 0);
+  // (a first launch for dz or the sums is there anyway)
+  const bool pack = (w.need_dz || a->dbias || 2.0 * a->rows * a->in * a->out >= kPackWork) &&
+                    (double)a->rows * a->in * a->out >= kPackGrad * values;
   w.dx = aecct::plan_gemm(t, a->rows, a->in, a->out, false, a->w_turned, a->ldw, pack || !(ragged_w || ragged_d));
   w.dw = aecct::plan_gemm(t, a->in, a->out, a->rows, true, true, 0, pack || !(ragged_x || ragged_d));
   if (pack) {
