@@ -20,13 +20,15 @@ __device__ __forceinline__ int exchange(int row) {
   if constexpr (RB % 256 == 0) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
   return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
 }
-// The lane, for LDS addresses.  In fp32 rows of 33 to 64 values take it as a new value each time: the addresses of a tile, the same for
-// every tile, are then computed where they are used instead of being kept over the loop, for which 60 to 160 registers a lane
-// were spilled under a mask (128 x 256 on 128 keys, 8 heads of 64, a band: 163 -> 104 us, its gradient 527 -> 311).
+// The lane, for LDS addresses.  In fp32 rows of 33 to 64 and of 193 to 256 values take it as a new value each time: the addresses of a
+// tile, the same for every tile, are then computed where they are used instead of being kept over the loop, for which 60 to 200
+// registers a lane were spilled (128 x 256 on 128 keys, 8 heads of 64, a band: 163 -> 104 us, its gradient 527 -> 311; 8 x 1024 on
+// 1024, 16/4 heads of 256: 2204 -> 1763, gradient of 2 x 1024 on 1024, 8/4 of 200: 1284 -> 974).  Between, where nothing spills, computing
+// them again costs 5 %.
 template <class T, int RB>
 __device__ __forceinline__ int lane_of() {
   int lane = threadIdx.x & 63;
-  if constexpr (sizeof(T) == 4 && RB == 256) asm volatile("" : "+v"(lane));
+  if constexpr (sizeof(T) == 4 && (RB == 256 || RB == 1024)) asm volatile("" : "+v"(lane));
   return lane;
 }
 // Chunk `chunk` of row `row`: of a product along d.
