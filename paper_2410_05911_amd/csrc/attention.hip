@@ -180,7 +180,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 128 ? 3 : DP * sizeo
       float top = -INFINITY;
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
-        const f32x16 x = times_rows<T, RB>(lk, (wk * SUB + u) * 32, q, a.d);
+        const f32x16 x = times_rows<T, RB, false>(lk, (wk * SUB + u) * 32, q, a.d);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[u][i] = x[i];
       }
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(WQ *WK * 64, DP * sizeof(T) <= 128 ? 3 : DP * sizeo
           s[u][i] = __builtin_amdgcn_exp2f(fmaf(s[u][i], to2, -lift));
           part[i & 3] += s[u][i];
         }
-        add_columns<T, RB, FD>(acc, lv, (wk * SUB + u) * 32, s[u], a.d);
+        add_columns<T, RB, false>(acc, lv, (wk * SUB + u) * 32, s[u], a.d);
       }
       sum += (part[0] + part[1]) + (part[2] + part[3]);
     }

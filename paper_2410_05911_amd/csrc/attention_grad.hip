@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
           continue;
         }
       }
-      const f32x16 s = times_rows<T, RB>(lk, u * 32, q, a.d), dp = times_rows<T, RB>(lv, u * 32, dout, a.d);
+      const f32x16 s = times_rows<T, RB, RB == 1024>(lk, u * 32, q, a.d), dp = times_rows<T, RB, RB == 1024>(lv, u * 32, dout, a.d);
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] = weight<T>(s[i], a.scale, l, 0.0f) * (dp[i] - dd);
@@ -249,13 +249,13 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 
         for (int f = 0; f < FD; ++f)
 #pragma unroll
           for (int i = 0; i < 16; ++i) fresh[f][i] = 0;
-        add_columns<T, RB, FD>(fresh, lk, u * 32, ds, a.d);
+        add_columns<T, RB, RB == 1024>(fresh, lk, u * 32, ds, a.d);
 #pragma unroll
         for (int f = 0; f < FD; ++f)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[f][i] += fresh[f][i];
       } else {
-        add_columns<T, RB, FD>(acc, lk, u * 32, ds, a.d);
+        add_columns<T, RB, RB == 1024>(acc, lk, u * 32, ds, a.d);
       }
     }
     t = next;
@@ -457,9 +457,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
       }
     }
     if (dense) {
-      const f32x16 s = times_rows<T, RB>(lq, 0, k, a.d);
+      const f32x16 s = times_rows<T, RB, RB == 1024 && DK>(lq, 0, k, a.d);
       f32x16 dp;
-      if constexpr (DK) dp = times_rows<T, RB>(ld, 0, v, a.d);
+      if constexpr (DK) dp = times_rows<T, RB, RB == 1024 && DK>(ld, 0, v, a.d);
       float p[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
@@ -483,10 +483,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= (DIRECT ? 256 : 128) ? 2 : 1
           }
         }
       }
-      if constexpr (DV) add_columns<T, RB, FD>(av, ld, 0, p, a.d);
+      if constexpr (DV) add_columns<T, RB, RB == 1024 && DK>(av, ld, 0, p, a.d);
       if constexpr (DK) {
         scaled.apply(ds, ak);
-        add_columns<T, RB, FD>(ak, lq, 0, ds, a.d);
+        add_columns<T, RB, RB == 1024 && DK>(ak, lq, 0, ds, a.d);
       }
     }
     t = next;
@@ -604,14 +604,32 @@ hipError_t launch_type(const AttentionGrad &g, hipStream_t s) {
 
 }  // namespace
 
+// Splits of `blocks` blocks that take `tiles` tiles each, at most `most`.  With rows of up to 256 bytes, or 16-bit ones, a compute unit
+// holds several blocks: as many splits as make `fill` blocks.  fp32 rows of more than 64 values leave room for one, so what counts is the
+// rounds of 256 blocks, each of its tiles and about two more for its begin and end (gradient of 2 x 1024 on 1024, 8/4 heads of 256,
+// with 768 and 512 blocks 1068 us, by rounds 915; 79 x 96 on 7, 32/4 of 128, 316 blocks unsplit 659, by rounds 533).
+static int splits_of(bool alone, int64_t blocks, int64_t tiles, int64_t most, int64_t fill) {
+  if (most > 32) most = 32;
+  if (blocks <= 0 || most < 2) return 1;
+  if (!alone) {
+    const int64_t s = fill / blocks < most ? fill / blocks : most;
+    return s > 1 ? (int)s : 1;
+  }
+  if (blocks > 1 << 16) return 1;      // many rounds either way
+  int64_t best = 1, least = 0;
+  for (int64_t s = 1; s <= most; ++s) {
+    const int64_t time = (blocks * s + 255) / 256 * ((tiles + s - 1) / s + 2);
+    if (s == 1 || time < least) best = s, least = time;
+  }
+  return (int)best;
+}
+
 AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, int64_t keys, int heads, int kv_heads, int d,
                                       bool masked) {
   AttentionGradPlan p{};
-  const int64_t rows = (int64_t)(heads / kv_heads) * queries, pairs = batch * kv_heads, blocks = (keys + 127) / 128 * pairs;
-  int64_t splits = blocks > 0 ? 768 / blocks : 1;
-  if (splits > rows / 128) splits = rows / 128;
-  if (splits > 32) splits = 32;
-  p.splits = splits > 1 ? (int)splits : 1;
+  const int64_t rows = (int64_t)(heads / kv_heads) * queries, pairs = batch * kv_heads;
+  const bool alone = type == AECCT_F32 && d > 64;
+  p.splits = splits_of(alone, (keys + 127) / 128 * pairs, (rows + 31) / 32, rows / 128, 768);
   if (masked) {
     p.words = (size_t)(queries * words_of(keys)) * 4;
     p.flags = (size_t)((queries + 31) / 32 * (words_of(keys) / 2));
@@ -619,11 +637,7 @@ AttentionGradPlan plan_attention_grad(int type, int64_t batch, int64_t queries, 
   p.rows = (size_t)(rows * pairs) * 8;
   if (p.splits > 1) p.part = (size_t)(p.splits * 2 * pairs * keys * d_of(d)) * 4;
   // dq's blocks of 128 rows, where they are few, split the keys: at least 256 keys each.
-  const int64_t row_blocks = (rows + 127) / 128 * pairs;
-  int64_t q = row_blocks > 0 ? 512 / row_blocks : 1;
-  if (q > keys / 256) q = keys / 256;
-  if (q > 32) q = 32;
-  p.splits_q = q > 1 ? (int)q : 1;
+  p.splits_q = splits_of(alone, (rows + 127) / 128 * pairs, (keys + 31) / 32, keys / 256, 512);
   if (p.splits_q > 1) p.part_q = (size_t)(p.splits_q * pairs * rows * d_of(d)) * 4;
   return p;
 }

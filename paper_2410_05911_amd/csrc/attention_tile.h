@@ -20,15 +20,14 @@ __device__ __forceinline__ int exchange(int row) {
   if constexpr (RB % 256 == 0) return ((row & 3) << 2 | (row >> 2 & 3)) << 4;
   return RB >= 128 ? ((row & 3) << 1 | (row >> 2 & 1)) << 4 : ((row & 2) | (row >> 2 & 1)) << 4;
 }
-// The lane, for LDS addresses.  In fp32 rows of 33 to 64 and of 193 to 256 values take it as a new value each time: the addresses of a
+// The lane, for LDS addresses.  In fp32 rows of 33 to 64 and of more than 128 values take it as a new value each time: the addresses of a
 // tile, the same for every tile, are then computed where they are used instead of being kept over the loop, for which 60 to 200
 // registers a lane were spilled (128 x 256 on 128 keys, 8 heads of 64, a band: 163 -> 104 us, its gradient 527 -> 311; 8 x 1024 on
-// 1024, 16/4 heads of 256: 2204 -> 1763, gradient of 2 x 1024 on 1024, 8/4 of 200: 1284 -> 974).  Between, where nothing spills, computing
-// them again costs 5 %.
+// 1024, 16/4 heads of 256: 2204 -> 1763).  Between, where nothing spills, computing them again costs 5 %.
 template <class T, int RB>
 __device__ __forceinline__ int lane_of() {
   int lane = threadIdx.x & 63;
-  if constexpr (sizeof(T) == 4 && (RB == 256 || RB == 1024)) asm volatile("" : "+v"(lane));
+  if constexpr (sizeof(T) == 4 && (RB == 256 || RB >= 768)) asm volatile("" : "+v"(lane));
   return lane;
 }
 // Chunk `chunk` of row `row`: of a product along d.
@@ -49,8 +48,13 @@ __device__ __forceinline__ u32x4 column_chunk(const char *tile, int row0, int t,
 __device__ __forceinline__ int row_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
 // acc[f] += the tile's columns (32 f + 0..31) times p, over the 32 rows from row0 on; p a result's registers.
-// Rows of 1024 bytes, so of 129 to 256 fp32 values, stop at d (200: 3850 -> 2157 us a gradient; narrower ones lose more by the branches).
-template <class T, int RB, int FD>
+//
+// fp32 rows of 129 to 256 values, one wavefront a SIMD: what a step reads from LDS is asked for before the step ahead of it is
+// multiplied, and the barriers keep it there: left alone, the compiler either waits for each or asks for so many that registers are
+// spilled (8 x 1024 on 1024, 16/4 heads of 256 1768 -> 1259 us, gradient of 4 x 1024 on 1024, 8/4 of 160 1117 -> 1096).  TIGHT (dq and
+// dk of more than 192 values: three times 128 registers are kept) has none for that; there a branch a step stops at d, and with
+// it the compiler's looking ahead (2 x 1024 on 1024, 8/4 of 256: dq 412 us, without the branches 494).
+template <class T, int RB, bool TIGHT, int FD>
 __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile, int row0, const float (&p)[16], int d) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -62,29 +66,68 @@ __device__ __forceinline__ void add_columns(f32x16 (&acc)[FD], const char *tile,
     }
   } else {
     const int lane = lane_of<T, RB>(), h = lane >> 5;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    auto value = [&](int i, int f) {
       const int row = row0 + row_of(i, h);
+      return *(const float *)(tile + row * RB + (((32 * f + (lane & 31)) * 4) ^ exchange<RB>(row)));
+    };
+    if constexpr (RB >= 768 && !TIGHT) {
+      float v[2][FD];
 #pragma unroll
-      for (int f = 0; f < FD; ++f) {
-        if (RB == 1024 && f && 32 * f >= d) break;
-        const float v = *(const float *)(tile + row * RB + (((32 * f + (lane & 31)) * 4) ^ exchange<RB>(row)));
-        acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, p[i], acc[f], 0, 0, 0);
+      for (int f = 0; f < FD; ++f) v[0][f] = value(0, f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (i < 15) {
+#pragma unroll
+          for (int f = 0; f < FD; ++f) v[(i + 1) & 1][f] = value(i + 1, f);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < FD; ++f) {
+          acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i & 1][f], p[i], acc[f], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int f = 0; f < FD; ++f) {
+          if (TIGHT && f && 32 * f >= d) break;
+          acc[f] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(i, f), p[i], acc[f], 0, 0, 0);
+        }
     }
   }
 }
 // The product of the tile's 32 rows from row0 on with a lane's row held in registers (chunks 2 s + h).
-template <class T, int RB>
+template <class T, int RB, bool TIGHT>
 __device__ __forceinline__ f32x16 times_rows(const char *tile, int row0, const u32x4 (&r)[RB / 32], int d) {
   const int lane = lane_of<T, RB>();
   f32x16 s;
 #pragma unroll
   for (int i = 0; i < 16; ++i) s[i] = 0;
+  auto chunk = [&](int c) { return row_chunk<RB>(tile, row0 + (lane & 31), 2 * c + (lane >> 5)); };
+  if constexpr (sizeof(T) == 4 && RB >= 768 && !TIGHT) {
+    constexpr int G = 2;
+    u32x4 x[2][G];
 #pragma unroll
-  for (int c = 0; c < RB / 32; ++c) {
-    if (RB == 1024 && c && 8 * c >= d) break;
-    step<T>(s, row_chunk<RB>(tile, row0 + (lane & 31), 2 * c + (lane >> 5)), r[c]);
+    for (int j = 0; j < G; ++j) x[0][j] = chunk(j);
+#pragma unroll
+    for (int c = 0; c < RB / 32; c += G) {
+      if (c + G < RB / 32) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) x[(c / G + 1) & 1][j] = chunk(c + G + j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < G; ++j) step<T>(s, x[c / G & 1][j], r[c + j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < RB / 32; ++c) {
+      if (TIGHT && c && 8 * c >= d) break;
+      step<T>(s, chunk(c), r[c]);
+    }
   }
   return s;
 }
