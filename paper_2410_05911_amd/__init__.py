@@ -721,6 +721,8 @@ def _attention_of(q, k, v, lengths, mask, scale):
     keys, kv_heads = k.shape[1], k.shape[2]
     if not kv_heads or not heads or heads % kv_heads:
         raise ValueError("kv_heads must divide heads")
+    if not d:
+        raise ValueError("d must be at least 1")
     if lengths is not None and (lengths.dtype != torch.int32 or lengths.shape != (batch,) or not lengths.is_contiguous() or
                                 lengths.get_device() != index):
         raise ValueError(f"lengths must be {batch} contiguous int32 values on cuda:{index}")

@@ -84,3 +84,22 @@ def test_captured(P):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), step
+
+
+def test_heads_of_no_values_are_refused(P):
+    q, k = torch.zeros(2, 3, 4, 0, device="cuda"), torch.zeros(2, 5, 2, 0, device="cuda")
+    lse = torch.zeros(2, 4, 3, device="cuda")
+    for call in (lambda: P.cross_attention(q, k, k), lambda: P.cross_attention(q, k, k, scale=1.0), lambda: P.cross_attention_grad(q, k, k, q, lse, q)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_one_row_of_a_mask_for_all_queries(P):
+    """A mask with a stride of 0."""
+    s = base._case(3, 70, 130, 4, 2, 32, "fp32", "tight", True, "none", 6)
+    row = torch.rand(1, 130, device="cuda", generator=torch.Generator(device="cuda").manual_seed(7)) < 0.3
+    outs = []
+    for mask in (row.expand(70, 130), row.repeat(70, 1)):
+        o, lse = P.cross_attention(s["q"], s["k"], s["v"], s["lengths"], mask, with_lse=True)
+        outs.append([o, lse, *P.cross_attention_grad(s["q"], s["k"], s["v"], o, lse, s["dout"], s["lengths"], mask)])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
