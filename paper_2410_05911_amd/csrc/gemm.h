@@ -16,38 +16,65 @@
 namespace aecct {
 
 // ---- activations, in fp32
+// 2^(hi + lo), lo small; 1 / x, after a step of Newton's where F32.
+__device__ __forceinline__ float exp2_of(float hi, float lo) {
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return fmaf(e, lo * 0.69314718f, e);
+}
+template <bool F32>
+__device__ __forceinline__ float inverse(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return F32 ? fmaf(fmaf(-x, r, 1.0f), r, r) : r;
+}
 // The normal distribution Phi(z) and e = e^(-z^2 / 2).  Its tail, half of erfc(x) at x = |z| / sqrt(2), is e times a polynomial in
-// 1 / (1 + 0.412 x) whose coefficients are fitted here for the smallest error against the larger of 1.4e-7 and 2^-14 of erfc(x), x to 9.6:
-// Phi is off by at most 2.3e-7, and by an eighth of fp16's half step where it is small (with one coefficient less, fitted for the
-// first alone, GELU at -4 was off by 2 half steps of fp16 and below -7 by several of bf16).  A third of erfc's instructions
-// (16384 x 4096 -> 8192 bf16 with erff 1097 us, so 1071); fp32 outputs take erfcf and expf.
-__device__ __forceinline__ float normal(float z, float &e, bool f32) {
-  if (f32) {
-    e = expf(-0.5f * z * z);
-    return 0.5f * erfcf(z * -0.70710678118654752f);
+// 1 / (1 + c x), x to 9.6.  For fp32 outputs its coefficients are fitted here to 3e-8 of erfc(x), and the exponent is taken in two
+// parts: z Phi(z) is within 7 2^-24 of itself from -12.5 on (with erfcf and expf in their place the epilogue took 23 registers more and
+// a compute unit one block less: 49152 x 128 -> 512 int8, ReLU, 31 -> 42 us).  For 16 bits they are fitted for the smallest error
+// against the larger of 1.4e-7 and 2^-14 of erfc(x), an eighth of fp16's half step where Phi is small (with one coefficient less,
+// fitted for 1.5e-7 alone, GELU at -4 was off by 2 half steps of fp16 and below -7 by several of bf16).  |z| is
+// bounded in fp32 so that both parts of the exponent stay finite.
+template <bool F32>
+__device__ __forceinline__ float normal(float z, float &e) {
+  const float a = F32 && fabsf(z) > 100.0f ? 100.0f : fabsf(z), x = a * 0.70710678118654752f;
+  const float t = inverse<F32>(fmaf(F32 ? 0.48f : 0.412f, x, 1.0f));
+  float p;
+  if constexpr (F32) {
+    const float s = a * a, c = -0.72134752f, hi = s * c;     // -log2(e) / 2 is c - 9.63e-9
+    e = exp2_of(hi, fmaf(s, c, -hi) + fmaf(fmaf(a, a, -s), c, s * -9.6298e-9f));
+    p = fmaf(t, -0.052127723f, 0.27955455f);
+    p = fmaf(t, p, -0.5505261f);
+    p = fmaf(t, p, 0.41219106f);
+    p = fmaf(t, p, -0.094040006f);
+    p = fmaf(t, p, 0.23274627f);
+    p = fmaf(t, p, 0.22962034f);
+    p = fmaf(t, p, 0.27181336f);
+    p = fmaf(t, p, 0.2707682f);
+  } else {
+    e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
+    p = fmaf(t, -0.17485723f, 0.55085403f);
+    p = fmaf(t, p, -0.1636966f);
+    p = fmaf(t, p, 0.3475389f);
+    p = fmaf(t, p, 0.20564933f);
+    p = fmaf(t, p, 0.23451155f);
   }
-  const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.412f, x, 1.0f));
-  e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
-  float p = fmaf(t, -0.17485723f, 0.55085403f);
-  p = fmaf(t, p, -0.1636966f);
-  p = fmaf(t, p, 0.3475389f);
-  p = fmaf(t, p, 0.20564933f);
-  p = fmaf(t, p, 0.23451155f);
   const float tail = 0.5f * (p * t) * e;
   return z > 0.0f ? 1.0f - tail : tail;
 }
 // 1 / (1 + e^-z) and q = 1 - that, each from e^-|z|, so that the smaller one keeps its bits and does not vanish before e^-|z| does.
-__device__ __forceinline__ float logistic(float z, float &q, bool f32) {
-  const float e = f32 ? expf(-fabsf(z)) : __builtin_amdgcn_exp2f(fabsf(z) * -1.4426950408889634f);
-  const float large = f32 ? 1.0f / (1.0f + e) : __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+template <bool F32>
+__device__ __forceinline__ float logistic(float z, float &q) {
+  const float a = F32 && fabsf(z) > 200.0f ? 200.0f : fabsf(z), c = -1.44269502f, hi = a * c;     // -log2(e) is c - 1.926e-8
+  const float e = F32 ? exp2_of(hi, fmaf(a, c, -hi) + a * -1.92596e-8f) : __builtin_amdgcn_exp2f(hi);
+  const float large = inverse<F32>(1.0f + e), small = e * large;
   q = z < 0.0f ? large : small;
   return z < 0.0f ? small : large;
 }
-__device__ __forceinline__ float activate(float z, int act, bool f32) {
+template <bool F32>
+__device__ __forceinline__ float activate(float z, int act) {
   float other;
   if (act == kActRelu) return z > 0.0f || z != z ? z : 0.0f;
-  if (act == kActGelu) return z * normal(z, other, f32);
-  if (act == kActSilu) return z * logistic(z, other, f32);
+  if (act == kActGelu) return z * normal<F32>(z, other);
+  if (act == kActSilu) return z * logistic<F32>(z, other);
   return z;
 }
 
@@ -76,8 +103,8 @@ struct Columns {
     if (e.bias) load_part<float, V>(e.bias + n0, count, bias);
   }
 };
-// The epilogue of those columns' values of row m.
-template <int V>
+// The epilogue of those columns' values of row m; F32: of an fp32 output.
+template <bool F32, int V>
 __device__ __forceinline__ void finish(const Epilogue &e, const Columns<V> &of, int64_t m, int64_t n0, int count, float (&v)[V]) {
   float r[V];
   if (e.res) load_values<V>(e.type, e.res, m * e.ldres + n0, count, r);
@@ -93,7 +120,7 @@ __device__ __forceinline__ void finish(const Epilogue &e, const Columns<V> &of, 
   if (e.z) store_values<V>(e.type, e.z, m * e.ldz + n0, count, v);
   if (e.act != kActNone) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = activate(v[i], e.act, e.type == AECCT_F32);
+    for (int i = 0; i < V; ++i) v[i] = activate<F32>(v[i], e.act);
   }
   if (e.res) {
 #pragma unroll
@@ -103,7 +130,8 @@ __device__ __forceinline__ void finish(const Epilogue &e, const Columns<V> &of, 
 }
 template <int V>
 __device__ __forceinline__ void finish(const Epilogue &e, int64_t m, int64_t n0, int count, float (&v)[V]) {
-  finish<V>(e, Columns<V>(e, n0, count), m, n0, count, v);
+  if (e.type == AECCT_F32) finish<true>(e, Columns<V>(e, n0, count), m, n0, count, v);
+  else finish<false>(e, Columns<V>(e, n0, count), m, n0, count, v);
 }
 
 // ---- staging: 16-byte pieces of a factor's tile, slot by slot
@@ -201,7 +229,7 @@ struct Share {
   }
 };
 
-// 32 rows of sums in LDS through the epilogue, V neighbouring columns a lane.
+// 32 rows of sums in LDS through the epilogue, V neighbouring columns a lane: four of fp32 outputs and sums, eight of 16-bit ones.
 template <int V, int FN, int TURNS>
 __device__ __forceinline__ void finish_strip(const Gemm &g, const float *strip, int split, int m0, int n0) {
   constexpr int LD = FN * 32 + 4, PER = FN * 32 / V, STEP = 64 / PER;   // lanes a row, rows at once
@@ -219,7 +247,7 @@ __device__ __forceinline__ void finish_strip(const Gemm &g, const float *strip, 
       for (int r = 0; r < 4; ++r) v[i + r] = x[r];
     }
     if (g.part) store_part<float, V>((float *)g.part + ((int64_t)split * g.m + m) * g.n + n, count, v);
-    else finish<V>(g.e, columns, m, n, count, v);
+    else finish<V == 4>(g.e, columns, m, n, count, v);
   }
 }
 // A wavefront's FM x FN sums from (m0, n0) on through the epilogue: 32 rows at a time go through LDS, so that a lane then has 16 bytes of

@@ -80,15 +80,16 @@ hipError_t launch_gemm(int type, const Gemm *g, const GemmPlan *plan, int count,
 namespace {
 
 // act'(z).  Where a factor is 0 the other may be infinite: such a product's limit is 0.
-__device__ __forceinline__ float slope(float z, int act, bool f32) {
+template <bool F32>
+__device__ __forceinline__ float slope(float z, int act) {
   if (act == kActRelu) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
   if (act == kActGelu) {
     float e;
-    const float phi = normal(z, e, f32), density = e * 0.39894228040143268f;
+    const float phi = normal<F32>(z, e), density = e * 0.39894228040143268f;
     return phi + (density == 0.0f ? 0.0f : z * density);
   }
   float q;
-  const float p = logistic(z, q, f32);
+  const float p = logistic<F32>(z, q);
   if (p == 0.0f || q == 0.0f) return p;
   return p * (1.0f + z * q);
 }
@@ -110,7 +111,7 @@ __device__ __forceinline__ void slope_block(const Slope &a, uint32_t block, uint
         float z[8];
         load_part<T, 8>((const T *)a.z + row * a.ldz + n0, count, z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] *= slope(z[i], a.act, sizeof(T) == 4);
+        for (int i = 0; i < 8; ++i) d[i] *= slope<sizeof(T) == 4>(z[i], a.act);
         if (a.dz) {   // zeros behind the row's end
           float e[8];
 #pragma unroll
