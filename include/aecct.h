@@ -588,7 +588,8 @@ aecct_status aecct_linear_map(const aecct_linear_map_args *a, void *workspace, s
 /*
  * Its gradient: dz = dy act'(z),  dx = dz W^T,  dw = x^T dz,  dbias = sum of dz over the rows.  (res has the gradient dy.)
  * z as aecct_linear_map wrote it; with 16-bit types dz is rounded to the type before the products (not for dbias), as the
- * matrix instructions take it.  relu'(0) = 0.
+ * matrix instructions take it: fp16's dz has dy's range, bits are lost below 2^-14, and past 65504 (slopes reach 1.13) it is
+ * infinite, also where dw is fp32.  relu'(0) = 0.
  */
 typedef struct aecct_linear_map_grad_args {
   int64_t rows, in, out;

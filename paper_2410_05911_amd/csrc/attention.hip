@@ -5,10 +5,14 @@
 // lane holds 16 keys of one row: the maximum and sum are taken in registers with one exchange between the halves, and the
 // weights are, as they lie, the second factor of the product with the values.
 //
-// What bounds it: many rows, the matrix instructions (47 % of the clocks) and the vector ones (52 %, half of them exponentials), which
-// two wavefronts a SIMD overlap little (2 x 4096 queries on 2111 keys, 32 heads of 128, bf16: 280 us, 0.92 PFLOP/s; one wavefront a
+// What bounds it: many rows, the matrix instructions (50 % of the clocks) and the vector ones (52 %, half of them exponentials), which
+// two wavefronts a SIMD overlap little (2 x 4096 queries on 2111 keys, 32 heads of 128, bf16: 290 us, 0.89 PFLOP/s; one wavefront a
 // SIMD 577).  Scores a tile ahead in the same wavefront, wavefront priorities and sums that begin with kept zeros were measured
 // without gain.  Few rows, memory: one query on 8192 keys, 16 sequences, 8 key heads of 128, bf16 in 89 us (4.5 TB/s).
+//
+// With 16-bit types the weights are rounded to the type, as the matrix instructions take them; their sum takes them unrounded.  o is then as
+// far from 64 bits as two such roundings (bf16 2.3e-3 of its norm, fp16 2.8e-4), its own alone 1.66e-3 and 2.1e-4: two
+// products instead, of the weights and of what their rounding leaves, would add half the matrix instructions again.
 #include "attention_tile.h"
 
 namespace aecct {

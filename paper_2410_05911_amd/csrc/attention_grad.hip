@@ -7,8 +7,12 @@
 // As in the forward pass the scores are computed so that a lane's registers are the second factor of the products that follow:
 // keys by rows for dq, rows by keys for dk and dv.
 //
-// Measured: 2 x 2049 queries on 1531 keys, 16 heads of 64 on 4 key heads, a band of a quarter, bf16: dq 28 us, dk and dv 49, their join
-// 10, all 86; 128 x 256 on 128 keys, 8 heads of 16, three keys a query, fp32: 35 and 53, all 86.  Both are bound by the instructions
+// With 16-bit types p and ds are rounded to the type, as the matrix instructions take them: dq, dk and dv are what the formula gives with
+// those rounded weights, rounded once more, 2.4e-3 (bf16) and 3.0e-4 (fp16) of their norms from 64 bits where an output's rounding alone
+// is 1.66e-3 and 2.1e-4.  What a second product with the rest would gain is not worth 3 products more beside 7.
+//
+// Measured: 2 x 2049 queries on 1531 keys, 16 heads of 64 on 4 key heads, a band of a quarter, bf16: dq 27 us, dk and dv 46, their join
+// 10, all 85; 128 x 256 on 128 keys, 8 heads of 16, three keys a query, fp32: 34 and 52, all 87.  Both are bound by the instructions
 // and latencies of short loops (dq has 9 tiles of keys a block, dk and dv 8 to 16 of rows), not by memory.
 #include "attention_tile.h"
 

@@ -96,6 +96,9 @@ __device__ __forceinline__ float slope(float z, int act) {
 
 constexpr int kSlopeColumns = 128;   // 16 threads of 8 values a row, 16 rows at once
 
+// dz is rounded to the type, as the products take it: dx and dw are what the formula gives with that dz, 2.35e-3 (bf16) and 2.9e-4 (fp16) of
+// their norms from 64 bits where their own rounding alone is 1.66e-3 and 2.1e-4; a second product of what the rounding leaves
+// would double the gradient's time.  The sums take dz unrounded.
 template <class T>
 __device__ __forceinline__ void slope_block(const Slope &a, uint32_t block, uint32_t across) {
   const uint32_t by = block / across, bx = block - by * across;
