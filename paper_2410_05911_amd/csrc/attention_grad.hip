@@ -608,9 +608,8 @@ hipError_t launch_type(const AttentionGrad &g, hipStream_t s) {
 
 }  // namespace
 
-// Splits of `blocks` blocks that take `tiles` tiles each, at most `most`.  With rows of up to 256 bytes, or 16-bit ones, a compute unit
-// holds several blocks: as many splits as make `fill` blocks.  fp32 rows of more than 64 values leave room for one, so what counts is the
-// rounds of 256 blocks, each of its tiles and about two more for its begin and end (gradient of 2 x 1024 on 1024, 8/4 heads of 256,
+// Splits of `blocks` blocks that take `tiles` tiles each, at most `most`: as many as make `fill` blocks.  fp32 rows of more than 64 values
+// (`alone`) leave a compute unit room for one block, so what counts there is the rounds of 256 blocks, each of its tiles and about two more for its begin and end (gradient of 2 x 1024 on 1024, 8/4 heads of 256,
 // with 768 and 512 blocks 1068 us, by rounds 915; 79 x 96 on 7, 32/4 of 128, 316 blocks unsplit 659, by rounds 533).
 static int splits_of(bool alone, int64_t blocks, int64_t tiles, int64_t most, int64_t fill) {
   if (most > 32) most = 32;

@@ -103,3 +103,23 @@ def test_one_row_of_a_mask_for_all_queries(P):
         o, lse = P.cross_attention(s["q"], s["k"], s["v"], s["lengths"], mask, with_lse=True)
         outs.append([o, lse, *P.cross_attention_grad(s["q"], s["k"], s["v"], o, lse, s["dout"], s["lengths"], mask)])
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_keys_and_values_in_turn(P):
+    """k and v, and dk and dv, in turn by heads ([batch][keys][heads][2][d]) and by sequences ([keys][batch][2][heads][d]): the bits that
+    contiguous tensors give."""
+    s = base._case(3, 70, 130, 4, 2, 32, "fp32", "tight", True, "none", 8)
+    k, v = s["k"].contiguous(), s["v"].contiguous()
+    o, lse = P.cross_attention(s["q"], k, v, s["lengths"], with_lse=True)
+    want = [o, lse, *P.cross_attention_grad(s["q"], k, v, o, lse, s["dout"], s["lengths"])]
+    by_heads = lambda: torch.full((3, 130, 2, 2, 32), 77.0, device="cuda")  # noqa: E731
+    by_batch = lambda: torch.full((130, 3, 2, 2, 32), 77.0, device="cuda")  # noqa: E731
+    for whole, parts in ((by_heads, lambda t: (t[:, :, :, 0], t[:, :, :, 1])),
+                         (by_batch, lambda t: (t[:, :, 0].transpose(0, 1), t[:, :, 1].transpose(0, 1)))):
+        kv, dkv = whole(), whole()
+        for part, t in zip(parts(kv), (k, v)):
+            part.copy_(t)
+        dk, dv = parts(dkv)
+        o, lse = P.cross_attention(s["q"], *parts(kv), s["lengths"], with_lse=True)
+        got = [o, lse, *P.cross_attention_grad(s["q"], *parts(kv), o, lse, s["dout"], s["lengths"], dk=dk, dv=dv)]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -3,8 +3,8 @@ and tolerances of test_gpu_linear.py.
 
 By plan_gemm, in 16 and 8 bits: 64 x 64 outputs a block below 192 blocks of 128 x 128; 256 x 256 from 256 of them on with a k of 1024
 bytes; k is split below 256 blocks.  fp32: 64 x 64 or 128 x 128, split or not, by the time they are estimated to take.  One stage where
-k is one tile of 128 bytes.  Four rows and fewer split k from 4 MB of weights on.  Factors whose rows are whole 16-byte pieces at such addresses go past the registers; others are copied into such from
-2 rows in out = 4e9 on."""
+k is one tile of 128 bytes.  Four rows and fewer split k from 4 MB of weights on.  Factors whose rows are whole 16-byte pieces at such
+addresses go past the registers; others are copied into such where each copied value enters enough products."""
 import pytest
 
 import test_gpu_linear as base
